@@ -224,6 +224,58 @@ int moe_unpermute_combine_route_bwd(const moe_shape* shape, const uint16_t* dout
                                     const int32_t* row_of_slot, const int32_t* topk_idx, const float* topk_w,
                                     const float* probs_save, uint16_t* dy_perm, float* dtopk_w, float* dlogits, void* stream);
 
+/* ---- Answering: microscaled 4-bit floating point (MXFP4 of the OCP Microscaling formats), and the whole layer for a few tokens.
+ *
+ * A quantised matrix [rows, cols] is `q` [rows, cols / 2] bytes (two E2M1 codes each, the even column in the low nibble) and `scales`
+ * [rows, cols / 32] bytes: block b of a row stands for codes times 2^(scales[b] - 127), codes +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}.  Blocks lie along
+ * the contraction: rows of activations, and an expert's weight W [K, C] as the C rows of its transpose.  scales = 255: the block is NaN. */
+
+/* Blocks along the rows.  Of a block with largest magnitude m: scale code = clamp(floor(log2 m) - 2, -127, 127) + 127, codes = x / scale rounded
+ * to nearest even, at most 6 in magnitude; m = 0: code 0 and zeros; an infinity or NaN in the block: scale code 255, codes 0.
+ *   x [rows, cols] bf16 in;  q [rows, cols / 2], scales [rows, cols / 32] out.  cols a multiple of 32; rows * cols <= 2^36. */
+int moe_mxfp4_quantize(const uint16_t* x, int64_t rows, int cols, uint8_t* q, uint8_t* scales, void* stream);
+
+/* Blocks along the columns of each of `batch` matrices, stored transposed (weights as they lie in this library, W_gate, W_up [E', d, f] and W_down
+ * [E', f, d], become what the calls below take).
+ *   w [batch, rows, cols] bf16 in;  q [batch, cols, rows / 2], scales [batch, cols, rows / 32] out.  rows a multiple of 32, cols one of 8,
+ *   batch <= 65535. */
+int moe_mxfp4_quantize_t(const uint16_t* w, int batch, int rows, int cols, uint8_t* q, uint8_t* scales, void* stream);
+
+/* What the codes stand for, in bf16 (exact where bf16 has the value: scale codes up to 252).
+ *   q [rows, cols / 2], scales [rows, cols / 32] in;  x [rows, cols] bf16 out. */
+int moe_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64_t rows, int cols, uint16_t* x, void* stream);
+
+/* Product of quantised rows, grouped by expert, with the experts' quantised weights:  for expert e over rows [offsets[e], offsets[e+1])
+ *   y[r, c] = sum_k x[r, k] w[e, c, k]     (products of the values the codes stand for, fp32 accumulation, one bf16 rounding).
+ *   xq [rows, k / 2], x_scales [rows, k / 32] in;  offsets [experts + 1] int32 in (device, as written by moe_permute; offsets[experts] <= rows)
+ *   wq [experts, n, k / 2], w_scales [experts, n, k / 32] in;  y [rows, n] bf16 out.  k a multiple of 32, n one of 8, both at most 2^22;
+ *   experts <= 1024; rows < 2^31. */
+int moe_mxfp4_grouped_gemm(int experts, int64_t rows, int n, int k, const uint8_t* xq, const uint8_t* x_scales, const int32_t* offsets,
+                           const uint8_t* wq, const uint8_t* w_scales, uint16_t* y, void* stream);
+
+/* moe_grouped_ffn_fwd on quantised weights, for answering (nothing is kept for a backward pass):
+ *   X = Q(x_perm);  G = X W_gate,  U = X W_up,  H = Q(silu(G) * U),  Y = H W_down     (Q: as moe_mxfp4_quantize; of H from fp32)
+ *   x_perm [N,d] bf16 in;  offsets [E'+1] int32 in;  wq_gate, wq_up [E', f, d / 2], s_gate, s_up [E', f, d / 32], wq_down [E', d, f / 2],
+ *   s_down [E', d, f / 32] in;  y_perm [N,d] bf16 out. */
+int moe_mxfp4_grouped_ffn_fwd(const moe_shape* shape, const uint16_t* x_perm, const int32_t* offsets, const uint8_t* wq_gate,
+                              const uint8_t* s_gate, const uint8_t* wq_up, const uint8_t* s_up, const uint8_t* wq_down,
+                              const uint8_t* s_down, uint16_t* y_perm, void* ws, size_t ws_bytes, void* stream);
+
+/* The whole layer for at most MOE_FEW_TOKENS_MAX tokens (T * K' <= 4096): routing, experts and combine, without permuted copies of the rows.
+ *   out[t] = sum_j topk_w[t,j] (silu(x_t W_gate[e]) * (x_t W_up[e])) W_down[e],  e = topk_idx[t,j]
+ * The hidden activation keeps 16 significand bits (a bf16 head and remainder), everything else between x and out is fp32; one bf16 rounding.
+ *   x [T,d] bf16 in;  w_router [E,d] bf16 in: topk_idx, topk_w [T,K'] are outputs, as of moe_router_route_fwd.  w_router NULL: they are
+ *   inputs (rows that arrive routed; ids outside [0,E') are clamped and the result is then unspecified).
+ *   weights as in moe_grouped_ffn_fwd, or quantised as in moe_mxfp4_grouped_ffn_fwd (the rows stay bf16);  out [T,d] bf16 out.
+ * The workspace is one of its own, moe_layer_few_workspace_bytes(shape) bytes (0 if the shape is invalid or over these limits). */
+#define MOE_FEW_TOKENS_MAX 64
+size_t moe_layer_few_workspace_bytes(const moe_shape* shape);
+int moe_layer_few_fwd(const moe_shape* shape, const uint16_t* x, const uint16_t* w_router, const uint16_t* w_gate, const uint16_t* w_up,
+                      const uint16_t* w_down, uint16_t* out, int32_t* topk_idx, float* topk_w, void* ws, size_t ws_bytes, void* stream);
+int moe_layer_few_mxfp4_fwd(const moe_shape* shape, const uint16_t* x, const uint16_t* w_router, const uint8_t* wq_gate, const uint8_t* s_gate,
+                            const uint8_t* wq_up, const uint8_t* s_up, const uint8_t* wq_down, const uint8_t* s_down, uint16_t* out,
+                            int32_t* topk_idx, float* topk_w, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- The single-GPU steps of the hierarchical all-to-all (Section V, Algorithm 1).  One rank's send buffer S has
  * N = num_nodes * R rows (R ranks per node) of row_bytes bytes (a multiple of 16; any element type): row n*R + l goes
  * to local rank l of node n.  M = num_nodes - 1; "the i-th remote node" counts the nodes other than node_id in

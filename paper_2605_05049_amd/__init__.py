@@ -12,5 +12,9 @@ from .binding import (  # noqa: F401
     moe_grouped_ffn_bwd, moe_unpermute_combine, moe_unpermute_combine_bwd, moe_unpermute_combine_route_bwd, EXPORTED_SYMBOLS,
     profile_enable, profile_reset, profile_records, load_accumulate, load_imbalance, rebalance_experts,
     moe_halo_pack_remote, moe_halo_repack, moe_halo_unpack,
+    moe_mxfp4_quantize, moe_mxfp4_quantize_t, moe_mxfp4_dequantize, moe_mxfp4_grouped_gemm, moe_mxfp4_grouped_ffn_fwd,
+    FEW_TOKENS_MAX, layer_few_workspace_bytes, moe_layer_few_fwd, moe_layer_few_mxfp4_fwd,
 )
-from .layer import MoeLayerBuffers, CapturedLayerStep, layer_forward, layer_backward  # noqa: F401
+from .layer import (  # noqa: F401
+    MoeLayerBuffers, CapturedLayerStep, layer_forward, layer_backward, FewTokenBuffers, layer_few_forward, quantize_experts, layer_mxfp4_forward,
+)

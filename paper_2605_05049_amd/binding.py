@@ -3,7 +3,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_int, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_int, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -19,7 +19,10 @@ EXPORTED_SYMBOLS = (
     "moe_unpermute_combine", "moe_unpermute_combine_bwd", "moe_unpermute_combine_route_bwd",
     "moe_load_accumulate", "moe_load_imbalance", "moe_rebalance_experts",
     "moe_halo_pack_remote", "moe_halo_repack", "moe_halo_unpack",
+    "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_ffn_fwd",
+    "moe_layer_few_workspace_bytes", "moe_layer_few_fwd", "moe_layer_few_mxfp4_fwd",
 )
+FEW_TOKENS_MAX = 64   # MOE_FEW_TOKENS_MAX: tokens of a moe_layer_few_* call
 
 
 class MoeError(RuntimeError):
@@ -93,6 +96,8 @@ def load_library():
     lib.moe_profile_get.argtypes = [c_int, POINTER(c_char_p), POINTER(ctypes.c_float)]
     lib.moe_profile_reset.restype = c_int
     lib.moe_profile_reset.argtypes = []
+    lib.moe_layer_few_workspace_bytes.restype = c_size_t
+    lib.moe_layer_few_workspace_bytes.argtypes = [sp]
     V = c_void_p
     sigs = {
         "moe_route_topk": [sp, V, V, V, V, V],
@@ -118,6 +123,13 @@ def load_library():
     sigs["moe_load_accumulate"] = [V, V, c_int]
     sigs["moe_load_imbalance"] = [V, c_int, c_int, V, POINTER(ctypes.c_double)]
     sigs["moe_rebalance_experts"] = [V, c_int, c_int, V, c_int, POINTER(ctypes.c_int32), V]
+    sigs["moe_mxfp4_quantize"] = [V, c_int64, c_int, V, V, V]
+    sigs["moe_mxfp4_quantize_t"] = [V, c_int, c_int, c_int, V, V, V]
+    sigs["moe_mxfp4_dequantize"] = [V, V, c_int64, c_int, V, V]
+    sigs["moe_mxfp4_grouped_gemm"] = [c_int, c_int64, c_int, c_int, V, V, V, V, V, V, V]
+    sigs["moe_mxfp4_grouped_ffn_fwd"] = [sp] + [V] * 10 + [c_size_t, V]
+    sigs["moe_layer_few_fwd"] = [sp] + [V] * 9 + [c_size_t, V]
+    sigs["moe_layer_few_mxfp4_fwd"] = [sp] + [V] * 12 + [c_size_t, V]
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.restype = c_int
@@ -136,6 +148,11 @@ def abi_version() -> int:
 
 def workspace_bytes(shape) -> int:
     return int(load_library().moe_workspace_bytes(ctypes.byref(Shape.of(shape)._c)))
+
+
+def layer_few_workspace_bytes(shape) -> int:
+    """Bytes of workspace of a moe_layer_few_* call (0: the shape is invalid, or has more tokens or slots than such a call takes)."""
+    return int(load_library().moe_layer_few_workspace_bytes(ctypes.byref(Shape.of(shape)._c)))
 
 
 def _gemm_names(bits: int) -> tuple:
@@ -438,6 +455,100 @@ def moe_unpermute_combine_route_bwd(shape, dout, y_perm, row_of_slot, topk_idx, 
         _ptr(dy_perm, bf, s.N * s.d_model, "dy_perm"), _ptr(dtopk_w, torch.float32, s.N, "dtopk_w"),
         _ptr(dlogits, torch.float32, s.T * s.E, "dlogits"), _stream(stream))
     _check("moe_unpermute_combine_route_bwd", rc)
+
+
+# ---- microscaled 4-bit floating point; the whole layer for a few tokens ------------------------------------------
+
+def _u8(t, numel, name):
+    return _ptr(t, (_torch_module or _torch()).uint8, numel, name)
+
+
+def _last(t, what):
+    if t.dim() < 1 or t.shape[-1] < 1:
+        raise ValueError(f"{what}: expected rows of at least one element")
+    return t.numel() // t.shape[-1], t.shape[-1]
+
+
+def moe_mxfp4_quantize(x, q, scales, stream=None):
+    """x [..., cols] bf16 -> q [..., cols / 2], scales [..., cols / 32] (uint8)."""
+    rows, cols = _last(x, "x")
+    rc = load_library().moe_mxfp4_quantize(_ptr(x, _bf16_types(), None, "x"), rows, cols, _u8(q, rows * cols // 2, "q"),
+                                           _u8(scales, rows * cols // 32, "scales"), _stream(stream))
+    _check("moe_mxfp4_quantize", rc)
+
+
+def moe_mxfp4_quantize_t(w, q, scales, stream=None):
+    """w [..., K, C] bf16 -> q [..., C, K / 2], scales [..., C, K / 32] (uint8): blocks along K."""
+    if w.dim() < 2:
+        raise ValueError("w: expected a matrix, or several")
+    n, (rows, cols) = w.numel(), w.shape[-2:]
+    batch = n // (rows * cols) if n else 0
+    rc = load_library().moe_mxfp4_quantize_t(_ptr(w, _bf16_types(), None, "w"), batch, rows, cols, _u8(q, n // 2, "q"), _u8(scales, n // 32, "scales"),
+                                             _stream(stream))
+    _check("moe_mxfp4_quantize_t", rc)
+
+
+def moe_mxfp4_dequantize(q, scales, x, stream=None):
+    """q [..., cols / 2], scales [..., cols / 32] (uint8) -> x [..., cols] bf16."""
+    rows, cols = _last(x, "x")
+    rc = load_library().moe_mxfp4_dequantize(_u8(q, rows * cols // 2, "q"), _u8(scales, rows * cols // 32, "scales"), rows, cols,
+                                             _ptr(x, _bf16_types(), None, "x"), _stream(stream))
+    _check("moe_mxfp4_dequantize", rc)
+
+
+def moe_mxfp4_grouped_gemm(xq, x_scales, offsets, wq, w_scales, y, stream=None):
+    """y [rows, n] bf16 = per expert xq [rows, k / 2] times wq [experts, n, k / 2], rows grouped by `offsets` [experts + 1]."""
+    torch = _torch_module or _torch()
+    if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
+        raise ValueError("xq, wq: expected [rows, k / 2] and [experts, n, k / 2]")
+    rows, (experts, n, half) = xq.shape[0], wq.shape
+    rc = load_library().moe_mxfp4_grouped_gemm(
+        experts, rows, n, 2 * half, _u8(xq, None, "xq"), _u8(x_scales, rows * half // 16, "x_scales"),
+        _ptr(offsets, torch.int32, experts + 1, "offsets"), _u8(wq, None, "wq"), _u8(w_scales, experts * n * half // 16, "w_scales"),
+        _ptr(y, _bf16_types(), rows * n, "y"), _stream(stream))
+    _check("moe_mxfp4_grouped_gemm", rc)
+
+
+def _mx_weights(s, wq_gate, s_gate, wq_up, s_up, wq_down, s_down):
+    n = s.E_total * s.d_model * s.d_ffn
+    return (_u8(wq_gate, n // 2, "wq_gate"), _u8(s_gate, n // 32, "s_gate"), _u8(wq_up, n // 2, "wq_up"), _u8(s_up, n // 32, "s_up"),
+            _u8(wq_down, n // 2, "wq_down"), _u8(s_down, n // 32, "s_down"))
+
+
+def moe_mxfp4_grouped_ffn_fwd(shape, x_perm, offsets, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, y_perm, ws, stream=None):
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    bf = _bf16_types()
+    rc = load_library().moe_mxfp4_grouped_ffn_fwd(
+        ctypes.byref(s._c), _ptr(x_perm, bf, s.N * s.d_model, "x_perm"), _ptr(offsets, torch.int32, s.E_total + 1, "offsets"),
+        *_mx_weights(s, wq_gate, s_gate, wq_up, s_up, wq_down, s_down), _ptr(y_perm, bf, s.N * s.d_model, "y_perm"), _ptr(ws, None, None, "ws"),
+        ws.numel() * ws.element_size(), _stream(stream))
+    _check("moe_mxfp4_grouped_ffn_fwd", rc)
+
+
+def moe_layer_few_fwd(shape, x, w_router, w_gate, w_up, w_down, out, topk_idx, topk_w, ws, stream=None):
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    bf = _bf16_types()
+    nw = s.E_total * s.d_model * s.d_ffn
+    rc = load_library().moe_layer_few_fwd(
+        ctypes.byref(s._c), _ptr(x, bf, s.T * s.d_model, "x"), _ptr(w_router, bf, s.E * s.d_model, "w_router"), _ptr(w_gate, bf, nw, "w_gate"),
+        _ptr(w_up, bf, nw, "w_up"), _ptr(w_down, bf, nw, "w_down"), _ptr(out, bf, s.T * s.d_model, "out"),
+        _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _ptr(ws, None, None, "ws"),
+        ws.numel() * ws.element_size(), _stream(stream))
+    _check("moe_layer_few_fwd", rc)
+
+
+def moe_layer_few_mxfp4_fwd(shape, x, w_router, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, out, topk_idx, topk_w, ws, stream=None):
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    bf = _bf16_types()
+    rc = load_library().moe_layer_few_mxfp4_fwd(
+        ctypes.byref(s._c), _ptr(x, bf, s.T * s.d_model, "x"), _ptr(w_router, bf, s.E * s.d_model, "w_router"),
+        *_mx_weights(s, wq_gate, s_gate, wq_up, s_up, wq_down, s_down), _ptr(out, bf, s.T * s.d_model, "out"),
+        _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _ptr(ws, None, None, "ws"),
+        ws.numel() * ws.element_size(), _stream(stream))
+    _check("moe_layer_few_mxfp4_fwd", rc)
 
 
 # ---- single-GPU steps of the hierarchical all-to-all (device tensors; rows of any dtype, 16-byte multiples) -----

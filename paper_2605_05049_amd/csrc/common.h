@@ -65,6 +65,7 @@ struct WsLayout {
   size_t dl_hi, dl_lo;      // [T, Epad] bf16: head and remainder of the fp32 dlogits (Epad = E rounded up to 64)
   size_t w_router_t;        // [d, 128] bf16 at most: W_r transposed and zero-padded (router backward, E <= 128)
   size_t router_dw_partial; // router_dw_parts() fp32 partial results [d, ldp] of dW_r^T
+  size_t mx_x, mx_xs, mx_h, mx_hs;   // rows and hidden rows in 4 bits with their scales: [N, d / 2], [N, d / 32], [N, f / 2], [N, f / 32]
   size_t total;
 };
 
@@ -118,7 +119,13 @@ inline WsLayout ws_layout(const Dims& D) {
   L.dl_lo = off; off += dl_bytes;
   L.w_router_t = off; off += D.E <= 128 ? round_up((size_t)D.d * 128 * sizeof(uint16_t), 256) : 0;
   L.router_dw_partial = off; off += round_up((size_t)router_dw_parts(D) * router_dw_part_bytes(D), 256);
-  L.total = off;
+  // the forward on 4-bit weights uses nothing of the above: its rows lie over it
+  size_t mx = 0;
+  L.mx_x = mx; mx += round_up((size_t)D.N * D.d / 2, 256);
+  L.mx_xs = mx; mx += round_up((size_t)D.N * D.d / 32, 256);
+  L.mx_h = mx; mx += round_up((size_t)D.N * D.f / 2, 256);
+  L.mx_hs = mx; mx += round_up((size_t)D.N * D.f / 32, 256);
+  L.total = off > mx ? off : mx;
   return L;
 }
 

@@ -114,3 +114,55 @@ class CapturedLayerStep:
 
     def replay(self):
         self.graph.replay()
+
+
+class FewTokenBuffers:
+    """Outputs and workspace of the layer for a few tokens (at most binding.FEW_TOKENS_MAX)."""
+
+    def __init__(self, shape, device="cuda"):
+        import torch
+        s = B.Shape.of(shape)
+        nbytes = B.layer_few_workspace_bytes(s)
+        if nbytes == 0:
+            raise ValueError(f"the layer for a few tokens takes at most {B.FEW_TOKENS_MAX} tokens of a valid shape")
+        self.shape = s
+        dev = torch.device(device)
+        self.topk_idx = torch.empty(s.T, s.K_slots, dtype=torch.int32, device=dev)
+        self.topk_w = torch.empty(s.T, s.K_slots, dtype=torch.float32, device=dev)
+        self.out = torch.empty(s.T, s.d_model, dtype=torch.bfloat16, device=dev)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+
+
+def layer_few_forward(buf: FewTokenBuffers, x, weights, w_router=None, stream=None):
+    """The whole layer for a few tokens.  weights: (w_gate, w_up, w_down) in bf16, or what quantize_experts returned.  Without `w_router`
+    buf.topk_idx / buf.topk_w were filled by the caller, as for an expert-parallel shard.  Returns buf.out."""
+    fn = B.moe_layer_few_fwd if len(weights) == 3 else B.moe_layer_few_mxfp4_fwd
+    fn(buf.shape, x, w_router, *weights, buf.out, buf.topk_idx, buf.topk_w, buf.ws, stream)
+    return buf.out
+
+
+def quantize_experts(w_gate, w_up, w_down, stream=None):
+    """The experts' weights in microscaled 4-bit floating point, blocks along each contraction: (q, scales) of W_gate, W_up [E', f, d / 2]
+    and W_down [E', d, f / 2].  Once, when a model is loaded."""
+    import torch
+    got = []
+    for w in (w_gate, w_up, w_down):
+        E, K, C = w.shape
+        q = torch.empty(E, C, K // 2, dtype=torch.uint8, device=w.device)
+        scales = torch.empty(E, C, K // 32, dtype=torch.uint8, device=w.device)
+        B.moe_mxfp4_quantize_t(w, q, scales, stream)
+        got += [q, scales]
+    return tuple(got)
+
+
+def layer_mxfp4_forward(buf: MoeLayerBuffers, x, weights, logits=None, w_router=None, stream=None):
+    """layer_forward on weights that quantize_experts returned (a prompt; nothing is kept for a backward pass).  Returns buf.out."""
+    s = buf.shape
+    if w_router is not None:
+        B.moe_router_route_fwd(s, x, w_router, buf.logits, buf.topk_idx, buf.topk_w, buf.probs, buf.ws, stream)
+    elif logits is not None:
+        B.moe_route_topk(s, logits, buf.topk_idx, buf.topk_w, buf.probs, stream)
+    B.moe_permute(s, x, buf.topk_idx, buf.x_perm, buf.counts, buf.offsets, buf.row_of_slot, buf.slot_of_row, buf.ws, stream)
+    B.moe_mxfp4_grouped_ffn_fwd(s, buf.x_perm, buf.offsets, *weights, buf.y_perm, buf.ws, stream)
+    B.moe_unpermute_combine(s, buf.y_perm, buf.row_of_slot, buf.topk_w, buf.out, stream)
+    return buf.out

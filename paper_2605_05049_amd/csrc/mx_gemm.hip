@@ -7,12 +7,15 @@
 // wavefront's columns (CPL = columns per lane), lane l ends up with columns CPL (l / 16) .. + CPL - 1 of row l % 16.
 #include "mx_gemm.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace moe {
 
 constexpr int MXR = 128;   // rows of a tile
 
 template <int KIND>
-__global__ __launch_bounds__(256) void mx_gemm_kernel(const MxGemmArgs A) {
+__global__ __launch_bounds__(256) void mx_small_kernel(const MxGemmArgs A) {
   constexpr int NW = KIND == MX_GATE_UP ? 2 : 1;
   constexpr int WC = 64 / NW;          // columns of a wavefront, of either weight
   constexpr int FR = WC / 16;          // their frags
@@ -21,9 +24,9 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(const MxGemmArgs A) {
   const int m = lane & 15, q = lane >> 4;
   const int n_ct = (A.n + 2 * WC - 1) / (2 * WC);
   const int u = blockIdx.x / n_ct, ct = blockIdx.x % n_ct;
-  MxTile T;
-  if (!mx_find_tile<MXR>(A.offsets, A.E, u, lane, T)) return;
-  const int r0 = T.lo + (wave & 1) * 64, c0 = (ct * 2 + (wave >> 1)) * WC;
+  MxSegment T;
+  if (!mx_find_expert<MXR>(A.offsets, A.E, u, lane, T)) return;
+  const int r0 = T.lo + (u - T.first) * MXR + (wave & 1) * 64, c0 = (ct * 2 + (wave >> 1)) * WC;
   if (r0 >= T.hi || c0 >= A.n) return;
   const int kb = A.k / kMxBlock;
   size_t xrow[4], wrow[FR];
@@ -97,12 +100,256 @@ __global__ __launch_bounds__(256) void mx_gemm_kernel(const MxGemmArgs A) {
   }
 }
 
+// ---- large problems ----------------------------------------------------------------------------------------------------------------------
+//
+// 256 rows x 256 weight rows (of a pair 128 columns of W_gate and the same of W_up) per block of 4 wavefronts, one per SIMD, each 128 x 128: at
+// 4 bits the matrix cores need an operand byte for every 64 multiplies, so what counts is how often a byte leaves LDS, and a wavefront's
+// tile of 128 x 128 reads half of what four of 64 x 64 would.  Its 256 accumulators leave half of the registers for two sets of fragments: one
+// is multiplied while the other is read.
+//
+// A stage is 256 k (128 bytes of a row), two of them in LDS; rows lie as in the bf16 kernels (chunk c of row r at c ^ ((r >> 1) & 7)), the
+// weights' rows in the order in which the fragments take them.  The scales of a stage go through registers into LDS, turned so that one
+// 8-byte read gives a lane the codes of all its fragments.  One barrier per stage, in its middle: what is read after it has landed
+// before, and what has been read before it is overwritten after.
+constexpr int MXT = 256;              // rows, and weight rows, of a tile
+constexpr int MX_STAGE = MXT * 128;   // bytes of an operand's stage
+constexpr int MX_XCDS = 8, MX_CHUNK = 32;   // consecutive tiles that go to one XCD
+constexpr int MX_BAND = 8;            // row tiles walked side by side
+
+template <int OW, int OX>
+__device__ __forceinline__ mx_f32x4 mx_mfma(const int4& w, const int4& x, const mx_f32x4& acc, int ws, int xs) {
+  const mx_i32x8 a = {w.x, w.y, w.z, w.w, 0, 0, 0, 0}, b = {x.x, x.y, x.z, x.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, OW, ws, OX, xs);
+}
+template <class F, int... I>
+__device__ __forceinline__ void mx_each(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void mx_for(F&& f) { mx_each(static_cast<F&&>(f), std::make_integer_sequence<int, N>{}); }
+
+// Frag a's row m of a wavefront's weight rows -> its column among the wavefront's 128 (64 of either of a pair): lane l's elements of frags 2 p
+// and 2 p + 1 are 8 consecutive columns, 32 p + 8 (l / 16) .. + 7, and the four lanes of a row hold a block of 32.
+__device__ __forceinline__ int mx_column(int a, int m) { return 32 * (a >> 1) + 8 * (m >> 2) + 4 * (a & 1) + (m & 3); }
+
+template <int KIND>
+__global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
+  constexpr bool PAIR = KIND == MX_GATE_UP;
+  constexpr int COLS = PAIR ? MXT / 2 : MXT;   // columns of the result per tile
+  __shared__ __attribute__((aligned(1024))) char lds[2][2][MX_STAGE];   // [stage][x, w]
+  __shared__ __attribute__((aligned(16))) char sc[2][2][8 * 256];      // scales: [stage][x, w][block][row group, m, frag]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int m = lane & 15, q = lane >> 4;
+  const int wr = wave & 1, wc = wave >> 1;
+
+  // block -> tile: chunks of consecutive tiles go to the XCDs in turn; an expert's tiles are walked in bands of row tiles, down the columns
+  const int n_ct = (A.n + COLS - 1) / COLS;
+  const int within = blockIdx.x / MX_XCDS, xcd = blockIdx.x % MX_XCDS;
+  const int lid = (within / MX_CHUNK * MX_XCDS + xcd) * MX_CHUNK + within % MX_CHUNK;
+  MxSegment S;
+  if (!mx_find_expert<MXT>(A.offsets, A.E, lid / n_ct, lane, S)) return;
+  const int e_tiles = (S.hi - S.lo + MXT - 1) / MXT;
+  const int local = lid - S.first * n_ct, band = local / (MX_BAND * n_ct), in_band = local - band * MX_BAND * n_ct;
+  const int b_rows = min(MX_BAND, e_tiles - band * MX_BAND);
+  const int ct = in_band / b_rows, rt = band * MX_BAND + in_band % b_rows;
+  const int r0 = S.lo + rt * MXT, n_rows = min(MXT, S.hi - r0);
+  const int c0 = ct * COLS;
+  const int kb = A.k / kMxBlock, nt = (kb + 7) / 8;
+
+  auto run = [&](auto rb_c) __attribute__((always_inline)) {
+    constexpr int RB = decltype(rb_c)::value;   // row frags of a wavefront: 32 RB rows in all
+    constexpr int XI = RB;                      // direct loads of x per wavefront and stage (of 8 rows)
+    // ---- addresses, from a base per tile and 32 bits.  Instruction i of wavefront w brings rows 8 (w XI + i) .. + 7 of x and LDS rows
+    // 8 (8 w + i) .. + 7 of the weights, LDS row r being frag (r / 16) % 8, m = r % 16 of wavefront column r / 128; lane l row l / 8 of them, and
+    // the chunk that belongs at position l % 8 (which depends on the parity of the instruction)
+    const unsigned pitch = (unsigned)kb * 16;
+    const uint8_t* const xb = A.x + (size_t)r0 * pitch;
+    const size_t e_row0 = (size_t)S.expert * A.n + c0;
+    const bool up = PAIR && (wave & 1);   // (wavefront w loads LDS rows 64 w .. 64 w + 63: of a pair either all gate or all up)
+    const uint8_t* const wb = (up ? A.w1 : A.w0) + e_row0 * pitch;
+    auto w_column = [&](int row) {   // LDS row -> column of the tile
+      const int g = row >> 7, a = (row >> 4) & 7;
+      return min(PAIR ? 64 * g + mx_column(a & 3, row & 15) : 128 * g + mx_column(a, row & 15), A.n - 1 - c0);
+    };
+    unsigned xo[XI], wo[8];
+#pragma unroll
+    for (int i = 0; i < XI; i++) xo[i] = (unsigned)min(8 * (wave * XI + i) + (lane >> 3), n_rows - 1) * pitch;
+#pragma unroll
+    for (int i = 0; i < 8; i++) wo[i] = (unsigned)w_column(8 * (wave * 8 + i) + (lane >> 3)) * pitch;
+    const int chunk = (lane & 7) ^ (lane >> 4);
+    auto chunk_offset = [&](int t, int instruction) __attribute__((always_inline)) {   // (blocks past the end: any bytes, their scales are zero)
+      return (unsigned)min(8 * t + (chunk ^ (4 * (instruction & 1))), kb - 1) * 16u;
+    };
+    auto load_x = [&](int t, int i) __attribute__((always_inline)) {
+      direct_load16(xb, xo[i] + chunk_offset(t, wave * XI + i), &lds[t & 1][0][(wave * XI + i) * 1024]);
+    };
+    auto load_w = [&](int t, int i) __attribute__((always_inline)) {
+      direct_load16(wb, wo[i] + chunk_offset(t, i), &lds[t & 1][1][(wave * 8 + i) * 1024]);
+    };
+    // ---- scales: thread r brings those of row r and of LDS row r of the weights
+    const int sr = min(tid, 32 * RB - 1);
+    const uint8_t* const xsp = A.xs + (size_t)(r0 + min(sr, n_rows - 1)) * kb;
+    const bool s_up = PAIR && ((tid >> 6) & 1);
+    const uint8_t* const wsp = (s_up ? A.ws1 : A.ws0) + (e_row0 + w_column(tid)) * kb;
+    const int xpos = (sr / (16 * RB)) * 128 + (sr & 15) * 8 + (sr % (16 * RB)) / 16;
+    const int wpos = (tid >> 7) * 128 + (tid & 15) * 8 + ((tid >> 4) & 7);
+    unsigned long long xsv, wsv;
+    auto load_scales = [&](int t) __attribute__((always_inline)) {   // (rows of scales have any alignment; the last 8 of a row: zeros follow)
+      const int o = min(8 * t, kb - 8);
+      __builtin_memcpy(&xsv, xsp + o, 8);
+      __builtin_memcpy(&wsv, wsp + o, 8);
+    };
+    auto write_scales = [&](int t) __attribute__((always_inline)) {
+      const int past = 8 * (8 * t - min(8 * t, kb - 8));
+      const unsigned long long x = xsv >> past, w = wsv >> past;
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        sc[t & 1][0][j * 256 + xpos] = (char)(x >> (8 * j));
+        sc[t & 1][1][j * 256 + wpos] = (char)(w >> (8 * j));
+      }
+    };
+    // ---- fragments
+    struct Set { int4 x[RB], w[8]; int xs[2], ws[2]; } set[2];
+    const unsigned frag_off = (unsigned)(m * 128 + ((q ^ ((m >> 1) & 7)) << 4));   // (half 1: chunk + 4, i.e. ^ 64)
+    auto read_x = [&](Set& F, int t, int h, int b) __attribute__((always_inline)) {
+      F.x[b] = *reinterpret_cast<const int4*>(&lds[t & 1][0][(wr * RB + b) * 2048 + (frag_off ^ (unsigned)(h * 64))]);
+    };
+    auto read_w = [&](Set& F, int t, int h, int a) __attribute__((always_inline)) {
+      F.w[a] = *reinterpret_cast<const int4*>(&lds[t & 1][1][(wc * 8 + a) * 2048 + (frag_off ^ (unsigned)(h * 64))]);
+    };
+    auto read_s = [&](Set& F, int t, int h) __attribute__((always_inline)) {
+      const int2 x = *reinterpret_cast<const int2*>(&sc[t & 1][0][(4 * h + q) * 256 + wr * 128 + m * 8]);
+      const int2 w = *reinterpret_cast<const int2*>(&sc[t & 1][1][(4 * h + q) * 256 + wc * 128 + m * 8]);
+      F.xs[0] = x.x; F.xs[1] = x.y; F.ws[0] = w.x; F.ws[1] = w.y;
+    };
+    mx_f32x4 acc[8][RB];
+#pragma unroll
+    for (int a = 0; a < 8; a++)
+#pragma unroll
+      for (int b = 0; b < RB; b++) acc[a][b] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+    // 8 groups of RB products, `between(a)` before each
+    auto multiply = [&](const Set& F, auto&& between) __attribute__((always_inline)) {
+      mx_for<8>([&](auto ac) __attribute__((always_inline)) {
+        constexpr int a = decltype(ac)::value;
+        between(a);
+        __builtin_amdgcn_sched_barrier(0);
+        mx_for<RB>([&](auto bc) __attribute__((always_inline)) {
+          constexpr int b = decltype(bc)::value;
+          acc[a][b] = mx_mfma<(a & 3), (b & 3)>(F.w[a], F.x[b], acc[a][b], F.ws[a >> 2], F.xs[b >> 2]);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    auto load_part = [&](int t, int a) __attribute__((always_inline)) {   // one eighth of a stage
+      if (a < XI) load_x(t, a);
+      load_w(t, a);
+    };
+#pragma unroll
+    for (int a = 0; a < 8; a++) load_part(0, a);
+    load_scales(0);
+    write_scales(0);
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0)
+    __syncthreads();
+    if (nt > 1) {
+#pragma unroll
+      for (int a = 0; a < 8; a++) load_part(1, a);
+      load_scales(1);
+    }
+    read_s(set[0], 0, 0);
+#pragma unroll
+    for (int b = 0; b < RB; b++) read_x(set[0], 0, 0, b);
+#pragma unroll
+    for (int a = 0; a < 8; a++) read_w(set[0], 0, 0, a);
+    // One stage: its first half is multiplied while the second is read, the second while the next stage's first half is read and the stage
+    // after that is requested.
+    auto stage = [&](int t, auto more_c, auto more2_c) __attribute__((always_inline)) {
+      constexpr bool MORE = decltype(more_c)::value, MORE2 = decltype(more2_c)::value;
+      multiply(set[0], [&](int a) __attribute__((always_inline)) {
+        if (a == 0) read_s(set[1], t, 1);
+        if (a < RB) read_x(set[1], t, 1, a);
+        read_w(set[1], t, 1, a);
+      });
+      if constexpr (MORE) {
+        write_scales(t + 1);
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __syncthreads();
+      } else {
+        if (kb - 8 * t <= 4) return;   // (the half has no blocks)
+      }
+      multiply(set[1], [&](int a) __attribute__((always_inline)) {
+        if constexpr (MORE) {
+          if (a == 0) read_s(set[0], t + 1, 0);
+          if (a < RB) read_x(set[0], t + 1, 0, a);
+          read_w(set[0], t + 1, 0, a);
+        }
+        if constexpr (MORE2) {
+          load_part(t + 2, a);
+          if (a == 7) load_scales(t + 2);
+        }
+      });
+    };
+    int t = 0;
+    for (; t + 2 < nt; t++) stage(t, std::true_type{}, std::true_type{});
+    if (t + 1 < nt) stage(t++, std::true_type{}, std::false_type{});
+    stage(t, std::false_type{}, std::false_type{});
+    // ---- results: acc[a][b][i] is row 16 (wr RB + b) + m, column mx_column(a, 4 q + i) of the wavefront's
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+      const int row = 16 * (wr * RB + b) + m;
+      if (row >= n_rows) continue;
+      if constexpr (!PAIR) {
+        uint16_t* const dst = A.y + (size_t)(r0 + row) * A.n;
+#pragma unroll
+        for (int p = 0; p < 4; p++) {
+          const int col = c0 + wc * 128 + 32 * p + 8 * q;
+          const mx_f32x4 lo = acc[2 * p][b], hi = acc[2 * p + 1][b];
+          const float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          if (col < A.n) *reinterpret_cast<uint4*>(dst + col) = pack8(f);
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < 2; p++) {
+          const int col = c0 + wc * 64 + 32 * p + 8 * q;
+          float f[8];
+          unsigned e = 0;
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            const float g = acc[2 * p + (i >> 2)][b][i & 3], v = acc[4 + 2 * p + (i >> 2)][b][i & 3];
+            f[i] = g / (1.0f + __expf(-g)) * v;
+            e = max(e, (__float_as_uint(f[i]) >> 23) & 255u);
+          }
+          // (the four lanes of a row are in or out together)
+          e = max(e, (unsigned)__shfl_xor((int)e, 16));
+          e = max(e, (unsigned)__shfl_xor((int)e, 32));
+          const unsigned s = mx_scale_code(e);
+          if (col < A.n) {
+            *reinterpret_cast<uint32_t*>(A.h + ((size_t)(r0 + row) * A.n + col) / 2) = mx_encode8(f, s);
+            if (q == 0) A.hs[((size_t)(r0 + row) * A.n + col) / kMxBlock] = (uint8_t)s;
+          }
+        }
+      }
+    }
+  };
+  if (n_rows > 192) run(std::integral_constant<int, 8>{});
+  else if (n_rows > 128) run(std::integral_constant<int, 6>{});
+  else if (n_rows > 64) run(std::integral_constant<int, 4>{});
+  else if (n_rows > 32) run(std::integral_constant<int, 2>{});
+  else run(std::integral_constant<int, 1>{});
+}
+
+template <int KIND>
+static void launch_kind(const char* label, hipStream_t st, const MxGemmArgs& A, long long rows) {
+  const int cols = KIND == MX_GATE_UP ? MXT / 2 : MXT, small_cols = KIND == MX_GATE_UP ? 64 : 128;
+  const long long tiles = (rows / MXT + A.E) * ((A.n + cols - 1) / cols);   // (at most)
+  if (A.k >= 8 * kMxBlock && rows * (A.n / cols) >= 64ll * MXT) {   // (the tile kernel reads 8 scales of a row at once)
+    const long long round = MX_XCDS * MX_CHUNK;
+    MOE_LAUNCH(label, st, (mx_tile_kernel<KIND>), dim3((unsigned)((tiles + round - 1) / round * round)), dim3(256), 0, st, A);
+  } else {
+    MOE_LAUNCH(label, st, (mx_small_kernel<KIND>), dim3((unsigned)((rows / MXR + A.E) * ((A.n + small_cols - 1) / small_cols))), dim3(256), 0, st, A);
+  }
+}
+
 void launch_mx_gemm(const char* label, hipStream_t st, MxKind kind, const MxGemmArgs& A, long long rows) {
-  const long long row_tiles = rows / MXR + A.E;   // (at most)
-  const int wc = kind == MX_GATE_UP ? 64 : 128;
-  const dim3 grid((unsigned)(row_tiles * ((A.n + wc - 1) / wc)));
-  if (kind == MX_GATE_UP) MOE_LAUNCH(label, st, (mx_gemm_kernel<MX_GATE_UP>), grid, dim3(256), 0, st, A);
-  else MOE_LAUNCH(label, st, (mx_gemm_kernel<MX_PRODUCT>), grid, dim3(256), 0, st, A);
+  if (kind == MX_GATE_UP) launch_kind<MX_GATE_UP>(label, st, A, rows);
+  else launch_kind<MX_PRODUCT>(label, st, A, rows);
 }
 
 }  // namespace moe

@@ -33,9 +33,9 @@ __device__ __forceinline__ unsigned mx_encode8(const float (&x)[8], unsigned s) 
 
 // The expert that row tile u belongs to, among tiles of TILE rows of each expert's segment; false past the last tile.  Every wavefront looks
 // for itself: 64 experts at a time, one per lane, until the running sum of their tiles passes u.
-struct MxTile { int expert, lo, hi; };   // rows lo .. hi - 1
+struct MxSegment { int expert, lo, hi, first; };   // rows lo .. hi - 1, index of the first tile
 template <int TILE>
-__device__ __forceinline__ bool mx_find_tile(const int32_t* __restrict__ offsets, int E, int u, int lane, MxTile& T) {
+__device__ __forceinline__ bool mx_find_expert(const int32_t* __restrict__ offsets, int E, int u, int lane, MxSegment& S) {
   int before = 0;
   for (int e0 = 0; e0 < E; e0 += kWave) {
     const int e = min(e0 + lane, E - 1);
@@ -45,10 +45,10 @@ __device__ __forceinline__ bool mx_find_tile(const int32_t* __restrict__ offsets
     const unsigned long long past = __ballot(incl > u);
     if (past) {
       const int l = __builtin_ctzll(past);
-      const int first = __builtin_amdgcn_readlane(incl - n, l), e_lo = __builtin_amdgcn_readlane(lo, l);
-      T.expert = e0 + l;
-      T.lo = e_lo + (u - first) * TILE;
-      T.hi = min(T.lo + TILE, __builtin_amdgcn_readlane(hi, l));
+      S.expert = e0 + l;
+      S.first = __builtin_amdgcn_readlane(incl - n, l);
+      S.lo = __builtin_amdgcn_readlane(lo, l);
+      S.hi = __builtin_amdgcn_readlane(hi, l);
       return true;
     }
     before = __builtin_amdgcn_readlane(incl, kWave - 1);

@@ -92,6 +92,8 @@ def _mx(rng, *shape, std=1.0):
 @pytest.mark.parametrize("E,rows,n,k,dead", [
     (1, 1, 8, 32, 0), (1, 17, 64, 64, 0), (3, 1, 64, 128, 0), (4, 100, 72, 96, 1), (8, 300, 256, 512, 2), (5, 777, 328, 1088, 0), (130, 500, 64, 160, 60),
     (2, 1000, 512, 2048, 0), (1000, 64, 64, 64, 0), (7, 129, 1000, 224, 3), (2, 512, 640, 4128, 0),
+    # enough rows for the large tiles: every height of an expert's last tile, results and contractions that end inside a tile
+    (3, 9000, 520, 1088, 0), (40, 12000, 600, 288, 3), (2, 5000, 1024, 4128, 0), (300, 20000, 264, 256, 100), (9, 8300, 776, 672, 0),
 ])
 def test_grouped_gemm(moe, E, rows, n, k, dead):
     rng = np.random.default_rng([E, rows, n, k])
@@ -126,6 +128,7 @@ def test_grouped_gemm_scales_and_nan_blocks(moe):
 
 @pytest.mark.parametrize("E,rows,d,f,dead", [
     (1, 1, 64, 64, 0), (4, 50, 128, 192, 1), (8, 512, 512, 1024, 0), (3, 333, 1088, 320, 0), (70, 256, 128, 64, 30), (2, 700, 320, 704, 0),
+    (6, 7000, 320, 704, 1), (40, 9000, 576, 448, 4), (2, 5000, 1088, 512, 0),
 ])
 def test_grouped_ffn(moe, E, rows, d, f, dead):
     rng = np.random.default_rng([E, rows, d, f])

@@ -22,6 +22,7 @@ constexpr int kFewSlots = 4096;       // T * K' at most
 constexpr int kFewWaves = 8;          // wavefronts of a block that share a contraction
 constexpr int kFewFusedSlots = 512, kFewFusedExperts = 256;   // at most, where every block makes the gate for itself
 constexpr int kFewGroup = 16;         // tokens of an MFMA
+constexpr int kFewBlocks = 512;       // two per CU
 
 // The experts that have tokens, in expert order, and the slots of each.
 struct FewSched {
@@ -30,13 +31,23 @@ struct FewSched {
   int32_t slots[kFewSlots];   // t * K' + j
 };
 
+// Cleared by the launch before the one that uses them.  Counters that many blocks use lie in lines of their own.
+constexpr int kFewLists = 64;
+struct FewLine { int32_t n, pad[31]; };
+struct FewCounters {
+  FewLine taken[2][kFewLists];    // tiles of H, tiles of W_down: taken of each list
+  FewLine ready[kMaxExperts];     // per live expert: tiles of H that are there
+  int32_t arrivals[1];            // per column tile of the down projection: parts that are there (d / 32 at most)
+};
+inline size_t few_counters_bytes(int d) { return sizeof(FewCounters) + (size_t)(d / 32) * sizeof(int32_t); }
+
 struct FewWeights { const uint8_t* w; const uint8_t* scales; };   // bf16 weights have no scales
 struct FewArgs {
   int T, d, f, E, Es, k, Kp, renorm, parts;   // parts of d_ffn in the down projection
-  int fused_gate;                // the gate is made by few_gate_up_kernel
+  int fused_gate;                // the gate is made by few_layer_kernel
   const uint16_t* x; const uint16_t* w_router;
   float* logits; int32_t* topk_idx; float* topk_w; FewSched* sched;
-  int32_t* arrivals;             // per column tile of the down projection
+  FewCounters* counters;
   FewWeights gate, up, down;
   uint16_t* h; size_t h_lo;      // [N, f] bf16 heads, the remainders h_lo elements further
   float* partial;                // [N, parts, d]
@@ -45,17 +56,37 @@ struct FewArgs {
 
 // ---- logits and gate ---------------------------------------------------------------------------------------------------------------
 
+__device__ __forceinline__ void few_clear(const FewArgs& A) {
+  int32_t* const lists = &A.counters->taken[0][0].n;
+  for (int i = threadIdx.x; i < 2 * kFewLists; i += blockDim.x) lists[32 * i] = 0;
+  for (int i = threadIdx.x; i < A.E + A.Es; i += blockDim.x) A.counters->ready[i].n = 0;
+  for (int i = threadIdx.x; i < A.d / 32; i += blockDim.x) A.counters->arrivals[i] = 0;
+}
+__global__ __launch_bounds__(256) void few_clear_kernel(const FewArgs A) { few_clear(A); }
+
 // 16 experts x 16 tokens per block, K split over the wavefronts, whose sums are added in order.
 __global__ __launch_bounds__(kFewWaves * kWave) void few_router_kernel(const FewArgs A) {
   __shared__ float part[kFewWaves][16][17];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
   const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
+  if (blockIdx.x == 0 && blockIdx.y == 0) few_clear(A);
   const uint16_t* const wr = A.w_router + (size_t)min(e0 + n, A.E - 1) * A.d + 8 * q;
   const uint16_t* const xr = A.x + (size_t)min(t0 + n, A.T - 1) * A.d + 8 * q;
   const int steps = A.d / 32, per = (steps + kFewWaves - 1) / kFewWaves;
   mx_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = wave * per; s < min(steps, (wave + 1) * per); s++)
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const mx_bf16x8*>(wr + s * 32), *reinterpret_cast<const mx_bf16x8*>(xr + s * 32), acc, 0, 0, 0);
+  const int end = min(steps, (wave + 1) * per);
+  for (int s0 = wave * per; s0 < end; s0 += 8) {   // (eight steps requested at once; past the end the last one, not multiplied)
+    mx_bf16x8 w[8], x[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+      const int s = min(s0 + u, end - 1);
+      w[u] = *reinterpret_cast<const mx_bf16x8*>(wr + s * 32);
+      x[u] = *reinterpret_cast<const mx_bf16x8*>(xr + s * 32);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; u++)
+      if (s0 + u < end) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u], x[u], acc, 0, 0, 0);
+  }
 #pragma unroll
   for (int i = 0; i < 4; i++) part[wave][n][4 * q + i] = acc[i];   // [token][expert]
   __syncthreads();
@@ -74,6 +105,7 @@ __global__ __launch_bounds__(1024) void few_gate_kernel(const FewArgs A) {
   __shared__ int count[kMaxExperts], first[kMaxExperts], live_before[kMaxExperts];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int Et = A.E + A.Es, N = A.T * A.Kp;
+  if (!A.w_router) few_clear(A);
   if (A.w_router)
     for (int t = wave; t < A.T; t += 16)
       route_token<kWave, PER>(A.logits + (size_t)t * A.E, t, lane, A.topk_idx, A.topk_w, nullptr, A.E, A.k, A.Es, A.renorm);
@@ -206,12 +238,19 @@ __device__ __forceinline__ int few_row_pitch(int k) { return 2 * k + 16; }
 template <bool LO>
 __device__ __forceinline__ int few_rows_at_once(int k) { return min(kFewGroup, kFewRowBytes / ((LO ? 2 : 1) * few_row_pitch(k))); }
 
+__device__ __forceinline__ uint4 few_load_agent(const uint16_t* p) {   // 16 bytes, past this XCD's L2
+  const unsigned long long* const q = reinterpret_cast<const unsigned long long*>(p);
+  const unsigned long long a = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), b = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_uint4((unsigned)a, (unsigned)(a >> 32), (unsigned)b, (unsigned)(b >> 32));
+}
+
 // acc[a] += over `n_steps` steps from step0 on: lane l's element i of acc[a] is column FR (4 (l / 16) + i) + a, token l % 16 (tokens past the last
 // repeat it).  row(i): element 0 of row i of X, its remainders (LO) x_lo elements further.  Wavefront `part` of PARTS takes its share of the steps;
 // their weights go into registers, DEPTH - 1 steps ahead.
-template <bool MX, int FR, bool LO, int DEPTH, int PARTS, class F>
-__device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<MX, FR>& W, F&& row, size_t x_lo, int K, int n_rows, int step0,
-                                             int n_steps, char* buf, int part, int lane) {
+// Between the first requests and the rows stands `ready()`.
+template <bool MX, int FR, bool LO, int DEPTH, int PARTS, class F, class G>
+__device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<MX, FR>& W, F&& row, G&& ready, size_t x_lo, int K, int n_rows,
+                                             int step0, int n_steps, char* buf, int part, int tid, int lane) {
   typedef FewTile<MX, FR> Tile;
   constexpr int STEP = MX ? 128 : 32, THREADS = kFewWaves * kWave;
   const int pitch = few_row_pitch(n_steps * STEP), pieces = n_steps * STEP / 8, total = n_rows * pieces;
@@ -225,8 +264,12 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<
     const int r = i / pieces, k = step0 * STEP + 8 * (i - r * pieces);
     if (i < total && k < K) {
       const uint16_t* const src = row(r) + k;
-      p.v = *reinterpret_cast<const uint4*>(src);
-      if constexpr (LO) p.w = *reinterpret_cast<const uint4*>(src + x_lo);
+      if constexpr (LO) {   // (written in this launch)
+        p.v = few_load_agent(src);
+        p.w = few_load_agent(src + x_lo);
+      } else {
+        p.v = *reinterpret_cast<const uint4*>(src);
+      }
     }
     return p;
   };
@@ -237,10 +280,11 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<
     *reinterpret_cast<uint4*>(to) = p.v;
     if constexpr (LO) *reinterpret_cast<uint4*>(to + n_rows * pitch) = p.w;
   };
-  const int tid = threadIdx.x;
-  const Piece p0 = bring(tid);
 #pragma unroll
-  for (int i = 0; i < DEPTH - 1; i++) W.load(st[i], step0 + min(first + i, last));
+  for (int i = 0; i < DEPTH; i++)
+    if (i < count) W.load(st[i], step0 + first + i);
+  ready();
+  const Piece p0 = bring(tid);
   __syncthreads();   // (what was in LDS has been read)
   put(tid, p0);
   for (int i = tid + THREADS; i < total; i += 2 * THREADS) {
@@ -271,13 +315,12 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<
   for (; i < body; i += DEPTH) {
 #pragma unroll
     for (int u = 0; u < DEPTH; u++) {
-      W.load(st[(u + DEPTH - 1) % DEPTH], step0 + min(first + i + u + DEPTH - 1, last));
-      __builtin_amdgcn_sched_barrier(0);
       consume(st[u], i + u);
+      __builtin_amdgcn_sched_barrier(0);
+      W.load(st[u], step0 + min(first + i + u + DEPTH, last));
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  W.load(st[DEPTH - 1], step0 + last);
 #pragma unroll
   for (int u = 0; u < DEPTH; u++) {
     if (i + u < count) {
@@ -302,213 +345,251 @@ __device__ __forceinline__ void few_put(float* dst, const mx_f32x4 (&acc)[FR]) {
   }
 }
 
-// The live expert `index` among the slots' experts `idx` (in LDS, N of them): its id, its slots into `slots`; false if there are fewer.  With `all`,
-// the whole schedule goes there as well.
-struct FewLive { int expert, count; };
-__device__ __forceinline__ bool few_find_live(const int* idx, int N, int index, int* slots, unsigned* words, int* found, FewSched* all, FewLive& L) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  if (tid < kFewFusedExperts / 32) words[tid] = 0;   // (the fused gate has at most 256 ids)
-  __syncthreads();
-  for (int s = tid; s < N; s += kFewWaves * kWave) atomicOr(&words[idx[s] >> 5], 1u << (idx[s] & 31));
-  __syncthreads();
-  if (tid < kWave) {   // 4 ids per lane
-    const unsigned bits = (words[lane >> 3] >> (4 * (lane & 7))) & 15u;
-    const int n = __popc(bits), incl = wave_prefix_sum(n), total = __builtin_amdgcn_readlane(incl, kWave - 1);
-    const unsigned long long past = __ballot(incl > index);
-    int expert = -1;
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      unsigned b = __builtin_amdgcn_readlane(bits, l);
-      for (int skip = index - __builtin_amdgcn_readlane(incl - n, l); skip > 0; skip--) b &= b - 1;
-      expert = 4 * l + __builtin_ctz(b);
-    }
-    int count = 0;
-    if (past)
-      for (int s0 = 0; s0 < N; s0 += kWave) {
-        const bool mine = s0 + lane < N && idx[s0 + lane] == expert;
-        const unsigned long long who = __ballot(mine);
-        if (mine) slots[count + __popcll(who & ((1ull << lane) - 1))] = s0 + lane;
-        count += __popcll(who);
-      }
-    if (lane == 0) { found[0] = expert; found[1] = count; }
-    if (all) {   // every live expert's turn, one after the other
-      int at = 0, i = 0;
-      for (int l = 0; l < kWave; l++)
-        for (unsigned b = __builtin_amdgcn_readlane(bits, l); b; b &= b - 1, i++) {
-          const int e = 4 * l + __builtin_ctz(b), first = at;
-          for (int s0 = 0; s0 < N; s0 += kWave) {
-            const bool mine = s0 + lane < N && idx[s0 + lane] == e;
-            const unsigned long long who = __ballot(mine);
-            if (mine) all->slots[at + __popcll(who & ((1ull << lane) - 1))] = s0 + lane;
-            at += __popcll(who);
-          }
-          if (lane == 0) all->live[i] = make_int4(e, first, at - first, 0);
-        }
-      if (lane == 0) all->n_live = total;
-    }
-  }
-  __syncthreads();
-  L.expert = __builtin_amdgcn_readfirstlane(found[0]);
-  L.count = __builtin_amdgcn_readfirstlane(found[1]);
-  return L.expert >= 0;
-}
-
-// H = silu(x W_gate) * (x W_up) of 16 FR columns of one expert; wavefronts 0, 2, 4, 6 make G, the others U, each over a quarter of d.  With the gate
-// fused, every block makes it from the logits for itself (a launch and the wait for it cost more).
-template <bool MX, int FR, int DEPTH>
-__global__ __launch_bounds__(kFewWaves * kWave, 4) void few_gate_up_kernel(const FewArgs A) {
-  constexpr int COLS = 16 * FR, PITCH = COLS + 4;
-  __shared__ __attribute__((aligned(16))) union { char rows[kFewRowBytes]; float part[kFewWaves][kFewGroup][PITCH]; } lds;
-  __shared__ int idx[kFewFusedSlots], list[kFewFusedSlots];
-  __shared__ float weight[kFewFusedSlots];
-  __shared__ unsigned words[kFewFusedExperts / 32];
-  __shared__ int found[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool first_block = blockIdx.x == 0 && blockIdx.y == 0;
-  if (first_block)
-    for (int i = tid; i < (A.d + 31) / 32; i += kFewWaves * kWave) A.arrivals[i] = 0;
-  FewLive L;
-  const int32_t* slots;
-  if (A.fused_gate) {
-    const int N = A.T * A.Kp;
-    if (A.w_router) {
-      for (int t = wave; t < A.T; t += kFewWaves) {
-        if (A.E <= kWave) route_token<kWave, 1>(A.logits + (size_t)t * A.E, t, lane, idx, weight, nullptr, A.E, A.k, A.Es, A.renorm);
-        else route_token<kWave, 4>(A.logits + (size_t)t * A.E, t, lane, idx, weight, nullptr, A.E, A.k, A.Es, A.renorm);
-      }
-    } else {
-      for (int s = tid; s < N; s += kFewWaves * kWave) idx[s] = min(max(A.topk_idx[s], 0), A.E + A.Es - 1);
-    }
-    __syncthreads();
-    if (first_block && A.w_router)
-      for (int s = tid; s < N; s += kFewWaves * kWave) { A.topk_idx[s] = idx[s]; A.topk_w[s] = weight[s]; }
-    if (!few_find_live(idx, N, blockIdx.y, list, words, found, first_block ? A.sched : nullptr, L)) return;
-    slots = list;
-  } else {
-    if ((int)blockIdx.y >= A.sched->n_live) return;
-    const int4 v = few_live(A, blockIdx.y);
-    L.expert = v.x;
-    L.count = v.z;
-    slots = A.sched->slots + v.y;
-  }
-  const int col0 = blockIdx.x * COLS;
-  const FewTile<MX, FR> W(wave & 1 ? A.up : A.gate, L.expert, A.d, A.f, col0, lane);
-  const int steps = few_steps(MX, A.d), at_once = few_rows_at_once<false>(steps * (MX ? 128 : 32));
-  for (int r0 = 0; r0 < L.count; r0 += at_once) {
-    const int n_rows = min(at_once, L.count - r0);
-    mx_f32x4 acc[FR];
-#pragma unroll
-    for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-    few_multiply<MX, FR, false, DEPTH, 4>(acc, W, [&](int r) { return A.x + (size_t)(slots[r0 + r] / A.Kp) * A.d; }, 0, A.d,
-                                          n_rows, 0, steps, lds.rows, wave >> 1, lane);
-    __syncthreads();   // (the rows have been read)
-    few_put(lds.part[wave][lane & 15] + FR * 4 * (lane >> 4), acc);
-    __syncthreads();
-    const int t = tid / (COLS / 2), c = 2 * (tid % (COLS / 2)), row = r0 + t;   // pairs of columns
-    if (t < n_rows) {
-      float v[2][2] = {};
-#pragma unroll
-      for (int w = 0; w < kFewWaves; w++) {
-        const float2 p = *reinterpret_cast<const float2*>(&lds.part[w][t][c]);
-        v[w & 1][0] += p.x;
-        v[w & 1][1] += p.y;
-      }
-      float h[2], lo[2];
-#pragma unroll
-      for (int i = 0; i < 2; i++) few_swiglu(v[0][i], v[1][i], h[i], lo[i]);
-      uint16_t* const o = A.h + (size_t)slots[row] * A.f + col0 + c;
-      *reinterpret_cast<uint32_t*>(o) = pack_bf16(h[0], h[1]);
-      *reinterpret_cast<uint32_t*>(o + A.h_lo) = pack_bf16(lo[0], lo[1]);
-    }
-  }
-}
-
-// The partial sums travel between blocks of one launch, which may run on different XCDs with an L2 each: they are stored and loaded at agent scope,
-// past those caches.  A block counts itself as arrived when its stores have been acknowledged.  (Ordinary stores and a device-wide fence, which
-// writes the L2 back and empties it, make the down projection 3 to 8 times as long.)
-__device__ __forceinline__ void few_store_partial(float* p, float a, float b) {
-  const unsigned long long v = (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a);
-  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// What blocks of one launch hand to each other (they may run on different XCDs, with an L2 each) is stored and loaded at agent scope, past those
+// caches.  A block counts itself as arrived when its stores have been acknowledged.  (Ordinary stores and a device-wide fence, which writes
+// the L2 back and empties it, make the down projection 3 to 8 times as long.)
+__device__ __forceinline__ void few_store_agent(void* p, unsigned a, unsigned b) {
+  __hip_atomic_store(static_cast<unsigned long long*>(p), (unsigned long long)b << 32 | a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ float2 few_load_partial(const float* p) {
   const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
+// Counts this block: all that its threads have stored is then where every block sees it.  True for thread 0 of the one that completes `of`.
+__device__ __forceinline__ bool few_arrive(int32_t* counter, int of) {
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wavefront's stores have been acknowledged
+  __syncthreads();
+  return threadIdx.x == 0 && __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
+}
 
-// out[t] = sum_j w[t, j] sum_parts partial, of `cols` columns from col0 on: by the block that arrives last of the `blocks` that make them.  Slots in
-// order, parts in order, fp32, one rounding.
-__device__ __forceinline__ void few_combine(const FewArgs& A, int tile, int col0, int cols, int blocks, int* last) {
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wavefront's partial sums are where everyone sees them
-  __syncthreads();
-  if (threadIdx.x == 0) *last = __hip_atomic_fetch_add(&A.arrivals[tile], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
-  __syncthreads();
-  if (!*last) return;
-  const int per = min(cols, A.d - col0) / 2;
-  for (int i = threadIdx.x; i < A.T * per; i += blockDim.x) {
-    const int t = i / per, c = col0 + 2 * (i % per);
-    float2 sum = make_float2(0.f, 0.f), y = sum;
-    const int n = A.Kp * A.parts;
-    const float* const src = A.partial + (size_t)t * n * A.d + c;
-    for (int i0 = 0; i0 < n; i0 += 8) {   // (eight at a time: each takes the way to memory)
-      float2 v[8];
-#pragma unroll
-      for (int u = 0; u < 8; u++) v[u] = few_load_partial(src + (size_t)min(i0 + u, n - 1) * A.d);
-#pragma unroll
-      for (int u = 0; u < 8; u++) {
-        if (i0 + u < n) {
-          y.x += v[u].x; y.y += v[u].y;
-          if ((i0 + u) % A.parts == A.parts - 1) {
-            const float w = A.topk_w[t * A.Kp + (i0 + u) / A.parts];
-            sum.x += w * y.x; sum.y += w * y.y;
-            y = make_float2(0.f, 0.f);
+// The live expert `index` among the slots' experts `idx` (in LDS, N of them), its slots into `slots`; n_live: how many there are.  Ends with the
+// answers in `found` ({expert, slots, n_live}), before a barrier.
+__device__ __forceinline__ void few_find_live(const int* idx, int N, int index, int* slots, const unsigned* words, int* found) {
+  const int lane = threadIdx.x & 63;
+  if (threadIdx.x >= kWave) return;
+  // 4 ids per lane
+  const unsigned bits = (words[lane >> 3] >> (4 * (lane & 7))) & 15u;
+  const int n = __popc(bits), incl = wave_prefix_sum(n);
+  const unsigned long long past = __ballot(incl > index);
+  int expert = -1, count = 0;
+  if (past) {
+    const int l = __builtin_ctzll(past);
+    unsigned b = __builtin_amdgcn_readlane(bits, l);
+    for (int skip = index - __builtin_amdgcn_readlane(incl - n, l); skip > 0; skip--) b &= b - 1;
+    expert = 4 * l + __builtin_ctz(b);
+    for (int s0 = 0; s0 < N; s0 += kWave) {
+      const bool mine = s0 + lane < N && idx[s0 + lane] == expert;
+      const unsigned long long who = __ballot(mine);
+      if (mine) slots[count + __popcll(who & ((1ull << lane) - 1))] = s0 + lane;
+      count += __popcll(who);
+    }
+  }
+  if (lane == 0) { found[0] = expert; found[1] = count; found[2] = __builtin_amdgcn_readlane(incl, kWave - 1); }
+}
+
+// The whole layer from the logits on, in one launch.  Its work is a list of tiles: H = silu(x W_gate) * (x W_up) of 16 FR columns, expert after
+// expert, then the parts of H W_down of 16 FR columns, expert after expert.  A block takes the next tile when it has done one, so that no CU waits at
+// the end of an expert or of the first half.  The tiles are dealt to 64 lists of either kind, each with a counter (one counter for all costs 35 ns
+// for every tile, one after the other); a block takes from its own list, then from those that have tiles left.  A tile of W_down waits for its
+// expert's tiles of H, with its own first weights on the way, and no block comes to one before all tiles of H have been taken: by blocks that are
+// running, whatever else is on the GPU, so every wait ends.  The last part of a column tile of W_down adds the parts and experts.
+//
+// Of the pair wavefronts 0, 2, 4, 6 make G, the others U, each over a quarter of d; of W_down each takes an eighth of its part of d_ffn.  With the
+// gate fused, every block makes it from the logits for itself (a launch and the wait for it cost more).
+template <bool MX, int FR, int DEPTH>
+__global__ __launch_bounds__(kFewWaves * kWave, 4) void few_layer_kernel(const FewArgs A) {
+  constexpr int COLS = 16 * FR, PITCH = COLS + 4, STEP = MX ? 128 : 32;
+  __shared__ __attribute__((aligned(16))) union { char rows[kFewRowBytes]; float part[kFewWaves][kFewGroup][PITCH]; } lds;
+  __shared__ int idx[kFewFusedSlots], list[kFewFusedSlots];
+  __shared__ float weight[kFewFusedSlots];
+  __shared__ unsigned words[kFewFusedExperts / 32];
+  __shared__ int found[3], next, last;
+  int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int N = A.T * A.Kp;
+  const int list_id = blockIdx.x % kFewLists;
+  auto take = [&](int kind, int l) __attribute__((always_inline)) {   // the next tile of list l
+    return __hip_atomic_fetch_add(&A.counters->taken[kind][l].n, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) * kFewLists + l;
+  };
+  int h_ticket = 0, d_ticket = 0;   // (thread 0)
+  if (tid == 0) { h_ticket = take(0, list_id); d_ticket = take(1, list_id); }
+  const float* topk_w = A.topk_w;
+  int n_live;
+  if (A.fused_gate) {
+    if (tid < kFewFusedExperts / 32) words[tid] = 0;
+    if (A.w_router) {
+      for (int t = wave; t < A.T; t += kFewWaves) {
+        if (A.E <= kWave) route_token<kWave, 1>(A.logits + (size_t)t * A.E, t, lane, idx, weight, nullptr, A.E, A.k, A.Es, A.renorm);
+        else route_token<kWave, 4>(A.logits + (size_t)t * A.E, t, lane, idx, weight, nullptr, A.E, A.k, A.Es, A.renorm);
+      }
+      topk_w = weight;
+    } else {
+      for (int s = tid; s < N; s += kFewWaves * kWave) idx[s] = min(max(A.topk_idx[s], 0), A.E + A.Es - 1);
+    }
+    __syncthreads();
+    for (int s = tid; s < N; s += kFewWaves * kWave) {
+      atomicOr(&words[idx[s] >> 5], 1u << (idx[s] & 31));
+      if (blockIdx.x == 0 && A.w_router) { A.topk_idx[s] = idx[s]; A.topk_w[s] = weight[s]; }
+    }
+    __syncthreads();
+    int n = 0;
+    for (int i = 0; i < kFewFusedExperts / 32; i++) n += __popc(words[i]);
+    n_live = __builtin_amdgcn_readfirstlane(n);
+  } else {
+    n_live = __builtin_amdgcn_readfirstlane(A.sched->n_live);
+  }
+  const int h_tiles = A.f / COLS, d_tiles = A.d / COLS, n_h = n_live * h_tiles, n_d = n_live * d_tiles * A.parts;
+  const int h_steps = few_steps(MX, A.d), d_steps = few_steps(MX, A.f), per = (d_steps + A.parts - 1) / A.parts;
+  int current = -1, expert = 0, count = 0;   // the live expert whose slots are at hand
+  const int* slots = list;
+
+  int kind = 0;
+  while (true) {
+    asm volatile("" : "+v"(tid), "+v"(lane));   // (nothing that a tile makes of them is kept in registers from one tile to the next)
+    const bool down = kind == 1;
+    const int n_tiles = down ? n_d : n_h;
+    if (tid == 0) next = down ? d_ticket : h_ticket;
+    __syncthreads();   // (and what the tile before has left in LDS has been read)
+    int item = __builtin_amdgcn_readfirstlane(next);
+    if (item >= n_tiles) {   // this list is empty: which are not?
+      if (tid < kWave) {
+        const int taken = __hip_atomic_load(&A.counters->taken[kind][tid].n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        unsigned long long left = __ballot((long long)taken * kFewLists + tid < n_tiles);
+        if (tid == 0) {
+          int got = -1;
+          if (left) {
+            const unsigned long long after = left & ~((2ull << list_id) - 1);   // (from the own one on, so that not all take from the same)
+            got = take(kind, __builtin_ctzll(after ? after : left));
           }
+          last = got;
+        }
+      }
+      __syncthreads();
+      item = __builtin_amdgcn_readfirstlane(last);
+      if (item < 0) {
+        if (down) break;
+        kind = 1;
+        continue;
+      }
+      if (item >= n_tiles) continue;
+    } else if (tid == 0) {
+      if (down) d_ticket = take(1, list_id);
+      else h_ticket = take(0, list_id);
+    }
+    const int local = item, tiles = down ? d_tiles * A.parts : h_tiles;
+    const int live = local / tiles, in_expert = local - live * tiles;
+    if (live != current) {
+      current = live;
+      if (A.fused_gate) {
+        few_find_live(idx, N, live, list, words, found);
+        __syncthreads();
+        expert = __builtin_amdgcn_readfirstlane(found[0]);
+        count = __builtin_amdgcn_readfirstlane(found[1]);
+      } else {
+        const int4 v = few_live(A, live);
+        expert = v.x;
+        count = v.z;
+        slots = A.sched->slots + v.y;
+      }
+    }
+    if (!down) {
+      const int col0 = in_expert * COLS;
+      const FewTile<MX, FR> W(wave & 1 ? A.up : A.gate, expert, A.d, A.f, col0, lane);
+      const int at_once = few_rows_at_once<false>(h_steps * STEP);
+      for (int r0 = 0; r0 < count; r0 += at_once) {
+        const int n_rows = min(at_once, count - r0);
+        mx_f32x4 acc[FR];
+#pragma unroll
+        for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+        few_multiply<MX, FR, false, DEPTH, 4>(acc, W, [&](int r) { return A.x + (size_t)(slots[r0 + r] / A.Kp) * A.d; }, [] {}, 0, A.d, n_rows, 0, h_steps,
+                                              lds.rows, wave >> 1, tid, lane);
+        __syncthreads();   // (the rows have been read)
+        few_put(lds.part[wave][lane & 15] + FR * 4 * (lane >> 4), acc);
+        __syncthreads();
+        const int t = tid / (COLS / 4), c = 4 * (tid % (COLS / 4));   // four columns
+        if (t < n_rows) {
+          float v[2][4] = {};
+#pragma unroll
+          for (int w = 0; w < kFewWaves; w++) {
+            const float4 p = *reinterpret_cast<const float4*>(&lds.part[w][t][c]);
+            v[w & 1][0] += p.x; v[w & 1][1] += p.y; v[w & 1][2] += p.z; v[w & 1][3] += p.w;
+          }
+          float h[4], lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; i++) few_swiglu(v[0][i], v[1][i], h[i], lo[i]);
+          uint16_t* const o = A.h + (size_t)slots[r0 + t] * A.f + col0 + c;
+          few_store_agent(o, pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+          few_store_agent(o + A.h_lo, pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]));
+        }
+      }
+      few_arrive(&A.counters->ready[live].n, h_tiles);
+    } else {
+      const int ct = in_expert % d_tiles, part = in_expert / d_tiles, col0 = ct * COLS;
+      const int step0 = min(d_steps, part * per), step1 = min(d_steps, step0 + per);
+      const FewTile<MX, FR> W(A.down, expert, A.f, A.d, col0, lane);
+      const int at_once = few_rows_at_once<true>(per * STEP);
+      auto ready = [&]() __attribute__((always_inline)) {
+        if (tid == 0)
+          while (__hip_atomic_load(&A.counters->ready[live].n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < h_tiles) __builtin_amdgcn_s_sleep(8);
+        __syncthreads();
+      };
+      for (int r0 = 0; r0 < count; r0 += at_once) {
+        const int n_rows = min(at_once, count - r0);
+        mx_f32x4 acc[FR];
+#pragma unroll
+        for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+        if (step1 > step0)
+          few_multiply<MX, FR, true, DEPTH, kFewWaves>(acc, W, [&](int r) { return A.h + (size_t)slots[r0 + r] * A.f; }, ready, A.h_lo, A.f, n_rows, step0,
+                                                       step1 - step0, lds.rows, wave, tid, lane);
+        __syncthreads();
+        few_put(lds.part[wave][lane & 15] + FR * 4 * (lane >> 4), acc);
+        __syncthreads();
+        const int t = tid / (COLS / 2), c = 2 * (tid % (COLS / 2));
+        if (t < n_rows) {
+          float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kFewWaves; w++) {
+            const float2 p = *reinterpret_cast<const float2*>(&lds.part[w][t][c]);
+            v.x += p.x;
+            v.y += p.y;
+          }
+          few_store_agent(A.partial + ((size_t)slots[r0 + t] * A.parts + part) * A.d + col0 + c, __float_as_uint(v.x), __float_as_uint(v.y));
+        }
+      }
+      const bool complete = few_arrive(&A.counters->arrivals[ct], n_live * A.parts);
+      if (tid == 0) last = complete;
+      __syncthreads();
+      // out[t] = sum_j w[t, j] sum_parts partial of this column tile: slots in order, parts in order, fp32, one rounding
+      if (last) {
+        for (int i = tid; i < A.T * (COLS / 2); i += kFewWaves * kWave) {
+          const int t = i / (COLS / 2), c = col0 + 2 * (i % (COLS / 2));
+          float2 sum = make_float2(0.f, 0.f), y = sum;
+          const int n = A.Kp * A.parts;
+          const float* const src = A.partial + (size_t)t * n * A.d + c;
+          int j = 0, p = 0;
+          for (int i0 = 0; i0 < n; i0 += 8) {   // (eight at a time: each takes the way to memory)
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++) v[u] = few_load_partial(src + (size_t)min(i0 + u, n - 1) * A.d);
+#pragma unroll
+            for (int u = 0; u < 8; u++) {
+              if (i0 + u < n) {
+                y.x += v[u].x; y.y += v[u].y;
+                if (++p == A.parts) {
+                  const float w = topk_w[t * A.Kp + j];
+                  sum.x += w * y.x; sum.y += w * y.y;
+                  y = make_float2(0.f, 0.f);
+                  p = 0;
+                  j++;
+                }
+              }
+            }
+          }
+          *reinterpret_cast<uint32_t*>(A.out + (size_t)t * A.d + c) = pack_bf16(sum.x, sum.y);
         }
       }
     }
-    *reinterpret_cast<uint32_t*>(A.out + (size_t)t * A.d + c) = pack_bf16(sum.x, sum.y);
   }
-}
-
-// 16 FR columns of H W_down of one expert over one part of d_ffn, which the wavefronts share; the last block of a column tile combines.
-template <bool MX, int FR, int DEPTH>
-__global__ __launch_bounds__(kFewWaves * kWave, 4) void few_down_kernel(const FewArgs A) {
-  constexpr int COLS = 16 * FR, PITCH = COLS + 4;
-  __shared__ __attribute__((aligned(16))) union { char rows[kFewRowBytes]; float part[kFewWaves][kFewGroup][PITCH]; } lds;
-  __shared__ int last;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n_live = A.sched->n_live;
-  if ((int)blockIdx.y >= n_live) return;
-  const int4 L = few_live(A, blockIdx.y);
-  const int32_t* const slots = A.sched->slots + L.y;
-  const int col0 = blockIdx.x * COLS;
-  const int steps = few_steps(MX, A.f), per = (steps + A.parts - 1) / A.parts;
-  const int step0 = min(steps, (int)blockIdx.z * per), step1 = min(steps, step0 + per);
-  const FewTile<MX, FR> W(A.down, L.x, A.f, A.d, col0, lane);
-  const int at_once = few_rows_at_once<true>(per * (MX ? 128 : 32));
-  for (int r0 = 0; r0 < L.z; r0 += at_once) {
-    const int n_rows = min(at_once, L.z - r0);
-    mx_f32x4 acc[FR];
-#pragma unroll
-    for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-    if (step1 > step0)
-      few_multiply<MX, FR, true, DEPTH, kFewWaves>(acc, W, [&](int r) { return A.h + (size_t)slots[r0 + r] * A.f; }, A.h_lo, A.f,
-                                                   n_rows, step0, step1 - step0, lds.rows, wave, lane);
-    __syncthreads();
-    few_put(lds.part[wave][lane & 15] + FR * 4 * (lane >> 4), acc);
-    __syncthreads();
-    const int t = tid / (COLS / 2), c = 2 * (tid % (COLS / 2)), row = r0 + t;
-    if (t < n_rows) {
-      float2 v = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kFewWaves; w++) {
-        const float2 p = *reinterpret_cast<const float2*>(&lds.part[w][t][c]);
-        v.x += p.x;
-        v.y += p.y;
-      }
-      few_store_partial(A.partial + ((size_t)slots[row] * A.parts + blockIdx.z) * A.d + col0 + c, v.x, v.y);
-    }
-  }
-  few_combine(A, blockIdx.x, col0, COLS, n_live * A.parts, &last);
 }
 
 // ---- 17 to 64 tokens: the wavefronts of a block share the rows ----------------------------------------------------------------------------
@@ -761,13 +842,13 @@ int few_parts(const Dims& D, bool mx) {
   return max(least, (int)min((long long)most, max(1ll, (512 + blocks - 1) / blocks)));
 }
 
-struct FewLayout { size_t logits, sched, arrivals, h, partial, total; };
+struct FewLayout { size_t logits, sched, counters, h, partial, total; };
 FewLayout few_layout(const Dims& D) {
   FewLayout L;
   size_t o = 0;
   L.sched = o; o += round_up(sizeof(FewSched), 256);
   L.logits = o; o += round_up((size_t)D.T * D.E * sizeof(float), 256);
-  L.arrivals = o; o += round_up((size_t)(D.d / 32 + 1) * sizeof(int32_t), 256);
+  L.counters = o; o += round_up(few_counters_bytes(D.d), 256);
   L.h = o; o += round_up((size_t)D.N * D.f * 2 * sizeof(uint16_t), 256);
   L.partial = o; o += round_up((size_t)D.N * max(few_parts(D, false), few_parts(D, true)) * D.d * sizeof(float), 256);
   L.total = o;
@@ -794,9 +875,8 @@ void few_launch_experts(hipStream_t st, const FewArgs& A, const Dims& D) {
     return;
   }
   constexpr int FR = MX ? 2 : 4;
-  const dim3 block(kFewWaves * kWave);
-  MOE_LAUNCH("few_gate_up", st, (few_gate_up_kernel<MX, FR, 4>), dim3(A.f / (16 * FR), live), block, 0, st, A);
-  MOE_LAUNCH("few_down", st, (few_down_kernel<MX, FR, 4>), dim3(A.d / (16 * FR), live, A.parts), block, 0, st, A);
+  const int tiles = live * (D.f / (16 * FR) + D.d / (16 * FR) * A.parts);   // (at most)
+  MOE_LAUNCH("few_layer", st, (few_layer_kernel<MX, FR, 3>), dim3(min(tiles, kFewBlocks)), dim3(kFewWaves * kWave), 0, st, A);
 }
 
 template <bool MX>
@@ -822,13 +902,14 @@ int few_forward(const moe_shape* shape, const uint16_t* x, const uint16_t* w_rou
   A.gate = W[0]; A.up = W[1]; A.down = W[2];
   A.logits = reinterpret_cast<float*>(wsb + L.logits);
   A.sched = reinterpret_cast<FewSched*>(wsb + L.sched);
-  A.arrivals = reinterpret_cast<int32_t*>(wsb + L.arrivals);
+  A.counters = reinterpret_cast<FewCounters*>(wsb + L.counters);
   A.h = reinterpret_cast<uint16_t*>(wsb + L.h);
   A.h_lo = (size_t)D.N * D.f;
   A.partial = reinterpret_cast<float*>(wsb + L.partial);
   hipStream_t st = (hipStream_t)stream;
   if (w_router)
     MOE_LAUNCH("few_router", st, few_router_kernel, dim3((D.E + 15) / 16, (D.T + 15) / 16), dim3(kFewWaves * kWave), 0, st, A);
+  if (!w_router && A.fused_gate) MOE_LAUNCH("few_clear", st, few_clear_kernel, dim3(1), dim3(256), 0, st, A);
   if (!A.fused_gate) {
     if (D.E <= 64) MOE_LAUNCH("few_gate", st, few_gate_kernel<1>, dim3(1), dim3(1024), 0, st, A);
     else if (D.E <= 256) MOE_LAUNCH("few_gate", st, few_gate_kernel<4>, dim3(1), dim3(1024), 0, st, A);

@@ -19,10 +19,10 @@ namespace {
 
 constexpr int kFewTokens = MOE_FEW_TOKENS_MAX;
 constexpr int kFewSlots = 4096;       // T * K' at most
-constexpr int kFewWaves = 8;          // wavefronts of a block that share a contraction
+constexpr int kFewWaves = 8;          // wavefronts of a block, at most 16 tokens
+constexpr int kFewRouterWaves = 8;    // ... of few_router_kernel: they share a contraction
 constexpr int kFewFusedSlots = 512, kFewFusedExperts = 256;   // at most, where every block makes the gate for itself
 constexpr int kFewGroup = 16;         // tokens of an MFMA
-constexpr int kFewBlocks = 512;       // two per CU
 
 // The experts that have tokens, in expert order, and the slots of each.
 struct FewSched {
@@ -31,48 +31,30 @@ struct FewSched {
   int32_t slots[kFewSlots];   // t * K' + j
 };
 
-// Cleared by the launch before the one that uses them.  Counters that many blocks use lie in lines of their own.
-constexpr int kFewLists = 64;
-struct FewLine { int32_t n, pad[31]; };
-struct FewCounters {
-  FewLine taken[2][kFewLists];    // tiles of H, tiles of W_down: taken of each list
-  FewLine ready[kMaxExperts];     // per live expert: tiles of H that are there
-  int32_t arrivals[1];            // per column tile of the down projection: parts that are there (d / 32 at most)
-};
-inline size_t few_counters_bytes(int d) { return sizeof(FewCounters) + (size_t)(d / 32) * sizeof(int32_t); }
-
 struct FewWeights { const uint8_t* w; const uint8_t* scales; };   // bf16 weights have no scales
 struct FewArgs {
-  int T, d, f, E, Es, k, Kp, renorm, parts;   // parts of d_ffn in the down projection
-  int fused_gate;                // the gate is made by few_layer_kernel
+  int T, d, f, E, Es, k, Kp, renorm;
+  int parts, h_parts;            // of d_ffn in the down projection; of d in the other two, at most 16 tokens
+  int fused_gate;                // the gate is made by few_gate_up_kernel
   const uint16_t* x; const uint16_t* w_router;
   float* logits; int32_t* topk_idx; float* topk_w; FewSched* sched;
-  FewCounters* counters;
   FewWeights gate, up, down;
   uint16_t* h; size_t h_lo;      // [N, f] bf16 heads, the remainders h_lo elements further
   float* partial;                // [N, parts, d]
+  float* h_partial;              // [N, h_parts, 2, f]
   uint16_t* out;
 };
 
 // ---- logits and gate ---------------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ void few_clear(const FewArgs& A) {
-  int32_t* const lists = &A.counters->taken[0][0].n;
-  for (int i = threadIdx.x; i < 2 * kFewLists; i += blockDim.x) lists[32 * i] = 0;
-  for (int i = threadIdx.x; i < A.E + A.Es; i += blockDim.x) A.counters->ready[i].n = 0;
-  for (int i = threadIdx.x; i < A.d / 32; i += blockDim.x) A.counters->arrivals[i] = 0;
-}
-__global__ __launch_bounds__(256) void few_clear_kernel(const FewArgs A) { few_clear(A); }
-
 // 16 experts x 16 tokens per block, K split over the wavefronts, whose sums are added in order.
-__global__ __launch_bounds__(kFewWaves * kWave) void few_router_kernel(const FewArgs A) {
-  __shared__ float part[kFewWaves][16][17];
+__global__ __launch_bounds__(kFewRouterWaves * kWave) void few_router_kernel(const FewArgs A) {
+  __shared__ float part[kFewRouterWaves][16][17];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
   const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
-  if (blockIdx.x == 0 && blockIdx.y == 0) few_clear(A);
   const uint16_t* const wr = A.w_router + (size_t)min(e0 + n, A.E - 1) * A.d + 8 * q;
   const uint16_t* const xr = A.x + (size_t)min(t0 + n, A.T - 1) * A.d + 8 * q;
-  const int steps = A.d / 32, per = (steps + kFewWaves - 1) / kFewWaves;
+  const int steps = A.d / 32, per = (steps + kFewRouterWaves - 1) / kFewRouterWaves;
   mx_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const int end = min(steps, (wave + 1) * per);
   for (int s0 = wave * per; s0 < end; s0 += 8) {   // (eight steps requested at once; past the end the last one, not multiplied)
@@ -94,7 +76,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_router_kernel(const Few
     const int t = threadIdx.x >> 4, e = threadIdx.x & 15;
     float sum = 0.f;
 #pragma unroll
-    for (int p = 0; p < kFewWaves; p++) sum += part[p][t][e];
+    for (int p = 0; p < kFewRouterWaves; p++) sum += part[p][t][e];
     if (t0 + t < A.T && e0 + e < A.E) A.logits[(size_t)(t0 + t) * A.E + e0 + e] = sum;
   }
 }
@@ -105,7 +87,6 @@ __global__ __launch_bounds__(1024) void few_gate_kernel(const FewArgs A) {
   __shared__ int count[kMaxExperts], first[kMaxExperts], live_before[kMaxExperts];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int Et = A.E + A.Es, N = A.T * A.Kp;
-  if (!A.w_router) few_clear(A);
   if (A.w_router)
     for (int t = wave; t < A.T; t += 16)
       route_token<kWave, PER>(A.logits + (size_t)t * A.E, t, lane, A.topk_idx, A.topk_w, nullptr, A.E, A.k, A.Es, A.renorm);
@@ -140,27 +121,36 @@ __global__ __launch_bounds__(1024) void few_gate_kernel(const FewArgs A) {
 // cut short: its codes are zero past the end).
 template <bool MX, int FR> struct FewTile;
 
+__device__ __forceinline__ int few_scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }   // the same in all lanes: the compiler is told so
+
+// Global memory by a scalar address: the compiler is told that it is the same in all lanes.
+typedef const uint8_t __attribute__((address_space(1)))* FewBase;
+__device__ __forceinline__ FewBase few_base(const uint8_t* p) {
+  const unsigned long long v = (unsigned long long)p;
+  return (FewBase)((unsigned long long)(unsigned)few_scalar((int)(v >> 32)) << 32 | (unsigned)few_scalar((int)v));
+}
 // From a scalar base and 32 bits of the lane's own (left to itself the compiler keeps a 64-bit address per lane and load, 48 registers in all).
 template <class T>
-__device__ __forceinline__ T few_load(const uint8_t* base, unsigned off) {
+__device__ __forceinline__ T few_load(FewBase base, unsigned off) {
   asm("" : "+s"(base));
-  return *reinterpret_cast<const T*>(base + off);
+  return *(const T __attribute__((address_space(1)))*)(base + off);
 }
 
 template <int FR> struct FewTile<false, FR> {
   static constexpr int KS = 1;   // MFMAs of 32 k per step and frag
   typedef uint32_t word __attribute__((ext_vector_type(FR / 2)));   // the lane's FR columns of a k-row
   struct Stage { word w[8]; };
-  const uint8_t* base;
+  FewBase base;
   unsigned lane_off;
   size_t row;
   __device__ __forceinline__ FewTile(const FewWeights& W, int expert, int K, int C, int col0, int lane) {
-    base = W.w + ((size_t)expert * K * C + col0) * 2;
+    base = few_base(W.w + ((size_t)expert * K * C + col0) * 2);
     row = (size_t)C * 2;
     lane_off = ((unsigned)(8 * (lane >> 4)) * (unsigned)C + FR * (lane & 15)) * 2;
   }
   __device__ __forceinline__ void load(Stage& s, int step) const {
-    const uint8_t* p = base + (size_t)step * 32 * row;   // (scalar: a load's address is this and 32 bits of the lane's own)
+    step = few_scalar(step);
+    FewBase p = base + (size_t)step * 32 * row;   // (scalar: a load's address is this and 32 bits of the lane's own)
 #pragma unroll
     for (int i = 0; i < 8; i++, p += row) s.w[i] = few_load<word>(p, lane_off);
   }
@@ -176,24 +166,26 @@ template <int FR> struct FewTile<false, FR> {
 
 template <int FR> struct FewTile<true, FR> {
   static constexpr int KS = 4;
-  struct Stage { uint4 w[FR]; unsigned s[FR]; };
-  const uint8_t* base; const uint8_t* sbase;   // of column 0
+  typedef uint32_t quad __attribute__((ext_vector_type(4)));   // a block of 32 k
+  struct Stage { quad w[FR]; unsigned s[FR]; };
+  FewBase base, sbase;                         // of column 0
   unsigned lane_off, lane_soff;                // this lane's first column, block q
   int kb, q;
   __device__ __forceinline__ FewTile(const FewWeights& W, int expert, int K, int C, int col0, int lane) {
     kb = K / kMxBlock;
     q = lane >> 4;
     const size_t row = (size_t)expert * C + col0;
-    base = W.w + row * (kb * 16);
-    sbase = W.scales + row * kb;
+    base = few_base(W.w + row * (kb * 16));
+    sbase = few_base(W.scales + row * kb);
     lane_soff = (unsigned)(FR * (lane & 15)) * (unsigned)kb + q;
     lane_off = lane_soff * 16;
   }
   __device__ __forceinline__ void load(Stage& s, int step) const {
+    step = few_scalar(step);
     const int b = min(4 * step, kb - 1 - q);   // (a block past the end: the last one)
 #pragma unroll
     for (int a = 0; a < FR; a++) {
-      s.w[a] = few_load<uint4>(base + (size_t)a * (kb * 16), lane_off + b * 16);
+      s.w[a] = few_load<quad>(base + (size_t)a * (kb * 16), lane_off + b * 16);
       s.s[a] = few_load<uint8_t>(sbase + (size_t)a * kb, lane_soff + b);
     }
   }
@@ -211,7 +203,7 @@ template <int FR> struct FewTile<true, FR> {
   __device__ __forceinline__ void end(Stage& s, int step) const {
     if (4 * step + q >= kb) {
 #pragma unroll
-      for (int a = 0; a < FR; a++) { s.w[a] = make_uint4(0, 0, 0, 0); s.s[a] = 127; }
+      for (int a = 0; a < FR; a++) { s.w[a] = quad{0, 0, 0, 0}; s.s[a] = 127; }
     }
   }
 };
@@ -229,71 +221,123 @@ __device__ __forceinline__ void few_swiglu(float g, float u, float& h, float& lo
   lo = h - bf16_to_f32(f32_to_bf16(h));
 }
 
-// ---- at most 16 tokens: the wavefronts of a block share a tile's contraction ------------------------------------------------------------
-
-// The rows of a product lie in LDS for the whole range of k that a block works on: as many rows as fit go through the weights together.
-constexpr int kFewRowBytes = 64 * 1024;
-constexpr int kFewRowK = 8192;   // k at most (LO: half of them): two rows fit
-__device__ __forceinline__ int few_row_pitch(int k) { return 2 * k + 16; }
-template <bool LO>
-__device__ __forceinline__ int few_rows_at_once(int k) { return min(kFewGroup, kFewRowBytes / ((LO ? 2 : 1) * few_row_pitch(k))); }
-
-__device__ __forceinline__ uint4 few_load_agent(const uint16_t* p) {   // 16 bytes, past this XCD's L2
-  const unsigned long long* const q = reinterpret_cast<const unsigned long long*>(p);
-  const unsigned long long a = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), b = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_uint4((unsigned)a, (unsigned)(a >> 32), (unsigned)b, (unsigned)(b >> 32));
+// A lane's sums of one token, 4 FR consecutive columns.
+template <int FR>
+__device__ __forceinline__ void few_put(float* dst, const mx_f32x4 (&acc)[FR]) {
+  typedef float vec __attribute__((ext_vector_type(FR)));
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    vec v;
+#pragma unroll
+    for (int a = 0; a < FR; a++) v[a] = acc[a][i];
+    *reinterpret_cast<vec*>(dst + FR * i) = v;
+  }
 }
 
-// acc[a] += over `n_steps` steps from step0 on: lane l's element i of acc[a] is column FR (4 (l / 16) + i) + a, token l % 16 (tokens past the last
-// repeat it).  row(i): element 0 of row i of X, its remainders (LO) x_lo elements further.  Wavefront `part` of PARTS takes its share of the steps;
-// their weights go into registers, DEPTH - 1 steps ahead.
-// Between the first requests and the rows stands `ready()`.
-template <bool MX, int FR, bool LO, int DEPTH, int PARTS, class F, class G>
-__device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<MX, FR>& W, F&& row, G&& ready, size_t x_lo, int K, int n_rows,
-                                             int step0, int n_steps, char* buf, int part, int tid, int lane) {
-  typedef FewTile<MX, FR> Tile;
-  constexpr int STEP = MX ? 128 : 32, THREADS = kFewWaves * kWave;
-  const int pitch = few_row_pitch(n_steps * STEP), pieces = n_steps * STEP / 8, total = n_rows * pieces;
-  const int per = (n_steps + PARTS - 1) / PARTS;
-  const int first = min(n_steps, part * per), count = min(n_steps, first + per) - first, last = max(first + count - 1, 0);
-  typename Tile::Stage st[DEPTH];
-  // rows into LDS, zeros past the end of K; the first weights are requested while the first of them come
-  struct Piece { uint4 v, w; };
-  auto bring = [&](int i) __attribute__((always_inline)) {
-    Piece p = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    const int r = i / pieces, k = step0 * STEP + 8 * (i - r * pieces);
-    if (i < total && k < K) {
-      const uint16_t* const src = row(r) + k;
-      if constexpr (LO) {   // (written in this launch)
-        p.v = few_load_agent(src);
-        p.w = few_load_agent(src + x_lo);
-      } else {
-        p.v = *reinterpret_cast<const uint4*>(src);
-      }
+// ---- at most 16 tokens: the wavefronts of a block have columns next to each other ------------------------------------------------------------
+//
+// and the contraction is shared between blocks, whose partial sums the next launch adds.  A step of bf16 weights takes 32 k-rows that lie 2 C bytes
+// apart: if each wavefront of a block goes through rows of its own, a CU has 8 times as many pages in use at once (reading two pairs of 4096 x 14336
+// alone, 5.0 against 6.1 TB/s).  A launch that goes on from the logits to the end by itself was slower: its wavefronts take their work from counters
+// and wait for each other through memory, and 512 blocks that begin with an atomic each have their answers after 25 us.
+
+// The gate of the call for one block, in LDS; the experts that have slots.
+struct FewGate {
+  int idx[kFewFusedSlots], list[kFewFusedSlots];   // the slots' experts; the slots of the expert at hand
+  float weight[kFewFusedSlots];
+  unsigned words[kFewFusedExperts / 32];
+  int found[2];
+};
+// Live expert blockIdx.y of the call: its id and its slots; count = 0: there is none.  With the gate fused, every block makes it from the logits for
+// itself (a launch and the wait for it cost more); block (0, 0) leaves ids and weights in memory, block (0, `last_row`) the schedule.
+struct FewExpert { int id, count; const int* slots; };
+__device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, int last_row) {
+  FewExpert X;
+  if (!A.fused_gate) {
+    const bool live = (int)blockIdx.y < A.sched->n_live;
+    const int4 v = few_live(A, blockIdx.y);
+    X.id = v.x;
+    X.count = live ? v.z : 0;
+    X.slots = A.sched->slots + v.y;
+    return X;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = few_scalar(tid >> 6), N = A.T * A.Kp, Et = A.E + A.Es;
+  if (tid < kFewFusedExperts / 32) S.words[tid] = 0;
+  if (A.w_router) {
+    for (int t = wave; t < A.T; t += kFewWaves) {
+      if (A.E <= kWave) route_token<kWave, 1>(A.logits + (size_t)t * A.E, t, lane, S.idx, S.weight, nullptr, A.E, A.k, A.Es, A.renorm);
+      else route_token<kWave, 4>(A.logits + (size_t)t * A.E, t, lane, S.idx, S.weight, nullptr, A.E, A.k, A.Es, A.renorm);
     }
-    return p;
-  };
-  auto put = [&](int i, const Piece& p) __attribute__((always_inline)) {
-    if (i >= total) return;
-    const int r = i / pieces;
-    char* const to = buf + r * pitch + 16 * (i - r * pieces);
-    *reinterpret_cast<uint4*>(to) = p.v;
-    if constexpr (LO) *reinterpret_cast<uint4*>(to + n_rows * pitch) = p.w;
-  };
-#pragma unroll
-  for (int i = 0; i < DEPTH; i++)
-    if (i < count) W.load(st[i], step0 + first + i);
-  ready();
-  const Piece p0 = bring(tid);
-  __syncthreads();   // (what was in LDS has been read)
-  put(tid, p0);
-  for (int i = tid + THREADS; i < total; i += 2 * THREADS) {
-    const Piece a = bring(i), b = bring(i + THREADS);
-    put(i, a);
-    put(i + THREADS, b);
+  } else {
+    for (int s = tid; s < N; s += kFewWaves * kWave) S.idx[s] = min(max(A.topk_idx[s], 0), Et - 1);
   }
   __syncthreads();
-  const char* const at = buf + min(lane & 15, n_rows - 1) * pitch + first * (STEP * 2) + (MX ? 64 : 16) * (lane >> 4);
+  for (int s = tid; s < N; s += kFewWaves * kWave) {
+    atomicOr(&S.words[S.idx[s] >> 5], 1u << (S.idx[s] & 31));
+    if (blockIdx.x == 0 && blockIdx.y == 0 && A.w_router) { A.topk_idx[s] = S.idx[s]; A.topk_w[s] = S.weight[s]; }
+  }
+  __syncthreads();
+  if (wave == 0) {
+    // 4 ids per lane
+    const unsigned bits = (S.words[lane >> 3] >> (4 * (lane & 7))) & 15u;
+    const int n = __popc(bits), incl = wave_prefix_sum(n), total = __builtin_amdgcn_readlane(incl, kWave - 1);
+    auto slots_of = [&](int e, int32_t* to) __attribute__((always_inline)) {   // the slots of expert e, in order; how many
+      int count = 0;
+      for (int s0 = 0; s0 < N; s0 += kWave) {
+        const bool mine = s0 + lane < N && S.idx[s0 + lane] == e;
+        const unsigned long long who = __ballot(mine);
+        if (mine) to[count + __popcll(who & ((1ull << lane) - 1))] = s0 + lane;
+        count += __popcll(who);
+      }
+      return count;
+    };
+    int expert = -1, count = 0;
+    const unsigned long long past = __ballot(incl > (int)blockIdx.y);
+    if (past && (int)blockIdx.y != last_row) {
+      const int l = __builtin_ctzll(past);
+      unsigned b = __builtin_amdgcn_readlane(bits, l);
+      for (int skip = (int)blockIdx.y - __builtin_amdgcn_readlane(incl - n, l); skip > 0; skip--) b &= b - 1;
+      expert = 4 * l + __builtin_ctz(b);
+      count = slots_of(expert, S.list);
+    }
+    if (lane == 0) { S.found[0] = expert; S.found[1] = count; }
+    if ((int)blockIdx.y == last_row && blockIdx.x == 0) {   // every live expert's turn
+      int at = 0, i = 0;
+      for (int l = 0; l < kWave; l++)
+        for (unsigned b = __builtin_amdgcn_readlane(bits, l); b; b &= b - 1, i++) {
+          const int e = 4 * l + __builtin_ctz(b), c = slots_of(e, A.sched->slots + at);
+          if (lane == 0) A.sched->live[i] = make_int4(e, at, c, 0);
+          at += c;
+        }
+      if (lane == 0) A.sched->n_live = total;
+    }
+  }
+  __syncthreads();
+  X.id = few_scalar(S.found[0]);
+  X.count = few_scalar(S.found[1]);
+  X.slots = S.list;
+  return X;
+}
+
+// Rows of a product in LDS, for all the k that a block works on: as many rows as fit go through the weights together.
+constexpr int kFewRowBytes = 60 * 1024;
+constexpr int kFewRowK = 1792;   // k at most: of 16 rows (LO: half of them)
+__device__ __forceinline__ int few_row_pitch(int k) { return 2 * k + 16; }
+
+// acc[a] += over `count` steps from step0 on: lane l's element i of acc[a] is column FR (4 (l / 16) + i) + a, row l % 16 of `rows` (LO: with the
+// remainders after all rows; rows past the last repeat it).  Between the first weights' requests and their use stands `bring`, which fills `rows`.
+template <bool MX, int FR, bool LO, int DEPTH, class F>
+__device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<MX, FR>& W, F&& bring, const char* rows, int n_rows, int pitch, int step0,
+                                             int count, int lane) {
+  typedef FewTile<MX, FR> Tile;
+  constexpr int STEP = MX ? 128 : 32;
+  const int last = step0 + count - 1;
+  typename Tile::Stage st[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH; i++)
+    if (i < count) W.load(st[i], step0 + i);
+  bring();
+  const char* const at = rows + min(lane & 15, n_rows - 1) * pitch + (MX ? 64 : 16) * (lane >> 4);
   auto consume = [&](const typename Tile::Stage& s, int i) __attribute__((always_inline)) {
     const char* const x = at + i * (STEP * 2);
 #pragma unroll
@@ -317,14 +361,14 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<
     for (int u = 0; u < DEPTH; u++) {
       consume(st[u], i + u);
       __builtin_amdgcn_sched_barrier(0);
-      W.load(st[u], step0 + min(first + i + u + DEPTH, last));
+      W.load(st[u], min(step0 + i + u + DEPTH, last));
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
   for (int u = 0; u < DEPTH; u++) {
     if (i + u < count) {
-      if (i + u == count - 1) W.end(st[u], step0 + first + i + u);
+      if (i + u == count - 1) W.end(st[u], last);
       __builtin_amdgcn_sched_barrier(0);
       consume(st[u], i + u);
       __builtin_amdgcn_sched_barrier(0);
@@ -332,263 +376,104 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<
   }
 }
 
-// A lane's sums of one token, 4 FR consecutive columns.
-template <int FR>
-__device__ __forceinline__ void few_put(float* dst, const mx_f32x4 (&acc)[FR]) {
-  typedef float vec __attribute__((ext_vector_type(FR)));
+// One of `h_parts` parts of G and U of 256 columns of one expert: wavefronts 0, 2, 4, 6 make G, the others U, of 64 columns each.
+template <bool MX, int DEPTH>
+__global__ __launch_bounds__(kFewWaves * kWave, 4) void few_gate_up_kernel(const FewArgs A) {
+  constexpr int FR = 4, WC = 16 * FR, STEP = MX ? 128 : 32, THREADS = kFewWaves * kWave;
+  __shared__ __attribute__((aligned(16))) char rows[kFewRowBytes];
+  __shared__ FewGate S;
+  const int tid = threadIdx.x, lane = tid & 63, wave = few_scalar(tid >> 6);
+  const FewExpert X = few_expert(A, S, gridDim.y - 1);
+  if (X.count == 0) return;
+  const int ct = blockIdx.x / A.h_parts, part = blockIdx.x - ct * A.h_parts;
+  const int steps = few_steps(MX, A.d), per = (steps + A.h_parts - 1) / A.h_parts;
+  const int step0 = min(steps, part * per), count = min(steps, step0 + per) - step0;
+  const int col0 = ct * 4 * WC + WC * (wave >> 1);
+  const bool active = col0 < A.f;   // (widths are multiples of 64: a wavefront has all its columns or none)
+  const FewTile<MX, FR> W(wave & 1 ? A.up : A.gate, X.id, A.d, A.f, active ? col0 : 0, lane);
+  const int pitch = few_row_pitch(per * STEP), pieces = per * STEP / 8;
+  for (int r0 = 0; r0 < X.count; r0 += kFewGroup) {
+    const int n_rows = min(kFewGroup, X.count - r0);
+    mx_f32x4 acc[FR];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    vec v;
-#pragma unroll
-    for (int a = 0; a < FR; a++) v[a] = acc[a][i];
-    *reinterpret_cast<vec*>(dst + FR * i) = v;
-  }
-}
-
-// What blocks of one launch hand to each other (they may run on different XCDs, with an L2 each) is stored and loaded at agent scope, past those
-// caches.  A block counts itself as arrived when its stores have been acknowledged.  (Ordinary stores and a device-wide fence, which writes
-// the L2 back and empties it, make the down projection 3 to 8 times as long.)
-__device__ __forceinline__ void few_store_agent(void* p, unsigned a, unsigned b) {
-  __hip_atomic_store(static_cast<unsigned long long*>(p), (unsigned long long)b << 32 | a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 few_load_partial(const float* p) {
-  const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
-}
-// Counts this block: all that its threads have stored is then where every block sees it.  True for thread 0 of the one that completes `of`.
-__device__ __forceinline__ bool few_arrive(int32_t* counter, int of) {
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wavefront's stores have been acknowledged
-  __syncthreads();
-  return threadIdx.x == 0 && __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
-}
-
-// The live expert `index` among the slots' experts `idx` (in LDS, N of them), its slots into `slots`; n_live: how many there are.  Ends with the
-// answers in `found` ({expert, slots, n_live}), before a barrier.
-__device__ __forceinline__ void few_find_live(const int* idx, int N, int index, int* slots, const unsigned* words, int* found) {
-  const int lane = threadIdx.x & 63;
-  if (threadIdx.x >= kWave) return;
-  // 4 ids per lane
-  const unsigned bits = (words[lane >> 3] >> (4 * (lane & 7))) & 15u;
-  const int n = __popc(bits), incl = wave_prefix_sum(n);
-  const unsigned long long past = __ballot(incl > index);
-  int expert = -1, count = 0;
-  if (past) {
-    const int l = __builtin_ctzll(past);
-    unsigned b = __builtin_amdgcn_readlane(bits, l);
-    for (int skip = index - __builtin_amdgcn_readlane(incl - n, l); skip > 0; skip--) b &= b - 1;
-    expert = 4 * l + __builtin_ctz(b);
-    for (int s0 = 0; s0 < N; s0 += kWave) {
-      const bool mine = s0 + lane < N && idx[s0 + lane] == expert;
-      const unsigned long long who = __ballot(mine);
-      if (mine) slots[count + __popcll(who & ((1ull << lane) - 1))] = s0 + lane;
-      count += __popcll(who);
-    }
-  }
-  if (lane == 0) { found[0] = expert; found[1] = count; found[2] = __builtin_amdgcn_readlane(incl, kWave - 1); }
-}
-
-// The whole layer from the logits on, in one launch.  Its work is a list of tiles: H = silu(x W_gate) * (x W_up) of 16 FR columns, expert after
-// expert, then the parts of H W_down of 16 FR columns, expert after expert.  A block takes the next tile when it has done one, so that no CU waits at
-// the end of an expert or of the first half.  The tiles are dealt to 64 lists of either kind, each with a counter (one counter for all costs 35 ns
-// for every tile, one after the other); a block takes from its own list, then from those that have tiles left.  A tile of W_down waits for its
-// expert's tiles of H, with its own first weights on the way, and no block comes to one before all tiles of H have been taken: by blocks that are
-// running, whatever else is on the GPU, so every wait ends.  The last part of a column tile of W_down adds the parts and experts.
-//
-// Of the pair wavefronts 0, 2, 4, 6 make G, the others U, each over a quarter of d; of W_down each takes an eighth of its part of d_ffn.  With the
-// gate fused, every block makes it from the logits for itself (a launch and the wait for it cost more).
-template <bool MX, int FR, int DEPTH>
-__global__ __launch_bounds__(kFewWaves * kWave, 4) void few_layer_kernel(const FewArgs A) {
-  constexpr int COLS = 16 * FR, PITCH = COLS + 4, STEP = MX ? 128 : 32;
-  __shared__ __attribute__((aligned(16))) union { char rows[kFewRowBytes]; float part[kFewWaves][kFewGroup][PITCH]; } lds;
-  __shared__ int idx[kFewFusedSlots], list[kFewFusedSlots];
-  __shared__ float weight[kFewFusedSlots];
-  __shared__ unsigned words[kFewFusedExperts / 32];
-  __shared__ int found[3], next, last;
-  int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int N = A.T * A.Kp;
-  const int list_id = blockIdx.x % kFewLists;
-  auto take = [&](int kind, int l) __attribute__((always_inline)) {   // the next tile of list l
-    return __hip_atomic_fetch_add(&A.counters->taken[kind][l].n, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) * kFewLists + l;
-  };
-  int h_ticket = 0, d_ticket = 0;   // (thread 0)
-  if (tid == 0) { h_ticket = take(0, list_id); d_ticket = take(1, list_id); }
-  const float* topk_w = A.topk_w;
-  int n_live;
-  if (A.fused_gate) {
-    if (tid < kFewFusedExperts / 32) words[tid] = 0;
-    if (A.w_router) {
-      for (int t = wave; t < A.T; t += kFewWaves) {
-        if (A.E <= kWave) route_token<kWave, 1>(A.logits + (size_t)t * A.E, t, lane, idx, weight, nullptr, A.E, A.k, A.Es, A.renorm);
-        else route_token<kWave, 4>(A.logits + (size_t)t * A.E, t, lane, idx, weight, nullptr, A.E, A.k, A.Es, A.renorm);
-      }
-      topk_w = weight;
-    } else {
-      for (int s = tid; s < N; s += kFewWaves * kWave) idx[s] = min(max(A.topk_idx[s], 0), A.E + A.Es - 1);
-    }
-    __syncthreads();
-    for (int s = tid; s < N; s += kFewWaves * kWave) {
-      atomicOr(&words[idx[s] >> 5], 1u << (idx[s] & 31));
-      if (blockIdx.x == 0 && A.w_router) { A.topk_idx[s] = idx[s]; A.topk_w[s] = weight[s]; }
-    }
-    __syncthreads();
-    int n = 0;
-    for (int i = 0; i < kFewFusedExperts / 32; i++) n += __popc(words[i]);
-    n_live = __builtin_amdgcn_readfirstlane(n);
-  } else {
-    n_live = __builtin_amdgcn_readfirstlane(A.sched->n_live);
-  }
-  const int h_tiles = A.f / COLS, d_tiles = A.d / COLS, n_h = n_live * h_tiles, n_d = n_live * d_tiles * A.parts;
-  const int h_steps = few_steps(MX, A.d), d_steps = few_steps(MX, A.f), per = (d_steps + A.parts - 1) / A.parts;
-  int current = -1, expert = 0, count = 0;   // the live expert whose slots are at hand
-  const int* slots = list;
-
-  int kind = 0;
-  while (true) {
-    asm volatile("" : "+v"(tid), "+v"(lane));   // (nothing that a tile makes of them is kept in registers from one tile to the next)
-    const bool down = kind == 1;
-    const int n_tiles = down ? n_d : n_h;
-    if (tid == 0) next = down ? d_ticket : h_ticket;
-    __syncthreads();   // (and what the tile before has left in LDS has been read)
-    int item = __builtin_amdgcn_readfirstlane(next);
-    if (item >= n_tiles) {   // this list is empty: which are not?
-      if (tid < kWave) {
-        const int taken = __hip_atomic_load(&A.counters->taken[kind][tid].n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        unsigned long long left = __ballot((long long)taken * kFewLists + tid < n_tiles);
-        if (tid == 0) {
-          int got = -1;
-          if (left) {
-            const unsigned long long after = left & ~((2ull << list_id) - 1);   // (from the own one on, so that not all take from the same)
-            got = take(kind, __builtin_ctzll(after ? after : left));
-          }
-          last = got;
-        }
+    for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+    few_multiply<MX, FR, false, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
+      if (r0 > 0) __syncthreads();
+      for (int i = tid; i < n_rows * pieces; i += THREADS) {
+        const int r = i / pieces, c = i - r * pieces, k = step0 * STEP + 8 * c;
+        uint4 v = make_uint4(0, 0, 0, 0);   // (past the end of K)
+        if (k < A.d) v = *reinterpret_cast<const uint4*>(A.x + (size_t)(X.slots[r0 + r] / A.Kp) * A.d + k);
+        *reinterpret_cast<uint4*>(rows + r * pitch + 16 * c) = v;
       }
       __syncthreads();
-      item = __builtin_amdgcn_readfirstlane(last);
-      if (item < 0) {
-        if (down) break;
-        kind = 1;
-        continue;
-      }
-      if (item >= n_tiles) continue;
-    } else if (tid == 0) {
-      if (down) d_ticket = take(1, list_id);
-      else h_ticket = take(0, list_id);
-    }
-    const int local = item, tiles = down ? d_tiles * A.parts : h_tiles;
-    const int live = local / tiles, in_expert = local - live * tiles;
-    if (live != current) {
-      current = live;
-      if (A.fused_gate) {
-        few_find_live(idx, N, live, list, words, found);
-        __syncthreads();
-        expert = __builtin_amdgcn_readfirstlane(found[0]);
-        count = __builtin_amdgcn_readfirstlane(found[1]);
-      } else {
-        const int4 v = few_live(A, live);
-        expert = v.x;
-        count = v.z;
-        slots = A.sched->slots + v.y;
-      }
-    }
-    if (!down) {
-      const int col0 = in_expert * COLS;
-      const FewTile<MX, FR> W(wave & 1 ? A.up : A.gate, expert, A.d, A.f, col0, lane);
-      const int at_once = few_rows_at_once<false>(h_steps * STEP);
-      for (int r0 = 0; r0 < count; r0 += at_once) {
-        const int n_rows = min(at_once, count - r0);
-        mx_f32x4 acc[FR];
+    }, rows, n_rows, pitch, step0, active ? count : 0, lane);
+    const int row = r0 + (lane & 15);
+    if (active && row < X.count)
+      few_put(A.h_partial + (((size_t)X.slots[row] * A.h_parts + part) * 2 + (wave & 1)) * A.f + col0 + 4 * FR * (lane >> 4), acc);
+  }
+}
+
+// 512 columns of H W_down of one expert over one of `parts` parts of d_ffn.  H = silu(G) * U of that part is made here, from the partial sums of G and U
+// (in order): head and remainder.
+template <bool MX, int DEPTH>
+__global__ __launch_bounds__(kFewWaves * kWave, 4) void few_down_kernel(const FewArgs A) {
+  constexpr int FR = 4, WC = 16 * FR, STEP = MX ? 128 : 32, THREADS = kFewWaves * kWave;
+  __shared__ __attribute__((aligned(16))) char rows[kFewRowBytes];
+  const int tid = threadIdx.x, lane = tid & 63, wave = few_scalar(tid >> 6);
+  const int n_live = A.sched->n_live;
+  const int4 L = few_live(A, blockIdx.y);
+  if ((int)blockIdx.y >= n_live) return;
+  const int32_t* const slots = A.sched->slots + L.y;
+  const int ct = blockIdx.x / A.parts, part = blockIdx.x - ct * A.parts;
+  const int steps = few_steps(MX, A.f), per = (steps + A.parts - 1) / A.parts;
+  const int step0 = min(steps, part * per), count = min(steps, step0 + per) - step0;
+  const int col0 = ct * 8 * WC + WC * wave;
+  const bool active = col0 < A.d;
+  const FewTile<MX, FR> W(A.down, L.x, A.f, A.d, active ? col0 : 0, lane);
+  const int pitch = few_row_pitch(per * STEP), quads = per * STEP / 4;
+  for (int r0 = 0; r0 < L.z; r0 += kFewGroup) {
+    const int n_rows = min(kFewGroup, L.z - r0);
+    mx_f32x4 acc[FR];
 #pragma unroll
-        for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-        few_multiply<MX, FR, false, DEPTH, 4>(acc, W, [&](int r) { return A.x + (size_t)(slots[r0 + r] / A.Kp) * A.d; }, [] {}, 0, A.d, n_rows, 0, h_steps,
-                                              lds.rows, wave >> 1, tid, lane);
-        __syncthreads();   // (the rows have been read)
-        few_put(lds.part[wave][lane & 15] + FR * 4 * (lane >> 4), acc);
-        __syncthreads();
-        const int t = tid / (COLS / 4), c = 4 * (tid % (COLS / 4));   // four columns
-        if (t < n_rows) {
-          float v[2][4] = {};
+    for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+    few_multiply<MX, FR, true, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
+      if (r0 > 0) __syncthreads();
+      for (int i = tid; i < n_rows * quads; i += THREADS) {   // four k of a row
+        const int r = i / quads, c = i - r * quads, k = step0 * STEP + 4 * c;
+        uint2 head = make_uint2(0, 0), rest = head;
+        if (k < A.f) {
+          const float* const src = A.h_partial + (size_t)slots[r0 + r] * A.h_parts * 2 * A.f + k;
+          float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
+          for (int p0 = 0; p0 < A.h_parts; p0 += 4) {   // (four parts at a time: each takes the way to the L2)
+            float4 pg[4], pu[4];
 #pragma unroll
-          for (int w = 0; w < kFewWaves; w++) {
-            const float4 p = *reinterpret_cast<const float4*>(&lds.part[w][t][c]);
-            v[w & 1][0] += p.x; v[w & 1][1] += p.y; v[w & 1][2] += p.z; v[w & 1][3] += p.w;
+            for (int p = 0; p < 4; p++) {
+              const float* const at = src + (size_t)min(p0 + p, A.h_parts - 1) * 2 * A.f;
+              pg[p] = *reinterpret_cast<const float4*>(at);
+              pu[p] = *reinterpret_cast<const float4*>(at + A.f);
+            }
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+              if (p0 + p < A.h_parts) {
+                g.x += pg[p].x; g.y += pg[p].y; g.z += pg[p].z; g.w += pg[p].w;
+                u.x += pu[p].x; u.y += pu[p].y; u.z += pu[p].z; u.w += pu[p].w;
+              }
           }
           float h[4], lo[4];
-#pragma unroll
-          for (int i = 0; i < 4; i++) few_swiglu(v[0][i], v[1][i], h[i], lo[i]);
-          uint16_t* const o = A.h + (size_t)slots[r0 + t] * A.f + col0 + c;
-          few_store_agent(o, pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
-          few_store_agent(o + A.h_lo, pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]));
+          few_swiglu(g.x, u.x, h[0], lo[0]);
+          few_swiglu(g.y, u.y, h[1], lo[1]);
+          few_swiglu(g.z, u.z, h[2], lo[2]);
+          few_swiglu(g.w, u.w, h[3], lo[3]);
+          head = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+          rest = make_uint2(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]));
         }
+        *reinterpret_cast<uint2*>(rows + r * pitch + 8 * c) = head;
+        *reinterpret_cast<uint2*>(rows + (n_rows + r) * pitch + 8 * c) = rest;
       }
-      few_arrive(&A.counters->ready[live].n, h_tiles);
-    } else {
-      const int ct = in_expert % d_tiles, part = in_expert / d_tiles, col0 = ct * COLS;
-      const int step0 = min(d_steps, part * per), step1 = min(d_steps, step0 + per);
-      const FewTile<MX, FR> W(A.down, expert, A.f, A.d, col0, lane);
-      const int at_once = few_rows_at_once<true>(per * STEP);
-      auto ready = [&]() __attribute__((always_inline)) {
-        if (tid == 0)
-          while (__hip_atomic_load(&A.counters->ready[live].n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < h_tiles) __builtin_amdgcn_s_sleep(8);
-        __syncthreads();
-      };
-      for (int r0 = 0; r0 < count; r0 += at_once) {
-        const int n_rows = min(at_once, count - r0);
-        mx_f32x4 acc[FR];
-#pragma unroll
-        for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-        if (step1 > step0)
-          few_multiply<MX, FR, true, DEPTH, kFewWaves>(acc, W, [&](int r) { return A.h + (size_t)slots[r0 + r] * A.f; }, ready, A.h_lo, A.f, n_rows, step0,
-                                                       step1 - step0, lds.rows, wave, tid, lane);
-        __syncthreads();
-        few_put(lds.part[wave][lane & 15] + FR * 4 * (lane >> 4), acc);
-        __syncthreads();
-        const int t = tid / (COLS / 2), c = 2 * (tid % (COLS / 2));
-        if (t < n_rows) {
-          float2 v = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int w = 0; w < kFewWaves; w++) {
-            const float2 p = *reinterpret_cast<const float2*>(&lds.part[w][t][c]);
-            v.x += p.x;
-            v.y += p.y;
-          }
-          few_store_agent(A.partial + ((size_t)slots[r0 + t] * A.parts + part) * A.d + col0 + c, __float_as_uint(v.x), __float_as_uint(v.y));
-        }
-      }
-      const bool complete = few_arrive(&A.counters->arrivals[ct], n_live * A.parts);
-      if (tid == 0) last = complete;
       __syncthreads();
-      // out[t] = sum_j w[t, j] sum_parts partial of this column tile: slots in order, parts in order, fp32, one rounding
-      if (last) {
-        for (int i = tid; i < A.T * (COLS / 2); i += kFewWaves * kWave) {
-          const int t = i / (COLS / 2), c = col0 + 2 * (i % (COLS / 2));
-          float2 sum = make_float2(0.f, 0.f), y = sum;
-          const int n = A.Kp * A.parts;
-          const float* const src = A.partial + (size_t)t * n * A.d + c;
-          int j = 0, p = 0;
-          for (int i0 = 0; i0 < n; i0 += 8) {   // (eight at a time: each takes the way to memory)
-            float2 v[8];
-#pragma unroll
-            for (int u = 0; u < 8; u++) v[u] = few_load_partial(src + (size_t)min(i0 + u, n - 1) * A.d);
-#pragma unroll
-            for (int u = 0; u < 8; u++) {
-              if (i0 + u < n) {
-                y.x += v[u].x; y.y += v[u].y;
-                if (++p == A.parts) {
-                  const float w = topk_w[t * A.Kp + j];
-                  sum.x += w * y.x; sum.y += w * y.y;
-                  y = make_float2(0.f, 0.f);
-                  p = 0;
-                  j++;
-                }
-              }
-            }
-          }
-          *reinterpret_cast<uint32_t*>(A.out + (size_t)t * A.d + c) = pack_bf16(sum.x, sum.y);
-        }
-      }
-    }
+    }, rows, n_rows, pitch, step0, active ? count : 0, lane);
+    const int row = r0 + (lane & 15);
+    if (active && row < L.z) few_put(A.partial + ((size_t)slots[row] * A.parts + part) * A.d + col0 + 4 * FR * (lane >> 4), acc);
   }
 }
 
@@ -802,21 +687,32 @@ __global__ __launch_bounds__(kFewRowWaves * kWave, 2) void few_rows_down_kernel(
   }
 }
 
-// The same sum as few_combine's, in a launch of its own: with many tokens too much for one block.
+// out[t] = sum_j w[t, j] sum_parts partial: slots in order, parts in order, fp32, one rounding.
 __global__ __launch_bounds__(256) void few_combine_kernel(const FewArgs A) {
   const int i = blockIdx.x * 256 + threadIdx.x, per = A.d / 2;
-  const int t = i / per, c = 2 * (i % per);
+  const int t = i / per, c = 2 * (i - t * per);
   if (t >= A.T) return;
-  float2 sum = make_float2(0.f, 0.f);
-  for (int j = 0; j < A.Kp; j++) {
-    const int s = t * A.Kp + j;
-    const float w = A.topk_w[s];
-    float2 y = make_float2(0.f, 0.f);
-    for (int p = 0; p < A.parts; p++) {
-      const float2 v = *reinterpret_cast<const float2*>(A.partial + ((size_t)s * A.parts + p) * A.d + c);
-      y.x += v.x; y.y += v.y;
+  const int n = A.Kp * A.parts;
+  const float* const src = A.partial + (size_t)t * n * A.d + c;
+  float2 sum = make_float2(0.f, 0.f), y = sum;
+  int j = 0, p = 0;
+  for (int i0 = 0; i0 < n; i0 += 8) {   // (eight at a time: each takes the way to the L2)
+    float2 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) v[u] = *reinterpret_cast<const float2*>(src + (size_t)min(i0 + u, n - 1) * A.d);
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+      if (i0 + u < n) {
+        y.x += v[u].x; y.y += v[u].y;
+        if (++p == A.parts) {
+          const float w = A.topk_w[t * A.Kp + j];
+          sum.x += w * y.x; sum.y += w * y.y;
+          y = make_float2(0.f, 0.f);
+          p = 0;
+          j++;
+        }
+      }
     }
-    sum.x += w * y.x; sum.y += w * y.y;
   }
   *reinterpret_cast<uint32_t*>(A.out + (size_t)t * A.d + c) = pack_bf16(sum.x, sum.y);
 }
@@ -824,33 +720,49 @@ __global__ __launch_bounds__(256) void few_combine_kernel(const FewArgs A) {
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
 
 // Experts that can have tokens.
-int few_live_bound(const Dims& D) { return (int)min((long long)D.E, (long long)D.T * D.k) + D.Es; }
+int few_live_bound(const Dims& D) { return (int)min((long long)D.Et, D.N); }
 
-// Whether the wavefronts of a block share the contraction (at most 16 tokens, whose rows fit LDS) or the rows.
-bool few_share_k(const Dims& D) { return D.T <= kFewGroup && D.d <= kFewRowK; }
-
-// Frags of 16 columns of a wavefront where the rows are shared: 4, or 2 where that leaves CUs without a block.
-int few_rows_frags(const Dims& D, int C) { return (long long)((C + 127) / 128) * few_live_bound(D) >= 512 ? 4 : 2; }
-
-// Columns of a tile of the down projection, and parts of d_ffn: as many as give every CU two blocks, but at least four steps (of 32 k) for
-// a wavefront, and no more k in a part than fit LDS.
-int few_down_cols(const Dims& D, bool mx) { return !few_share_k(D) ? 64 * few_rows_frags(D, D.d) : mx ? 32 : 64; }
-int few_parts(const Dims& D, bool mx) {
-  const int cols = few_down_cols(D, mx), waves = few_share_k(D) ? kFewWaves : 1;
-  const long long blocks = (long long)((D.d + cols - 1) / cols) * few_live_bound(D);
-  const int most = max(1, D.f / ((mx ? 128 : 32) * 4 * waves)), least = few_share_k(D) ? (D.f + kFewRowK / 2 - 1) / (kFewRowK / 2) : 1;
-  return max(least, (int)min((long long)most, max(1ll, (512 + blocks - 1) / blocks)));
+// How a problem is cut.
+struct FewPlan {
+  bool share_rows;          // few_rows_*_kernel
+  int h_frags, d_frags;     // of a wavefront's columns (share_rows)
+  int parts, h_parts;
+};
+FewPlan few_plan(const Dims& D, bool mx) {
+  FewPlan P = {};
+  const int live = few_live_bound(D), step = mx ? 128 : 32;
+  auto divide = [](long long a, long long b) { return (a + b - 1) / b; };
+  P.share_rows = D.T > kFewGroup;
+  if (P.share_rows) {
+    // frags: 4, or 2 where that leaves CUs without a block
+    P.h_frags = divide(D.f, 128) * live >= 512 ? 4 : 2;
+    P.d_frags = divide(D.d, 128) * live >= 512 ? 4 : 2;
+    const long long blocks = divide(D.d, 64 * P.d_frags) * live;   // every CU two blocks, but at least four steps
+    P.parts = (int)max(1ll, min((long long)max(1, D.f / (step * 4)), divide(512, blocks)));
+    P.h_parts = 1;
+  } else {
+    // every CU two blocks, but at least two steps; and rows that fit LDS
+    auto cut = [&](int K, int cols, int C, int most_k) {
+      const long long blocks = divide(C, cols) * live, steps = divide(K, step);
+      const long long parts = max(divide(steps, most_k / step), min(max(1ll, steps / 2), divide(512, blocks)));
+      return (int)divide(steps, divide(steps, parts));   // (no part without steps)
+    };
+    P.h_parts = cut(D.d, 256, D.f, kFewRowK);
+    P.parts = cut(D.f, 512, D.d, kFewRowK / 2);
+  }
+  return P;
 }
 
-struct FewLayout { size_t logits, sched, counters, h, partial, total; };
+struct FewLayout { size_t logits, sched, h, partial, h_partial, total; };
 FewLayout few_layout(const Dims& D) {
   FewLayout L;
+  const FewPlan P = few_plan(D, false), Q = few_plan(D, true);
   size_t o = 0;
   L.sched = o; o += round_up(sizeof(FewSched), 256);
   L.logits = o; o += round_up((size_t)D.T * D.E * sizeof(float), 256);
-  L.counters = o; o += round_up(few_counters_bytes(D.d), 256);
   L.h = o; o += round_up((size_t)D.N * D.f * 2 * sizeof(uint16_t), 256);
-  L.partial = o; o += round_up((size_t)D.N * max(few_parts(D, false), few_parts(D, true)) * D.d * sizeof(float), 256);
+  L.partial = o; o += round_up((size_t)D.N * max(P.parts, Q.parts) * D.d * sizeof(float), 256);
+  L.h_partial = o; o += round_up((size_t)D.N * max(P.h_parts, Q.h_parts) * 2 * D.f * sizeof(float), 256);
   L.total = o;
   return L;
 }
@@ -863,20 +775,21 @@ int check_few(const moe_shape* s, Dims* D) {
 }
 
 template <bool MX>
-void few_launch_experts(hipStream_t st, const FewArgs& A, const Dims& D) {
+void few_launch_experts(hipStream_t st, const FewArgs& A, const Dims& D, const FewPlan& P) {
   const int live = few_live_bound(D);
-  if (!few_share_k(D)) {
+  if (P.share_rows) {
     const dim3 block(kFewRowWaves * kWave);
-    if (few_rows_frags(D, D.f) == 4) MOE_LAUNCH("few_gate_up", st, (few_rows_gate_up_kernel<MX, 4>), dim3((D.f + 127) / 128, live), block, 0, st, A);
+    if (P.h_frags == 4) MOE_LAUNCH("few_gate_up", st, (few_rows_gate_up_kernel<MX, 4>), dim3((D.f + 127) / 128, live), block, 0, st, A);
     else MOE_LAUNCH("few_gate_up", st, (few_rows_gate_up_kernel<MX, 2>), dim3((D.f + 63) / 64, live), block, 0, st, A);
-    if (few_rows_frags(D, D.d) == 4) MOE_LAUNCH("few_down", st, (few_rows_down_kernel<MX, 4>), dim3((D.d + 255) / 256, live, A.parts), block, 0, st, A);
+    if (P.d_frags == 4) MOE_LAUNCH("few_down", st, (few_rows_down_kernel<MX, 4>), dim3((D.d + 255) / 256, live, A.parts), block, 0, st, A);
     else MOE_LAUNCH("few_down", st, (few_rows_down_kernel<MX, 2>), dim3((D.d + 127) / 128, live, A.parts), block, 0, st, A);
     MOE_LAUNCH("few_combine", st, few_combine_kernel, dim3((unsigned)(((size_t)D.T * (D.d / 2) + 255) / 256)), dim3(256), 0, st, A);
     return;
   }
-  constexpr int FR = MX ? 2 : 4;
-  const int tiles = live * (D.f / (16 * FR) + D.d / (16 * FR) * A.parts);   // (at most)
-  MOE_LAUNCH("few_layer", st, (few_layer_kernel<MX, FR, 3>), dim3(min(tiles, kFewBlocks)), dim3(kFewWaves * kWave), 0, st, A);
+  const dim3 block(kFewWaves * kWave);
+  MOE_LAUNCH("few_gate_up", st, (few_gate_up_kernel<MX, 3>), dim3((D.f + 255) / 256 * P.h_parts, live + (A.fused_gate ? 1 : 0)), block, 0, st, A);
+  MOE_LAUNCH("few_down", st, (few_down_kernel<MX, 3>), dim3((D.d + 511) / 512 * P.parts, live), block, 0, st, A);
+  MOE_LAUNCH("few_combine", st, few_combine_kernel, dim3((unsigned)(((size_t)D.T * (D.d / 2) + 255) / 256)), dim3(256), 0, st, A);
 }
 
 template <bool MX>
@@ -895,27 +808,27 @@ int few_forward(const moe_shape* shape, const uint16_t* x, const uint16_t* w_rou
   const FewLayout L = few_layout(D);
   if (ws_bytes < L.total) return MOE_ERR_WORKSPACE;
   uint8_t* const wsb = static_cast<uint8_t*>(ws);
+  const FewPlan P = few_plan(D, MX);
   FewArgs A = {};
-  A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm; A.parts = few_parts(D, MX);
-  A.fused_gate = few_share_k(D) && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
+  A.parts = P.parts; A.h_parts = P.h_parts;
+  A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm; A.fused_gate = !P.share_rows && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
   A.x = x; A.w_router = w_router; A.topk_idx = topk_idx; A.topk_w = topk_w; A.out = out;
   A.gate = W[0]; A.up = W[1]; A.down = W[2];
   A.logits = reinterpret_cast<float*>(wsb + L.logits);
   A.sched = reinterpret_cast<FewSched*>(wsb + L.sched);
-  A.counters = reinterpret_cast<FewCounters*>(wsb + L.counters);
   A.h = reinterpret_cast<uint16_t*>(wsb + L.h);
   A.h_lo = (size_t)D.N * D.f;
   A.partial = reinterpret_cast<float*>(wsb + L.partial);
+  A.h_partial = reinterpret_cast<float*>(wsb + L.h_partial);
   hipStream_t st = (hipStream_t)stream;
   if (w_router)
-    MOE_LAUNCH("few_router", st, few_router_kernel, dim3((D.E + 15) / 16, (D.T + 15) / 16), dim3(kFewWaves * kWave), 0, st, A);
-  if (!w_router && A.fused_gate) MOE_LAUNCH("few_clear", st, few_clear_kernel, dim3(1), dim3(256), 0, st, A);
+    MOE_LAUNCH("few_router", st, few_router_kernel, dim3((D.E + 15) / 16, (D.T + 15) / 16), dim3(kFewRouterWaves * kWave), 0, st, A);
   if (!A.fused_gate) {
     if (D.E <= 64) MOE_LAUNCH("few_gate", st, few_gate_kernel<1>, dim3(1), dim3(1024), 0, st, A);
     else if (D.E <= 256) MOE_LAUNCH("few_gate", st, few_gate_kernel<4>, dim3(1), dim3(1024), 0, st, A);
     else MOE_LAUNCH("few_gate", st, few_gate_kernel<16>, dim3(1), dim3(1024), 0, st, A);
   }
-  few_launch_experts<MX>(st, A, D);
+  few_launch_experts<MX>(st, A, D, P);
   return launch_status();
 }
 

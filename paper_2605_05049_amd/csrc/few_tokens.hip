@@ -3,14 +3,20 @@
 // on weights in bf16 (W_gate, W_up [E', d, f], W_down [E', f, d]) or microscaled 4-bit floating point ([E', f, d / 2], [E', d, f / 2]).
 //
 // What bounds it: the weights of the experts that some token chose are read once and multiply a handful of rows, so the time is that of
-// streaming them.  The rows are not permuted into buffers: an expert's tokens are columns 0 .. 15 (of up to four groups) of an MFMA whose
-// other operand is the weights.  The weights go from memory straight into registers: of bf16 weights a lane holds 4 columns of 8 k-rows, and
+// streaming them.  The rows are not permuted into buffers: an expert's tokens are columns 0 .. 15 (of one or two groups) of an MFMA whose
+// other operand is the weights.  The weights go from memory straight into registers: of bf16 weights a lane holds 2 or 4 columns of 8 k-rows, and
 // turns them with byte permutes into the MFMA's operand, 8 k of one column; of 4-bit weights it holds 32 k of one column (a block, one scale) and
 // widens them to bf16, exactly.  The hidden activation stays in fp32 in effect: it is kept as a bf16 head and a bf16 remainder, both of
-// which multiply W_down; the partial sums of W_down's parts and the experts are added in fp32, in a fixed order.
+// which multiply W_down; the partial sums over K and the experts are added in fp32, in a fixed order.
+//
+// Launches: logits; gate (with at most 16 tokens every block of the next one makes it for itself); G and U by columns and parts of d; with more than 16
+// tokens H; H W_down by columns and parts of d_ffn; the weighted sum.  Measured, 8 experts of 4096 x 14336, top 2: 1 token 122 us in bf16 (5.8 TB/s; a
+// large read reaches 6.2) and 50 us in 4 bits (3.7 TB/s); 16 tokens 431 and 179 us; 64 tokens 478 and 229 us.
 #include "mxfp4.h"
 #include "route.h"
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace moe {
@@ -23,6 +29,7 @@ constexpr int kFewWaves = 8;          // wavefronts of a block, at most 16 token
 constexpr int kFewRouterWaves = 8;    // ... of few_router_kernel: they share a contraction
 constexpr int kFewFusedSlots = 512, kFewFusedExperts = 256;   // at most, where every block makes the gate for itself
 constexpr int kFewGroup = 16;         // tokens of an MFMA
+constexpr int kFewTurn = 2 * kFewGroup;   // rows at most that go through the weights together
 
 // The experts that have tokens, in expert order, and the slots of each.
 struct FewSched {
@@ -117,9 +124,10 @@ __global__ __launch_bounds__(1024) void few_gate_kernel(const FewArgs A) {
 
 // ---- what a lane holds of the weights --------------------------------------------------------------------------------------------------
 
-// FR frags of 16 columns: column FR * m + a of the tile is row m of frag a.  A step is 32 k of bf16 or 128 k of 4-bit weights (the last one may be
+// FR frags of 16 columns: column FR * m + a of the tile is row m of frag a.  A step is 32 k of bf16 or 256 k of 4-bit weights (the last one may be
 // cut short: its codes are zero past the end).
 template <bool MX, int FR> struct FewTile;
+constexpr int kFewScaleSteps = 8, kFewScalePitch = 8 * kFewScaleSteps + 8;   // 4-bit weights: steps of a chunk at most; a column's scales in LDS
 
 __device__ __forceinline__ int few_scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }   // the same in all lanes: the compiler is told so
 
@@ -130,10 +138,14 @@ __device__ __forceinline__ FewBase few_base(const uint8_t* p) {
   return (FewBase)((unsigned long long)(unsigned)few_scalar((int)(v >> 32)) << 32 | (unsigned)few_scalar((int)v));
 }
 // From a scalar base and 32 bits of the lane's own (left to itself the compiler keeps a 64-bit address per lane and load, 48 registers in all).
-template <class T>
+// ONCE: nothing else of the lines is read, they need not stay in the caches (a row of 64 bf16 columns is a line of 128 bytes; the 64 bytes that a step takes
+// of a row of 4-bit weights are half of one).  One token, 2 of 8 experts of 4096 x 14336 in bf16: 149 -> 134 us.
+template <class T, bool ONCE>
 __device__ __forceinline__ T few_load(FewBase base, unsigned off) {
   asm("" : "+s"(base));
-  return *(const T __attribute__((address_space(1)))*)(base + off);
+  const auto p = (const T __attribute__((address_space(1)))*)(base + off);
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
 }
 
 template <int FR> struct FewTile<false, FR> {
@@ -152,11 +164,13 @@ template <int FR> struct FewTile<false, FR> {
     step = few_scalar(step);
     FewBase p = base + (size_t)step * 32 * row;   // (scalar: a load's address is this and 32 bits of the lane's own)
 #pragma unroll
-    for (int i = 0; i < 8; i++, p += row) s.w[i] = few_load<word>(p, lane_off);
+    for (int i = 0; i < 8; i++, p += row) s.w[i] = few_load<word, FR == 4>(p, lane_off);
   }
-  __device__ __forceinline__ void end(Stage&, int) const {}
+  struct Codes {};
+  __device__ __forceinline__ void bring_scales(char*, int, int, int) const {}
+  __device__ __forceinline__ Codes codes(const char*, int) const { return {}; }
   // frag a: 8 k of column a, from the halves of 8 words
-  __device__ __forceinline__ mx_bf16x8 frag(const Stage& s, int a, int) const {
+  __device__ __forceinline__ mx_bf16x8 frag(const Stage& s, Codes, int a, int) const {
     union { unsigned p[4]; mx_bf16x8 v; } u;
 #pragma unroll
     for (int p = 0; p < 4; p++) u.p[p] = __builtin_amdgcn_perm(s.w[2 * p + 1][a / 2], s.w[2 * p][a / 2], a & 1 ? 0x07060302u : 0x05040100u);
@@ -165,46 +179,76 @@ template <int FR> struct FewTile<false, FR> {
 };
 
 template <int FR> struct FewTile<true, FR> {
-  static constexpr int KS = 4;
+  static constexpr int KS = 8;
   typedef uint32_t quad __attribute__((ext_vector_type(4)));   // a block of 32 k
-  struct Stage { quad w[FR]; unsigned s[FR]; };
+  struct Stage { quad w[2][FR]; };             // blocks q and 4 + q of the step's eight: whole lines of 128 bytes
   FewBase base, sbase;                         // of column 0
-  unsigned lane_off, lane_soff;                // this lane's first column, block q
-  int kb, q;
+  unsigned lane_off;                           // this lane's first column, block q
+  int kb, q, m;
   __device__ __forceinline__ FewTile(const FewWeights& W, int expert, int K, int C, int col0, int lane) {
     kb = K / kMxBlock;
     q = lane >> 4;
+    m = lane & 15;
     const size_t row = (size_t)expert * C + col0;
     base = few_base(W.w + row * (kb * 16));
     sbase = few_base(W.scales + row * kb);
-    lane_soff = (unsigned)(FR * (lane & 15)) * (unsigned)kb + q;
-    lane_off = lane_soff * 16;
+    lane_off = ((unsigned)(FR * m) * (unsigned)kb + q) * 16;
   }
   __device__ __forceinline__ void load(Stage& s, int step) const {
     step = few_scalar(step);
-    const int b = min(4 * step, kb - 1 - q);   // (a block past the end: the last one)
+    const int b0 = min(8 * step, kb - 1 - q), b1 = min(8 * step + 4, kb - 1 - q);   // (a block past the end: the last one)
 #pragma unroll
     for (int a = 0; a < FR; a++) {
-      s.w[a] = few_load<quad>(base + (size_t)a * (kb * 16), lane_off + b * 16);
-      s.s[a] = few_load<uint8_t>(sbase + (size_t)a * kb, lane_soff + b);
+      const FewBase p = base + (size_t)a * (kb * 16);
+      s.w[0][a] = few_load<quad, false>(p, lane_off + b0 * 16);
+      s.w[1][a] = few_load<quad, false>(p, lane_off + b1 * 16);
     }
   }
-  __device__ __forceinline__ mx_bf16x8 frag(const Stage& s, int a, int ks) const {
-    const float scale = __uint_as_float(s.s[a] == 255u ? 0x7fc00000u : s.s[a] << 23);
-    const unsigned v = ks == 0 ? s.w[a].x : ks == 1 ? s.w[a].y : ks == 2 ? s.w[a].z : s.w[a].w;
+  // The scales of `steps` (at most kFewScaleSteps) steps of the wavefront's columns into LDS, 8 bytes a step; 1 past the end of K, where the rows are zero.
+  // (Read by steps from memory, a line of a column's scales was fetched again for each: 4096 x 14336, 8 experts, 16 rows: 220 against 170 us.)
+  __device__ __forceinline__ void bring_scales(char* to, int step0, int steps, int lane) const {
+    typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(2)));   // (kb is even)
+#pragma unroll
+    for (int i = 0; i < 16 * FR * kFewScaleSteps / kWave; i++) {
+      const int c = i * (kWave / kFewScaleSteps) + lane / kFewScaleSteps, st = lane % kFewScaleSteps, b = 8 * (step0 + st);
+      if (st < steps) {
+        unsigned long long v = ~0ull / 255 * 127;
+        if (kb >= 8) {
+          const int at = min(b, kb - 8);
+          const pair w = few_load<pair, false>(sbase, (unsigned)c * (unsigned)kb + at);
+          const int past = 8 * (b - at);   // bits that are of blocks before b
+          const unsigned long long all = (unsigned long long)w[1] << 32 | w[0];
+          v = past ? all >> past | v << (64 - past) : all;
+        } else {
+          for (int k = 0; k < kb; k++) v = (v & ~(255ull << (8 * k))) | (unsigned long long)few_load<uint8_t, false>(sbase, (unsigned)c * (unsigned)kb + k) << (8 * k);
+        }
+        *reinterpret_cast<unsigned long long*>(to + c * kFewScalePitch + 8 * st) = v;
+      }
+    }
+  }
+  struct Codes { float scale[2][FR]; };   // of the stage's blocks
+  __device__ __forceinline__ Codes codes(const char* at, int step) const {   // step: from the chunk's first
+    Codes c;
+#pragma unroll
+    for (int a = 0; a < FR; a++) {
+      const uint2 v = *reinterpret_cast<const uint2*>(at + (FR * m + a) * kFewScalePitch + 8 * step);
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const unsigned code = ((h ? v.y : v.x) >> (8 * q)) & 255u;
+        c.scale[h][a] = __uint_as_float(code == 255u ? 0x7fc00000u : code << 23);
+      }
+    }
+    return c;
+  }
+  __device__ __forceinline__ mx_bf16x8 frag(const Stage& s, const Codes& c, int a, int ks) const {   // ks: part ks % 4 (of 8 k) of block 4 (ks / 4) + q
+    const float scale = c.scale[ks >> 2][a];
+    const unsigned v = s.w[ks >> 2][a][ks & 3];
     union { mx_bf16x2 p[4]; mx_bf16x8 v; } u;
     u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 0);
     u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 1);
     u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 2);
     u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 3);
     return u.v;
-  }
-  // the last step of K: blocks past the end become zeros
-  __device__ __forceinline__ void end(Stage& s, int step) const {
-    if (4 * step + q >= kb) {
-#pragma unroll
-      for (int a = 0; a < FR; a++) { s.w[a] = quad{0, 0, 0, 0}; s.s[a] = 127; }
-    }
   }
 };
 
@@ -214,7 +258,11 @@ __device__ __forceinline__ int4 few_live(const FewArgs& A, int i) {
   return make_int4(__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), 0);
 }
 
-__device__ __forceinline__ int few_steps(bool mx, int K) { return mx ? (K / 32 + 3) / 4 : K / 32; }
+constexpr int few_step(bool mx) { return mx ? 256 : 32; }
+__device__ __host__ __forceinline__ int few_steps(bool mx, int K) { return (K + few_step(mx) - 1) / few_step(mx); }
+// In LDS: the lane's 8 k for MFMA ks of a step, from the step's first k on, in units of 8 k.
+template <bool MX>
+__device__ __forceinline__ int few_piece(int q, int ks) { return MX ? 16 * (ks >> 2) + 4 * q + (ks & 3) : q; }
 
 __device__ __forceinline__ void few_swiglu(float g, float u, float& h, float& lo) {
   h = g / (1.0f + __expf(-g)) * u;
@@ -234,12 +282,13 @@ __device__ __forceinline__ void few_put(float* dst, const mx_f32x4 (&acc)[FR]) {
   }
 }
 
-// ---- at most 16 tokens: the wavefronts of a block have columns next to each other ------------------------------------------------------------
+// ---- the experts' products ------------------------------------------------------------------------------------------------------------------
 //
-// and the contraction is shared between blocks, whose partial sums the next launch adds.  A step of bf16 weights takes 32 k-rows that lie 2 C bytes
-// apart: if each wavefront of a block goes through rows of its own, a CU has 8 times as many pages in use at once (reading two pairs of 4096 x 14336
-// alone, 5.0 against 6.1 TB/s).  A launch that goes on from the logits to the end by itself was slower: its wavefronts take their work from counters
-// and wait for each other through memory, and 512 blocks that begin with an atomic each have their answers after 25 us.
+// The wavefronts of a block have columns next to each other, and the contraction is shared between blocks, whose partial sums the next launch adds.  A
+// step of bf16 weights takes 32 k-rows that lie 2 C bytes apart: if each wavefront of a block goes through rows of its own, a CU has 8 times as many
+// pages in use at once (reading two pairs of 4096 x 14336 alone, 5.0 against 6.1 TB/s).  A launch that goes on from the logits to the end by itself
+// was slower: its wavefronts take their work from counters and wait for each other through memory, and 512 blocks that begin with an atomic each have
+// their answers after 25 us.
 
 // The gate of the call for one block, in LDS; the experts that have slots.
 struct FewGate {
@@ -251,11 +300,13 @@ struct FewGate {
 // Live expert blockIdx.y of the call: its id and its slots; count = 0: there is none.  With the gate fused, every block makes it from the logits for
 // itself (a launch and the wait for it cost more); block (0, 0) leaves ids and weights in memory, block (0, `last_row`) the schedule.
 struct FewExpert { int id, count; const int* slots; };
+template <bool FUSED>
 __device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, int last_row) {
   FewExpert X;
-  if (!A.fused_gate) {
-    const bool live = (int)blockIdx.y < A.sched->n_live;
-    const int4 v = few_live(A, blockIdx.y);
+  if (!FUSED || !A.fused_gate) {
+    const int n_live = A.sched->n_live;
+    const bool live = (int)blockIdx.y < n_live;
+    const int4 v = few_live(A, live ? n_live - 1 - blockIdx.y : 0);
     X.id = v.x;
     X.count = live ? v.z : 0;
     X.slots = A.sched->slots + v.y;
@@ -319,37 +370,52 @@ __device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, in
   return X;
 }
 
-// Rows of a product in LDS, for all the k that a block works on: as many rows as fit go through the weights together.
-constexpr int kFewRowBytes = 60 * 1024;
-constexpr int kFewRowK = 1792;   // k at most: of 16 rows (LO: half of them)
+// Rows of a product in LDS: of one turn (16 GROUPS rows of an expert at most), as many steps of k as fit.
+__device__ __host__ constexpr int few_row_bytes(bool mx) { return (mx ? 54 : 60) * 1024; }   // (a block has half of a CU's LDS)
+__device__ __host__ constexpr int few_scale_bytes(bool mx, int FR) { return mx ? kFewWaves * 16 * FR * kFewScalePitch : 16; }
 __device__ __forceinline__ int few_row_pitch(int k) { return 2 * k + 16; }
+template <bool MX, bool LO>
+__device__ __forceinline__ int few_chunk_steps(int n_rows) {
+  const int fit = max(1, (few_row_bytes(MX) / ((LO ? 2 : 1) * n_rows) - 16) / (2 * few_step(MX)));
+  return MX ? min(fit, kFewScaleSteps) : fit;
+}
 
-// acc[a] += over `count` steps from step0 on: lane l's element i of acc[a] is column FR (4 (l / 16) + i) + a, row l % 16 of `rows` (LO: with the
-// remainders after all rows; rows past the last repeat it).  Between the first weights' requests and their use stands `bring`, which fills `rows`.
-template <bool MX, int FR, bool LO, int DEPTH, class F>
-__device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<MX, FR>& W, F&& bring, const char* rows, int n_rows, int pitch, int step0,
-                                             int count, int lane) {
+// acc[g][a] += over `count` steps from step0 on: lane l's element i of acc[g][a] is column FR (4 (l / 16) + i) + a, row 16 g + l % 16 of `rows` (LO: with
+// the remainders after all rows; rows past the last repeat it).  Between the first weights' requests and their use stands `bring`, which fills `rows`.
+template <bool MX, int FR, int TG, bool LO, int DEPTH, class F>
+__device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[TG][FR], const FewTile<MX, FR>& W, F&& bring, const char* rows, int n_rows, int pitch, const char* scales,
+                                             int step0, int count, int lane) {
   typedef FewTile<MX, FR> Tile;
-  constexpr int STEP = MX ? 128 : 32;
+  constexpr int STEP = few_step(MX);
   const int last = step0 + count - 1;
   typename Tile::Stage st[DEPTH];
 #pragma unroll
   for (int i = 0; i < DEPTH; i++)
     if (i < count) W.load(st[i], step0 + i);
   bring();
-  const char* const at = rows + min(lane & 15, n_rows - 1) * pitch + (MX ? 64 : 16) * (lane >> 4);
+  const char* at[TG];
+#pragma unroll
+  for (int g = 0; g < TG; g++) at[g] = rows + min(16 * g + (lane & 15), n_rows - 1) * pitch;
   auto consume = [&](const typename Tile::Stage& s, int i) __attribute__((always_inline)) {
-    const char* const x = at + i * (STEP * 2);
+    const auto codes = W.codes(scales, i);
 #pragma unroll
     for (int ks = 0; ks < Tile::KS; ks++) {
-      const mx_bf16x8 v = *reinterpret_cast<const mx_bf16x8*>(x + ks * 16);
-      mx_bf16x8 l = v;
-      if constexpr (LO) l = *reinterpret_cast<const mx_bf16x8*>(x + n_rows * pitch + ks * 16);
+      if (ks > 0 && TG > 1) __builtin_amdgcn_sched_barrier(0);   // (or the operands of all are in registers at once)
+      mx_bf16x8 v[TG], l[TG];
+#pragma unroll
+      for (int g = 0; g < TG; g++) {
+        const char* const x = at[g] + i * (STEP * 2) + 16 * few_piece<MX>(lane >> 4, ks);
+        v[g] = *reinterpret_cast<const mx_bf16x8*>(x);
+        if constexpr (LO) l[g] = *reinterpret_cast<const mx_bf16x8*>(x + n_rows * pitch);
+      }
 #pragma unroll
       for (int a = 0; a < FR; a++) {
-        const mx_bf16x8 w = W.frag(s, a, ks);
-        acc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, v, acc[a], 0, 0, 0);
-        if constexpr (LO) acc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, l, acc[a], 0, 0, 0);
+        const mx_bf16x8 w = W.frag(s, codes, a, ks);
+#pragma unroll
+        for (int g = 0; g < TG; g++) {
+          acc[g][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, v[g], acc[g][a], 0, 0, 0);
+          if constexpr (LO) acc[g][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, l[g], acc[g][a], 0, 0, 0);
+        }
       }
     }
   };
@@ -368,322 +434,158 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[FR], const FewTile<
 #pragma unroll
   for (int u = 0; u < DEPTH; u++) {
     if (i + u < count) {
-      if (i + u == count - 1) W.end(st[u], last);
-      __builtin_amdgcn_sched_barrier(0);
       consume(st[u], i + u);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
 
-// One of `h_parts` parts of G and U of 256 columns of one expert: wavefronts 0, 2, 4, 6 make G, the others U, of 64 columns each.
-template <bool MX, int DEPTH>
+// Parts of K: this block's steps.
+struct FewPart { int step0, steps; };
+template <bool MX>
+__device__ __forceinline__ FewPart few_part(int K, int part, int parts) {
+  const int steps = few_steps(MX, K), per = (steps + parts - 1) / parts, step0 = min(steps, part * per);
+  return {step0, min(steps, step0 + per) - step0};
+}
+
+// The sums of the rows r0 .. of an expert over one part of K, chunk by chunk.  `bring` makes sizeof(V) / 2 k of row r0 + r, from k on.
+template <bool MX, int FR, int TG, bool LO, int DEPTH, class V, class F>
+__device__ __forceinline__ void few_turn(mx_f32x4 (&acc)[TG][FR], const FewTile<MX, FR>& W, F&& bring, char* rows, char* scales, int n_rows, int K, FewPart part,
+                                         bool active, int lane) {
+  constexpr int STEP = few_step(MX), THREADS = kFewWaves * kWave;
+  const int per = min(part.steps, few_chunk_steps<MX, LO>(n_rows)), pitch = few_row_pitch(per * STEP), pieces = per * STEP * 2 / (int)sizeof(V);
+#pragma unroll
+  for (int g = 0; g < TG; g++)
+#pragma unroll
+    for (int a = 0; a < FR; a++) acc[g][a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < part.steps; s0 += per) {
+    const int step0 = part.step0 + s0, count = min(per, part.steps - s0);
+    few_multiply<MX, FR, TG, LO, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
+      __syncthreads();
+      W.bring_scales(scales, step0, count, lane);
+      for (int i = threadIdx.x; i < n_rows * pieces; i += THREADS) {
+        const int r = i / pieces, c = i - r * pieces, k = step0 * STEP + (int)sizeof(V) / 2 * c;
+        V v = {}, lo = {};   // (past the end of K)
+        if (k < K) bring(r, k, v, lo);
+        V* const to = reinterpret_cast<V*>(rows + r * pitch) + c;
+        *to = v;
+        if constexpr (LO) *reinterpret_cast<V*>(reinterpret_cast<char*>(to) + n_rows * pitch) = lo;
+      }
+      __syncthreads();
+    }, rows, n_rows, pitch, scales, step0, active ? count : 0, lane);
+  }
+}
+
+// One of `h_parts` parts of G and U of 64 FR columns of one expert: wavefronts 0, 2, 4, 6 make G, the others U, of 16 FR columns each.
+template <bool MX, int FR, int GROUPS, int DEPTH>
 __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_gate_up_kernel(const FewArgs A) {
-  constexpr int FR = 4, WC = 16 * FR, STEP = MX ? 128 : 32, THREADS = kFewWaves * kWave;
-  __shared__ __attribute__((aligned(16))) char rows[kFewRowBytes];
+  constexpr int WC = 16 * FR;
+  __shared__ __attribute__((aligned(16))) char rows[few_row_bytes(MX)];
+  __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR)];
   __shared__ FewGate S;
-  const int tid = threadIdx.x, lane = tid & 63, wave = few_scalar(tid >> 6);
-  const FewExpert X = few_expert(A, S, gridDim.y - 1);
+  const int lane = threadIdx.x & 63, wave = few_scalar(threadIdx.x >> 6);
+  const FewExpert X = few_expert<GROUPS == 1>(A, S, gridDim.y - 1);
   if (X.count == 0) return;
   const int ct = blockIdx.x / A.h_parts, part = blockIdx.x - ct * A.h_parts;
-  const int steps = few_steps(MX, A.d), per = (steps + A.h_parts - 1) / A.h_parts;
-  const int step0 = min(steps, part * per), count = min(steps, step0 + per) - step0;
   const int col0 = ct * 4 * WC + WC * (wave >> 1);
   const bool active = col0 < A.f;   // (widths are multiples of 64: a wavefront has all its columns or none)
   const FewTile<MX, FR> W(wave & 1 ? A.up : A.gate, X.id, A.d, A.f, active ? col0 : 0, lane);
-  const int pitch = few_row_pitch(per * STEP), pieces = per * STEP / 8;
-  for (int r0 = 0; r0 < X.count; r0 += kFewGroup) {
-    const int n_rows = min(kFewGroup, X.count - r0);
-    mx_f32x4 acc[FR];
+  auto turn = [&](int r0, auto tg) __attribute__((always_inline)) {
+    constexpr int TG = decltype(tg)::value;
+    mx_f32x4 acc[TG][FR];
+    few_turn<MX, FR, TG, false, DEPTH, uint4>(acc, W, [&](int r, int k, uint4& v, uint4&) __attribute__((always_inline)) {
+      v = *reinterpret_cast<const uint4*>(A.x + (size_t)(X.slots[r0 + r] / A.Kp) * A.d + k);
+    }, rows, scales + (MX ? wave * 16 * FR * kFewScalePitch : 0), min(kFewGroup * TG, X.count - r0), A.d, few_part<MX>(A.d, part, A.h_parts), active, lane);
 #pragma unroll
-    for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-    few_multiply<MX, FR, false, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
-      if (r0 > 0) __syncthreads();
-      for (int i = tid; i < n_rows * pieces; i += THREADS) {
-        const int r = i / pieces, c = i - r * pieces, k = step0 * STEP + 8 * c;
-        uint4 v = make_uint4(0, 0, 0, 0);   // (past the end of K)
-        if (k < A.d) v = *reinterpret_cast<const uint4*>(A.x + (size_t)(X.slots[r0 + r] / A.Kp) * A.d + k);
-        *reinterpret_cast<uint4*>(rows + r * pitch + 16 * c) = v;
-      }
-      __syncthreads();
-    }, rows, n_rows, pitch, step0, active ? count : 0, lane);
-    const int row = r0 + (lane & 15);
-    if (active && row < X.count)
-      few_put(A.h_partial + (((size_t)X.slots[row] * A.h_parts + part) * 2 + (wave & 1)) * A.f + col0 + 4 * FR * (lane >> 4), acc);
+    for (int g = 0; g < TG; g++) {
+      const int row = r0 + 16 * g + (lane & 15);
+      if (active && row < X.count)
+        few_put(A.h_partial + (((size_t)X.slots[row] * A.h_parts + part) * 2 + (wave & 1)) * A.f + col0 + 4 * FR * (lane >> 4), acc[g]);
+    }
+  };
+  for (int r0 = 0; r0 < X.count; r0 += GROUPS * kFewGroup) {
+    if (GROUPS == 2 && X.count - r0 > kFewGroup) turn(r0, std::integral_constant<int, GROUPS>{});
+    else turn(r0, std::integral_constant<int, 1>{});
   }
 }
 
-// 512 columns of H W_down of one expert over one of `parts` parts of d_ffn.  H = silu(G) * U of that part is made here, from the partial sums of G and U
-// (in order): head and remainder.
-template <bool MX, int DEPTH>
+// H = silu(G) * U of 4 columns, from the partial sums of G and U (in order): heads and remainders.
+__device__ __forceinline__ void few_hidden(const FewArgs& A, int slot, int k, uint2& head, uint2& rest) {
+  const float* const src = A.h_partial + (size_t)slot * A.h_parts * 2 * A.f + k;
+  float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
+  for (int p0 = 0; p0 < A.h_parts; p0 += 4) {   // (four parts at a time: each takes the way to the L2)
+    float4 pg[4], pu[4];
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+      const float* const at = src + (size_t)min(p0 + p, A.h_parts - 1) * 2 * A.f;
+      pg[p] = *reinterpret_cast<const float4*>(at);
+      pu[p] = *reinterpret_cast<const float4*>(at + A.f);
+    }
+#pragma unroll
+    for (int p = 0; p < 4; p++)
+      if (p0 + p < A.h_parts) {
+        g.x += pg[p].x; g.y += pg[p].y; g.z += pg[p].z; g.w += pg[p].w;
+        u.x += pu[p].x; u.y += pu[p].y; u.z += pu[p].z; u.w += pu[p].w;
+      }
+  }
+  float h[4], lo[4];
+  few_swiglu(g.x, u.x, h[0], lo[0]);
+  few_swiglu(g.y, u.y, h[1], lo[1]);
+  few_swiglu(g.z, u.z, h[2], lo[2]);
+  few_swiglu(g.w, u.w, h[3], lo[3]);
+  head = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+  rest = make_uint2(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]));
+}
+
+// H of every slot, where more than 16 tokens would have few_down_kernel's blocks make it over and over.
+__global__ __launch_bounds__(256) void few_hidden_kernel(const FewArgs A) {
+  const int k = 4 * (blockIdx.x * 256 + threadIdx.x);
+  if (k >= A.f) return;
+  uint2 head, rest;
+  few_hidden(A, blockIdx.y, k, head, rest);
+  uint16_t* const o = A.h + (size_t)blockIdx.y * A.f + k;
+  *reinterpret_cast<uint2*>(o) = head;
+  *reinterpret_cast<uint2*>(o + A.h_lo) = rest;
+}
+
+// 128 FR columns of H W_down of one expert over one of `parts` parts of d_ffn.
+template <bool MX, int FR, int GROUPS, int DEPTH>
 __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_down_kernel(const FewArgs A) {
-  constexpr int FR = 4, WC = 16 * FR, STEP = MX ? 128 : 32, THREADS = kFewWaves * kWave;
-  __shared__ __attribute__((aligned(16))) char rows[kFewRowBytes];
-  const int tid = threadIdx.x, lane = tid & 63, wave = few_scalar(tid >> 6);
+  constexpr int WC = 16 * FR;
+  __shared__ __attribute__((aligned(16))) char rows[few_row_bytes(MX)];
+  __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR)];
+  const int lane = threadIdx.x & 63, wave = few_scalar(threadIdx.x >> 6);
   const int n_live = A.sched->n_live;
-  const int4 L = few_live(A, blockIdx.y);
   if ((int)blockIdx.y >= n_live) return;
+  const int4 L = few_live(A, n_live - 1 - blockIdx.y);
   const int32_t* const slots = A.sched->slots + L.y;
   const int ct = blockIdx.x / A.parts, part = blockIdx.x - ct * A.parts;
-  const int steps = few_steps(MX, A.f), per = (steps + A.parts - 1) / A.parts;
-  const int step0 = min(steps, part * per), count = min(steps, step0 + per) - step0;
   const int col0 = ct * 8 * WC + WC * wave;
   const bool active = col0 < A.d;
   const FewTile<MX, FR> W(A.down, L.x, A.f, A.d, active ? col0 : 0, lane);
-  const int pitch = few_row_pitch(per * STEP), quads = per * STEP / 4;
-  for (int r0 = 0; r0 < L.z; r0 += kFewGroup) {
-    const int n_rows = min(kFewGroup, L.z - r0);
-    mx_f32x4 acc[FR];
-#pragma unroll
-    for (int a = 0; a < FR; a++) acc[a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-    few_multiply<MX, FR, true, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
-      if (r0 > 0) __syncthreads();
-      for (int i = tid; i < n_rows * quads; i += THREADS) {   // four k of a row
-        const int r = i / quads, c = i - r * quads, k = step0 * STEP + 4 * c;
-        uint2 head = make_uint2(0, 0), rest = head;
-        if (k < A.f) {
-          const float* const src = A.h_partial + (size_t)slots[r0 + r] * A.h_parts * 2 * A.f + k;
-          float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
-          for (int p0 = 0; p0 < A.h_parts; p0 += 4) {   // (four parts at a time: each takes the way to the L2)
-            float4 pg[4], pu[4];
-#pragma unroll
-            for (int p = 0; p < 4; p++) {
-              const float* const at = src + (size_t)min(p0 + p, A.h_parts - 1) * 2 * A.f;
-              pg[p] = *reinterpret_cast<const float4*>(at);
-              pu[p] = *reinterpret_cast<const float4*>(at + A.f);
-            }
-#pragma unroll
-            for (int p = 0; p < 4; p++)
-              if (p0 + p < A.h_parts) {
-                g.x += pg[p].x; g.y += pg[p].y; g.z += pg[p].z; g.w += pg[p].w;
-                u.x += pu[p].x; u.y += pu[p].y; u.z += pu[p].z; u.w += pu[p].w;
-              }
-          }
-          float h[4], lo[4];
-          few_swiglu(g.x, u.x, h[0], lo[0]);
-          few_swiglu(g.y, u.y, h[1], lo[1]);
-          few_swiglu(g.z, u.z, h[2], lo[2]);
-          few_swiglu(g.w, u.w, h[3], lo[3]);
-          head = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
-          rest = make_uint2(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]));
-        }
-        *reinterpret_cast<uint2*>(rows + r * pitch + 8 * c) = head;
-        *reinterpret_cast<uint2*>(rows + (n_rows + r) * pitch + 8 * c) = rest;
+  auto turn = [&](int r0, auto tg) __attribute__((always_inline)) {
+    constexpr int TG = decltype(tg)::value;
+    mx_f32x4 acc[TG][FR];
+    typedef std::conditional_t<(GROUPS > 1), uint4, uint2> piece;
+    few_turn<MX, FR, TG, true, DEPTH, piece>(acc, W, [&](int r, int k, piece& v, piece& lo) __attribute__((always_inline)) {
+      const int slot = slots[r0 + r];
+      if constexpr (GROUPS > 1) {
+        const uint16_t* const h = A.h + (size_t)slot * A.f + k;
+        v = *reinterpret_cast<const uint4*>(h);
+        lo = *reinterpret_cast<const uint4*>(h + A.h_lo);
+      } else {
+        few_hidden(A, slot, k, v, lo);
       }
-      __syncthreads();
-    }, rows, n_rows, pitch, step0, active ? count : 0, lane);
-    const int row = r0 + (lane & 15);
-    if (active && row < L.z) few_put(A.partial + ((size_t)slots[row] * A.parts + part) * A.d + col0 + 4 * FR * (lane >> 4), acc);
-  }
-}
-
-// ---- 17 to 64 tokens: the wavefronts of a block share the rows ----------------------------------------------------------------------------
-
-constexpr int kFewChunk = 128;        // k of the rows in LDS at a time
-constexpr int kFewRowWaves = 4;       // wavefronts, of 64 columns each
-
-// Until at most N of this wavefront's vector memory loads are outstanding (they come back in order).
-template <int N>
-__device__ __forceinline__ void few_wait_loads() {
-  static_assert(N < 64, "the counter has 6 bits");
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
-  asm volatile("" ::: "memory");
-}
-constexpr int few_rows_bytes(int TG) { return kFewGroup * TG * kFewChunk * 2; }   // of a buffer
-constexpr int kFewRowsLds = 64 * 1024;   // all buffers: 2 (64 rows with remainders) to 4
-
-// acc[g][a] += over the chunks c0 .. c1 - 1 of K: lane l's element i is column FR (4 (l / 16) + i) + a of the wavefront's 16 FR, token 16 g + l % 16.
-// The rows go directly into a ring of buffers (LO: with the remainders after them), all but one chunks ahead: chunk c (8 k) of row r lies at position
-// c ^ (r % 16), so that 16 rows' chunks lie in different banks.  src: lane l's row 4 (wave + 4 i) + l / 16 of instruction i, at the 8 k that belong
-// at position l % 16.  The weights of a step go into registers, DEPTH - 1 steps ahead.
-//
-// What is waited for: the rows of chunk c + 1, before the barrier that ends chunk c.  They were requested NBUF - 2 chunks before, and since then this
-// wavefront has requested the rows and weights of NBUF - 2 chunks; every step requests the same number (past the end the last ones again).
-template <bool MX, int FR, int TG, bool LO>
-__device__ __forceinline__ void few_multiply_rows(mx_f32x4 (&acc)[TG][FR], const FewTile<MX, FR>& W, const uint16_t* const (&src)[TG], size_t x_lo,
-                                                  char* buf, int K, int c0, int c1, int wave, int lane) {
-  typedef FewTile<MX, FR> Tile;
-  constexpr int PER = MX ? 1 : kFewChunk / 32;   // steps of a chunk
-  constexpr int HALF = few_rows_bytes(TG), BUF = HALF * (LO ? 2 : 1);
-  constexpr int NBUF = kFewRowsLds / BUF < 4 ? kFewRowsLds / BUF : 4;
-  constexpr int DEPTH = TG == 4 && LO && FR == 4 ? 2 : MX && TG == 4 ? 3 : 4;
-  constexpr int ROW_LOADS = TG * (LO ? 2 : 1), WEIGHT_LOADS = MX ? 2 * FR : 8;
-  constexpr int SINCE = (NBUF - 2) * (ROW_LOADS + PER * WEIGHT_LOADS);   // requests of this wavefront since those of the chunk after this one
-  constexpr int NEWER = SINCE < 63 ? SINCE : 63;                         // (as many as can be waited for)
-  if (c0 >= c1) return;
-  const int n = lane & 15, q = lane >> 4;
-  const int last_step = few_steps(MX, K) - 1, step1 = min(c1 * PER, last_step + 1);
-  typename Tile::Stage st[DEPTH];
-  const int k_of = 8 * ((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15));   // (the row's position mod 16 is the same in all instructions)
-  auto load_rows = [&](int chunk) __attribute__((always_inline)) {   // (past the end of K: its last values; the weights there are zero or not multiplied)
-    const int k = min(min(chunk, c1 - 1) * kFewChunk + k_of, K - 8);
-    char* const to = buf + (unsigned)(chunk - c0) % NBUF * BUF + wave * 1024;
+    }, rows, scales + (MX ? wave * 16 * FR * kFewScalePitch : 0), min(kFewGroup * TG, L.z - r0), A.f, few_part<MX>(A.f, part, A.parts), active, lane);
 #pragma unroll
-    for (int i = 0; i < TG; i++) {
-      direct_load16(src[i] + k, to + i * 4096);
-      if constexpr (LO) direct_load16(src[i] + x_lo + k, to + HALF + i * 4096);
+    for (int g = 0; g < TG; g++) {
+      const int row = r0 + 16 * g + (lane & 15);
+      if (active && row < L.z) few_put(A.partial + ((size_t)slots[row] * A.parts + part) * A.d + col0 + 4 * FR * (lane >> 4), acc[g]);
     }
   };
-  auto consume = [&](const typename Tile::Stage& s, const char* rows, int part) __attribute__((always_inline)) {
-#pragma unroll
-    for (int ks = 0; ks < Tile::KS; ks++) {
-      mx_bf16x8 f[FR];
-#pragma unroll
-      for (int a = 0; a < FR; a++) f[a] = W.frag(s, a, ks);
-      const int c = MX ? 4 * q + ks : 4 * part + q;
-#pragma unroll
-      for (int g = 0; g < TG; g++) {
-        const char* const at = rows + (16 * g + n) * (kFewChunk * 2) + ((c ^ n) << 4);
-        const mx_bf16x8 x = *reinterpret_cast<const mx_bf16x8*>(at);
-#pragma unroll
-        for (int a = 0; a < FR; a++) acc[g][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[a], x, acc[g][a], 0, 0, 0);
-        if constexpr (LO) {
-          const mx_bf16x8 l = *reinterpret_cast<const mx_bf16x8*>(at + HALF);
-#pragma unroll
-          for (int a = 0; a < FR; a++) acc[g][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[a], l, acc[g][a], 0, 0, 0);
-        }
-      }
-    }
-  };
-  __syncthreads();   // (the buffers may still be read)
-#pragma unroll
-  for (int i = 0; i < NBUF - 1; i++) load_rows(c0 + i);
-  const int s_begin = c0 * PER;
-#pragma unroll
-  for (int i = 0; i < DEPTH - 1; i++) W.load(st[i], min(s_begin + i, last_step));
-  __builtin_amdgcn_s_waitcnt(0x0F70);
-  __syncthreads();
-  // (no branch in the loop: what the registers of a stage are is then fixed, and a wait is for the oldest stage alone)
-  constexpr int UNROLL = MX ? DEPTH : PER;   // a multiple of DEPTH and of PER
-  const int body = max(step1 - s_begin - 1, 0) / UNROLL * UNROLL;
-  int s = s_begin;
-  for (; s < s_begin + body; s += UNROLL) {
-#pragma unroll
-    for (int i = 0; i < UNROLL; i++) {
-      const int chunk = s / PER + i / PER;
-      if (i % PER == 0) load_rows(chunk + NBUF - 1);
-      W.load(st[(i + DEPTH - 1) % DEPTH], min(s + i + DEPTH - 1, last_step));
-      __builtin_amdgcn_sched_barrier(0);
-      consume(st[i % DEPTH], buf + (unsigned)(chunk - c0) % NBUF * BUF, i % PER);
-      __builtin_amdgcn_sched_barrier(0);
-      if (i % PER == PER - 1) {
-        few_wait_loads<NEWER>();
-        __syncthreads();
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < UNROLL; i++) {
-    const int chunk = s / PER + i / PER;
-    if (s + i < step1) {
-      if (i % PER == 0) load_rows(chunk + NBUF - 1);
-      W.load(st[(i + DEPTH - 1) % DEPTH], min(s + i + DEPTH - 1, last_step));
-      if (s + i == last_step) W.end(st[i % DEPTH], s + i);
-      consume(st[i % DEPTH], buf + (unsigned)(chunk - c0) % NBUF * BUF, i % PER);
-    }
-    if (i % PER == PER - 1 && s + i + 1 < step1) {
-      __builtin_amdgcn_s_waitcnt(0x0F70);
-      __syncthreads();
-    }
-  }
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // (nothing may land in LDS any more)
-}
-
-template <class F>
-__device__ __forceinline__ void few_groups(int rows, F&& body) {
-  if (rows > 32) body(std::integral_constant<int, 4>{});
-  else if (rows > 16) body(std::integral_constant<int, 2>{});
-  else body(std::integral_constant<int, 1>{});
-}
-
-// H of 32 FR columns of one expert: wavefront w makes G (w even) or U of columns 16 FR (w / 2) .. of them.
-template <bool MX, int FR>
-__global__ __launch_bounds__(kFewRowWaves * kWave, 2) void few_rows_gate_up_kernel(const FewArgs A) {
-  constexpr int COLS = 16 * FR;
-  __shared__ __attribute__((aligned(1024))) char buf[kFewRowsLds];
-  __shared__ __attribute__((aligned(16))) float half[2][kFewGroup][COLS + 4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if ((int)blockIdx.y >= A.sched->n_live) return;
-  const int4 L = few_live(A, blockIdx.y);
-  const int32_t* const slots = A.sched->slots + L.y;
-  const int col0 = blockIdx.x * 2 * COLS + COLS * (wave >> 1);
-  const bool active = col0 < A.f;   // (widths are multiples of 64: a wavefront has all its columns, or none and repeats the first ones)
-  const FewTile<MX, FR> W(wave & 1 ? A.up : A.gate, L.x, A.d, A.f, active ? col0 : 0, lane);
-  for (int r0 = 0; r0 < L.z; r0 += 64) {
-    few_groups(L.z - r0, [&](auto tg) __attribute__((always_inline)) {
-      constexpr int TG = decltype(tg)::value;
-      const uint16_t* src[TG];
-      mx_f32x4 acc[TG][FR];
-#pragma unroll
-      for (int g = 0; g < TG; g++) {
-        src[g] = A.x + (size_t)(slots[min(r0 + 16 * g + 4 * wave + (lane >> 4), L.z - 1)] / A.Kp) * A.d;
-#pragma unroll
-        for (int a = 0; a < FR; a++) acc[g][a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      few_multiply_rows<MX, FR, TG, false>(acc, W, src, 0, buf, A.d, 0, (A.d + kFewChunk - 1) / kFewChunk, wave, lane);
-#pragma unroll
-      for (int g = 0; g < TG; g++) {
-        __syncthreads();
-        float* const mine = &half[wave >> 1][lane & 15][4 * FR * (lane >> 4)];
-        if (wave & 1) few_put(mine, acc[g]);
-        __syncthreads();
-        const int row = r0 + 16 * g + (lane & 15);
-        if (!(wave & 1) && active && row < L.z) {
-          uint32_t h[2 * FR], lo[2 * FR];
-#pragma unroll
-          for (int i = 0; i < 4; i++)
-#pragma unroll
-            for (int a = 0; a < FR; a += 2) {
-              float v[2], l[2];
-              few_swiglu(acc[g][a][i], mine[FR * i + a], v[0], l[0]);
-              few_swiglu(acc[g][a + 1][i], mine[FR * i + a + 1], v[1], l[1]);
-              h[(FR * i + a) / 2] = pack_bf16(v[0], v[1]);
-              lo[(FR * i + a) / 2] = pack_bf16(l[0], l[1]);
-            }
-          uint16_t* const o = A.h + (size_t)slots[row] * A.f + col0 + 4 * FR * (lane >> 4);
-#pragma unroll
-          for (int i = 0; i < FR / 2; i++) {
-            *reinterpret_cast<uint4*>(o + 8 * i) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-            *reinterpret_cast<uint4*>(o + A.h_lo + 8 * i) = make_uint4(lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3]);
-          }
-        }
-      }
-    });
-  }
-}
-
-// 64 FR columns of H W_down of one expert over one part of d_ffn.
-template <bool MX, int FR>
-__global__ __launch_bounds__(kFewRowWaves * kWave, 2) void few_rows_down_kernel(const FewArgs A) {
-  constexpr int COLS = 16 * FR;
-  __shared__ __attribute__((aligned(1024))) char buf[kFewRowsLds];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if ((int)blockIdx.y >= A.sched->n_live) return;
-  const int4 L = few_live(A, blockIdx.y);
-  const int32_t* const slots = A.sched->slots + L.y;
-  const int col0 = (blockIdx.x * kFewRowWaves + wave) * COLS;
-  const bool active = col0 < A.d;
-  const int chunks = (A.f + kFewChunk - 1) / kFewChunk, per = (chunks + A.parts - 1) / A.parts;
-  const int chunk0 = min(chunks, (int)blockIdx.z * per), chunk1 = min(chunks, chunk0 + per);
-  const FewTile<MX, FR> W(A.down, L.x, A.f, A.d, active ? col0 : 0, lane);
-  for (int r0 = 0; r0 < L.z; r0 += 64) {
-    few_groups(L.z - r0, [&](auto tg) __attribute__((always_inline)) {
-      constexpr int TG = decltype(tg)::value;
-      const uint16_t* src[TG];
-      mx_f32x4 acc[TG][FR];
-#pragma unroll
-      for (int g = 0; g < TG; g++) {
-        src[g] = A.h + (size_t)slots[min(r0 + 16 * g + 4 * wave + (lane >> 4), L.z - 1)] * A.f;
-#pragma unroll
-        for (int a = 0; a < FR; a++) acc[g][a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      few_multiply_rows<MX, FR, TG, true>(acc, W, src, A.h_lo, buf, A.f, chunk0, chunk1, wave, lane);
-#pragma unroll
-      for (int g = 0; g < TG; g++) {
-        const int row = r0 + 16 * g + (lane & 15);
-        if (active && row < L.z) few_put(A.partial + ((size_t)slots[row] * A.parts + blockIdx.z) * A.d + col0 + 4 * FR * (lane >> 4), acc[g]);
-      }
-    });
+  for (int r0 = 0; r0 < L.z; r0 += GROUPS * kFewGroup) {
+    if (GROUPS == 2 && L.z - r0 > kFewGroup) turn(r0, std::integral_constant<int, GROUPS>{});
+    else turn(r0, std::integral_constant<int, 1>{});
   }
 }
 
@@ -720,36 +622,31 @@ __global__ __launch_bounds__(256) void few_combine_kernel(const FewArgs A) {
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
 
 // Experts that can have tokens.
-int few_live_bound(const Dims& D) { return (int)min((long long)D.Et, D.N); }
+int few_live_bound(const Dims& D) { return (int)std::min((long long)D.Et, D.N); }
 
 // How a problem is cut.
 struct FewPlan {
-  bool share_rows;          // few_rows_*_kernel
-  int h_frags, d_frags;     // of a wavefront's columns (share_rows)
+  bool turns;             // of 32 rows
+  int frags;              // of a wavefront's columns
   int parts, h_parts;
 };
 FewPlan few_plan(const Dims& D, bool mx) {
   FewPlan P = {};
-  const int live = few_live_bound(D), step = mx ? 128 : 32;
+  // experts with tokens, if the tokens choose evenly
+  const double live = std::min((double)few_live_bound(D), D.Es + D.E * -expm1(D.T * log1p(-(double)D.k / (D.E + 1e-9))));
+  const long long step = few_step(mx);
   auto divide = [](long long a, long long b) { return (a + b - 1) / b; };
-  P.share_rows = D.T > kFewGroup;
-  if (P.share_rows) {
-    // frags: 4, or 2 where that leaves CUs without a block
-    P.h_frags = divide(D.f, 128) * live >= 512 ? 4 : 2;
-    P.d_frags = divide(D.d, 128) * live >= 512 ? 4 : 2;
-    const long long blocks = divide(D.d, 64 * P.d_frags) * live;   // every CU two blocks, but at least four steps
-    P.parts = (int)max(1ll, min((long long)max(1, D.f / (step * 4)), divide(512, blocks)));
-    P.h_parts = 1;
-  } else {
-    // every CU two blocks, but at least two steps; and rows that fit LDS
-    auto cut = [&](int K, int cols, int C, int most_k) {
-      const long long blocks = divide(C, cols) * live, steps = divide(K, step);
-      const long long parts = max(divide(steps, most_k / step), min(max(1ll, steps / 2), divide(512, blocks)));
-      return (int)divide(steps, divide(steps, parts));   // (no part without steps)
-    };
-    P.h_parts = cut(D.d, 256, D.f, kFewRowK);
-    P.parts = cut(D.f, 512, D.d, kFewRowK / 2);
-  }
+  P.turns = D.T > kFewGroup;
+  P.frags = mx || live * D.d * D.f < 48e6 ? 2 : 4;
+  // Blocks for 256 CUs: two each, but not a few more than that; and no part of fewer than `least` steps.
+  auto cut = [&](int K, int cols, int C, int at_least, int least) {
+    const double blocks = live * divide(C, cols);
+    const long long steps = divide(K, step), want = std::max((long long)at_least, std::max((long long)(512 / blocks), (long long)std::ceil(400 / blocks)));
+    const long long parts = std::max(1ll, std::min(want, steps / least));
+    return (int)divide(steps, divide(steps, parts));   // (no part without steps)
+  };
+  P.h_parts = cut(D.d, 64 * P.frags, D.f, D.Es > 0 && D.T > kFewTurn ? 2 : 1, mx ? 2 : 8);
+  P.parts = cut(D.f, 128 * P.frags, D.d, 2, mx ? 1 : 8);
   return P;
 }
 
@@ -777,18 +674,21 @@ int check_few(const moe_shape* s, Dims* D) {
 template <bool MX>
 void few_launch_experts(hipStream_t st, const FewArgs& A, const Dims& D, const FewPlan& P) {
   const int live = few_live_bound(D);
-  if (P.share_rows) {
-    const dim3 block(kFewRowWaves * kWave);
-    if (P.h_frags == 4) MOE_LAUNCH("few_gate_up", st, (few_rows_gate_up_kernel<MX, 4>), dim3((D.f + 127) / 128, live), block, 0, st, A);
-    else MOE_LAUNCH("few_gate_up", st, (few_rows_gate_up_kernel<MX, 2>), dim3((D.f + 63) / 64, live), block, 0, st, A);
-    if (P.d_frags == 4) MOE_LAUNCH("few_down", st, (few_rows_down_kernel<MX, 4>), dim3((D.d + 255) / 256, live, A.parts), block, 0, st, A);
-    else MOE_LAUNCH("few_down", st, (few_rows_down_kernel<MX, 2>), dim3((D.d + 127) / 128, live, A.parts), block, 0, st, A);
-    MOE_LAUNCH("few_combine", st, few_combine_kernel, dim3((unsigned)(((size_t)D.T * (D.d / 2) + 255) / 256)), dim3(256), 0, st, A);
-    return;
+  auto go = [&](auto fr) {
+  constexpr int FR = decltype(fr)::value, DH = MX ? 2 : FR == 2 ? 4 : 3;
+  const dim3 block(kFewWaves * kWave), h((D.f + 64 * FR - 1) / (64 * FR) * P.h_parts, live + (A.fused_gate ? 1 : 0)),
+      d((D.d + 128 * FR - 1) / (128 * FR) * P.parts, live);
+  if (P.turns) {
+    MOE_LAUNCH("few_gate_up", st, (few_gate_up_kernel<MX, FR, 2, FR == 2 && !MX ? 4 : 2>), h, block, 0, st, A);
+    MOE_LAUNCH("few_hidden", st, few_hidden_kernel, dim3((D.f / 4 + 255) / 256, (unsigned)D.N), dim3(256), 0, st, A);
+    MOE_LAUNCH("few_down", st, (few_down_kernel<MX, FR, 2, FR == 2 && !MX ? 4 : 2>), d, block, 0, st, A);
+  } else {
+    MOE_LAUNCH("few_gate_up", st, (few_gate_up_kernel<MX, FR, 1, DH>), h, block, 0, st, A);
+    MOE_LAUNCH("few_down", st, (few_down_kernel<MX, FR, 1, FR == 2 && !MX ? 4 : 2>), d, block, 0, st, A);
   }
-  const dim3 block(kFewWaves * kWave);
-  MOE_LAUNCH("few_gate_up", st, (few_gate_up_kernel<MX, 3>), dim3((D.f + 255) / 256 * P.h_parts, live + (A.fused_gate ? 1 : 0)), block, 0, st, A);
-  MOE_LAUNCH("few_down", st, (few_down_kernel<MX, 3>), dim3((D.d + 511) / 512 * P.parts, live), block, 0, st, A);
+  };
+  if constexpr (MX) go(std::integral_constant<int, 2>{});
+  else { if (P.frags == 4) go(std::integral_constant<int, 4>{}); else go(std::integral_constant<int, 2>{}); }
   MOE_LAUNCH("few_combine", st, few_combine_kernel, dim3((unsigned)(((size_t)D.T * (D.d / 2) + 255) / 256)), dim3(256), 0, st, A);
 }
 
@@ -811,7 +711,7 @@ int few_forward(const moe_shape* shape, const uint16_t* x, const uint16_t* w_rou
   const FewPlan P = few_plan(D, MX);
   FewArgs A = {};
   A.parts = P.parts; A.h_parts = P.h_parts;
-  A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm; A.fused_gate = !P.share_rows && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
+  A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm; A.fused_gate = !P.turns && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
   A.x = x; A.w_router = w_router; A.topk_idx = topk_idx; A.topk_w = topk_w; A.out = out;
   A.gate = W[0]; A.up = W[1]; A.down = W[2];
   A.logits = reinterpret_cast<float*>(wsb + L.logits);

@@ -1,0 +1,131 @@
+"""Answering with one MoE layer: the experts' weights are quantised to microscaled 4-bit floating point when the layer is loaded, a prompt goes
+through the grouped 4-bit products, and the tokens that follow go through the layer for a few tokens.
+
+    python -m paper_2605_05049_amd.serve --dims 2048x1408 --experts 64 --top-k 6 --shared 2 --prompt 4096 --batch 1 --steps 64
+
+prints one JSON line: what the weights take, the time of the prompt and of a step (its launches replayed as a graph), and how far the answers
+are from those of the bf16 weights."""
+import argparse
+import json
+import sys
+
+from . import binding as B
+from .layer import FewTokenBuffers, MoeLayerBuffers, layer_few_forward, layer_forward, layer_mxfp4_forward, quantize_experts
+
+
+class ServedLayer:
+    """A layer that only answers: `layer(x)` for x [T, d_model] bf16, any T.  At most FEW_TOKENS_MAX tokens are answered by layer_few_forward,
+    more by the grouped products.  `mxfp4`: the experts' weights are quantised here, and the bf16 ones are not kept.
+
+    Buffers are made for a token count at its first call and kept; what a call returns is theirs and is overwritten by the next call with as
+    many tokens.  Calls on one stream at a time."""
+
+    def __init__(self, w_router, w_gate, w_up, w_down, top_k, n_shared=0, renorm=1, mxfp4=True, stream=None):
+        E, d = w_router.shape
+        if w_gate.shape[0] != E + n_shared or w_gate.shape[1] != d:
+            raise ValueError(f"w_gate {tuple(w_gate.shape)}: expected [{E + n_shared}, {d}, d_ffn]")
+        self.w_router, self.mxfp4 = w_router, mxfp4
+        self.weights = quantize_experts(w_gate, w_up, w_down, stream) if mxfp4 else (w_gate, w_up, w_down)
+        self._fields = (d, w_gate.shape[2], E, top_k, n_shared, renorm)
+        self._buffers = {}
+
+    def buffers(self, T):
+        """The buffers of calls with T tokens (topk_idx, topk_w, out, ...)."""
+        if T not in self._buffers:
+            s = B.Shape(T, *self._fields)
+            few = T <= B.FEW_TOKENS_MAX and B.layer_few_workspace_bytes(s) > 0
+            device = self.w_router.device
+            self._buffers[T] = FewTokenBuffers(s, device) if few else MoeLayerBuffers(s, device, with_backward=False)
+        return self._buffers[T]
+
+    def __call__(self, x, stream=None):
+        buf = self.buffers(x.shape[0])
+        if isinstance(buf, FewTokenBuffers):
+            return layer_few_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
+        if self.mxfp4:
+            return layer_mxfp4_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
+        return layer_forward(buf, x, *self.weights, w_router=self.w_router, stream=stream)
+
+
+def _next(x, y):
+    """Inputs of the next step: a residual sum, normalised."""
+    h = x.float() + y.float()
+    return (h * h.square().mean(-1, keepdim=True).add(1e-6).rsqrt()).to(x.dtype)
+
+
+def answer(layer, prompt, batch, steps):
+    """The layer over the prompt, then `steps` steps of the prompt's last `batch` rows; (answers of the prompt, of every step)."""
+    import torch
+    first = layer(prompt).clone()
+    x, rows = _next(prompt[-batch:], first[-batch:]), []
+    for _ in range(steps):
+        y = layer(x)
+        rows.append(y.clone())
+        x = _next(x, y)
+    return first, torch.stack(rows)
+
+
+def _ms(fn, repeats):
+    import torch
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    fn()
+    start.record()
+    for _ in range(repeats):
+        fn()
+    end.record()
+    end.synchronize()
+    return start.elapsed_time(end) / repeats
+
+
+def run(d, f, experts, top_k, shared, prompt, batch, steps, seed=0):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *s, std: (torch.randn(*s, device="cuda", generator=g) * std).bfloat16()  # noqa: E731
+    n = experts + shared
+    weights = [torch.stack([normal(*s, std=std) for _ in range(n)]) for s, std in (((d, f), d ** -0.5), ((d, f), d ** -0.5), ((f, d), f ** -0.5))]
+    w_router, x = normal(experts, d, std=2 * d ** -0.5), normal(prompt, d, std=1.0)
+    full = ServedLayer(w_router, *weights, top_k, shared, mxfp4=False)
+    layer = ServedLayer(w_router, *weights, top_k, shared)
+    ref, got = full(x).float(), layer(x).float()
+    answer(layer, x, batch, steps)
+    static = x[-batch:].clone()
+    layer(static)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer(static)
+    step_ref = full(static).float()
+    graph.replay()
+    step = layer.buffers(batch).out.float()
+    off = lambda a, b: round(((a - b).norm() / b.norm()).item(), 4)  # noqa: E731
+    return {"d_model": d, "d_ffn": f, "experts": experts, "shared": shared, "top_k": top_k, "prompt": prompt, "batch": batch,
+            "weights_GB": round(sum(w.numel() * w.element_size() for w in layer.weights) / 1e9, 3),
+            "bf16_weights_GB": round(sum(w.numel() * w.element_size() for w in weights) / 1e9, 3),
+            "prompt_ms": round(_ms(lambda: layer(x), 5), 4), "bf16_prompt_ms": round(_ms(lambda: full(x), 5), 4),
+            "step_us": round(1e3 * _ms(graph.replay, max(1, steps)), 2), "off_prompt": off(got, ref), "off_step": off(step, step_ref)}
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--dims", default="2048x1408", help="d_model x d_ffn")
+    ap.add_argument("--experts", type=int, default=64)
+    ap.add_argument("--top-k", type=int, default=6)
+    ap.add_argument("--shared", type=int, default=2)
+    ap.add_argument("--prompt", type=int, default=4096, help="tokens")
+    ap.add_argument("--batch", type=int, default=1, help="tokens of a step")
+    ap.add_argument("--steps", type=int, default=64)
+    args = ap.parse_args(argv)
+    import torch
+    B.load_library()
+    if not 1 <= args.batch <= args.prompt:
+        ap.error("--batch is between 1 and --prompt")
+    if not torch.cuda.is_available():
+        print("answering needs a GPU", file=sys.stderr)
+        return 2
+    d, f = (int(v) for v in args.dims.lower().split("x"))
+    print(json.dumps(run(d, f, args.experts, args.top_k, args.shared, args.prompt, args.batch, args.steps)), flush=True)
+    return 0
+
+
+if __name__ == "__main__":
+    sys.exit(main())

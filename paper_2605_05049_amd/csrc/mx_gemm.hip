@@ -130,6 +130,25 @@ __device__ __forceinline__ void mx_for(F&& f) { mx_each(static_cast<F&&>(f), std
 // and 2 p + 1 are 8 consecutive columns, 32 p + 8 (l / 16) .. + 7, and the four lanes of a row hold a block of 32.
 __device__ __forceinline__ int mx_column(int a, int m) { return 32 * (a >> 1) + 8 * (m >> 2) + 4 * (a & 1) + (m & 3); }
 
+// Block -> tile: chunks of consecutive tiles go to the XCDs in turn; an expert's tiles are walked in bands of row tiles, down the columns.
+struct MxTile { int expert, r0, n_rows, c0; };
+template <int COLS>
+__device__ __forceinline__ bool mx_find_tile(const MxGemmArgs& A, int lane, MxTile& T) {
+  const int n_ct = (A.n + COLS - 1) / COLS;
+  const int within = blockIdx.x / MX_XCDS, xcd = blockIdx.x % MX_XCDS;
+  const int lid = (within / MX_CHUNK * MX_XCDS + xcd) * MX_CHUNK + within % MX_CHUNK;
+  MxSegment S;
+  if (!mx_find_expert<MXT>(A.offsets, A.E, lid / n_ct, lane, S)) return false;
+  const int e_tiles = (S.hi - S.lo + MXT - 1) / MXT;
+  const int local = lid - S.first * n_ct, band = local / (MX_BAND * n_ct), in_band = local - band * MX_BAND * n_ct;
+  const int b_rows = min(MX_BAND, e_tiles - band * MX_BAND);
+  T.expert = S.expert;
+  T.r0 = S.lo + (band * MX_BAND + in_band % b_rows) * MXT;
+  T.n_rows = min(MXT, S.hi - T.r0);
+  T.c0 = in_band / b_rows * COLS;
+  return true;
+}
+
 template <int KIND>
 __global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
   constexpr bool PAIR = KIND == MX_GATE_UP;
@@ -140,18 +159,9 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
   const int m = lane & 15, q = lane >> 4;
   const int wr = wave & 1, wc = wave >> 1;
 
-  // block -> tile: chunks of consecutive tiles go to the XCDs in turn; an expert's tiles are walked in bands of row tiles, down the columns
-  const int n_ct = (A.n + COLS - 1) / COLS;
-  const int within = blockIdx.x / MX_XCDS, xcd = blockIdx.x % MX_XCDS;
-  const int lid = (within / MX_CHUNK * MX_XCDS + xcd) * MX_CHUNK + within % MX_CHUNK;
-  MxSegment S;
-  if (!mx_find_expert<MXT>(A.offsets, A.E, lid / n_ct, lane, S)) return;
-  const int e_tiles = (S.hi - S.lo + MXT - 1) / MXT;
-  const int local = lid - S.first * n_ct, band = local / (MX_BAND * n_ct), in_band = local - band * MX_BAND * n_ct;
-  const int b_rows = min(MX_BAND, e_tiles - band * MX_BAND);
-  const int ct = in_band / b_rows, rt = band * MX_BAND + in_band % b_rows;
-  const int r0 = S.lo + rt * MXT, n_rows = min(MXT, S.hi - r0);
-  const int c0 = ct * COLS;
+  MxTile T;
+  if (!mx_find_tile<COLS>(A, lane, T)) return;
+  const int r0 = T.r0, n_rows = T.n_rows, c0 = T.c0;
   const int kb = A.k / kMxBlock, nt = (kb + 7) / 8;
 
   auto run = [&](auto rb_c) __attribute__((always_inline)) {
@@ -162,7 +172,7 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
     // the chunk that belongs at position l % 8 (which depends on the parity of the instruction)
     const unsigned pitch = (unsigned)kb * 16;
     const uint8_t* const xb = A.x + (size_t)r0 * pitch;
-    const size_t e_row0 = (size_t)S.expert * A.n + c0;
+    const size_t e_row0 = (size_t)T.expert * A.n + c0;
     const bool up = PAIR && (wave & 1);   // (wavefront w loads LDS rows 64 w .. 64 w + 63: of a pair either all gate or all up)
     const uint8_t* const wb = (up ? A.w1 : A.w0) + e_row0 * pitch;
     auto w_column = [&](int row) {   // LDS row -> column of the tile
@@ -290,6 +300,12 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
     for (; t + 2 < nt; t++) stage(t, std::true_type{}, std::true_type{});
     if (t + 1 < nt) stage(t++, std::true_type{}, std::false_type{});
     stage(t, std::false_type{}, std::false_type{});
+    // (the sums are complete here, in all lanes: left to itself the compiler moves the last products, and the reads of their operands, to the stores, past
+    // the branch for the rows that there are)
+#pragma unroll
+    for (int a = 0; a < 8; a++)
+#pragma unroll
+      for (int b = 0; b < RB; b++) asm volatile("" : "+a"(acc[a][b]));
     // ---- results: acc[a][b][i] is row 16 (wr RB + b) + m, column mx_column(a, 4 q + i) of the wavefront's
 #pragma unroll
     for (int b = 0; b < RB; b++) {
@@ -335,13 +351,259 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
   else run(std::integral_constant<int, 1>{});
 }
 
+// The same tile where rows of scales are whole dwords (K a multiple of 128): the scales, too, come directly into LDS, 32 bytes (1024 k) of a row at a time.
+// A load's cost goes by the lines of 128 bytes that it touches (L2 -> LDS: 56 bytes a clock and CU with rows of 128 bytes, 30 with rows of 64), and
+// 8 bytes of scales of each row for every stage cost as much as the stage itself: 8192 rows x 14336 x 4096,
+// 322 -> 308 us (3.1 PFLOP/s; without any loads, 216).  A ring of four stages
+// of 128 k, 64 bytes of a row each, was no faster than two of 256.  The products are 32x32x64: registers alone, 9.3 PFLOP/s on zeros and 6.4 on
+// random codes, where 16x16x128 makes 5.5 and 5.1.
+//
+// In LDS the dwords of scales of row r, d of 8, are at d ^ ((r >> 3) & 7).  A batch of 1024 k comes in four parts with four stages, one batch ahead.
+typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
+template <int BYTE>
+__device__ __forceinline__ mx_f32x16 mx_mfma32(const int4& w, const int4& x, const mx_f32x16& acc, int ws, int xs) {
+  const mx_i32x8 a = {w.x, w.y, w.z, w.w, 0, 0, 0, 0}, b = {x.x, x.y, x.z, x.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 4, BYTE, ws, BYTE, xs);
+}
+// Loads straight into LDS from a scalar base and the lane's offset; lane i's bytes land 16 i (4 i) further than `to`.
+__device__ __forceinline__ unsigned long long mx_uniform(const void* p) {   // the same in all lanes: the compiler is told so
+  const unsigned long long v = (unsigned long long)p;
+  return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ void mx_bring16(unsigned long long base, unsigned off, unsigned to) {
+  to = (unsigned)__builtin_amdgcn_readfirstlane((int)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void mx_bring4(unsigned long long base, unsigned off, unsigned to) {
+  to = (unsigned)__builtin_amdgcn_readfirstlane((int)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(off), "s"(base) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void mx_wait() {   // until at most N loads are on their way, and LDS has answered
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
+}
+
+// Frag a's row m of a wavefront's weight rows -> its column among the wavefront's 128 (64 of either of a pair): a frag is a block of 32 columns, and
+// lane l's 16 elements of it are its columns 16 (l / 32) .. + 15.
+__device__ __forceinline__ int mx_column32(int a, int m) { return 32 * a + 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
+
+constexpr int MX_BATCH = 2 * MXT * 32;   // bytes of a batch of scales of both operands
+
+template <int KIND>
+__global__ __launch_bounds__(256, 1) void mx_direct_kernel(const MxGemmArgs A) {
+  constexpr bool PAIR = KIND == MX_GATE_UP;
+  constexpr int COLS = PAIR ? MXT / 2 : MXT;   // columns of the result per tile
+  __shared__ __attribute__((aligned(1024))) char lds[2][2][MX_STAGE];   // [stage][x, w]
+  __shared__ __attribute__((aligned(1024))) char sc[2][2][MXT * 32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 31, q = lane >> 5;
+  const int wr = wave & 1, wc = wave >> 1;
+  MxTile T;
+  if (!mx_find_tile<COLS>(A, lane, T)) return;
+  const int kb = A.k / kMxBlock, dwords = kb / 4, nt = (kb + 7) / 8;
+
+  auto run = [&](auto rb_c) __attribute__((always_inline)) {
+    constexpr int RB = decltype(rb_c)::value;   // row frags of a wavefront: 64 RB rows in all
+    constexpr int XI = 2 * RB;                  // loads of x per wavefront and stage
+    // ---- addresses: a base per tile and 32 bits.  Load i of wavefront w brings rows 8 (w XI + i) .. + 7 of x and LDS rows 8 (8 w + i) .. + 7 of
+    // the weights, LDS row r being frag (r / 32) % 4, m = r % 32 of wavefront column r / 128; lane l row l / 8 of them, and the chunk
+    // (of scales the dword) that belongs at position l % 8.
+    const unsigned pitch = (unsigned)kb * 16;
+    const bool up = PAIR && (wave & 1);   // (LDS rows 64 w .. 64 w + 63: of a pair either all gate or all up)
+    const size_t e_row0 = (size_t)T.expert * A.n + T.c0;
+    const unsigned long long xb = mx_uniform(A.x + (size_t)T.r0 * pitch), wb = mx_uniform((up ? A.w1 : A.w0) + e_row0 * pitch);
+    const unsigned long long xsb = mx_uniform(A.xs + (size_t)T.r0 * kb), wsb = mx_uniform((up ? A.ws1 : A.ws0) + e_row0 * kb);
+    auto x_row = [&](int i) { return (unsigned)min(8 * (wave * XI + i) + (lane >> 3), T.n_rows - 1); };
+    auto w_row = [&](int i) {
+      const int row = 8 * (wave * 8 + i) + (lane >> 3), g = row >> 7, a = (row >> 5) & 3;
+      return (unsigned)min(PAIR ? 64 * g + mx_column32(a & 1, row & 31) : 128 * g + mx_column32(a, row & 31), A.n - 1 - T.c0);
+    };
+    unsigned xo[XI], wo[8];
+#pragma unroll
+    for (int i = 0; i < XI; i++) xo[i] = x_row(i) * pitch;
+#pragma unroll
+    for (int i = 0; i < 8; i++) wo[i] = w_row(i) * pitch;
+    const int chunk = (lane & 7) ^ (lane >> 4);
+    const unsigned lds0 = (unsigned)(size_t)(lptr_t)&lds[0][0][0], sc0 = (unsigned)(size_t)(lptr_t)&sc[0][0][0];
+    struct Part { unsigned offset[2], to; };   // of a stage: the chunk's offset by the parity of the load (blocks past the end: the last), LDS
+    auto part_of = [&](int t) __attribute__((always_inline)) {
+      return Part{{(unsigned)min(8 * t + chunk, kb - 1) * 16u, (unsigned)min(8 * t + (chunk ^ 4), kb - 1) * 16u}, lds0 + (t & 1) * 2 * MX_STAGE};
+    };
+    auto bring = [&](const Part& P, int i) __attribute__((always_inline)) {   // (load w XI + i is as odd as i: XI is even)
+      if (i < XI) mx_bring16(xb, xo[i] + P.offset[i & 1], P.to + (wave * XI + i) * 1024);
+      else mx_bring16(wb, wo[i - XI] + P.offset[(i - XI) & 1], P.to + MX_STAGE + (wave * 8 + i - XI) * 1024);
+    };
+    // two loads, v of them, of part u of batch b of x or (i) the weights; past the end of K: the last dword
+    auto bring_scales = [&](int b, int u, int i, int v) __attribute__((always_inline)) {
+      const int load = i ? 2 * u + v : min(2 * u + v, XI - 1), rows8 = wave * (i ? 8 : XI) + load;
+      const unsigned dword = (unsigned)min(8 * b + ((lane & 7) ^ (rows8 & 7)), dwords - 1) * 4u, to = sc0 + (b & 1) * MX_BATCH + (i ? MXT * 32 : 0) + rows8 * 256;
+      if (i) mx_bring4(wsb, w_row(load) * (unsigned)kb + dword, to);
+      else mx_bring4(xsb, x_row(load) * (unsigned)kb + dword, to);
+    };
+    // ---- fragments: quarter j of a stage, 64 k
+    struct Set { int4 x[RB], w[4]; } set[2];
+    int raw[RB + 4], code[RB + 4];   // scales of half a stage: of the next one as they lie in memory; of this one, the lane's own in bytes 0 and 2
+    const char* const f0 = &lds[0][0][0] + m * 128;
+    constexpr int READS = RB + 4;
+    auto read = [&](Set& F, int t, int j, int i) __attribute__((always_inline)) {
+      const int at = (t & 1) * (2 * MX_STAGE) + ((2 * j + q) ^ ((m >> 1) & 7)) * 16;
+      if (i < RB) F.x[i] = *reinterpret_cast<const int4*>(f0 + at + (wr * RB + i) * 4096);
+      else F.w[i - RB] = *reinterpret_cast<const int4*>(f0 + at + MX_STAGE + (wc * 4 + i - RB) * 4096);
+    };
+    auto read_scale = [&](int t, int half, int i) __attribute__((always_inline)) {
+      const int frag = i < RB ? wr * RB + i : wc * 4 + i - RB;   // (rows 32 frag + m)
+      const int d = (2 * (t & 3) + half) ^ ((4 * frag + (m >> 3)) & 7);
+      raw[i] = *reinterpret_cast<const int*>(&sc[0][0][0] + ((t >> 2) & 1) * MX_BATCH + (i < RB ? 0 : MXT * 32) + (32 * frag + m) * 32 + 4 * d);
+    };
+    mx_f32x16 acc[4][RB];
+#pragma unroll
+    for (int a = 0; a < 4; a++)
+#pragma unroll
+      for (int b = 0; b < RB; b++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) acc[a][b][i] = 0.f;
+    // 4 RB products, `between(i)` before product i: a wavefront alone on its SIMD issues what else there is while one is under way, a little at a time.
+    constexpr int PRODUCTS = 4 * RB;
+    auto multiply = [&](const Set& F, auto byte_c, auto&& between) __attribute__((always_inline)) {
+      mx_for<PRODUCTS>([&](auto ic) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value, a = i / RB, b = i % RB;
+        between(ic);
+        __builtin_amdgcn_sched_barrier(0);
+        acc[a][b] = mx_mfma32<decltype(byte_c)::value>(F.w[a], F.x[b], acc[a][b], code[RB + a], code[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    // those of N things that come before product i
+    auto share = [&](auto ic, auto nc, auto&& f) __attribute__((always_inline)) {
+      mx_for<decltype(nc)::value>([&](auto kc) __attribute__((always_inline)) {
+        if constexpr (decltype(kc)::value * PRODUCTS / decltype(nc)::value == decltype(ic)::value) f(decltype(kc)::value);
+      });
+    };
+    typedef std::integral_constant<int, READS> Reads;
+    typedef std::integral_constant<int, XI + 8> Loads;
+    typedef std::integral_constant<int, 4> Four;
+    auto shift_codes = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < READS; i++) code[i] = (int)((unsigned)raw[i] >> (8 * q));
+    };
+    // ---- the first two stages, the first batch and a part of the second
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+#pragma unroll
+      for (int v = 0; v < 4; v++) bring_scales(0, u, v >> 1, v & 1);
+    {
+      const Part P = part_of(0);
+#pragma unroll
+      for (int i = 0; i < XI + 8; i++) bring(P, i);
+    }
+    mx_wait<0>();
+    __syncthreads();
+    if (nt > 1) {
+      const Part P = part_of(1);
+#pragma unroll
+      for (int i = 0; i < XI + 8; i++) bring(P, i);
+#pragma unroll
+      for (int v = 0; v < 4; v++) bring_scales(1, 0, v >> 1, v & 1);
+    }
+#pragma unroll
+    for (int i = 0; i < READS; i++) { read(set[0], 0, 0, i); read_scale(0, 0, i); }
+    // Quarter j of stage t (not its last) while the next one, and before a half its scales, are read.
+    auto quarter = [&](int t, auto jc) __attribute__((always_inline)) {
+      constexpr int j = decltype(jc)::value;
+      if constexpr (j != 1) shift_codes();
+      multiply(set[j & 1], std::integral_constant<int, j & 1 ? 2 : 0>{}, [&](auto ic) __attribute__((always_inline)) {
+        share(ic, Reads{}, [&](int i) __attribute__((always_inline)) {
+          read(set[(j + 1) & 1], t, j + 1, i);
+          if constexpr (j == 1) read_scale(t, 1, i);
+        });
+      });
+    };
+    // Stage t; before the barrier all of stage t + 1 has landed.  With its last quarter (MORE) stage t + 2 and a part of a batch are requested.
+    auto stage = [&](int t, auto more_c) __attribute__((always_inline)) {
+      constexpr bool MORE = decltype(more_c)::value;
+      mx_for<3>([&](auto jc) __attribute__((always_inline)) { quarter(t, jc); });
+      mx_wait<0>();
+      __syncthreads();
+      Part P;
+      if constexpr (MORE) P = part_of(t + 2);
+      multiply(set[1], std::integral_constant<int, 2>{}, [&](auto ic) __attribute__((always_inline)) {
+        share(ic, Reads{}, [&](int i) __attribute__((always_inline)) { read(set[0], t + 1, 0, i); read_scale(t + 1, 0, i); });
+        if constexpr (MORE) {
+          share(ic, Loads{}, [&](int i) __attribute__((always_inline)) { bring(P, i); });
+          share(ic, Four{}, [&](int v) __attribute__((always_inline)) { bring_scales((t + 5) >> 2, (t + 1) & 3, v >> 1, v & 1); });
+        }
+      });
+    };
+    int t = 0;
+    for (; t + 2 < nt; t++) stage(t, std::true_type{});
+    if (t + 1 < nt) stage(t++, std::false_type{});
+    quarter(t, std::integral_constant<int, 0>{});
+    quarter(t, std::integral_constant<int, 1>{});
+    if (kb - 8 * t > 4) {   // (else the half has no blocks)
+      quarter(t, std::integral_constant<int, 2>{});
+      multiply(set[1], std::integral_constant<int, 2>{}, [&](auto) __attribute__((always_inline)) {});
+    }
+    // (the sums are complete here, in all lanes: left to itself the compiler moves the last products, and the reads of their operands, to the stores, past
+    // the branch for the rows that there are)
+#pragma unroll
+    for (int a = 0; a < 4; a++)
+#pragma unroll
+      for (int b = 0; b < RB; b++) asm volatile("" : "+a"(acc[a][b]));
+    // ---- results: acc[a][b][i] is row 32 (wr RB + b) + m, column 32 a + 16 q + i of the wavefront's
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+      const int row = 32 * (wr * RB + b) + m;
+      if (row >= T.n_rows) continue;
+      const size_t out_row = (size_t)(T.r0 + row) * A.n;
+      if constexpr (!PAIR) {
+#pragma unroll
+        for (int a = 0; a < 4; a++)
+#pragma unroll
+          for (int h = 0; h < 2; h++) {
+            const int col = T.c0 + wc * 128 + 32 * a + 16 * q + 8 * h;
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) f[i] = acc[a][b][8 * h + i];
+            if (col < A.n) *reinterpret_cast<uint4*>(A.y + out_row + col) = pack8(f);
+          }
+      } else {
+#pragma unroll
+        for (int p = 0; p < 2; p++) {
+          const int col = T.c0 + wc * 64 + 32 * p + 16 * q;
+          float f[2][8];
+          unsigned e = 0;
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const float g = acc[p][b][i], h = g / (1.0f + __expf(-g)) * acc[2 + p][b][i];
+            f[i >> 3][i & 7] = h;
+            e = max(e, (__float_as_uint(h) >> 23) & 255u);
+          }
+          // (the two lanes of a row are in or out together)
+          e = max(e, (unsigned)__shfl_xor((int)e, 32));
+          const unsigned s = mx_scale_code(e);
+          if (col < A.n) {
+            *reinterpret_cast<uint2*>(A.h + (out_row + col) / 2) = make_uint2(mx_encode8(f[0], s), mx_encode8(f[1], s));
+            if (q == 0) A.hs[(out_row + col) / kMxBlock] = (uint8_t)s;
+          }
+        }
+      }
+    }
+  };
+  if (T.n_rows > 192) run(std::integral_constant<int, 4>{});
+  else if (T.n_rows > 128) run(std::integral_constant<int, 3>{});
+  else if (T.n_rows > 64) run(std::integral_constant<int, 2>{});
+  else run(std::integral_constant<int, 1>{});
+}
+
 template <int KIND>
 static void launch_kind(const char* label, hipStream_t st, const MxGemmArgs& A, long long rows) {
   const int cols = KIND == MX_GATE_UP ? MXT / 2 : MXT, small_cols = KIND == MX_GATE_UP ? 64 : 128;
   const long long tiles = (rows / MXT + A.E) * ((A.n + cols - 1) / cols);   // (at most)
   if (A.k >= 8 * kMxBlock && rows * (A.n / cols) >= 64ll * MXT) {   // (the tile kernel reads 8 scales of a row at once)
     const long long round = MX_XCDS * MX_CHUNK;
-    MOE_LAUNCH(label, st, (mx_tile_kernel<KIND>), dim3((unsigned)((tiles + round - 1) / round * round)), dim3(256), 0, st, A);
+    const dim3 grid((unsigned)((tiles + round - 1) / round * round));
+    if (A.k % (4 * kMxBlock) == 0) MOE_LAUNCH(label, st, (mx_direct_kernel<KIND>), grid, dim3(256), 0, st, A);
+    else MOE_LAUNCH(label, st, (mx_tile_kernel<KIND>), grid, dim3(256), 0, st, A);
   } else {
     MOE_LAUNCH(label, st, (mx_small_kernel<KIND>), dim3((unsigned)((rows / MXR + A.E) * ((A.n + small_cols - 1) / small_cols))), dim3(256), 0, st, A);
   }

@@ -10,8 +10,8 @@
 // which multiply W_down; the partial sums over K and the experts are added in fp32, in a fixed order.
 //
 // Launches: logits; gate (with at most 16 tokens every block of the next one makes it for itself); G and U by columns and parts of d; with more than 16
-// tokens H; H W_down by columns and parts of d_ffn; the weighted sum.  Measured, 8 experts of 4096 x 14336, top 2: 1 token 122 us in bf16 (5.8 TB/s; a
-// large read reaches 6.2) and 50 us in 4 bits (3.7 TB/s); 16 tokens 431 and 179 us; 64 tokens 478 and 229 us.
+// tokens H; H W_down by columns and parts of d_ffn; the weighted sum.  Measured, 8 experts of 4096 x 14336, top 2: 1 token 119 us in bf16 (5.9 TB/s; a
+// large read reaches 6.2) and 49 us in 4 bits (3.8 TB/s); 16 tokens 431 (6.5 TB/s) and 176 us; 64 tokens 478 and 231 us.
 #include "mxfp4.h"
 #include "route.h"
 
@@ -636,8 +636,13 @@ FewPlan few_plan(const Dims& D, bool mx) {
   const long long step = few_step(mx);
   auto divide = [](long long a, long long b) { return (a + b - 1) / b; };
   P.turns = D.T > kFewGroup;
+  // Of bf16 weights a wavefront's 64 columns are whole lines, 32 make twice as many blocks.  Measured, 64 and 32: 8 experts of 4096 x 14336, 1 and 16
+  // tokens, 118 and 431 us to 151 and 563; 66 of 2048 x 1408, 4 and 16 tokens, 90 and 171 to 104 and 187, but 1 token (23M values of a matrix
+  // read) 44 to 38; 14 of 1088 x 1984, 16 tokens (30M), 55 to 48.
   P.frags = mx || live * D.d * D.f < 48e6 ? 2 : 4;
-  // Blocks for 256 CUs: two each, but not a few more than that; and no part of fewer than `least` steps.
+  // Parts: two blocks for each of 256 CUs, or one and a half where that is all that fits in one go, and none of fewer than `least` steps (a block's start
+  // costs as much as some steps).  One part of d to three, 8 experts of 4096 x 14336, 443 blocks: 431 us to 464; 1 token, 112 blocks, one part to
+  // four: 156 to 120.
   auto cut = [&](int K, int cols, int C, int at_least, int least) {
     const double blocks = live * divide(C, cols);
     const long long steps = divide(K, step), want = std::max((long long)at_least, std::max((long long)(512 / blocks), (long long)std::ceil(400 / blocks)));
@@ -645,7 +650,7 @@ FewPlan few_plan(const Dims& D, bool mx) {
     return (int)divide(steps, divide(steps, parts));   // (no part without steps)
   };
   P.h_parts = cut(D.d, 64 * P.frags, D.f, 1, mx ? 2 : 8);
-  P.parts = cut(D.f, 128 * P.frags, D.d, 2, mx ? 1 : 8);
+  P.parts = cut(D.f, 128 * P.frags, D.d, 2, mx ? 1 : 8);   // (two at least: 66 experts of 2048 x 1408, 64 tokens, 303 us to 354)
   return P;
 }
 

@@ -1,8 +1,8 @@
 // Grouped products in microscaled 4-bit floating point (E2M1 values, a power-of-two scale per 32 along the contraction):
 //     y[r, c] = sum_k x[r, k] w[e(r)][c, k]      and the SwiGLU pair  h = Q(silu(x W_gate) (x W_up)),
-// on the block-scaled MFMA 16x16x128, which applies both scales and accumulates in fp32.
+// on the block-scaled MFMA, which applies both scales and accumulates in fp32.  H is quantised from those sums (one rounding, to 4 bits).
 //
-// Operand layout (both operands alike): lane l holds row l % 16, k = 32 (l / 16) .. + 31, i.e. one block and its scale.  The weights are the A
+// Operand layout of 16x16x128 (both operands alike): lane l holds row l % 16, k = 32 (l / 16) .. + 31, i.e. one block and its scale.  The weights are the A
 // operand, so that a lane owns consecutive columns of a result row: with frag a's row m taken from column CPL (m / 4) + 4 a + m % 4 of the
 // wavefront's columns (CPL = columns per lane), lane l ends up with columns CPL (l / 16) .. + CPL - 1 of row l % 16.
 #include "mx_gemm.h"
@@ -14,6 +14,8 @@ namespace moe {
 
 constexpr int MXR = 128;   // rows of a tile
 
+// Small problems: 128 rows x 128 columns (of a pair 64 of either) per block of 4 wavefronts, each 64 x 64, the fragments from memory straight into
+// registers; what it takes is the time of a few loads for each 128 k.  512 rows of 8 experts, 1024 columns, K = 512: 8.9 us.
 template <int KIND>
 __global__ __launch_bounds__(256) void mx_small_kernel(const MxGemmArgs A) {
   constexpr int NW = KIND == MX_GATE_UP ? 2 : 1;
@@ -599,7 +601,11 @@ template <int KIND>
 static void launch_kind(const char* label, hipStream_t st, const MxGemmArgs& A, long long rows) {
   const int cols = KIND == MX_GATE_UP ? MXT / 2 : MXT, small_cols = KIND == MX_GATE_UP ? 64 : 128;
   const long long tiles = (rows / MXT + A.E) * ((A.n + cols - 1) / cols);   // (at most)
-  if (A.k >= 8 * kMxBlock && rows * (A.n / cols) >= 64ll * MXT) {   // (the tile kernel reads 8 scales of a row at once)
+  // Large tiles (8 scales of a row at once: 256 k at least) where there is work for the CUs, or where the contraction is long and most experts have
+  // rows.  Measured, large to small tiles: 8 experts, 4096 columns, K = 4096, 128 rows 22 to 28 us, 1024 rows 28 to 60, 8192 rows 80 to 451; 64 experts,
+  // 2048 columns, K = 1408, 512 rows 23 to 22, 2048 rows (64 tiles) 25 to 26, 8192 rows 33 to 50; 8 experts, 1024 columns, K = 512, 2048 rows 15 to 10,
+  // 8192 rows 16 to 19; 1000 experts, 2048 columns, K = 2048, 16 rows 144 to 96 (a block has all of a CU's LDS), 1024 rows 581 to 606.
+  if (A.k >= 8 * kMxBlock && (rows * (A.n / cols) >= 64ll * MXT || (A.k >= 2048 && rows >= A.E / 2))) {
     const long long round = MX_XCDS * MX_CHUNK;
     const dim3 grid((unsigned)((tiles + round - 1) / round * round));
     if (A.k % (4 * kMxBlock) == 0) MOE_LAUNCH(label, st, (mx_direct_kernel<KIND>), grid, dim3(256), 0, st, A);

@@ -1,6 +1,7 @@
 // Quantisation to microscaled 4-bit floating point, along rows and along columns, and the way back.
 //
-// All three are bound by HBM: 2 + 17/32 bytes per value.
+// All three are bound by HBM: 2 + 17/32 bytes per value.  Measured: rows 65536 x 4096, 118 us (5.8 TB/s); columns of 66 matrices of 2048 x 1408, 118 us
+// (4.1 TB/s), and back, 73 us (6.6 TB/s).  A copy of 8.6 GB reaches 4.75 TB/s of both ways, a read 6.2, a fill 6.85.
 #include "mxfp4.h"
 
 namespace moe {

@@ -128,7 +128,9 @@ __global__ __launch_bounds__(1024) void few_gate_kernel(const FewArgs A) {
 // FR frags of 16 columns: column FR * m + a of the tile is row m of frag a.  A step is 32 k of bf16 or 256 k of 4-bit weights (the last one may be
 // cut short: its codes are zero past the end).
 template <bool MX, int FR> struct FewTile;
-constexpr int kFewScaleSteps = 8, kFewScalePitch = 8 * kFewScaleSteps + 8;   // 4-bit weights: steps of a chunk at most; a column's scales in LDS
+// 4-bit weights: steps of a chunk at most; bytes of a column's scales in LDS.
+constexpr int few_scale_steps(int groups) { return groups > 1 ? 4 : 8; }
+constexpr int few_scale_pitch(int groups) { return 8 * few_scale_steps(groups) + 8; }
 
 __device__ __forceinline__ int few_scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }   // the same in all lanes: the compiler is told so
 
@@ -168,8 +170,8 @@ template <int FR> struct FewTile<false, FR> {
     for (int i = 0; i < 8; i++, p += row) s.w[i] = few_load<word, FR == 4>(p, lane_off);
   }
   struct Codes {};
-  __device__ __forceinline__ void bring_scales(char*, int, int, int) const {}
-  __device__ __forceinline__ Codes codes(const char*, int) const { return {}; }
+  template <int GROUPS> __device__ __forceinline__ void bring_scales(char*, int, int, int) const {}
+  template <int GROUPS> __device__ __forceinline__ Codes codes(const char*, int) const { return {}; }
   // frag a: 8 k of column a, from the halves of 8 words
   __device__ __forceinline__ mx_bf16x8 frag(const Stage& s, Codes, int a, int) const {
     union { unsigned p[4]; mx_bf16x8 v; } u;
@@ -205,13 +207,15 @@ template <int FR> struct FewTile<true, FR> {
       s.w[1][a] = few_load<quad, false>(p, lane_off + b1 * 16);
     }
   }
-  // The scales of `steps` (at most kFewScaleSteps) steps of the wavefront's columns into LDS, 8 bytes a step; 1 past the end of K, where the rows are zero.
+  // The scales of `steps` (at most few_scale_steps) steps of the wavefront's columns into LDS, 8 bytes a step; 1 past the end of K, where the rows are zero.
   // (Read by steps from memory, a line of a column's scales was fetched again for each: 4096 x 14336, 8 experts, 16 rows: 220 against 170 us.)
+  template <int GROUPS>
   __device__ __forceinline__ void bring_scales(char* to, int step0, int steps, int lane) const {
+    constexpr int MOST = few_scale_steps(GROUPS);
     typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(2)));   // (kb is even)
 #pragma unroll
-    for (int i = 0; i < 16 * FR * kFewScaleSteps / kWave; i++) {
-      const int c = i * (kWave / kFewScaleSteps) + lane / kFewScaleSteps, st = lane % kFewScaleSteps, b = 8 * (step0 + st);
+    for (int i = 0; i < 16 * FR * MOST / kWave; i++) {
+      const int c = i * (kWave / MOST) + lane / MOST, st = lane % MOST, b = 8 * (step0 + st);
       if (st < steps) {
         unsigned long long v = ~0ull / 255 * 127;
         if (kb >= 8) {
@@ -223,16 +227,17 @@ template <int FR> struct FewTile<true, FR> {
         } else {
           for (int k = 0; k < kb; k++) v = (v & ~(255ull << (8 * k))) | (unsigned long long)few_load<uint8_t, false>(sbase, (unsigned)c * (unsigned)kb + k) << (8 * k);
         }
-        *reinterpret_cast<unsigned long long*>(to + c * kFewScalePitch + 8 * st) = v;
+        *reinterpret_cast<unsigned long long*>(to + c * few_scale_pitch(GROUPS) + 8 * st) = v;
       }
     }
   }
   struct Codes { float scale[2][FR]; };   // of the stage's blocks
+  template <int GROUPS>
   __device__ __forceinline__ Codes codes(const char* at, int step) const {   // step: from the chunk's first
     Codes c;
 #pragma unroll
     for (int a = 0; a < FR; a++) {
-      const uint2 v = *reinterpret_cast<const uint2*>(at + (FR * m + a) * kFewScalePitch + 8 * step);
+      const uint2 v = *reinterpret_cast<const uint2*>(at + (FR * m + a) * few_scale_pitch(GROUPS) + 8 * step);
 #pragma unroll
       for (int h = 0; h < 2; h++) {
         const unsigned code = ((h ? v.y : v.x) >> (8 * q)) & 255u;
@@ -372,18 +377,19 @@ __device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, in
 }
 
 // Rows of a product in LDS: of one turn (16 GROUPS rows of an expert at most), as many steps of k as fit.
-__device__ __host__ constexpr int few_row_bytes(bool mx) { return (mx ? 54 : 60) * 1024; }   // (a block has half of a CU's LDS)
-__device__ __host__ constexpr int few_scale_bytes(bool mx, int FR) { return mx ? kFewWaves * 16 * FR * kFewScalePitch : 16; }
+// A block has half of a CU's LDS, 80 KB: with the gate (at most 16 tokens) or without it, and the scales.
+__device__ __host__ constexpr int few_row_bytes(bool mx, int groups) { return (groups > 1 ? mx ? 66 : 79 : mx ? 54 : 72) * 1024; }
+__device__ __host__ constexpr int few_scale_bytes(bool mx, int FR, int groups) { return mx ? kFewWaves * 16 * FR * few_scale_pitch(groups) : 16; }
 __device__ __forceinline__ int few_row_pitch(int k) { return 2 * k + 16; }
-template <bool MX, bool LO>
+template <bool MX, int GROUPS, bool LO>
 __device__ __forceinline__ int few_chunk_steps(int n_rows) {
-  const int fit = max(1, (few_row_bytes(MX) / ((LO ? 2 : 1) * n_rows) - 16) / (2 * few_step(MX)));
-  return MX ? min(fit, kFewScaleSteps) : fit;
+  const int fit = max(1, (few_row_bytes(MX, GROUPS) / ((LO ? 2 : 1) * n_rows) - 16) / (2 * few_step(MX)));
+  return MX ? min(fit, few_scale_steps(GROUPS)) : fit;
 }
 
 // acc[g][a] += over `count` steps from step0 on: lane l's element i of acc[g][a] is column FR (4 (l / 16) + i) + a, row 16 g + l % 16 of `rows` (LO: with
 // the remainders after all rows; rows past the last repeat it).  Between the first weights' requests and their use stands `bring`, which fills `rows`.
-template <bool MX, int FR, int TG, bool LO, int DEPTH, class F>
+template <bool MX, int FR, int GROUPS, int TG, bool LO, int DEPTH, class F>
 __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[TG][FR], const FewTile<MX, FR>& W, F&& bring, const char* rows, int n_rows, int pitch, const char* scales,
                                              int step0, int count, int lane) {
   typedef FewTile<MX, FR> Tile;
@@ -398,7 +404,7 @@ __device__ __forceinline__ void few_multiply(mx_f32x4 (&acc)[TG][FR], const FewT
 #pragma unroll
   for (int g = 0; g < TG; g++) at[g] = rows + min(16 * g + (lane & 15), n_rows - 1) * pitch;
   auto consume = [&](const typename Tile::Stage& s, int i) __attribute__((always_inline)) {
-    const auto codes = W.codes(scales, i);
+    const auto codes = W.template codes<GROUPS>(scales, i);
 #pragma unroll
     for (int ks = 0; ks < Tile::KS; ks++) {
       if (ks > 0 && TG > 1) __builtin_amdgcn_sched_barrier(0);   // (or the operands of all are in registers at once)
@@ -450,20 +456,20 @@ __device__ __forceinline__ FewPart few_part(int K, int part, int parts) {
 }
 
 // The sums of the rows r0 .. of an expert over one part of K, chunk by chunk.  `bring` makes sizeof(V) / 2 k of row r0 + r, from k on.
-template <bool MX, int FR, int TG, bool LO, int DEPTH, class V, class F>
+template <bool MX, int FR, int GROUPS, int TG, bool LO, int DEPTH, class V, class F>
 __device__ __forceinline__ void few_turn(mx_f32x4 (&acc)[TG][FR], const FewTile<MX, FR>& W, F&& bring, char* rows, char* scales, int n_rows, int K, FewPart part,
                                          bool active, int lane) {
   constexpr int STEP = few_step(MX), THREADS = kFewWaves * kWave;
-  const int per = min(part.steps, few_chunk_steps<MX, LO>(n_rows)), pitch = few_row_pitch(per * STEP), pieces = per * STEP * 2 / (int)sizeof(V);
+  const int fills = (part.steps - 1) / few_chunk_steps<MX, GROUPS, LO>(n_rows) + 1, per = (part.steps + fills - 1) / fills, pitch = few_row_pitch(per * STEP), pieces = per * STEP * 2 / (int)sizeof(V);
 #pragma unroll
   for (int g = 0; g < TG; g++)
 #pragma unroll
     for (int a = 0; a < FR; a++) acc[g][a] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < part.steps; s0 += per) {
     const int step0 = part.step0 + s0, count = min(per, part.steps - s0);
-    few_multiply<MX, FR, TG, LO, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
+    few_multiply<MX, FR, GROUPS, TG, LO, DEPTH>(acc, W, [&]() __attribute__((always_inline)) {
       __syncthreads();
-      W.bring_scales(scales, step0, count, lane);
+      W.template bring_scales<GROUPS>(scales, step0, count, lane);
       for (int i = threadIdx.x; i < n_rows * pieces; i += THREADS) {
         const int r = i / pieces, c = i - r * pieces, k = step0 * STEP + (int)sizeof(V) / 2 * c;
         V v = {}, lo = {};   // (past the end of K)
@@ -481,8 +487,8 @@ __device__ __forceinline__ void few_turn(mx_f32x4 (&acc)[TG][FR], const FewTile<
 template <bool MX, int FR, int GROUPS, int DEPTH>
 __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_gate_up_kernel(const FewArgs A) {
   constexpr int WC = 16 * FR;
-  __shared__ __attribute__((aligned(16))) char rows[few_row_bytes(MX)];
-  __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR)];
+  __shared__ __attribute__((aligned(16))) char rows[few_row_bytes(MX, GROUPS)];
+  __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR, GROUPS)];
   __shared__ FewGate S;
   const int lane = threadIdx.x & 63, wave = few_scalar(threadIdx.x >> 6);
   const FewExpert X = few_expert<GROUPS == 1>(A, S, gridDim.y - 1);
@@ -494,9 +500,9 @@ __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_gate_up_kernel(const
   auto turn = [&](int r0, auto tg) __attribute__((always_inline)) {
     constexpr int TG = decltype(tg)::value;
     mx_f32x4 acc[TG][FR];
-    few_turn<MX, FR, TG, false, DEPTH, uint4>(acc, W, [&](int r, int k, uint4& v, uint4&) __attribute__((always_inline)) {
+    few_turn<MX, FR, GROUPS, TG, false, DEPTH, uint4>(acc, W, [&](int r, int k, uint4& v, uint4&) __attribute__((always_inline)) {
       v = *reinterpret_cast<const uint4*>(A.x + (size_t)(X.slots[r0 + r] / A.Kp) * A.d + k);
-    }, rows, scales + (MX ? wave * 16 * FR * kFewScalePitch : 0), min(kFewGroup * TG, X.count - r0), A.d, few_part<MX>(A.d, part, A.h_parts), active, lane);
+    }, rows, scales + (MX ? wave * 16 * FR * few_scale_pitch(GROUPS) : 0), min(kFewGroup * TG, X.count - r0), A.d, few_part<MX>(A.d, part, A.h_parts), active, lane);
 #pragma unroll
     for (int g = 0; g < TG; g++) {
       const int row = r0 + 16 * g + (lane & 15);
@@ -552,8 +558,8 @@ __global__ __launch_bounds__(256) void few_hidden_kernel(const FewArgs A) {
 template <bool MX, int FR, int GROUPS, int DEPTH>
 __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_down_kernel(const FewArgs A) {
   constexpr int WC = 16 * FR;
-  __shared__ __attribute__((aligned(16))) char rows[few_row_bytes(MX)];
-  __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR)];
+  __shared__ __attribute__((aligned(16))) char rows[few_row_bytes(MX, GROUPS)];
+  __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR, GROUPS)];
   const int lane = threadIdx.x & 63, wave = few_scalar(threadIdx.x >> 6);
   const int n_live = A.sched->n_live;
   if ((int)blockIdx.y >= n_live) return;
@@ -567,7 +573,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_down_kernel(const Fe
     constexpr int TG = decltype(tg)::value;
     mx_f32x4 acc[TG][FR];
     typedef std::conditional_t<(GROUPS > 1), uint4, uint2> piece;
-    few_turn<MX, FR, TG, true, DEPTH, piece>(acc, W, [&](int r, int k, piece& v, piece& lo) __attribute__((always_inline)) {
+    few_turn<MX, FR, GROUPS, TG, true, DEPTH, piece>(acc, W, [&](int r, int k, piece& v, piece& lo) __attribute__((always_inline)) {
       const int slot = slots[r0 + r];
       if constexpr (GROUPS > 1) {
         const uint16_t* const h = A.h + (size_t)slot * A.f + k;
@@ -576,7 +582,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_down_kernel(const Fe
       } else {
         few_hidden(A, slot, k, v, lo);
       }
-    }, rows, scales + (MX ? wave * 16 * FR * kFewScalePitch : 0), min(kFewGroup * TG, L.z - r0), A.f, few_part<MX>(A.f, part, A.parts), active, lane);
+    }, rows, scales + (MX ? wave * 16 * FR * few_scale_pitch(GROUPS) : 0), min(kFewGroup * TG, L.z - r0), A.f, few_part<MX>(A.f, part, A.parts), active, lane);
 #pragma unroll
     for (int g = 0; g < TG; g++) {
       const int row = r0 + 16 * g + (lane & 15);

@@ -126,7 +126,7 @@ __global__ __launch_bounds__(1024) void few_gate_kernel(const FewArgs A) {
 // ---- what a lane holds of the weights --------------------------------------------------------------------------------------------------
 
 // FR frags of 16 columns: column FR * m + a of the tile is row m of frag a.  A step is 32 k of bf16 or 256 k of 4-bit weights (the last one may be
-// cut short: its codes are zero past the end).
+// cut short: past the end the rows are zero).
 template <bool MX, int FR> struct FewTile;
 // 4-bit weights: steps of a chunk at most; bytes of a column's scales in LDS.
 constexpr int few_scale_steps(int groups) { return groups > 1 ? 4 : 8; }
@@ -141,8 +141,8 @@ __device__ __forceinline__ FewBase few_base(const uint8_t* p) {
   return (FewBase)((unsigned long long)(unsigned)few_scalar((int)(v >> 32)) << 32 | (unsigned)few_scalar((int)v));
 }
 // From a scalar base and 32 bits of the lane's own (left to itself the compiler keeps a 64-bit address per lane and load, 48 registers in all).
-// ONCE: nothing else of the lines is read, they need not stay in the caches (a row of 64 bf16 columns is a line of 128 bytes; the 64 bytes that a step takes
-// of a row of 4-bit weights are half of one).  One token, 2 of 8 experts of 4096 x 14336 in bf16: 149 -> 134 us.
+// ONCE: nothing else of the lines is read, they need not stay in the caches (a row of 64 bf16 columns is a line of 128 bytes).  One token, 2 of 8 experts of
+// 4096 x 14336 in bf16: 149 -> 134 us; of 4-bit weights, whose lines are read in halves, 50 -> 59.
 template <class T, bool ONCE>
 __device__ __forceinline__ T few_load(FewBase base, unsigned off) {
   asm("" : "+s"(base));

@@ -14,6 +14,10 @@ namespace moe {
 
 constexpr int MXR = 128;   // rows of a tile
 
+// silu(g) within 2 units in the last place of fp32, of which H keeps 4 bits; below -87, where the reciprocal is flushed, 0 for at most 2e-36 in magnitude.
+// (A division is ten instructions, which nothing hides behind the last product of a tile: 8192 rows of 8 experts of 4096 x 14336, 907 -> 872 us in all.)
+__device__ __forceinline__ float mx_silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+
 // Small problems: 128 rows x 128 columns (of a pair 64 of either) per block of 4 wavefronts, each 64 x 64, the fragments from memory straight into
 // registers; what it takes is the time of a few loads for each 128 k.  512 rows of 8 experts, 1024 columns, K = 512: 8.9 us.
 template <int KIND>
@@ -86,7 +90,7 @@ __global__ __launch_bounds__(256) void mx_small_kernel(const MxGemmArgs A) {
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const float g = acc[0][i >> 2][b][i & 3], v = acc[NW - 1][i >> 2][b][i & 3];
-        f[i] = g / (1.0f + __expf(-g)) * v;
+        f[i] = mx_silu(g) * v;
       }
       unsigned e = 0;
 #pragma unroll
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(256, 1) void mx_tile_kernel(const MxGemmArgs A) {
 #pragma unroll
           for (int i = 0; i < 8; i++) {
             const float g = acc[2 * p + (i >> 2)][b][i & 3], v = acc[4 + 2 * p + (i >> 2)][b][i & 3];
-            f[i] = g / (1.0f + __expf(-g)) * v;
+            f[i] = mx_silu(g) * v;
             e = max(e, (__float_as_uint(f[i]) >> 23) & 255u);
           }
           // (the four lanes of a row are in or out together)
@@ -576,7 +580,7 @@ __global__ __launch_bounds__(256, 1) void mx_direct_kernel(const MxGemmArgs A) {
           unsigned e = 0;
 #pragma unroll
           for (int i = 0; i < 16; i++) {
-            const float g = acc[p][b][i], h = g / (1.0f + __expf(-g)) * acc[2 + p][b][i];
+            const float g = acc[p][b][i], h = mx_silu(g) * acc[2 + p][b][i];
             f[i >> 3][i & 7] = h;
             e = max(e, (__float_as_uint(h) >> 23) & 255u);
           }

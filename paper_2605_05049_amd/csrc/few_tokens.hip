@@ -9,7 +9,7 @@
 // widens them to bf16, exactly.  The hidden activation stays in fp32 in effect: it is kept as a bf16 head and a bf16 remainder, both of
 // which multiply W_down; the partial sums over K and the experts are added in fp32, in a fixed order.
 //
-// Launches: logits; gate (with at most 16 tokens every block of the next one makes it for itself); G and U by columns and parts of d; with more than 16
+// Launches: logits; gate (with at most 16 tokens every block of the next one makes it for itself, and the logits of a small router); G and U by columns and parts of d; with more than 16
 // tokens H; H W_down by columns and parts of d_ffn; the weighted sum.  Measured, 8 experts of 4096 x 14336, top 2: 1 token 119 us in bf16 (5.9 TB/s; a
 // large read reaches 6.2) and 49 us in 4 bits (3.8 TB/s); 16 tokens 431 (6.5 TB/s) and 177 us; 64 tokens 473 and 224 us.
 #include "mxfp4.h"
@@ -25,9 +25,12 @@ namespace {
 
 constexpr int kFewTokens = MOE_FEW_TOKENS_MAX;
 constexpr int kFewSlots = 4096;       // T * K' at most
-constexpr int kFewWaves = 8;          // wavefronts of a block, at most 16 tokens
-constexpr int kFewRouterWaves = 8;    // ... of few_router_kernel: they share a contraction
+constexpr int kFewWaves = 8;          // wavefronts of a block
 constexpr int kFewFusedSlots = 512, kFewFusedExperts = 256;   // at most, where every block makes the gate for itself
+// Bytes of router weights at most, where it makes the logits too.  Measured, with and without that launch: 8 KB (8 experts, 512 wide), 1 and 16 tokens, 16.4
+// and 20.4 us to 17.8 and 21.9; 28 KB (13 experts, 1088 wide) 23.8 and 48.8 to 25.0 and 47.9, in 4 bits 19.5 and 44.2 to 21.0 and 38.7; 64 KB (32 experts,
+// 1024 wide) 21.1 and 52.3 to 19.8 and 38.3.
+constexpr size_t kFewFusedRouter = 16 * 1024;
 constexpr int kFewGroup = 16;         // tokens of an MFMA
 constexpr int kFewTurn = 2 * kFewGroup;   // rows at most that go through the weights together
 
@@ -42,7 +45,7 @@ struct FewWeights { const uint8_t* w; const uint8_t* scales; };   // bf16 weight
 struct FewArgs {
   int T, d, f, E, Es, k, Kp, renorm;
   int parts, h_parts;            // of d_ffn in the down projection; of d in the other two, at most 16 tokens
-  int fused_gate;                // the gate is made by few_gate_up_kernel
+  int fused_gate, fused_router;  // the gate, and the logits, are made by few_gate_up_kernel
   const uint16_t* x; const uint16_t* w_router;
   float* logits; int32_t* topk_idx; float* topk_w; FewSched* sched;
   FewWeights gate, up, down;
@@ -54,14 +57,13 @@ struct FewArgs {
 
 // ---- logits and gate ---------------------------------------------------------------------------------------------------------------
 
-// 16 experts x 16 tokens per block, K split over the wavefronts, whose sums are added in order.
-__global__ __launch_bounds__(kFewRouterWaves * kWave) void few_router_kernel(const FewArgs A) {
-  __shared__ float part[kFewRouterWaves][16][17];
+// Logits of 16 experts x 16 tokens by one block: K split over the wavefronts, whose sums are added in order.
+typedef float FewLogitParts[kFewWaves][16][17];
+__device__ __forceinline__ void few_logits(const FewArgs& A, int e0, int t0, FewLogitParts& part, float* logits) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
-  const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
   const uint16_t* const wr = A.w_router + (size_t)min(e0 + n, A.E - 1) * A.d + 8 * q;
   const uint16_t* const xr = A.x + (size_t)min(t0 + n, A.T - 1) * A.d + 8 * q;
-  const int steps = A.d / 32, per = (steps + kFewRouterWaves - 1) / kFewRouterWaves;
+  const int steps = A.d / 32, per = (steps + kFewWaves - 1) / kFewWaves;
   mx_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const int end = min(steps, (wave + 1) * per);
   for (int s0 = wave * per; s0 < end; s0 += 8) {   // (eight steps requested at once; past the end the last one, not multiplied)
@@ -83,9 +85,13 @@ __global__ __launch_bounds__(kFewRouterWaves * kWave) void few_router_kernel(con
     const int t = threadIdx.x >> 4, e = threadIdx.x & 15;
     float sum = 0.f;
 #pragma unroll
-    for (int p = 0; p < kFewRouterWaves; p++) sum += part[p][t][e];
-    if (t0 + t < A.T && e0 + e < A.E) A.logits[(size_t)(t0 + t) * A.E + e0 + e] = sum;
+    for (int p = 0; p < kFewWaves; p++) sum += part[p][t][e];
+    if (t0 + t < A.T && e0 + e < A.E) logits[(size_t)(t0 + t) * A.E + e0 + e] = sum;
   }
+}
+__global__ __launch_bounds__(kFewWaves * kWave) void few_router_kernel(const FewArgs A) {
+  __shared__ FewLogitParts part;
+  few_logits(A, blockIdx.x * 16, blockIdx.y * 16, part, A.logits);
 }
 
 // One block: the gate of every token (unless the caller brought it), then the experts that have tokens and the slots of each.
@@ -307,7 +313,7 @@ struct FewGate {
 // itself (a launch and the wait for it cost more); block (0, 0) leaves ids and weights in memory, block (0, `last_row`) the schedule.
 struct FewExpert { int id, count; const int* slots; };
 template <bool FUSED>
-__device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, int last_row) {
+__device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, char* scratch, int last_row) {
   FewExpert X;
   if (!FUSED || !A.fused_gate) {
     const int n_live = A.sched->n_live;
@@ -321,9 +327,19 @@ __device__ __forceinline__ FewExpert few_expert(const FewArgs& A, FewGate& S, in
   const int tid = threadIdx.x, lane = tid & 63, wave = few_scalar(tid >> 6), N = A.T * A.Kp, Et = A.E + A.Es;
   if (tid < kFewFusedExperts / 32) S.words[tid] = 0;
   if (A.w_router) {
+    const float* logits = A.logits;
+    if (A.fused_router) {
+      float* const own = reinterpret_cast<float*>(scratch + sizeof(FewLogitParts));
+      for (int e0 = 0; e0 < A.E; e0 += 16) {
+        if (e0 > 0) __syncthreads();
+        few_logits(A, e0, 0, *reinterpret_cast<FewLogitParts*>(scratch), own);
+      }
+      __syncthreads();
+      logits = own;
+    }
     for (int t = wave; t < A.T; t += kFewWaves) {
-      if (A.E <= kWave) route_token<kWave, 1>(A.logits + (size_t)t * A.E, t, lane, S.idx, S.weight, nullptr, A.E, A.k, A.Es, A.renorm);
-      else route_token<kWave, 4>(A.logits + (size_t)t * A.E, t, lane, S.idx, S.weight, nullptr, A.E, A.k, A.Es, A.renorm);
+      if (A.E <= kWave) route_token<kWave, 1>(logits + (size_t)t * A.E, t, lane, S.idx, S.weight, nullptr, A.E, A.k, A.Es, A.renorm);
+      else route_token<kWave, 4>(logits + (size_t)t * A.E, t, lane, S.idx, S.weight, nullptr, A.E, A.k, A.Es, A.renorm);
     }
   } else {
     for (int s = tid; s < N; s += kFewWaves * kWave) S.idx[s] = min(max(A.topk_idx[s], 0), Et - 1);
@@ -491,7 +507,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 4) void few_gate_up_kernel(const
   __shared__ __attribute__((aligned(16))) char scales[few_scale_bytes(MX, FR, GROUPS)];
   __shared__ FewGate S;
   const int lane = threadIdx.x & 63, wave = few_scalar(threadIdx.x >> 6);
-  const FewExpert X = few_expert<GROUPS == 1>(A, S, gridDim.y - 1);
+  const FewExpert X = few_expert<GROUPS == 1>(A, S, rows, gridDim.y - 1);
   if (X.count == 0) return;
   const int ct = blockIdx.x / A.h_parts, part = blockIdx.x - ct * A.h_parts;
   const int col0 = ct * 4 * WC + WC * (wave >> 1);
@@ -724,6 +740,7 @@ int few_forward(const moe_shape* shape, const uint16_t* x, const uint16_t* w_rou
   FewArgs A = {};
   A.parts = P.parts; A.h_parts = P.h_parts;
   A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm; A.fused_gate = !P.turns && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
+  A.fused_router = A.fused_gate && (size_t)D.E * D.d * 2 <= kFewFusedRouter;
   A.x = x; A.w_router = w_router; A.topk_idx = topk_idx; A.topk_w = topk_w; A.out = out;
   A.gate = W[0]; A.up = W[1]; A.down = W[2];
   A.logits = reinterpret_cast<float*>(wsb + L.logits);
@@ -733,8 +750,8 @@ int few_forward(const moe_shape* shape, const uint16_t* x, const uint16_t* w_rou
   A.partial = reinterpret_cast<float*>(wsb + L.partial);
   A.h_partial = reinterpret_cast<float*>(wsb + L.h_partial);
   hipStream_t st = (hipStream_t)stream;
-  if (w_router)
-    MOE_LAUNCH("few_router", st, few_router_kernel, dim3((D.E + 15) / 16, (D.T + 15) / 16), dim3(kFewRouterWaves * kWave), 0, st, A);
+  if (w_router && !A.fused_router)
+    MOE_LAUNCH("few_router", st, few_router_kernel, dim3((D.E + 15) / 16, (D.T + 15) / 16), dim3(kFewWaves * kWave), 0, st, A);
   if (!A.fused_gate) {
     if (D.E <= 64) MOE_LAUNCH("few_gate", st, few_gate_kernel<1>, dim3(1), dim3(1024), 0, st, A);
     else if (D.E <= 256) MOE_LAUNCH("few_gate", st, few_gate_kernel<4>, dim3(1), dim3(1024), 0, st, A);

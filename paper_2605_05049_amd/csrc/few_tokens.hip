@@ -9,9 +9,10 @@
 // widens them to bf16, exactly.  The hidden activation stays in fp32 in effect: it is kept as a bf16 head and a bf16 remainder, both of
 // which multiply W_down; the partial sums over K and the experts are added in fp32, in a fixed order.
 //
-// Launches: logits; gate (with at most 16 tokens every block of the next one makes it for itself, and the logits of a small router); G and U by columns and parts of d; with more than 16
-// tokens H; H W_down by columns and parts of d_ffn; the weighted sum.  Measured, 8 experts of 4096 x 14336, top 2: 1 token 119 us in bf16 (5.9 TB/s; a
-// large read reaches 6.2) and 49 us in 4 bits (3.8 TB/s); 16 tokens 431 (6.5 TB/s) and 177 us; 64 tokens 473 and 224 us.
+// Launches: logits; gate (with at most 16 tokens every block of the next one makes it for itself, and the logits of a small router); G and U by columns
+// and parts of d; with more than 16 tokens H; H W_down by columns and parts of d_ffn; the weighted sum.  Measured, 8 experts of 4096 x 14336, top 2:
+// 1 token 119 us in bf16 (5.9 TB/s; a large read reaches 6.2) and 49 us in 4 bits (3.8 TB/s); 16 tokens 431 (6.5 TB/s) and 177 us; 64 tokens 473 and
+// 224 us.
 #include "mxfp4.h"
 #include "route.h"
 
@@ -476,7 +477,8 @@ template <bool MX, int FR, int GROUPS, int TG, bool LO, int DEPTH, class V, clas
 __device__ __forceinline__ void few_turn(mx_f32x4 (&acc)[TG][FR], const FewTile<MX, FR>& W, F&& bring, char* rows, char* scales, int n_rows, int K, FewPart part,
                                          bool active, int lane) {
   constexpr int STEP = few_step(MX), THREADS = kFewWaves * kWave;
-  const int fills = (part.steps - 1) / few_chunk_steps<MX, GROUPS, LO>(n_rows) + 1, per = (part.steps + fills - 1) / fills, pitch = few_row_pitch(per * STEP), pieces = per * STEP * 2 / (int)sizeof(V);
+  const int fills = (part.steps - 1) / few_chunk_steps<MX, GROUPS, LO>(n_rows) + 1, per = (part.steps + fills - 1) / fills;
+  const int pitch = few_row_pitch(per * STEP), pieces = per * STEP * 2 / (int)sizeof(V);
 #pragma unroll
   for (int g = 0; g < TG; g++)
 #pragma unroll
@@ -683,7 +685,7 @@ FewLayout few_layout(const Dims& D) {
   size_t o = 0;
   L.sched = o; o += round_up(sizeof(FewSched), 256);
   L.logits = o; o += round_up((size_t)D.T * D.E * sizeof(float), 256);
-  L.h = o; o += round_up((size_t)D.N * D.f * 2 * sizeof(uint16_t), 256);
+  L.h = o; o += P.turns ? round_up((size_t)D.N * D.f * 2 * sizeof(uint16_t), 256) : 0;
   L.partial = o; o += round_up((size_t)D.N * max(P.parts, Q.parts) * D.d * sizeof(float), 256);
   L.h_partial = o; o += round_up((size_t)D.N * max(P.h_parts, Q.h_parts) * 2 * D.f * sizeof(float), 256);
   L.total = o;
@@ -739,7 +741,8 @@ int few_forward(const moe_shape* shape, const uint16_t* x, const uint16_t* w_rou
   const FewPlan P = few_plan(D, MX);
   FewArgs A = {};
   A.parts = P.parts; A.h_parts = P.h_parts;
-  A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm; A.fused_gate = !P.turns && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
+  A.T = D.T; A.d = D.d; A.f = D.f; A.E = D.E; A.Es = D.Es; A.k = D.k; A.Kp = D.Kp; A.renorm = D.renorm;
+  A.fused_gate = !P.turns && D.Et <= kFewFusedExperts && D.N <= kFewFusedSlots;
   A.fused_router = A.fused_gate && (size_t)D.E * D.d * 2 <= kFewFusedRouter;
   A.x = x; A.w_router = w_router; A.topk_idx = topk_idx; A.topk_w = topk_w; A.out = out;
   A.gate = W[0]; A.up = W[1]; A.down = W[2];

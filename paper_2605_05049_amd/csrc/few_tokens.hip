@@ -277,9 +277,11 @@ __device__ __host__ __forceinline__ int few_steps(bool mx, int K) { return (K + 
 template <bool MX>
 __device__ __forceinline__ int few_piece(int q, int ks) { return MX ? 16 * (ks >> 2) + 4 * q + (ks & 3) : q; }
 
+// h and what its bf16 head leaves: nothing where the head is an infinity (h - head would be NaN, or an infinity of the other sign) or NaN.
 __device__ __forceinline__ void few_swiglu(float g, float u, float& h, float& lo) {
   h = g / (1.0f + __expf(-g)) * u;
-  lo = h - bf16_to_f32(f32_to_bf16(h));
+  const float head = bf16_to_f32(f32_to_bf16(h));
+  lo = fabsf(head) < __builtin_inff() ? h - head : 0.f;
 }
 
 // A lane's sums of one token, 4 FR consecutive columns.

@@ -56,18 +56,21 @@ struct FewArgs {
   uint16_t* out;
 };
 
+__device__ __forceinline__ int few_scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }   // the same in all lanes: the compiler is told so
+
 // ---- logits and gate ---------------------------------------------------------------------------------------------------------------
 
 // Logits of 16 experts x 16 tokens by one block: K split over the wavefronts, whose sums are added in order.
 typedef float FewLogitParts[kFewWaves][16][17];
 __device__ __forceinline__ void few_logits(const FewArgs& A, int e0, int t0, FewLogitParts& part, float* logits) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = few_scalar(threadIdx.x >> 6), n = lane & 15, q = lane >> 4;
   const uint16_t* const wr = A.w_router + (size_t)min(e0 + n, A.E - 1) * A.d + 8 * q;
   const uint16_t* const xr = A.x + (size_t)min(t0 + n, A.T - 1) * A.d + 8 * q;
   const int steps = A.d / 32, per = (steps + kFewWaves - 1) / kFewWaves;
   mx_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const int end = min(steps, (wave + 1) * per);
-  for (int s0 = wave * per; s0 < end; s0 += 8) {   // (eight steps requested at once; past the end the last one, not multiplied)
+  // Eight steps requested at once; past the end the last one, not multiplied.  (The guard is a scalar branch: a product ignores the lane mask.)
+  for (int s0 = wave * per; s0 < end; s0 += 8) {
     mx_bf16x8 w[8], x[8];
 #pragma unroll
     for (int u = 0; u < 8; u++) {
@@ -75,6 +78,8 @@ __device__ __forceinline__ void few_logits(const FewArgs& A, int e0, int t0, Few
       w[u] = *reinterpret_cast<const mx_bf16x8*>(wr + s * 32);
       x[u] = *reinterpret_cast<const mx_bf16x8*>(xr + s * 32);
     }
+#pragma unroll
+    for (int u = 0; u < 8; u++) asm volatile("" : "+v"(w[u]), "+v"(x[u]));   // (or the compiler moves a step's loads behind its guard)
 #pragma unroll
     for (int u = 0; u < 8; u++)
       if (s0 + u < end) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u], x[u], acc, 0, 0, 0);
@@ -138,8 +143,6 @@ template <bool MX, int FR> struct FewTile;
 // 4-bit weights: steps of a chunk at most; bytes of a column's scales in LDS.
 constexpr int few_scale_steps(int groups) { return groups > 1 ? 4 : 8; }
 constexpr int few_scale_pitch(int groups) { return 8 * few_scale_steps(groups) + 8; }
-
-__device__ __forceinline__ int few_scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }   // the same in all lanes: the compiler is told so
 
 // Global memory by a scalar address: the compiler is told that it is the same in all lanes.
 typedef const uint8_t __attribute__((address_space(1)))* FewBase;

@@ -659,7 +659,8 @@ struct FewPlan {
   int parts, h_parts;
 };
 FewPlan few_plan(const Dims& D, bool mx) {
-  FewPlan P = {};
+  FewPlan P = {false, 2, 1, 1};
+  if (D.N == 0) return P;   // (no token: nothing is cut, and the blocks below are a divisor)
   // experts with tokens, if the tokens choose evenly
   const double live = std::min((double)few_live_bound(D), D.Es + D.E * -expm1(D.T * log1p(-(double)D.k / (D.E + 1e-9))));
   const long long step = few_step(mx);

@@ -22,11 +22,13 @@ class ServedLayer:
 
     def __init__(self, w_router, w_gate, w_up, w_down, top_k, n_shared=0, renorm=1, mxfp4=True, stream=None):
         E, d = w_router.shape
-        if w_gate.shape[0] != E + n_shared or w_gate.shape[1] != d:
-            raise ValueError(f"w_gate {tuple(w_gate.shape)}: expected [{E + n_shared}, {d}, d_ffn]")
+        n, f = E + n_shared, w_gate.shape[-1]
+        for name, w, want in (("w_gate", w_gate, (n, d, f)), ("w_up", w_up, (n, d, f)), ("w_down", w_down, (n, f, d))):
+            if tuple(w.shape) != want:
+                raise ValueError(f"{name} {tuple(w.shape)}: expected {want}")
         self.w_router, self.mxfp4 = w_router, mxfp4
         self.weights = quantize_experts(w_gate, w_up, w_down, stream) if mxfp4 else (w_gate, w_up, w_down)
-        self._fields = (d, w_gate.shape[2], E, top_k, n_shared, renorm)
+        self._fields = (d, f, E, top_k, n_shared, renorm)
         self._buffers = {}
 
     def buffers(self, T):

@@ -1,0 +1,31 @@
+"""Host-side checks of a layer that only answers: what it refuses, and what it keeps."""
+import pytest
+import torch
+
+import paper_2605_05049_amd as moe
+from paper_2605_05049_amd import serve
+
+E, K, ES, D, F = 8, 2, 1, 128, 192
+
+
+def _weights():
+    z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    return z(E, D), [z(E + ES, D, F), z(E + ES, D, F), z(E + ES, F, D)]
+
+
+def _layer():
+    moe.load_library()
+    w_router, weights = _weights()
+    return serve.ServedLayer(w_router, *weights, K, ES, mxfp4=False)
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("mxfp4", [False, True])
+def test_weights_of_other_shapes_are_refused(which, mxfp4):
+    """Element counts alone would let a transposed matrix pass, to be quantised along the wrong axis."""
+    w_router, weights = _weights()
+    for wrong in (weights[which].transpose(1, 2).contiguous(), weights[which][:E].contiguous(), weights[which][0]):
+        bad = list(weights)
+        bad[which] = wrong
+        with pytest.raises(ValueError, match="w_gate" if which == 0 else "w_up" if which == 1 else "w_down"):
+            serve.ServedLayer(w_router, *bad, K, ES, mxfp4=mxfp4)

@@ -41,6 +41,8 @@ class ServedLayer:
         return self._buffers[T]
 
     def __call__(self, x, stream=None):
+        if x.dim() != 2 or x.shape[1] != self._fields[0]:
+            raise ValueError(f"x {tuple(x.shape)}: expected [T, {self._fields[0]}]")
         buf = self.buffers(x.shape[0])
         if isinstance(buf, FewTokenBuffers):
             return layer_few_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)

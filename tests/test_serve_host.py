@@ -29,3 +29,13 @@ def test_weights_of_other_shapes_are_refused(which, mxfp4):
         bad[which] = wrong
         with pytest.raises(ValueError, match="w_gate" if which == 0 else "w_up" if which == 1 else "w_down"):
             serve.ServedLayer(w_router, *bad, K, ES, mxfp4=mxfp4)
+
+
+@pytest.mark.parametrize("T", [4, 100])
+def test_rows_of_another_width_are_refused(T):
+    """... also wider ones, of which the calls would take the first T * d_model elements."""
+    layer = _layer()
+    for x in (torch.zeros(T, 2 * D, dtype=torch.bfloat16), torch.zeros(T, D // 2, dtype=torch.bfloat16), torch.zeros(T * D, dtype=torch.bfloat16),
+              torch.zeros(T, 1, D, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError, match=rf"expected \[T, {D}\]"):
+            layer(x)

@@ -123,10 +123,17 @@ def main(argv=None):
     B.load_library()
     if not 1 <= args.batch <= args.prompt:
         ap.error("--batch is between 1 and --prompt")
+    if args.steps < 1:
+        ap.error("--steps is at least 1")
+    try:
+        d, f = (int(v) for v in args.dims.lower().split("x"))
+    except ValueError:
+        ap.error("--dims is two numbers, as 2048x1408")
+    if B.workspace_bytes(B.Shape(args.prompt, d, f, args.experts, args.top_k, args.shared)) == 0:
+        ap.error("--dims are multiples of 64, --top-k at most --experts, and these with --shared (from 0) at most 1024")
     if not torch.cuda.is_available():
         print("answering needs a GPU", file=sys.stderr)
         return 2
-    d, f = (int(v) for v in args.dims.lower().split("x"))
     print(json.dumps(run(d, f, args.experts, args.top_k, args.shared, args.prompt, args.batch, args.steps)), flush=True)
     return 0
 

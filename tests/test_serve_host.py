@@ -39,3 +39,12 @@ def test_rows_of_another_width_are_refused(T):
               torch.zeros(T, 1, D, dtype=torch.bfloat16)):
         with pytest.raises(ValueError, match=rf"expected \[T, {D}\]"):
             layer(x)
+
+
+@pytest.mark.parametrize("args", ["--steps 0", "--steps -3", "--batch 0", "--batch 9 --prompt 8", "--dims 2048", "--dims 2048xwide", "--dims 100x64", "--experts 4 --top-k 5",
+                                  "--shared -1"])
+def test_command_refuses(args, capsys):
+    """As errors of the command line, before anything is made."""
+    with pytest.raises(SystemExit) as e:
+        serve.main(args.split())
+    assert e.value.code == 2 and "error: --" in capsys.readouterr().err

@@ -3,7 +3,17 @@ computation is one of the C-ABI entry points, called in the order of the per-lay
 experts -> unpack/combine, then the reverse for backward)."""
 from __future__ import annotations
 
+import contextlib
+
 from . import binding as B
+
+
+def on_stream(stream):
+    """Within it, memory is allocated for work on `stream`: another stream's pool hands out what its own work may still be reading."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(stream)
 
 
 class MoeLayerBuffers:
@@ -148,9 +158,12 @@ def quantize_experts(w_gate, w_up, w_down, stream=None):
     got = []
     for w in (w_gate, w_up, w_down):
         E, K, C = w.shape
-        q = torch.empty(E, C, K // 2, dtype=torch.uint8, device=w.device)
-        scales = torch.empty(E, C, K // 32, dtype=torch.uint8, device=w.device)
+        with on_stream(stream):
+            q = torch.empty(E, C, K // 2, dtype=torch.uint8, device=w.device)
+            scales = torch.empty(E, C, K // 32, dtype=torch.uint8, device=w.device)
         B.moe_mxfp4_quantize_t(w, q, scales, stream)
+        if stream is not None:
+            w.record_stream(stream)   # (the caller may drop it now)
         got += [q, scales]
     return tuple(got)
 

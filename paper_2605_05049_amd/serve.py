@@ -8,9 +8,10 @@ are from those of the bf16 weights."""
 import argparse
 import json
 import sys
+import weakref
 
 from . import binding as B
-from .layer import FewTokenBuffers, MoeLayerBuffers, layer_few_forward, layer_forward, layer_mxfp4_forward, quantize_experts
+from .layer import FewTokenBuffers, MoeLayerBuffers, layer_few_forward, layer_forward, layer_mxfp4_forward, on_stream, quantize_experts
 
 
 class ServedLayer:
@@ -18,7 +19,7 @@ class ServedLayer:
     more by the grouped products.  `mxfp4`: the experts' weights are quantised here, and the bf16 ones are not kept.
 
     Buffers are made for a token count at its first call and kept; what a call returns is theirs and is overwritten by the next call with as
-    many tokens.  Calls on one stream at a time."""
+    many tokens.  Calls on one stream at a time; the memory is freed for others when all streams that had calls are past them."""
 
     def __init__(self, w_router, w_gate, w_up, w_down, top_k, n_shared=0, renorm=1, mxfp4=True, stream=None):
         E, d = w_router.shape
@@ -30,6 +31,7 @@ class ServedLayer:
         self.weights = quantize_experts(w_gate, w_up, w_down, stream) if mxfp4 else (w_gate, w_up, w_down)
         self._fields = (d, f, E, top_k, n_shared, renorm)
         self._buffers = {}
+        self._streams = weakref.WeakKeyDictionary()   # streams that had calls with these weights, these buffers
 
     def buffers(self, T):
         """The buffers of calls with T tokens (topk_idx, topk_w, out, ...)."""
@@ -43,12 +45,29 @@ class ServedLayer:
     def __call__(self, x, stream=None):
         if x.dim() != 2 or x.shape[1] != self._fields[0]:
             raise ValueError(f"x {tuple(x.shape)}: expected [T, {self._fields[0]}]")
-        buf = self.buffers(x.shape[0])
+        with on_stream(stream):
+            buf = self.buffers(x.shape[0])
         if isinstance(buf, FewTokenBuffers):
-            return layer_few_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
-        if self.mxfp4:
-            return layer_mxfp4_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
-        return layer_forward(buf, x, *self.weights, w_router=self.w_router, stream=stream)
+            out = layer_few_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
+        elif self.mxfp4:
+            out = layer_mxfp4_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
+        else:
+            out = layer_forward(buf, x, *self.weights, w_router=self.w_router, stream=stream)
+        self._used(buf, stream)
+        return out
+
+    def _used(self, buf, stream):
+        """What the call used is not to be handed out again before `stream` is past it.  (Once per stream: the allocator waits for what a stream has
+        enqueued by the time the memory is freed.)"""
+        handle = B._stream(stream)
+        for owner, tensors in ((self, (self.w_router, *self.weights)), (buf, vars(buf).values())):
+            seen = self._streams.setdefault(owner, set())
+            if handle not in seen:
+                import torch
+                seen.add(handle)
+                for t in tensors:
+                    if isinstance(t, torch.Tensor):
+                        t.record_stream(stream or torch.cuda.current_stream())
 
 
 def _next(x, y):

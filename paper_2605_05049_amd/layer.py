@@ -4,6 +4,7 @@ experts -> unpack/combine, then the reverse for backward)."""
 from __future__ import annotations
 
 import contextlib
+import math
 
 from . import binding as B
 
@@ -17,16 +18,16 @@ def on_stream(stream):
 
 
 class MoeLayerBuffers:
-    """All device buffers one forward+backward of a layer touches, allocated once."""
+    """All device buffers one forward+backward of a layer touches, allocated once.  `empty(*size, dtype=...)` allocates them (all but out)."""
 
-    def __init__(self, shape, device="cuda", with_backward=True, with_router=True):
+    def __init__(self, shape, device="cuda", with_backward=True, with_router=True, empty=None):
         import torch
         s = B.Shape.of(shape)
         self.shape = s
         dev = torch.device(device)
         bf, i32, f32 = torch.bfloat16, torch.int32, torch.float32
         N, T, d, f, Et, Kp = s.N, s.T, s.d_model, s.d_ffn, s.E_total, s.K_slots
-        e = lambda *sz, dtype: torch.empty(*sz, dtype=dtype, device=dev)  # noqa: E731
+        e = empty or (lambda *sz, dtype: torch.empty(*sz, dtype=dtype, device=dev))
         self.topk_idx = e(T, Kp, dtype=i32)
         self.topk_w = e(T, Kp, dtype=f32)
         self.probs = e(T, s.E, dtype=f32) if with_router else None
@@ -38,8 +39,8 @@ class MoeLayerBuffers:
         self.save_g = e(N, f, dtype=bf)
         self.save_u = e(N, f, dtype=bf)
         self.y_perm = e(N, d, dtype=bf)
-        self.out = e(T, d, dtype=bf)
-        self.ws = torch.empty(max(B.workspace_bytes(s), 256), dtype=torch.uint8, device=dev)
+        self.out = torch.empty(T, d, dtype=bf, device=dev)
+        self.ws = e(max(B.workspace_bytes(s), 256), dtype=torch.uint8)
         if with_backward:
             self.dy_perm = e(N, d, dtype=bf)
             self.dtopk_w = e(T, Kp, dtype=f32)
@@ -54,6 +55,49 @@ class MoeLayerBuffers:
         if with_backward and with_router:
             self.dx_router = e(T, d, dtype=bf)
             self.dw_router = e(s.E, d, dtype=f32)
+
+
+class _Carved:
+    """Tensors next to each other in a block of bytes; without a block, how many they would take (`at`)."""
+
+    def __init__(self, block=None):
+        self.block, self.at = block, 0
+
+    def __call__(self, *size, dtype):
+        at, n = self.at, math.prod(size) * dtype.itemsize
+        self.at += -(-n // 256) * 256
+        return None if self.block is None else self.block[at:at + n].view(dtype).view(size)
+
+
+class PromptMemory:
+    """The memory of forward calls with any number of tokens, one after another: a block that the longest so far needs.  Each call's `out` is its
+    own; the other buffers of a shape are good until those of another one are asked for."""
+
+    _VIEWS = 256   # shapes whose buffers in the block are kept as they are (tensors without memory of their own)
+
+    def __init__(self, device="cuda"):
+        self.device, self.block, self._views, self._latest = device, None, {}, None
+        self.streams = set()   # that used the block
+
+    def buffers(self, shape) -> MoeLayerBuffers:
+        import torch
+        buf = self._views.get(shape.T)
+        if buf is None:
+            need = _Carved()
+            MoeLayerBuffers(shape, self.device, with_backward=False, empty=need)
+            if self.block is None or self.block.numel() < need.at:
+                self._views, self._latest, self.block, self.streams = {}, None, None, set()   # (the old block goes first)
+                self.block = torch.empty(need.at, dtype=torch.uint8, device=self.device)
+            elif len(self._views) >= self._VIEWS:
+                self._views = {}
+            buf = self._views[shape.T] = MoeLayerBuffers(shape, self.device, with_backward=False, empty=_Carved(self.block))
+        if buf is not self._latest:
+            if self._latest is not None:
+                self._latest.out = None
+            if buf.out is None:
+                buf.out = torch.empty(shape.T, shape.d_model, dtype=torch.bfloat16, device=self.device)
+            self._latest = buf
+        return buf
 
 
 def layer_forward(buf: MoeLayerBuffers, x, w_gate, w_up, w_down, logits=None, w_router=None, stream=None):
@@ -141,6 +185,7 @@ class FewTokenBuffers:
         self.topk_w = torch.empty(s.T, s.K_slots, dtype=torch.float32, device=dev)
         self.out = torch.empty(s.T, s.d_model, dtype=torch.bfloat16, device=dev)
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self.streams = set()   # that used them, if the user keeps account
 
 
 def layer_few_forward(buf: FewTokenBuffers, x, weights, w_router=None, stream=None):

@@ -8,18 +8,19 @@ are from those of the bf16 weights."""
 import argparse
 import json
 import sys
-import weakref
 
 from . import binding as B
-from .layer import FewTokenBuffers, MoeLayerBuffers, layer_few_forward, layer_forward, layer_mxfp4_forward, on_stream, quantize_experts
+from .layer import FewTokenBuffers, PromptMemory, layer_few_forward, layer_forward, layer_mxfp4_forward, on_stream, quantize_experts
 
 
 class ServedLayer:
     """A layer that only answers: `layer(x)` for x [T, d_model] bf16, any T.  At most FEW_TOKENS_MAX tokens are answered by layer_few_forward,
     more by the grouped products.  `mxfp4`: the experts' weights are quantised here, and the bf16 ones are not kept.
 
-    Buffers are made for a token count at its first call and kept; what a call returns is theirs and is overwritten by the next call with as
-    many tokens.  Calls on one stream at a time; the memory is freed for others when all streams that had calls are past them."""
+    The buffers of a few tokens are made for their count at its first call and kept; what a call returns is theirs and is overwritten by the next
+    call with as many tokens.  Longer calls share the memory of the longest so far, and each returns a tensor of its own.  Memory that a captured
+    call uses stays as long as the layer.  Calls on one stream at a time; the memory is freed for others when all streams that had calls are past
+    them."""
 
     def __init__(self, w_router, w_gate, w_up, w_down, top_k, n_shared=0, renorm=1, mxfp4=True, stream=None):
         E, d = w_router.shape
@@ -30,44 +31,51 @@ class ServedLayer:
         self.w_router, self.mxfp4 = w_router, mxfp4
         self.weights = quantize_experts(w_gate, w_up, w_down, stream) if mxfp4 else (w_gate, w_up, w_down)
         self._fields = (d, f, E, top_k, n_shared, renorm)
-        self._buffers = {}
-        self._streams = weakref.WeakKeyDictionary()   # streams that had calls with these weights, these buffers
+        self._few, self._prompts, self._captured = {}, PromptMemory(w_router.device), []
+        self._streams = set()   # that had calls
 
     def buffers(self, T):
-        """The buffers of calls with T tokens (topk_idx, topk_w, out, ...)."""
-        if T not in self._buffers:
+        """The buffers of calls with T tokens (topk_idx, topk_w, out, ...); of more than a few tokens good until a call with another number of them."""
+        buf = self._few.get(T)
+        if buf is None:
             s = B.Shape(T, *self._fields)
-            few = T <= B.FEW_TOKENS_MAX and B.layer_few_workspace_bytes(s) > 0
-            device = self.w_router.device
-            self._buffers[T] = FewTokenBuffers(s, device) if few else MoeLayerBuffers(s, device, with_backward=False)
-        return self._buffers[T]
+            if T > B.FEW_TOKENS_MAX or B.layer_few_workspace_bytes(s) == 0:
+                return self._prompts.buffers(s)
+            buf = self._few[T] = FewTokenBuffers(s, self.w_router.device)
+        return buf
 
     def __call__(self, x, stream=None):
         if x.dim() != 2 or x.shape[1] != self._fields[0]:
             raise ValueError(f"x {tuple(x.shape)}: expected [T, {self._fields[0]}]")
+        import torch
         with on_stream(stream):
             buf = self.buffers(x.shape[0])
-        if isinstance(buf, FewTokenBuffers):
-            out = layer_few_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
-        elif self.mxfp4:
-            out = layer_mxfp4_forward(buf, x, self.weights, w_router=self.w_router, stream=stream)
-        else:
-            out = layer_forward(buf, x, *self.weights, w_router=self.w_router, stream=stream)
-        self._used(buf, stream)
-        return out
+            if isinstance(buf, FewTokenBuffers):
+                out = layer_few_forward(buf, x, self.weights, w_router=self.w_router)
+                self._used(buf.streams, vars(buf).values())
+                return out
+            buf.out = torch.empty_like(buf.out)
+            if self.mxfp4:
+                out = layer_mxfp4_forward(buf, x, self.weights, w_router=self.w_router)
+            else:
+                out = layer_forward(buf, x, *self.weights, w_router=self.w_router)
+            block = self._prompts.block
+            self._used(self._prompts.streams, (block,))
+            if torch.cuda.is_current_stream_capturing() and not any(b is block for b in self._captured):
+                self._captured.append(block)
+            return out
 
-    def _used(self, buf, stream):
-        """What the call used is not to be handed out again before `stream` is past it.  (Once per stream: the allocator waits for what a stream has
-        enqueued by the time the memory is freed.)"""
-        handle = B._stream(stream)
-        for owner, tensors in ((self, (self.w_router, *self.weights)), (buf, vars(buf).values())):
-            seen = self._streams.setdefault(owner, set())
+    def _used(self, streams, tensors):
+        """What the call used, these tensors and the weights, is not to be handed out again before the current stream is past it.  (Once per stream: the
+        allocator waits for what a stream has enqueued by the time the memory is freed.)"""
+        import torch
+        handle = B._stream(None)
+        for seen, what in ((self._streams, (self.w_router, *self.weights)), (streams, tensors)):
             if handle not in seen:
-                import torch
                 seen.add(handle)
-                for t in tensors:
+                for t in what:
                     if isinstance(t, torch.Tensor):
-                        t.record_stream(stream or torch.cuda.current_stream())
+                        t.record_stream(torch.cuda.current_stream())
 
 
 def _next(x, y):
@@ -116,10 +124,10 @@ def run(d, f, experts, top_k, shared, prompt, batch, steps, seed=0):
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        layer(static)
+        step = layer(static)
     step_ref = full(static).float()
     graph.replay()
-    step = layer.buffers(batch).out.float()
+    step = step.float()
     off = lambda a, b: round(((a - b).norm() / b.norm()).item(), 4)  # noqa: E731
     return {"d_model": d, "d_ffn": f, "experts": experts, "shared": shared, "top_k": top_k, "prompt": prompt, "batch": batch,
             "weights_GB": round(sum(w.numel() * w.element_size() for w in layer.weights) / 1e9, 3),

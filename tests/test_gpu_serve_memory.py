@@ -70,3 +70,45 @@ def test_buffers_are_made_in_memory_of_the_calls_stream(moe, T):
     assert not busy.query(), "the stream was to be busy until here"
     assert not buffers & {t.data_ptr() for t in again}
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("mxfp4", [False, True], ids=["bf16", "mxfp4"])
+def test_prompts_of_many_lengths(moe, mxfp4):
+    """One after another, shorter and longer: each answer is right and stays, and the memory is that of the longest."""
+    w_router, weights = _weights()
+    layer = serve.ServedLayer(w_router, *weights, K, ES, mxfp4=mxfp4)
+    x = torch.randn(700, D, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    lengths = (100, 65, 300, 64, 299, 700, 66, 300, 100)
+    answers = [layer(x[:T]) for T in lengths]
+    for T, got in zip(lengths, answers):
+        want = serve.ServedLayer(w_router, *weights, K, ES, mxfp4=mxfp4)(x[:T])
+        assert torch.equal(got, want), T
+    del answers, got, want
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    for T in range(65, 700, 31):
+        layer(x[:T])
+    assert torch.cuda.memory_allocated() <= held + (1 << 20)
+
+
+def test_captured_prompts_keep_their_memory(moe):
+    """A longer prompt takes another block; the graph's stays its own."""
+    w_router, weights = _weights()
+    layer = serve.ServedLayer(w_router, *weights, K, ES)
+    xs = [torch.randn(90, D, generator=torch.Generator().manual_seed(i)).bfloat16().cuda() for i in range(3)]
+    eager = [layer(x) for x in xs]
+    static = xs[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layer(static)
+    used = layer._prompts.block.data_ptr()
+    layer(torch.cat(xs * 4))
+    assert layer._prompts.block.data_ptr() != used
+    filler = [torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    for x, want in list(zip(xs, eager)) * 2:
+        static.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert all((t == 255).all() for t in filler)

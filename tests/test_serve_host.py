@@ -48,3 +48,49 @@ def test_command_refuses(args, capsys):
     with pytest.raises(SystemExit) as e:
         serve.main(args.split())
     assert e.value.code == 2 and "error: --" in capsys.readouterr().err
+
+
+def _held(layer):
+    """Bytes of the tensors that a layer keeps beside its weights."""
+    seen, todo, found = set(), [layer], {}
+    while todo:
+        o = todo.pop()
+        if id(o) in seen:
+            continue
+        seen.add(id(o))
+        if isinstance(o, torch.Tensor):
+            found[o.untyped_storage().data_ptr()] = o.untyped_storage().nbytes()
+        elif isinstance(o, dict):
+            todo += o.values()
+        elif isinstance(o, (list, tuple, set)):
+            todo += o
+        elif hasattr(o, "__dict__"):
+            todo += vars(o).values()
+    for w in (layer.w_router, *layer.weights):
+        found.pop(w.untyped_storage().data_ptr())
+    return sum(found.values())
+
+
+def test_prompts_of_many_lengths_keep_the_memory_of_the_longest():
+    layer = _layer()
+    layer.buffers(2000)
+    longest = _held(layer)
+    for T in (65, 100, 1999, 700, 66, 2000):
+        s = layer.buffers(T)
+        assert s.shape.T == T and s.out.shape == (T, D) and s.topk_idx.shape == (T, K + ES) and s.x_perm.shape == (T * (K + ES), D)
+        assert all(t.is_contiguous() and t.storage_offset() * t.itemsize % 256 == 0 for t in vars(s).values() if isinstance(t, torch.Tensor))
+        assert _held(layer) <= longest
+    fresh = _layer()
+    for T in range(65, 500, 29):   # ever longer ones
+        fresh.buffers(T)
+    only = _layer()
+    only.buffers(T)
+    assert _held(fresh) == _held(only)
+
+
+def test_buffers_of_few_tokens_stay():
+    """... for each count, at most 64 of them: a step's graph is replayed on them."""
+    layer = _layer()
+    first = [layer.buffers(T) for T in (1, 7, 64)]
+    layer.buffers(300)
+    assert [layer.buffers(T) for T in (1, 7, 64)] == first and all(isinstance(b, moe.FewTokenBuffers) for b in first)

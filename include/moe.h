@@ -16,8 +16,8 @@
  *     uint16_t bit patterns.  All tensors are dense, row-major, and 16-byte aligned.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls only enqueue work on it:
  *     they never allocate, free, or synchronise the host.  Scratch comes from the caller's workspace `ws`
- *     (at least moe_workspace_bytes(shape) bytes, 256-byte aligned); calls that share a workspace must be
- *     ordered on one stream.
+ *     (at least moe_workspace_bytes(shape) bytes, 256-byte aligned; the calls that answer take less, as said
+ *     there); calls that share a workspace must be ordered on one stream.
  *   - Return value: a moe_status.  Argument checks (NULL pointers, shape limits, alignment, workspace size)
  *     run on the host before anything is launched; on any error nothing is enqueued and no output is touched.
  *   - Outputs are fully overwritten, except the weight gradients when `accumulate` is 1.
@@ -53,7 +53,7 @@ typedef enum {
   MOE_ERR_NULL = -1,      /* a required pointer is NULL */
   MOE_ERR_SHAPE = -2,     /* shape outside the limits above */
   MOE_ERR_ALIGN = -3,     /* a pointer is not 16-byte aligned (workspace: 256) */
-  MOE_ERR_WORKSPACE = -4, /* workspace smaller than moe_workspace_bytes() */
+  MOE_ERR_WORKSPACE = -4, /* workspace smaller than the call needs (moe_workspace_bytes() and the like) */
   MOE_ERR_RUNTIME = -5    /* a HIP launch failed; hipGetLastError() holds the cause */
 } moe_status;
 
@@ -256,7 +256,10 @@ int moe_mxfp4_grouped_gemm(int experts, int64_t rows, int n, int k, const uint8_
 /* moe_grouped_ffn_fwd on quantised weights, for answering (nothing is kept for a backward pass):
  *   X = Q(x_perm);  G = X W_gate,  U = X W_up,  H = Q(silu(G) * U),  Y = H W_down     (Q: as moe_mxfp4_quantize; of H from fp32)
  *   x_perm [N,d] bf16 in;  offsets [E'+1] int32 in;  wq_gate, wq_up [E', f, d / 2], s_gate, s_up [E', f, d / 32], wq_down [E', d, f / 2],
- *   s_down [E', d, f / 32] in;  y_perm [N,d] bf16 out. */
+ *   s_down [E', d, f / 32] in;  y_perm [N,d] bf16 out.
+ * moe_mxfp4_workspace_bytes(shape) bytes of workspace are enough for it and for what comes before it, moe_router_fwd, moe_router_route_fwd
+ * and moe_permute (0 if the shape is invalid): the rows and H in 4 bits, without what only the forward on bf16 weights and the backward need. */
+size_t moe_mxfp4_workspace_bytes(const moe_shape* shape);
 int moe_mxfp4_grouped_ffn_fwd(const moe_shape* shape, const uint16_t* x_perm, const int32_t* offsets, const uint8_t* wq_gate,
                               const uint8_t* s_gate, const uint8_t* wq_up, const uint8_t* s_up, const uint8_t* wq_down,
                               const uint8_t* s_down, uint16_t* y_perm, void* ws, size_t ws_bytes, void* stream);

@@ -13,8 +13,10 @@ from .binding import (  # noqa: F401
     profile_enable, profile_reset, profile_records, load_accumulate, load_imbalance, rebalance_experts,
     moe_halo_pack_remote, moe_halo_repack, moe_halo_unpack,
     moe_mxfp4_quantize, moe_mxfp4_quantize_t, moe_mxfp4_dequantize, moe_mxfp4_grouped_gemm, moe_mxfp4_grouped_ffn_fwd,
+    mxfp4_workspace_bytes,
     FEW_TOKENS_MAX, layer_few_workspace_bytes, moe_layer_few_fwd, moe_layer_few_mxfp4_fwd,
 )
 from .layer import (  # noqa: F401
-    MoeLayerBuffers, CapturedLayerStep, layer_forward, layer_backward, FewTokenBuffers, layer_few_forward, quantize_experts, layer_mxfp4_forward,
+    MoeLayerBuffers, CapturedLayerStep, layer_forward, layer_backward, FewTokenBuffers, PromptMemory, layer_few_forward, quantize_experts,
+    layer_mxfp4_forward,
 )

@@ -19,7 +19,7 @@ EXPORTED_SYMBOLS = (
     "moe_unpermute_combine", "moe_unpermute_combine_bwd", "moe_unpermute_combine_route_bwd",
     "moe_load_accumulate", "moe_load_imbalance", "moe_rebalance_experts",
     "moe_halo_pack_remote", "moe_halo_repack", "moe_halo_unpack",
-    "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_ffn_fwd",
+    "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_ffn_fwd", "moe_mxfp4_workspace_bytes",
     "moe_layer_few_workspace_bytes", "moe_layer_few_fwd", "moe_layer_few_mxfp4_fwd",
 )
 FEW_TOKENS_MAX = 64   # MOE_FEW_TOKENS_MAX: tokens of a moe_layer_few_* call
@@ -96,6 +96,8 @@ def load_library():
     lib.moe_profile_get.argtypes = [c_int, POINTER(c_char_p), POINTER(ctypes.c_float)]
     lib.moe_profile_reset.restype = c_int
     lib.moe_profile_reset.argtypes = []
+    lib.moe_mxfp4_workspace_bytes.restype = c_size_t
+    lib.moe_mxfp4_workspace_bytes.argtypes = [sp]
     lib.moe_layer_few_workspace_bytes.restype = c_size_t
     lib.moe_layer_few_workspace_bytes.argtypes = [sp]
     V = c_void_p
@@ -148,6 +150,11 @@ def abi_version() -> int:
 
 def workspace_bytes(shape) -> int:
     return int(load_library().moe_workspace_bytes(ctypes.byref(Shape.of(shape)._c)))
+
+
+def mxfp4_workspace_bytes(shape) -> int:
+    """Bytes of workspace of a forward on 4-bit weights: the router, the permutation and moe_mxfp4_grouped_ffn_fwd (0: the shape is invalid)."""
+    return int(load_library().moe_mxfp4_workspace_bytes(ctypes.byref(Shape.of(shape)._c)))
 
 
 def layer_few_workspace_bytes(shape) -> int:

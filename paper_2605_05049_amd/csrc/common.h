@@ -54,6 +54,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 struct WsLayout {
   size_t perm_hist, perm_hist_bytes;
   size_t perm_rank, perm_rank_bytes;
+  size_t perm_total;        // all that the permutation needs
   size_t sched, sched_few, sched_bytes;
   size_t order;
   size_t zero_page;
@@ -66,6 +67,7 @@ struct WsLayout {
   size_t w_router_t;        // [d, 128] bf16 at most: W_r transposed and zero-padded (router backward, E <= 128)
   size_t router_dw_partial; // router_dw_parts() fp32 partial results [d, ldp] of dW_r^T
   size_t mx_x, mx_xs, mx_h, mx_hs;   // rows and hidden rows in 4 bits with their scales: [N, d / 2], [N, d / 32], [N, f / 2], [N, f / 32]
+  size_t mx_total;          // all that the permutation and then the forward on 4-bit weights need
   size_t total;
 };
 
@@ -95,6 +97,7 @@ inline WsLayout ws_layout(const Dims& D) {
   L.perm_rank = off;
   L.perm_rank_bytes = round_up((size_t)D.N * sizeof(int32_t) + 256, 256);
   off += L.perm_rank_bytes;
+  L.perm_total = off;
   L.sched_bytes = round_up((size_t)(64 + 4 * sched_max_tiles(D) + kMaxExperts) * sizeof(int32_t), 256);
   L.sched = off; off += L.sched_bytes;
   L.sched_few = off; off += L.sched_bytes;
@@ -125,6 +128,7 @@ inline WsLayout ws_layout(const Dims& D) {
   L.mx_xs = mx; mx += round_up((size_t)D.N * D.d / 32, 256);
   L.mx_h = mx; mx += round_up((size_t)D.N * D.f / 2, 256);
   L.mx_hs = mx; mx += round_up((size_t)D.N * D.f / 32, 256);
+  L.mx_total = L.perm_total > mx ? L.perm_total : mx;
   L.total = off > mx ? off : mx;
   return L;
 }

@@ -643,6 +643,11 @@ extern "C" int moe_mxfp4_grouped_gemm(int experts, int64_t rows, int n, int k, c
   return launch_status();
 }
 
+extern "C" size_t moe_mxfp4_workspace_bytes(const moe_shape* shape) {
+  moe::Dims D;
+  return moe::check_shape(shape, &D) == MOE_OK ? moe::ws_layout(D).mx_total : 0;
+}
+
 extern "C" int moe_mxfp4_grouped_ffn_fwd(const moe_shape* shape, const uint16_t* x_perm, const int32_t* offsets, const uint8_t* wq_gate,
                                          const uint8_t* s_gate, const uint8_t* wq_up, const uint8_t* s_up, const uint8_t* wq_down,
                                          const uint8_t* s_down, uint16_t* y_perm, void* ws, size_t ws_bytes, void* stream) {
@@ -657,7 +662,7 @@ extern "C" int moe_mxfp4_grouped_ffn_fwd(const moe_shape* shape, const uint16_t*
   for (const void* p : ptrs) MOE_REQUIRE_ALIGNED(p);
   if (!aligned(ws, 256)) return MOE_ERR_ALIGN;
   const WsLayout L = ws_layout(D);
-  if (ws_bytes < L.total) return MOE_ERR_WORKSPACE;
+  if (ws_bytes < L.mx_total) return MOE_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   uint8_t* const wsb = static_cast<uint8_t*>(ws);
   uint8_t* const xq = wsb + L.mx_x; uint8_t* const xs = wsb + L.mx_xs; uint8_t* const hq = wsb + L.mx_h; uint8_t* const hs = wsb + L.mx_hs;

@@ -765,7 +765,7 @@ extern "C" int moe_permute(const moe_shape* shape, const uint16_t* x, const int3
   MOE_REQUIRE_PTR(ws);
   if (!aligned(ws, 256)) return MOE_ERR_ALIGN;
   const WsLayout L = ws_layout(D);
-  if (ws_bytes < L.total) return MOE_ERR_WORKSPACE;
+  if (ws_bytes < L.perm_total) return MOE_ERR_WORKSPACE;
   return permute_launch(D, x, topk_idx, x_perm, counts, offsets, row_of_slot, slot_of_row,
                         reinterpret_cast<int32_t*>(static_cast<char*>(ws) + L.perm_hist),
                         reinterpret_cast<int32_t*>(static_cast<char*>(ws) + L.perm_rank), (hipStream_t)stream);

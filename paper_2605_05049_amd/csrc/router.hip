@@ -524,7 +524,7 @@ static int router_fwd_checks(const moe_shape* shape, Dims* D, const uint16_t* x,
   if (rc != MOE_OK) return rc;
   if (!ws) return MOE_ERR_NULL;
   if (!aligned(ws, 256)) return MOE_ERR_ALIGN;
-  if (ws_bytes < ws_layout(*D).total) return MOE_ERR_WORKSPACE;   // (kept in the signature; this kernel needs no scratch)
+  if (ws_bytes < ws_layout(*D).perm_total) return MOE_ERR_WORKSPACE;   // (kept in the signature: this kernel needs no scratch, the call after it does)
   MOE_REQUIRE_PTR(x); MOE_REQUIRE_PTR(w_router); MOE_REQUIRE_PTR(logits);
   MOE_REQUIRE_ALIGNED(x); MOE_REQUIRE_ALIGNED(w_router); MOE_REQUIRE_ALIGNED(logits);
   return MOE_OK;

@@ -18,9 +18,10 @@ def on_stream(stream):
 
 
 class MoeLayerBuffers:
-    """All device buffers one forward+backward of a layer touches, allocated once.  `empty(*size, dtype=...)` allocates them (all but out)."""
+    """All device buffers one forward+backward of a layer touches, allocated once.  `empty(*size, dtype=...)` allocates them (all but out).  Without
+    `with_saved` nothing is kept for a backward (save_g and save_u are None), and of `mxfp4` the workspace is that of layer_mxfp4_forward."""
 
-    def __init__(self, shape, device="cuda", with_backward=True, with_router=True, empty=None):
+    def __init__(self, shape, device="cuda", with_backward=True, with_router=True, empty=None, with_saved=True, mxfp4=False):
         import torch
         s = B.Shape.of(shape)
         self.shape = s
@@ -36,11 +37,11 @@ class MoeLayerBuffers:
         self.row_of_slot = e(N, dtype=i32)
         self.slot_of_row = e(N, dtype=i32)
         self.x_perm = e(N, d, dtype=bf)
-        self.save_g = e(N, f, dtype=bf)
-        self.save_u = e(N, f, dtype=bf)
+        self.save_g = e(N, f, dtype=bf) if with_saved else None
+        self.save_u = e(N, f, dtype=bf) if with_saved else None
         self.y_perm = e(N, d, dtype=bf)
         self.out = torch.empty(T, d, dtype=bf, device=dev)
-        self.ws = e(max(B.workspace_bytes(s), 256), dtype=torch.uint8)
+        self.ws = e(max((B.mxfp4_workspace_bytes if mxfp4 else B.workspace_bytes)(s), 256), dtype=torch.uint8)
         if with_backward:
             self.dy_perm = e(N, d, dtype=bf)
             self.dtopk_w = e(T, Kp, dtype=f32)
@@ -71,11 +72,12 @@ class _Carved:
 
 class PromptMemory:
     """The memory of forward calls with any number of tokens, one after another: a block that the longest so far needs.  Each call's `out` is its
-    own; the other buffers of a shape are good until those of another one are asked for."""
+    own; the other buffers of a shape are good until those of another one are asked for.  `mxfp4`: of layer_mxfp4_forward."""
 
     _VIEWS = 256   # shapes whose buffers in the block are kept as they are (tensors without memory of their own)
 
-    def __init__(self, device="cuda"):
+    def __init__(self, device="cuda", mxfp4=False):
+        self._kind = {"with_backward": False, "with_saved": False, "mxfp4": mxfp4}
         self.device, self.block, self._views, self._latest = device, None, {}, None
         self.streams = set()   # that used the block
 
@@ -84,13 +86,13 @@ class PromptMemory:
         buf = self._views.get(shape.T)
         if buf is None:
             need = _Carved()
-            MoeLayerBuffers(shape, self.device, with_backward=False, empty=need)
+            MoeLayerBuffers(shape, self.device, empty=need, **self._kind)
             if self.block is None or self.block.numel() < need.at:
                 self._views, self._latest, self.block, self.streams = {}, None, None, set()   # (the old block goes first)
                 self.block = torch.empty(need.at, dtype=torch.uint8, device=self.device)
             elif len(self._views) >= self._VIEWS:
                 self._views = {}
-            buf = self._views[shape.T] = MoeLayerBuffers(shape, self.device, with_backward=False, empty=_Carved(self.block))
+            buf = self._views[shape.T] = MoeLayerBuffers(shape, self.device, empty=_Carved(self.block), **self._kind)
         if buf is not self._latest:
             if self._latest is not None:
                 self._latest.out = None

@@ -31,7 +31,7 @@ class ServedLayer:
         self.w_router, self.mxfp4 = w_router, mxfp4
         self.weights = quantize_experts(w_gate, w_up, w_down, stream) if mxfp4 else (w_gate, w_up, w_down)
         self._fields = (d, f, E, top_k, n_shared, renorm)
-        self._few, self._prompts, self._captured = {}, PromptMemory(w_router.device), []
+        self._few, self._prompts, self._captured = {}, PromptMemory(w_router.device, mxfp4), []
         self._streams = set()   # that had calls
 
     def buffers(self, T):

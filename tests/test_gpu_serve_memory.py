@@ -112,3 +112,23 @@ def test_captured_prompts_keep_their_memory(moe):
         torch.cuda.synchronize()
         assert torch.equal(out, want)
         assert all((t == 255).all() for t in filler)
+
+
+@pytest.mark.parametrize("T,d,f,E,k", [(65, 64, 64, 1024, 8), (100, 256, 448, 8, 2), (1500, 320, 64, 300, 3), (3000, 64, 192, 16, 4), (1, 128, 64, 4, 2)])
+def test_the_smaller_workspace_is_enough(moe, T, d, f, E, k):
+    """Router, permutation and 4-bit FFN with mxfp4_workspace_bytes exactly: the same answers, and nothing written past it."""
+    g = torch.Generator().manual_seed(T)
+    normal = lambda *s: (torch.randn(*s, generator=g) * s[-2] ** -0.5).bfloat16().cuda()  # noqa: E731
+    w_router, weights = normal(E, d), moe.quantize_experts(normal(E, d, f), normal(E, d, f), normal(E, f, d))
+    x = normal(T, d)
+    s = moe.Shape(T, d, f, E, k)
+    n = moe.mxfp4_workspace_bytes(s)
+    full, small = moe.MoeLayerBuffers(s, with_backward=False), moe.MoeLayerBuffers(s, with_backward=False, with_saved=False, mxfp4=True)
+    assert small.ws.numel() == max(n, 256)
+    room = torch.full((n + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda")
+    small.ws = room[:n]
+    full.ws.fill_(0xFF)
+    want = moe.layer_mxfp4_forward(full, x, weights, w_router=w_router)
+    got = moe.layer_mxfp4_forward(small, x, weights, w_router=w_router)
+    assert torch.equal(got, want) and torch.equal(small.row_of_slot, full.row_of_slot)
+    assert (room[n:] == 0xA5).all()

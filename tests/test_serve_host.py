@@ -1,4 +1,6 @@
 """Host-side checks of a layer that only answers: what it refuses, and what it keeps."""
+import ctypes
+
 import pytest
 import torch
 
@@ -94,3 +96,30 @@ def test_buffers_of_few_tokens_stay():
     first = [layer.buffers(T) for T in (1, 7, 64)]
     layer.buffers(300)
     assert [layer.buffers(T) for T in (1, 7, 64)] == first and all(isinstance(b, moe.FewTokenBuffers) for b in first)
+
+
+def test_memory_of_a_prompt_on_4_bit_weights():
+    """The rows before and after the experts, the rows and H in 4 bits, and the maps: nothing that only a backward or bf16 weights need."""
+    for T, d, f, e, k, es in ((4096, 2048, 1408, 64, 6, 2), (8192, 4096, 14336, 8, 2, 0), (65, 64, 64, 1024, 8, 0)):
+        s = moe.Shape(T, d, f, e, k, es)
+        buf = moe.PromptMemory("cpu", mxfp4=True).buffers(s)
+        rows, codes = 2 * s.N * d * 2, s.N * (d + f) * 17 // 32
+        maps = 4 * (4 * s.N + 2 * T * e + 2 * s.E_total) + 4 * (s.N + (s.N // 1024 + 1) * s.E_total)   # (the last two: the permutation's scratch)
+        assert buf.x_perm.untyped_storage().nbytes() <= rows + codes + maps + 64 * 256
+        assert buf.save_g is None and buf.save_u is None
+    plain = moe.PromptMemory("cpu").buffers(s)
+    assert plain.save_g is None and plain.ws.numel() == moe.workspace_bytes(s)
+
+
+def test_workspace_of_the_forward_on_4_bit_weights():
+    lib = moe.load_library()
+    s = moe.Shape(256, 512, 1024, 8, 2)
+    n = moe.mxfp4_workspace_bytes(s)
+    assert s.N * (512 + 1024) * 17 // 32 <= n < moe.workspace_bytes(s) and n % 256 == 0
+    assert moe.mxfp4_workspace_bytes(moe.Shape(256, 500, 1024, 8, 2)) == 0
+    fake = ctypes.c_void_p(0x10000)   # (never dereferenced: the call fails its host checks)
+    call = lambda size: lib.moe_mxfp4_grouped_ffn_fwd(ctypes.byref(s._c), *[fake] * 10, size, None)  # noqa: E731
+    assert call(n - 1) == -4
+    many = moe.Shape(4000, 64, 64, 1024, 2)   # the permutation's scratch: 8 x 1024 and 8000 ints
+    perm = lambda size: lib.moe_permute(ctypes.byref(many._c), *[fake] * 8, size, None)  # noqa: E731
+    assert perm(4 * (8 * 1024 + 8000) - 1) == -4

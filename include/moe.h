@@ -252,6 +252,9 @@ int moe_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64_t rows, 
  *   experts <= 1024; rows < 2^31. */
 int moe_mxfp4_grouped_gemm(int experts, int64_t rows, int n, int k, const uint8_t* xq, const uint8_t* x_scales, const int32_t* offsets,
                            const uint8_t* wq, const uint8_t* w_scales, uint16_t* y, void* stream);
+/* 1 where the product runs on tiles of 256 x 256, 0 on those of 128 x 128 (or for sizes that it refuses).  For tests and benchmarks: the choice
+ * does not change what the call computes, up to the order of the sums. */
+int moe_mxfp4_grouped_gemm_large_tiles(int experts, int64_t rows, int n, int k);
 
 /* moe_grouped_ffn_fwd on quantised weights, for answering (nothing is kept for a backward pass):
  *   X = Q(x_perm);  G = X W_gate,  U = X W_up,  H = Q(silu(G) * U),  Y = H W_down     (Q: as moe_mxfp4_quantize; of H from fp32)

@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     profile_enable, profile_reset, profile_records, load_accumulate, load_imbalance, rebalance_experts,
     moe_halo_pack_remote, moe_halo_repack, moe_halo_unpack,
     moe_mxfp4_quantize, moe_mxfp4_quantize_t, moe_mxfp4_dequantize, moe_mxfp4_grouped_gemm, moe_mxfp4_grouped_ffn_fwd,
-    mxfp4_workspace_bytes,
+    mxfp4_workspace_bytes, mxfp4_grouped_gemm_large_tiles,
     FEW_TOKENS_MAX, layer_few_workspace_bytes, moe_layer_few_fwd, moe_layer_few_mxfp4_fwd,
 )
 from .layer import (  # noqa: F401

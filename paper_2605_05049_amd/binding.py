@@ -19,7 +19,8 @@ EXPORTED_SYMBOLS = (
     "moe_unpermute_combine", "moe_unpermute_combine_bwd", "moe_unpermute_combine_route_bwd",
     "moe_load_accumulate", "moe_load_imbalance", "moe_rebalance_experts",
     "moe_halo_pack_remote", "moe_halo_repack", "moe_halo_unpack",
-    "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_ffn_fwd", "moe_mxfp4_workspace_bytes",
+    "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_gemm_large_tiles",
+    "moe_mxfp4_grouped_ffn_fwd", "moe_mxfp4_workspace_bytes",
     "moe_layer_few_workspace_bytes", "moe_layer_few_fwd", "moe_layer_few_mxfp4_fwd",
 )
 FEW_TOKENS_MAX = 64   # MOE_FEW_TOKENS_MAX: tokens of a moe_layer_few_* call
@@ -129,6 +130,7 @@ def load_library():
     sigs["moe_mxfp4_quantize_t"] = [V, c_int, c_int, c_int, V, V, V]
     sigs["moe_mxfp4_dequantize"] = [V, V, c_int64, c_int, V, V]
     sigs["moe_mxfp4_grouped_gemm"] = [c_int, c_int64, c_int, c_int, V, V, V, V, V, V, V]
+    sigs["moe_mxfp4_grouped_gemm_large_tiles"] = [c_int, c_int64, c_int, c_int]
     sigs["moe_mxfp4_grouped_ffn_fwd"] = [sp] + [V] * 10 + [c_size_t, V]
     sigs["moe_layer_few_fwd"] = [sp] + [V] * 9 + [c_size_t, V]
     sigs["moe_layer_few_mxfp4_fwd"] = [sp] + [V] * 12 + [c_size_t, V]
@@ -150,6 +152,11 @@ def abi_version() -> int:
 
 def workspace_bytes(shape) -> int:
     return int(load_library().moe_workspace_bytes(ctypes.byref(Shape.of(shape)._c)))
+
+
+def mxfp4_grouped_gemm_large_tiles(experts, rows, n, k) -> bool:
+    """Whether moe_mxfp4_grouped_gemm runs on tiles of 256 x 256 at these sizes."""
+    return bool(load_library().moe_mxfp4_grouped_gemm_large_tiles(experts, rows, n, k))
 
 
 def mxfp4_workspace_bytes(shape) -> int:

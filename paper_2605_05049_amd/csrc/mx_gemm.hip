@@ -601,15 +601,25 @@ __global__ __launch_bounds__(256, 1) void mx_direct_kernel(const MxGemmArgs A) {
   else run(std::integral_constant<int, 1>{});
 }
 
+// Large tiles (8 scales of a row at once: 256 k at least) where there is work for the CUs, or where the contraction is long and most experts have
+// rows; small ones elsewhere.  Measured, large to small tiles: 8 experts, 4096 columns, K = 4096, 128 rows 22 to 28 us, 1024 rows 28 to 60, 8192 rows 80 to
+// 451; 64 experts, 2048 columns, K = 1408, 512 rows 23 to 22, 2048 rows (64 tiles) 25 to 26, 8192 rows 33 to 50; 8 experts, 1024 columns, K = 512, 2048 rows
+// 15 to 10, 8192 rows 16 to 19; 1000 experts, 2048 columns, K = 2048, 16 rows 144 to 96 (a block has all of a CU's LDS), 1024 rows 581 to 606.
+// Work is rows times columns (of a pair those of both weights), 2^22 of them: a round of small tiles.  A tile that its columns do not fill pays from 512 k
+// on: 8 experts, 60000 rows of 96 columns, K = 512 11 to 16 us, 1920 22 to 32; 65536 rows of 192, K = 512 16 to 34, 1920 30 to 73; a pair of 64, 50000 rows,
+// K = 512 15 to 19, 1920 28 to 40.  With K = 256 and 320 these are 8.6 to 9.9 and 9.5 to 8.7, 13 to 11 and 15 to 11: there only whole tiles count.  Of 64
+// columns and fewer a tile is mostly empty: 131072 rows of 64, K = 512 24 to 21, 1920 56 to 47.
+static bool mx_large_tiles(MxKind kind, long long rows, int E, int n, int k) {
+  const int columns = kind == MX_GATE_UP ? 2 * n : n;
+  const bool fills = k >= 512 ? columns > 64 && rows * columns >= 64ll * MXT * MXT : rows * (columns / MXT) >= 64ll * MXT;
+  return k >= 8 * kMxBlock && (fills || (k >= 2048 && rows >= E / 2));
+}
+
 template <int KIND>
 static void launch_kind(const char* label, hipStream_t st, const MxGemmArgs& A, long long rows) {
   const int cols = KIND == MX_GATE_UP ? MXT / 2 : MXT, small_cols = KIND == MX_GATE_UP ? 64 : 128;
   const long long tiles = (rows / MXT + A.E) * ((A.n + cols - 1) / cols);   // (at most)
-  // Large tiles (8 scales of a row at once: 256 k at least) where there is work for the CUs, or where the contraction is long and most experts have
-  // rows.  Measured, large to small tiles: 8 experts, 4096 columns, K = 4096, 128 rows 22 to 28 us, 1024 rows 28 to 60, 8192 rows 80 to 451; 64 experts,
-  // 2048 columns, K = 1408, 512 rows 23 to 22, 2048 rows (64 tiles) 25 to 26, 8192 rows 33 to 50; 8 experts, 1024 columns, K = 512, 2048 rows 15 to 10,
-  // 8192 rows 16 to 19; 1000 experts, 2048 columns, K = 2048, 16 rows 144 to 96 (a block has all of a CU's LDS), 1024 rows 581 to 606.
-  if (A.k >= 8 * kMxBlock && (rows * (A.n / cols) >= 64ll * MXT || (A.k >= 2048 && rows >= A.E / 2))) {
+  if (mx_large_tiles((MxKind)KIND, rows, A.E, A.n, A.k)) {
     const long long round = MX_XCDS * MX_CHUNK;
     const dim3 grid((unsigned)((tiles + round - 1) / round * round));
     if (A.k % (4 * kMxBlock) == 0) MOE_LAUNCH(label, st, (mx_direct_kernel<KIND>), grid, dim3(256), 0, st, A);
@@ -626,13 +636,22 @@ void launch_mx_gemm(const char* label, hipStream_t st, MxKind kind, const MxGemm
 
 }  // namespace moe
 
+static int check_gemm(int experts, int64_t rows, int n, int k) {
+  if (experts < 1 || experts > moe::kMaxExperts || rows < 0 || rows >= (1ll << 31)) return MOE_ERR_SHAPE;
+  if (n < 8 || n % 8 || n > moe::kMaxWidth || k < moe::kMxBlock || k % moe::kMxBlock || k > moe::kMaxWidth) return MOE_ERR_SHAPE;
+  if ((rows / moe::MXR + experts) * ((n + 127) / 128) >= (1ll << 24)) return MOE_ERR_SHAPE;   // (a launch has fewer than 2^32 threads)
+  return MOE_OK;
+}
+
+extern "C" int moe_mxfp4_grouped_gemm_large_tiles(int experts, int64_t rows, int n, int k) {
+  return check_gemm(experts, rows, n, k) == MOE_OK && moe::mx_large_tiles(moe::MX_PRODUCT, rows, experts, n, k);
+}
+
 extern "C" int moe_mxfp4_grouped_gemm(int experts, int64_t rows, int n, int k, const uint8_t* xq, const uint8_t* x_scales, const int32_t* offsets,
                                       const uint8_t* wq, const uint8_t* w_scales, uint16_t* y, void* stream) {
   using namespace moe;
-  if (experts < 1 || experts > kMaxExperts || rows < 0 || rows >= (1ll << 31)) return MOE_ERR_SHAPE;
-  if (n < 8 || n % 8 || n > kMaxWidth || k < kMxBlock || k % kMxBlock || k > kMaxWidth) return MOE_ERR_SHAPE;
-  if ((rows / MXR + experts) * ((n + 127) / 128) >= (1ll << 24)) return MOE_ERR_SHAPE;   // (a launch has fewer than 2^32 threads)
-  if (rows == 0) return MOE_OK;
+  const int rc = check_gemm(experts, rows, n, k);
+  if (rc != MOE_OK || rows == 0) return rc;
   MOE_REQUIRE_PTR(xq); MOE_REQUIRE_PTR(x_scales); MOE_REQUIRE_PTR(offsets); MOE_REQUIRE_PTR(wq); MOE_REQUIRE_PTR(w_scales); MOE_REQUIRE_PTR(y);
   MOE_REQUIRE_ALIGNED(xq); MOE_REQUIRE_ALIGNED(x_scales); MOE_REQUIRE_ALIGNED(offsets); MOE_REQUIRE_ALIGNED(wq); MOE_REQUIRE_ALIGNED(w_scales);
   MOE_REQUIRE_ALIGNED(y);

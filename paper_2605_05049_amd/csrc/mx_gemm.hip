@@ -605,13 +605,15 @@ __global__ __launch_bounds__(256, 1) void mx_direct_kernel(const MxGemmArgs A) {
 // rows; small ones elsewhere.  Measured, large to small tiles: 8 experts, 4096 columns, K = 4096, 128 rows 22 to 28 us, 1024 rows 28 to 60, 8192 rows 80 to
 // 451; 64 experts, 2048 columns, K = 1408, 512 rows 23 to 22, 2048 rows (64 tiles) 25 to 26, 8192 rows 33 to 50; 8 experts, 1024 columns, K = 512, 2048 rows
 // 15 to 10, 8192 rows 16 to 19; 1000 experts, 2048 columns, K = 2048, 16 rows 144 to 96 (a block has all of a CU's LDS), 1024 rows 581 to 606.
-// Work is rows times columns (of a pair those of both weights), 2^22 of them: a round of small tiles.  A tile that its columns do not fill pays from 512 k
-// on: 8 experts, 60000 rows of 96 columns, K = 512 11 to 16 us, 1920 22 to 32; 65536 rows of 192, K = 512 16 to 34, 1920 30 to 73; a pair of 64, 50000 rows,
-// K = 512 15 to 19, 1920 28 to 40.  With K = 256 and 320 these are 8.6 to 9.9 and 9.5 to 8.7, 13 to 11 and 15 to 11: there only whole tiles count.  Of 64
-// columns and fewer a tile is mostly empty: 131072 rows of 64, K = 512 24 to 21, 1920 56 to 47.
+// Work is rows times columns (of a pair those of both weights), 2^22 of them: a round of small tiles.  From 512 k on a tile that its columns do not fill
+// pays, too: 8 experts, 60000 rows of 96 columns, K = 512 11 to 16 us, 1920 22 to 32; 65536 rows of 192, K = 512 14 to 31, 1920 27 to 66; a pair of 64, 50000
+// rows, K = 512 15 to 19, 1920 28 to 40.  With K = 256 and 320 the first and the last are 8.6 to 9.9 and 9.5 to 8.7, 13 to 11 and 15 to 11: there only whole tiles
+// count, or three rounds' work of more than 128 columns (65536 rows of 192, 12 to 19 and 12 to 16).  Of 64 columns and fewer a tile is mostly empty: 131072
+// rows of 64, K = 512 24 to 21, 1920 56 to 47.
 static bool mx_large_tiles(MxKind kind, long long rows, int E, int n, int k) {
   const int columns = kind == MX_GATE_UP ? 2 * n : n;
-  const bool fills = k >= 512 ? columns > 64 && rows * columns >= 64ll * MXT * MXT : rows * (columns / MXT) >= 64ll * MXT;
+  const long long work = rows * columns, round = 64ll * MXT * MXT;
+  const bool fills = k >= 512 ? columns > 64 && work >= round : rows * (columns / MXT) >= 64ll * MXT || (columns > 128 && work >= 3 * round);
   return k >= 8 * kMxBlock && (fills || (k >= 2048 && rows >= E / 2));
 }
 

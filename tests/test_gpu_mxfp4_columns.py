@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("rows,n,k", [(45000, 96, 512), (45000, 96, 544), (35000, 120, 640), (22000, 192, 1152), (22000, 200, 736), (17000, 248, 1024),
-                                      (9000, 504, 672)])
+                                      (9000, 504, 672), (66000, 192, 256), (66000, 192, 320)])
 def test_product(moe, rows, n, k):
     assert paper_2605_05049_amd.mxfp4_grouped_gemm_large_tiles(4, rows, n, k)
     rng = np.random.default_rng([rows, n, k])

@@ -8,8 +8,8 @@ import paper_2605_05049_amd as moe
     # work is rows times columns, also where these do not fill a tile of 256
     (8, 65536, 192, 1024, True), (8, 65536, 192, 512, True), (8, 60000, 96, 1920, True), (64, 24000, 200, 1408, True), (8, 17000, 248, 1024, True),
     (8, 16000, 248, 1024, False), (8, 10000, 504, 1024, True), (8, 8000, 504, 1024, False), (1, 33000, 128, 512, True), (1, 32000, 128, 512, False),
-    # ... but from 512 k on
-    (8, 65536, 192, 320, False), (8, 65536, 256, 320, True), (8, 16384, 256, 256, True), (8, 16383, 256, 256, False),
+    # ... from 512 k on; below it whole tiles, or three rounds of small tiles
+    (8, 60000, 192, 320, False), (8, 65536, 192, 320, True), (8, 65536, 192, 256, True), (8, 10 ** 6, 128, 320, False), (8, 65536, 256, 320, True), (8, 16384, 256, 256, True), (8, 16383, 256, 256, False),
     # mostly empty tiles
     (8, 65536, 64, 1024, False), (8, 2 ** 20, 64, 1920, False), (8, 2 ** 20, 8, 1024, False),
     # whole tiles as before: their work alone, or a long contraction

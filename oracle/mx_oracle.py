@@ -7,7 +7,12 @@ import numpy as np
 CODES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 U32 = 2.0 ** -24          # unit roundoff of fp32
 UBF16 = 2.0 ** -8         # ... and of bf16, with its 8 significant bits, doubled: a rounding may start from either side of a tie
-EXP = 2.0 ** -20          # relative error of the sigmoid's exponential and quotient, with room
+EXP = 2.0 ** -20          # relative error of the sigmoid's exponential and quotient for g > -5, with room
+
+
+def silu_error(g):
+    """Relative error of silu(g) in fp32: far below zero that of the exponential, 2^t of a rounded t = -g log2 e (|g| 2^-24, and a quarter of that for log2 e)."""
+    return np.maximum(EXP, (8 - 1.5 * np.minimum(g, 0)) * U32)
 
 
 def scale_codes(blocks):
@@ -74,7 +79,7 @@ def swiglu(x, wg, wu):
     dg, du = n * (np.abs(x) @ np.abs(wg)), n * (np.abs(x) @ np.abs(wu))
     s = g / (1 + np.exp(-np.clip(g, -700, None)))
     h = s * u
-    return h, 1.1 * dg * np.abs(u) + np.abs(s) * du + 1.1 * dg * du + EXP * np.abs(h)
+    return h, 1.1 * dg * np.abs(u) + np.abs(s) * du + 1.1 * dg * du + silu_error(g) * np.abs(h)
 
 
 def quantized_spread(h, dh):

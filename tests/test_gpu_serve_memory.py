@@ -132,3 +132,10 @@ def test_the_smaller_workspace_is_enough(moe, T, d, f, E, k):
     got = moe.layer_mxfp4_forward(small, x, weights, w_router=w_router)
     assert torch.equal(got, want) and torch.equal(small.row_of_slot, full.row_of_slot)
     assert (room[n:] == 0xA5).all()
+
+
+def test_no_tokens(moe):
+    w_router, weights = _weights()
+    for mxfp4 in (False, True):
+        layer = serve.ServedLayer(w_router, *weights, K, ES, mxfp4=mxfp4)
+        assert layer(torch.empty(0, D, dtype=torch.bfloat16, device="cuda")).shape == (0, D)

@@ -28,9 +28,9 @@ constexpr int kFewTokens = MOE_FEW_TOKENS_MAX;
 constexpr int kFewSlots = 4096;       // T * K' at most
 constexpr int kFewWaves = 8;          // wavefronts of a block
 constexpr int kFewFusedSlots = 512, kFewFusedExperts = 256;   // at most, where every block makes the gate for itself
-// Bytes of router weights at most, where it makes the logits too.  Measured, with and without that launch: 8 KB (8 experts, 512 wide), 1 and 16 tokens, 16.4
-// and 20.4 us to 17.8 and 21.9; 28 KB (13 experts, 1088 wide) 23.8 and 48.8 to 25.0 and 47.9, in 4 bits 19.5 and 44.2 to 21.0 and 38.7; 64 KB (32 experts,
-// 1024 wide) 21.1 and 52.3 to 19.8 and 38.3.
+// Bytes of router weights at most, where it makes the logits too.  Measured, the layer with the logits made so and by a launch of their own: 8 KB (8 experts
+// of 512 x 1024), 1 and 16 tokens, 16.5 and 20.0 us to 17.8 and 21.4; 28 KB (13 of 1088 x 1984) 21.7 and 43.0 to 23.0 and 44.0, in 4 bits 18.1 and 34.8 to 19.3
+// and 34.8; 64 KB (32 of 1024 x 1024) 20.7 and 58 to 19.3 and 43.
 constexpr size_t kFewFusedRouter = 16 * 1024;
 constexpr int kFewGroup = 16;         // tokens of an MFMA
 constexpr int kFewTurn = 2 * kFewGroup;   // rows at most that go through the weights together

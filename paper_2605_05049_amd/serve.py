@@ -1,5 +1,6 @@
 """Answering with one MoE layer: the experts' weights are quantised to microscaled 4-bit floating point when the layer is loaded, a prompt goes
-through the grouped 4-bit products, and the tokens that follow go through the layer for a few tokens.
+through the grouped 4-bit products, and the tokens that follow go through the layer for a few tokens.  The grouped products quantise a prompt's rows
+and hidden activations to 4 bits, too; the layer for a few tokens (at most 64) keeps the rows in bf16 and 16 significand bits of the hidden activations.
 
     python -m paper_2605_05049_amd.serve --dims 2048x1408 --experts 64 --top-k 6 --shared 2 --prompt 4096 --batch 1 --steps 64
 
@@ -15,7 +16,9 @@ from .layer import FewTokenBuffers, PromptMemory, layer_few_forward, layer_forwa
 
 class ServedLayer:
     """A layer that only answers: `layer(x)` for x [T, d_model] bf16, any T.  At most FEW_TOKENS_MAX tokens are answered by layer_few_forward,
-    more by the grouped products.  `mxfp4`: the experts' weights are quantised here, and the bf16 ones are not kept.
+    more by the grouped products.  `mxfp4`: the experts' weights are quantised here, and the bf16 ones are not kept; and a call with more than a few tokens
+    quantises its rows and hidden activations to 4 bits on the way (its answers are 30 % off those of bf16, of random weights and rows, where a call
+    with a few tokens, whose rows stay bf16, is 20 % off).  Without it everything is bf16.
 
     The buffers of a few tokens are made for their count at its first call and kept; what a call returns is theirs and is overwritten by the next
     call with as many tokens.  Longer calls share the memory of the longest so far, and each returns a tensor of its own.  Memory that a captured

@@ -82,22 +82,26 @@ class PromptMemory:
         self.streams = set()   # that used the block
 
     def buffers(self, shape) -> MoeLayerBuffers:
+        s = B.Shape.of(shape)
+        key = (s.T, s.d_model, s.d_ffn, s.E, s.k, s.E_shared, s.renorm)
+        buf = self._views.get(key)
+        if buf is not None and buf is self._latest:
+            return buf
         import torch
-        buf = self._views.get(shape.T)
         if buf is None:
             need = _Carved()
-            MoeLayerBuffers(shape, self.device, empty=need, **self._kind)
+            MoeLayerBuffers(s, self.device, empty=need, **self._kind)
             if self.block is None or self.block.numel() < need.at:
                 self._views, self._latest, self.block, self.streams = {}, None, None, set()   # (the old block goes first)
                 self.block = torch.empty(need.at, dtype=torch.uint8, device=self.device)
             elif len(self._views) >= self._VIEWS:
                 self._views = {}
-            buf = self._views[shape.T] = MoeLayerBuffers(shape, self.device, empty=_Carved(self.block), **self._kind)
+            buf = self._views[key] = MoeLayerBuffers(s, self.device, empty=_Carved(self.block), **self._kind)
         if buf is not self._latest:
             if self._latest is not None:
                 self._latest.out = None
             if buf.out is None:
-                buf.out = torch.empty(shape.T, shape.d_model, dtype=torch.bfloat16, device=self.device)
+                buf.out = torch.empty(s.T, s.d_model, dtype=torch.bfloat16, device=self.device)
             self._latest = buf
         return buf
 

@@ -123,3 +123,13 @@ def test_workspace_of_the_forward_on_4_bit_weights():
     many = moe.Shape(4000, 64, 64, 1024, 2)   # the permutation's scratch: 8 x 1024 and 8000 ints
     perm = lambda size: lib.moe_permute(ctypes.byref(many._c), *[fake] * 8, size, None)  # noqa: E731
     assert perm(4 * (8 * 1024 + 8000) - 1) == -4
+
+
+def test_prompt_memory_of_several_shapes():
+    """Shapes with as many tokens have buffers of their own sizes."""
+    memory = moe.PromptMemory("cpu")
+    a, b, c = moe.Shape(100, 128, 192, 8, 2), moe.Shape(100, 256, 64, 4, 3, 1), moe.Shape(100, 128, 192, 8, 2, 0, 0)
+    for s in (a, b, c, a, b):
+        buf = memory.buffers(s)
+        assert buf.out.shape == (100, s.d_model) and buf.x_perm.shape == (s.N, s.d_model) and buf.shape.renorm == s.renorm
+        assert buf.ws.numel() == moe.workspace_bytes(s)

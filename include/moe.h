@@ -119,6 +119,73 @@ int moe_router_route_fwd(const moe_shape* shape, const uint16_t* x, const uint16
 int moe_router_bwd(const moe_shape* shape, const uint16_t* x, const uint16_t* w_router, const float* dlogits,
                    uint16_t* dx_router, float* dw_router, int accumulate, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Routing with scores of another kind, a bias that balances, and groups of experts (Section II-A "learned gating function", in the forms that
+ * layers of many experts use).  For a token with logits l over the E routed experts:
+ *   s_e = softmax(l)_e  or  1 / (1 + exp(-l_e));     c_e = s_e + bias_e, or l_e without a bias (of which s_e is a monotone function)
+ *   the experts are `groups` equal groups of neighbours; a group's score is the sum of its group_best best c (without a bias and with group_best 2:
+ *   of its best s); the groups_kept best groups stay, ties to the lowest group
+ *   topk_idx = the k best c of the groups that stay, in that order, ties to the lowest id
+ *   topk_w_j = scale s_j / sum_i s_i (shape->renorm; the sum over the k chosen), else scale s_j.   Shared slots as in moe_route_topk, weight 1.
+ * An expert whose logit is NaN or at most -1e30 is masked: s = 0, it comes after all others of its group and does not count in the group's score (a
+ * group of masked experts alone comes after all others); so does one whose c is NaN or -infinity.  An infinite logit counts as the largest finite one.
+ * A token without experts gets its lowest ids with weights 0.  Decisions are those of s and c in 64 bits; weights are fp32. */
+#define MOE_SCORES_SOFTMAX 0
+#define MOE_SCORES_SIGMOID 1
+typedef struct {
+  int32_t scores;       /* MOE_SCORES_SOFTMAX or MOE_SCORES_SIGMOID */
+  int32_t groups;       /* divides E; 1: no groups */
+  int32_t groups_kept;  /* 1 .. groups, with k <= groups_kept * E / groups */
+  int32_t group_best;   /* 1 or 2, at most E / groups */
+  float scale;          /* positive and finite */
+} moe_gate;
+
+/*   logits [T,E] fp32 in;  bias [E] fp32 in, may be NULL;  topk_idx [T,K'] int32 out;  topk_w [T,K'] fp32 out. */
+int moe_gate_fwd(const moe_shape* shape, const moe_gate* gate, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w,
+                 void* stream);
+
+/* moe_router_fwd and moe_gate_fwd in one.  Arguments as those of the two calls. */
+int moe_router_gate_fwd(const moe_shape* shape, const moe_gate* gate, const uint16_t* x, const uint16_t* w_router, const float* bias, float* logits,
+                        int32_t* topk_idx, float* topk_w, void* ws, size_t ws_bytes, void* stream);
+
+/* Derivative of the weights with respect to the logits (the choice and the bias are constants), plus, with `counts`, that of the balance loss
+ *   L = balance E / (k T^2) sum_e n_e sum_t q_te,    q_t = s_t / sum_e s_te,    n_e = counts[e], a constant
+ * (balance times the mean share of slots times the mean share of score, summed over the experts, times E; 1 times balance where all are even).
+ *   dtopk_w [T,K'] fp32 in;  logits [T,E] fp32, topk_idx, topk_w [T,K'] in, as read and written by moe_gate_fwd;  counts [E'] int32 in, as of
+ *   moe_permute, may be NULL (balance is then not read);  dlogits [T,E] fp32 out;  loss [1] fp32 out, L: may be NULL, needs counts and 16 KB of
+ *   workspace `ws`, which is not read without it (T = 0: L = 0).
+ * A masked expert's logit has gradient 0; an expert that topk_idx names twice gets the sum.  The loss is summed in a fixed order. */
+int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const float* dtopk_w, const float* logits, const int32_t* topk_idx,
+                 const float* topk_w, const int32_t* counts, float balance, float* dlogits, float* loss, void* ws, size_t ws_bytes, void* stream);
+
+/* A step of the bias that balances: bias[e] += rate where expert e has fewer slots than the mean of the E routed experts, -= rate where it has more.
+ *   counts [E'] int32 in, as of moe_permute (T = 0: no step);  rate >= 0 and finite;  bias [E] fp32 in and out. */
+int moe_gate_bias_step(const moe_shape* shape, const int32_t* counts, float rate, float* bias, void* stream);
+
+/* ---- The norm in front of a layer, with the residual sum in front of it.  For every row:
+ *   h = x + addend (rounded to bf16; without an addend h = x)
+ *   y = (h - mean(h)) rstd gamma + beta,  rstd = 1 / sqrt(mean((h - mean(h))^2) + eps)      (centre != 0: layer norm)
+ *   y = h rstd gamma + beta,              rstd = 1 / sqrt(mean(h^2) + eps)                  (centre == 0: RMS norm)
+ * fp32 between h and y; one bf16 rounding.  As in the calls above, without rows (T = 0) tensors that have no elements may be NULL.
+ *   x [rows, cols] bf16 in;  addend [rows, cols] bf16 in, may be NULL;  gamma, beta [cols] bf16 in, may be NULL (1 and 0)
+ *   sum [rows, cols] bf16 out: h, may be NULL, may be x or addend itself;  y [rows, cols] bf16 out, no other buffer of the call
+ *   mean, rstd [rows] fp32 out, may be NULL (what the backward pass needs; mean only with centre, else it is not touched).
+ * rows from 0 (a no-op) to 2^31 - 1, cols a multiple of 8 up to MOE_NORM_COLS_MAX, eps positive and finite.  The squares' sum is fp32: it has to stay below 3e38. */
+#define MOE_NORM_COLS_MAX 16384
+int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const uint16_t* x, const uint16_t* addend, const uint16_t* gamma, const uint16_t* beta,
+                 uint16_t* sum, uint16_t* y, float* mean, float* rstd, void* stream);
+
+/* Derivative of moe_norm_fwd, with g = dy gamma and xh = (h - mean) rstd:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)) + dx_addend     (without mean(g) where centre == 0), fp32, one bf16 rounding
+ *   dgamma = sum over the rows of dy xh,  dbeta = sum over the rows of dy: fp32, overwritten (accumulate == 0; zeros without rows) or added to
+ *   dy [rows, cols] bf16 in;  h [rows, cols] bf16 in (x, or what the forward call wrote to `sum`);  gamma, mean, rstd as of the forward call
+ *   dx_addend [rows, cols] bf16 in, may be NULL (the gradient that reaches h past the norm);  dx [rows, cols] bf16 out, may be dy or dx_addend itself
+ *   dgamma, dbeta [cols] fp32 out, may be NULL each.
+ * dx is the gradient of x and of addend alike.  Workspace: moe_norm_workspace_bytes(rows, cols) bytes (0 if these are outside the limits).  Sums over
+ * the rows are made in a fixed order. */
+size_t moe_norm_workspace_bytes(int64_t rows, int cols);
+int moe_norm_bwd(int64_t rows, int cols, int centre, const uint16_t* dy, const uint16_t* h, const uint16_t* gamma, const float* mean, const float* rstd,
+                 const uint16_t* dx_addend, uint16_t* dx, float* dgamma, float* dbeta, int accumulate, void* ws, size_t ws_bytes, void* stream);
+
 /* Local pack (the per-GPU half of the dispatch of Section III-B: b*s*k rows of d_model bf16 values grouped by
  * expert).  A stable counting sort of the slots by expert id:
  *   counts[e]      = number of slots routed to e                                   [E']   int32 out

@@ -22,7 +22,10 @@ EXPORTED_SYMBOLS = (
     "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_gemm_large_tiles",
     "moe_mxfp4_grouped_ffn_fwd", "moe_mxfp4_workspace_bytes",
     "moe_layer_few_workspace_bytes", "moe_layer_few_fwd", "moe_layer_few_mxfp4_fwd",
+    "moe_gate_fwd", "moe_router_gate_fwd", "moe_gate_bwd", "moe_gate_bias_step",
+    "moe_norm_fwd", "moe_norm_bwd", "moe_norm_workspace_bytes",
 )
+NORM_COLS_MAX = 16384   # MOE_NORM_COLS_MAX: columns of a moe_norm_* call
 FEW_TOKENS_MAX = 64   # MOE_FEW_TOKENS_MAX: tokens of a moe_layer_few_* call
 
 
@@ -61,6 +64,30 @@ class Shape:
     def of(cls, s) -> "Shape":
         """From any object with the same attribute names (e.g. a workloads.MoEShape)."""
         return s if isinstance(s, Shape) else cls(s.T, s.d_model, s.d_ffn, s.E, s.k, s.E_shared, s.renorm)
+
+
+class _CGate(Structure):
+    _fields_ = [("scores", c_int32), ("groups", c_int32), ("groups_kept", c_int32), ("group_best", c_int32), ("scale", ctypes.c_float)]
+
+
+class Gate:
+    """How a layer routes: scores "softmax" or "sigmoid", the experts in `groups` equal groups of which a token's best `groups_kept` stay (a group's
+    score: the sum of its `group_best` best selection scores), `scale` on the weights.  top-k and renormalisation are the Shape's."""
+
+    _SCORES = ("softmax", "sigmoid")
+
+    def __init__(self, scores="softmax", groups=1, groups_kept=None, group_best=1, scale=1.0):
+        if scores not in self._SCORES:
+            raise ValueError(f"scores {scores!r}: expected one of {self._SCORES}")
+        groups = int(groups)
+        self.scores, self.groups, self.groups_kept = scores, groups, groups if groups_kept is None else int(groups_kept)
+        self.group_best, self.scale = int(group_best), float(scale)
+        self._c = _CGate(self._SCORES.index(scores), groups, self.groups_kept, self.group_best, self.scale)
+
+    def __setattr__(self, name, value):
+        if "_c" in self.__dict__:
+            raise AttributeError("a Gate does not change: make another one")
+        object.__setattr__(self, name, value)
 
 
 def library_path() -> str:
@@ -134,6 +161,15 @@ def load_library():
     sigs["moe_mxfp4_grouped_ffn_fwd"] = [sp] + [V] * 10 + [c_size_t, V]
     sigs["moe_layer_few_fwd"] = [sp] + [V] * 9 + [c_size_t, V]
     sigs["moe_layer_few_mxfp4_fwd"] = [sp] + [V] * 12 + [c_size_t, V]
+    gp, c_float = POINTER(_CGate), ctypes.c_float
+    sigs["moe_gate_fwd"] = [sp, gp, V, V, V, V, V]
+    sigs["moe_router_gate_fwd"] = [sp, gp, V, V, V, V, V, V, V, c_size_t, V]
+    sigs["moe_gate_bwd"] = [sp, gp, V, V, V, V, V, c_float, V, V, V, c_size_t, V]
+    sigs["moe_gate_bias_step"] = [sp, V, c_float, V, V]
+    sigs["moe_norm_fwd"] = [c_int64, c_int, c_int, c_float] + [V] * 9
+    sigs["moe_norm_bwd"] = [c_int64, c_int, c_int] + [V] * 9 + [c_int, V, c_size_t, V]
+    lib.moe_norm_workspace_bytes.restype = c_size_t
+    lib.moe_norm_workspace_bytes.argtypes = [c_int64, c_int]
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.restype = c_int
@@ -563,6 +599,82 @@ def moe_layer_few_mxfp4_fwd(shape, x, w_router, wq_gate, s_gate, wq_up, s_up, wq
         _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _ptr(ws, None, None, "ws"),
         ws.numel() * ws.element_size(), _stream(stream))
     _check("moe_layer_few_mxfp4_fwd", rc)
+
+
+# ---- in front of the experts: routing with scores of another kind, and the norm ------------------------------------
+
+def norm_workspace_bytes(rows, cols) -> int:
+    """Bytes of workspace of moe_norm_bwd (0: sizes outside the limits)."""
+    return int(load_library().moe_norm_workspace_bytes(rows, cols))
+
+
+def _workspace(ws):
+    return (None, 0) if ws is None else (_ptr(ws, None, None, "ws"), ws.numel() * ws.element_size())
+
+
+def moe_gate_fwd(shape, gate, logits, bias, topk_idx, topk_w, stream=None):
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    rc = load_library().moe_gate_fwd(
+        ctypes.byref(s._c), ctypes.byref(gate._c), _ptr(logits, torch.float32, s.T * s.E, "logits"), _ptr(bias, torch.float32, s.E, "bias"),
+        _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _stream(stream))
+    _check("moe_gate_fwd", rc)
+
+
+def moe_router_gate_fwd(shape, gate, x, w_router, bias, logits, topk_idx, topk_w, ws, stream=None):
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    bf = _bf16_types()
+    rc = load_library().moe_router_gate_fwd(
+        ctypes.byref(s._c), ctypes.byref(gate._c), _ptr(x, bf, s.T * s.d_model, "x"), _ptr(w_router, bf, s.E * s.d_model, "w_router"),
+        _ptr(bias, torch.float32, s.E, "bias"), _ptr(logits, torch.float32, s.T * s.E, "logits"), _ptr(topk_idx, torch.int32, s.N, "topk_idx"),
+        _ptr(topk_w, torch.float32, s.N, "topk_w"), *_workspace(ws), _stream(stream))
+    _check("moe_router_gate_fwd", rc)
+
+
+def moe_gate_bwd(shape, gate, dtopk_w, logits, topk_idx, topk_w, counts, balance, dlogits, loss=None, ws=None, stream=None):
+    """counts None: no balance loss.  loss [1] fp32 needs counts and a workspace."""
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    rc = load_library().moe_gate_bwd(
+        ctypes.byref(s._c), ctypes.byref(gate._c), _ptr(dtopk_w, torch.float32, s.N, "dtopk_w"), _ptr(logits, torch.float32, s.T * s.E, "logits"),
+        _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _ptr(counts, torch.int32, s.E_total, "counts"),
+        float(balance), _ptr(dlogits, torch.float32, s.T * s.E, "dlogits"), _ptr(loss, torch.float32, 1, "loss"), *_workspace(ws), _stream(stream))
+    _check("moe_gate_bwd", rc)
+
+
+def moe_gate_bias_step(shape, counts, rate, bias, stream=None):
+    torch = _torch_module or _torch()
+    s = Shape.of(shape)
+    rc = load_library().moe_gate_bias_step(ctypes.byref(s._c), _ptr(counts, torch.int32, s.E_total, "counts"), float(rate),
+                                           _ptr(bias, torch.float32, s.E, "bias"), _stream(stream))
+    _check("moe_gate_bias_step", rc)
+
+
+def moe_norm_fwd(centre, eps, x, addend, gamma, beta, sum, y, mean, rstd, stream=None):
+    """x [..., cols] bf16; addend, gamma, beta, sum, mean and rstd may be None."""
+    torch = _torch_module or _torch()
+    bf = _bf16_types()
+    rows, cols = _last(x, "x")
+    n = rows * cols
+    rc = load_library().moe_norm_fwd(
+        rows, cols, int(bool(centre)), float(eps), _ptr(x, bf, n, "x"), _ptr(addend, bf, n, "addend"), _ptr(gamma, bf, cols, "gamma"),
+        _ptr(beta, bf, cols, "beta"), _ptr(sum, bf, n, "sum"), _ptr(y, bf, n, "y"), _ptr(mean, torch.float32, rows, "mean"),
+        _ptr(rstd, torch.float32, rows, "rstd"), _stream(stream))
+    _check("moe_norm_fwd", rc)
+
+
+def moe_norm_bwd(centre, dy, h, gamma, mean, rstd, dx_addend, dx, dgamma, dbeta, accumulate, ws, stream=None):
+    """dy, h [..., cols] bf16; gamma, dx_addend, dgamma, dbeta and (without centre) mean may be None, ws without dgamma and dbeta."""
+    torch = _torch_module or _torch()
+    bf = _bf16_types()
+    rows, cols = _last(h, "h")
+    n = rows * cols
+    rc = load_library().moe_norm_bwd(
+        rows, cols, int(bool(centre)), _ptr(dy, bf, n, "dy"), _ptr(h, bf, n, "h"), _ptr(gamma, bf, cols, "gamma"),
+        _ptr(mean, torch.float32, rows, "mean"), _ptr(rstd, torch.float32, rows, "rstd"), _ptr(dx_addend, bf, n, "dx_addend"), _ptr(dx, bf, n, "dx"),
+        _ptr(dgamma, torch.float32, cols, "dgamma"), _ptr(dbeta, torch.float32, cols, "dbeta"), int(bool(accumulate)), *_workspace(ws), _stream(stream))
+    _check("moe_norm_bwd", rc)
 
 
 # ---- single-GPU steps of the hierarchical all-to-all (device tensors; rows of any dtype, 16-byte multiples) -----

@@ -127,7 +127,7 @@ int moe_router_bwd(const moe_shape* shape, const uint16_t* x, const uint16_t* w_
  *   topk_idx = the k best c of the groups that stay, in that order, ties to the lowest id
  *   topk_w_j = scale s_j / sum_i s_i (shape->renorm; the sum over the k chosen), else scale s_j.   Shared slots as in moe_route_topk, weight 1.
  * An expert whose logit is NaN or at most -1e30 is masked: s = 0, it comes after all others of its group and does not count in the group's score (a
- * group of masked experts alone comes after all others); so does one whose c is NaN or -infinity.  An infinite logit counts as the largest finite one.
+ * group of masked experts alone comes after all others); one whose c is NaN or at most -1e30 comes last in the same way.  An infinite logit counts as the largest finite one.
  * A token without experts gets its lowest ids with weights 0.  Decisions are those of s and c in 64 bits; weights are fp32. */
 #define MOE_SCORES_SOFTMAX 0
 #define MOE_SCORES_SIGMOID 1

@@ -49,7 +49,7 @@ def gate_fwd(logits, bias, k, scores, groups=1, kept=1, best=1, renorm=True, sca
         l, masked, s = _scores(logits[t], scores)
         with np.errstate(invalid="ignore"):
             c = l if bias is None else s + bias.astype(np.float64)
-        c = np.where(masked | np.isnan(c), -np.inf, c)
+        c = np.where(masked | ~(c > np.float32(MASKED)), -np.inf, c)
         of = s if bias is None and best == 2 else c
         rating = []
         for g in range(groups):

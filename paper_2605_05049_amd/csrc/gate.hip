@@ -7,6 +7,8 @@
 // Decisions (which groups, which experts, in which order) are those of scores in 64 bits; the weights are fp32.
 #include "common.h"
 
+#include <type_traits>
+
 namespace moe {
 
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
@@ -22,42 +24,43 @@ struct GateArgs {
 __device__ __forceinline__ bool gate_masked(float l) { return !(l > kMaskedLogit); }
 __device__ __forceinline__ float gate_finite(float l) { return l > kMaxLogit ? kMaxLogit : l; }   // (NaN stays)
 
-template <int W>
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, W);
-  return v;
+// v of another lane: 1, 2 and, where the lanes of a quad (of eight) hold the same, 4 and 8 further on by moves inside the rows of 16, else through LDS.
+template <int STEP>
+__device__ __forceinline__ int from_lane(int v) {
+  if constexpr (STEP == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);         // quad_perm 1 0 3 2
+  else if constexpr (STEP == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);    // quad_perm 2 3 0 1
+  else if constexpr (STEP == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);   // row_half_mirror
+  else if constexpr (STEP == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);   // row_mirror
+  else return __shfl_xor(v, STEP, kWave);
 }
-template <int W>
+template <int STEP>
+__device__ __forceinline__ float from_lane(float v) { return __int_as_float(from_lane<STEP>(__float_as_int(v))); }
+template <int STEP>
+__device__ __forceinline__ double from_lane(double v) { return __hiloint2double(from_lane<STEP>(__double2hiint(v)), from_lane<STEP>(__double2loint(v))); }
+
+// Over W neighbouring lanes, for each of them.
+template <int W, int STEP = 1, typename T>
+__device__ __forceinline__ T lanes_sum(T v) {
+  if constexpr (STEP < W) return lanes_sum<W, 2 * STEP>(v + from_lane<STEP>(v));
+  else return v;
+}
+template <int W, int STEP = 1>
 __device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, W));
-  return v;
-}
-__device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
+  if constexpr (STEP < W) return lanes_max<W, 2 * STEP>(fmaxf(v, from_lane<STEP>(v)));
+  else return v;
 }
 
 // sigmoid(l) / sigmoid-like factor exp(top) with top = min(0, the largest logit that is looked at): scores far below zero keep their ratios.
 __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f / (expf(top - l) + expf(top)); }
 
-// Any number of groups and experts, any k: a wavefront per token, lane g holds experts g, g + 64, ..., everything in 64 bits.  k rounds of finding
-// the best one left.
+// A token's choices in 64 bits by a wavefront: any number of groups and experts, any k.  Lane g holds experts g, g + 64, ...; k rounds of finding the best
+// one left.  Choice j comes back on lane j % 64 in held[j / 64].  row_c: LDS of E + groups doubles.
 template <int PER>
-__global__ __launch_bounds__(256) void gate_general_kernel(const float* __restrict__ logits, const float* __restrict__ bias,
-                                                           int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, GateArgs A) {
-  __shared__ double row_c[4][PER * kWave];    // c of every expert, for the groups' scores
-  __shared__ double group_c[4][PER * kWave];  // the groups' scores
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int t = blockIdx.x * 4 + wave;
-  if (t >= A.T) return;   // (whole wavefronts; no barrier below)
-  const int E = A.E, k = A.k, Kp = k + A.Es;
+__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* row_c, int (&held)[PER], const GateArgs& A) {
+  const int lane = threadIdx.x % kWave, E = A.E;
   const double NEG = -__builtin_inf();
-  const float* row = logits + (size_t)t * E;
-  float l[PER];
-  float m = -kMaxLogit;
+  const bool by_logits = bias == nullptr, need_scores = !by_logits || A.group_best > 1;
+  float l[PER], m = -kMaxLogit;
 #pragma unroll
   for (int p = 0; p < PER; p++) {
     const int e = lane + p * kWave;
@@ -65,12 +68,10 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
     if (!gate_masked(l[p])) m = fmaxf(m, l[p]);
   }
   m = lanes_max<kWave>(m);
-  const bool by_logits = bias == nullptr, need_scores = !by_logits || A.group_best > 1 || (!A.sigmoid && !A.renorm);
-  double s[PER];
+  double s[PER], z = 0.0;
 #pragma unroll
   for (int p = 0; p < PER; p++) s[p] = 0.0;
   if (need_scores) {
-    double z = 0.0;
 #pragma unroll
     for (int p = 0; p < PER; p++)
       if (!gate_masked(l[p])) {
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
         z += s[p];
       }
     if (!A.sigmoid) {
-      z = wave_sum_f64(z);
+      z = lanes_sum<kWave>(z);
 #pragma unroll
       for (int p = 0; p < PER; p++)
         if (!gate_masked(l[p])) s[p] /= z;
@@ -91,26 +92,27 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
     const int e = lane + p * kWave;
     taken[p] = e >= E;
     c[p] = NEG;
-    if (e < E && !gate_masked(l[p])) {
+    if (!gate_masked(l[p])) {
       const double b = by_logits ? (double)l[p] : s[p] + (double)bias[e];
-      c[p] = b == b ? b : NEG;
+      if (b > (double)kMaskedLogit) c[p] = b;
     }
   }
   if (A.groups > 1) {
     const int S = E / A.groups;
     const bool by_score = by_logits && A.group_best > 1;   // (a sum of logits would say nothing)
+    double* group_c = row_c + E;
 #pragma unroll
     for (int p = 0; p < PER; p++)
-      if (lane + p * kWave < E) row_c[wave][lane + p * kWave] = by_score && c[p] != NEG ? s[p] : c[p];
+      if (lane + p * kWave < E) row_c[lane + p * kWave] = by_score && c[p] != NEG ? s[p] : c[p];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     for (int g = lane; g < A.groups; g += kWave) {
       double first = NEG, second = NEG;
       for (int i = 0; i < S; i++) {
-        const double v = row_c[wave][g * S + i];
+        const double v = row_c[g * S + i];
         second = fmax(second, fmin(first, v));
         first = fmax(first, v);
       }
-      group_c[wave][g] = A.group_best > 1 && second != NEG ? first + second : first;
+      group_c[g] = A.group_best > 1 && second != NEG ? first + second : first;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -118,21 +120,20 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
       const int e = lane + p * kWave;
       if (e < E) {
         const int g = e / S;
-        const double v = group_c[wave][g];
+        const double v = group_c[g];
         int better = 0;
         for (int o = 0; o < A.groups; o++) {
-          const double u = group_c[wave][o];
+          const double u = group_c[o];
           better += u > v || (u == v && o < g);
         }
         if (better >= A.groups_kept) taken[p] = true;
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (before the next token's)
   }
-  // selection j stays on lane j % 64, slot j / 64, until all are known
-  int held[PER];
 #pragma unroll
   for (int p = 0; p < PER; p++) held[p] = 0;
-  for (int j = 0; j < k; j++) {
+  for (int j = 0; j < A.k; j++) {
     double bv = NEG;
     int bi = 0x7fffffff;
 #pragma unroll
@@ -150,6 +151,34 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
       if (lane == j % kWave && p == j / kWave) held[p] = bi;
     }
   }
+}
+
+// Any number of groups and experts, any k: a wavefront per token.
+template <int PER>
+__global__ __launch_bounds__(256) void gate_general_kernel(const float* __restrict__ logits, const float* __restrict__ bias,
+                                                           int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, GateArgs A) {
+  __shared__ double row_c[4][2 * PER * kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int t = blockIdx.x * 4 + wave;
+  if (t >= A.T) return;   // (whole wavefronts; no barrier below)
+  const int E = A.E, k = A.k, Kp = k + A.Es;
+  const float* row = logits + (size_t)t * E;
+  int held[PER];
+  choose_exactly<PER>(row, bias, row_c[wave], held, A);
+  float m = -kMaxLogit, all = 0.f;
+  if (!A.sigmoid && !A.renorm) {
+    float l[PER];
+#pragma unroll
+    for (int p = 0; p < PER; p++) {
+      l[p] = lane + p * kWave < E ? gate_finite(row[lane + p * kWave]) : -__builtin_inff();
+      if (!gate_masked(l[p])) m = fmaxf(m, l[p]);
+    }
+    m = lanes_max<kWave>(m);
+#pragma unroll
+    for (int p = 0; p < PER; p++)
+      if (!gate_masked(l[p])) all += expf(l[p] - m);
+    all = lanes_sum<kWave>(all);
+  }
   // the weights: over the largest chosen logit where they are renormalised (scores far below zero keep their ratios)
   float top = -kMaxLogit, chosen[PER], w[PER], sum = 0.f;
 #pragma unroll
@@ -163,13 +192,7 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
     if (A.sigmoid) top = fminf(top, 0.f);
   } else {
     top = A.sigmoid ? 0.f : m;
-    if (!A.sigmoid) {
-      z = 0.f;
-#pragma unroll
-      for (int p = 0; p < PER; p++)
-        if (!gate_masked(l[p])) z += expf(l[p] - m);
-      z = lanes_sum<kWave>(z);
-    }
+    if (!A.sigmoid) z = all;
   }
 #pragma unroll
   for (int p = 0; p < PER; p++) {
@@ -190,6 +213,300 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
     topk_idx[(size_t)t * Kp + k + j] = E + j;
     topk_w[(size_t)t * Kp + k + j] = 1.0f;
   }
+}
+
+// ---- k <= 16, groups <= 64: W lanes per token, each with a run of neighbouring experts of one group.
+//
+// A value to select by (c, or l) is a key: a double whose high word is the fp32 value and whose low word its expert, so that one comparison orders by
+// value and then by the lower id, keys are never equal, and a maximum and a minimum (an instruction each) exchange two of them.  A lane sorts its
+// experts' keys, K at a time, by a network and keeps the K best; two lists of K join by K maxima (of one and the other backwards) and a merging
+// network, first in the lane, then lane by lane in log2 W steps, at the end of which all lanes have the token's K best.  When a list is a group's, its
+// first two give the group's score, and the lists of groups that do not stay are emptied.  256 experts, top-8: about 1000 instructions for 8 tokens;
+// k rounds of finding the best one left take 9 times that.
+// The logits come in through LDS: a wavefront's tokens lie next to each other in memory whatever E is.
+//
+// fp32 orders two values right if they are further apart than twice what either may be off.  Where a choice or its order hangs on less, which adjacent
+// keys, the first one left out and the groups next to the cut tell, the wavefront makes its choices again in 64 bits.
+
+constexpr float kDeadKey = -3.0e38f;   // masked experts: after all others
+constexpr float kNoKey = -3.3e38f;     // of groups that do not stay, and behind the last expert
+
+__device__ __forceinline__ double make_key(float v, int e) {   // (of negative values the larger low word is the smaller number)
+  const int bits = __float_as_int(v + 0.0f);
+  return __hiloint2double(bits, ~e ^ (bits >> 31));
+}
+__device__ __forceinline__ float key_value(double key) { return __int_as_float(__double2hiint(key)); }
+__device__ __forceinline__ int key_expert(double key) { return ~(__double2loint(key) ^ (__double2hiint(key) >> 31)); }
+
+// The instructions themselves: fmax and fmin first rewrite each operand that could be a signalling NaN, and no key is a NaN.
+__device__ __forceinline__ double key_max(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ double key_min(double a, double b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ void exchange(double& a, double& b) {
+  const double hi = key_max(a, b);
+  b = key_min(a, b);
+  a = hi;
+}
+// Falling order (Batcher's odd-even merge sort: 19 exchanges for 8, 63 for 16).
+template <int K>
+__device__ __forceinline__ void sort_keys(double (&a)[K]) {
+#pragma unroll
+  for (int p = 1; p < K; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < K; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; i++)
+          if (i + j + q < K && (i + j) / (2 * p) == (i + j + q) / (2 * p)) exchange(a[i + j], a[i + j + q]);
+}
+// a: the K best of a and b, both falling.
+template <int K>
+__device__ __forceinline__ void join_keys(double (&a)[K], const double (&b)[K]) {
+#pragma unroll
+  for (int i = 0; i < K; i++) a[i] = key_max(a[i], b[K - 1 - i]);
+#pragma unroll
+  for (int q = K / 2; q >= 1; q /= 2)
+#pragma unroll
+    for (int i = 0; i < K; i++)
+      if (!(i & q)) exchange(a[i], a[i + q]);
+}
+
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// Where the i-th float of a wavefront's logits lies in LDS: 4 floats after every 32 keep the lanes' runs off each other's banks.
+__device__ __forceinline__ int gate_place(int i) { return i + ((i >> 5) << 2); }
+
+struct GatePlan {   // how a token's experts lie on its lanes
+  int lanes_of_group;   // a power of two
+  int piece;            // experts of a lane at most
+};
+
+template <int K, int W, int PER>
+__global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ logits, const float* __restrict__ bias, int32_t* __restrict__ topk_idx,
+                                                   float* __restrict__ topk_w, GateArgs A, GatePlan P) {
+  static_assert(K <= W && PER % K == 0 && PER <= 32, "a choice for each of the first K lanes, a bit for each expert of a lane");
+  constexpr int TOKENS = kWave / W;
+  constexpr int MAX_E = W * PER < kMaxExperts ? W * PER : kMaxExperts;
+  constexpr int ROW_FLOATS = TOKENS * MAX_E + TOKENS * MAX_E / 8 + 8;   // (gate_place)
+  constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave);                     // what choose_exactly takes of them
+  __shared__ __attribute__((aligned(16))) float rows[4][ROW_FLOATS > EXACT_FLOATS ? ROW_FLOATS : EXACT_FLOATS];
+  __shared__ float group_scores[4][kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane % W, tt = lane / W;
+  const int t0 = (blockIdx.x * 4 + wave) * TOKENS, t = t0 + tt;
+  if (t0 >= A.T) return;   // (whole wavefronts; no barrier below)
+  const int E = A.E, k = A.k, Kp = k + A.Es;
+
+  // the tokens' logits into LDS (t0 E is a multiple of 4 but for two tokens of odd E)
+  const int n = min(TOKENS, A.T - t0) * E;
+  const float* src = logits + (size_t)t0 * E;
+  if (TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) {
+    for (int i = 4 * lane; i + 3 < n; i += 4 * kWave) *reinterpret_cast<float4*>(&rows[wave][gate_place(i)]) = *reinterpret_cast<const float4*>(src + i);
+    if (lane < (n & 3)) rows[wave][gate_place((n & ~3) + lane)] = src[(n & ~3) + lane];
+  } else {
+    for (int i = lane; i < n; i += kWave) rows[wave][gate_place(i)] = src[i];
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+
+  const int size = E / A.groups;
+  const int group = g / P.lanes_of_group;
+  const int begin = (g % P.lanes_of_group) * P.piece;
+  const int first = group * size + begin, count = group < A.groups && t < A.T ? max(0, min(P.piece, size - begin)) : 0;
+  // runs of whole fours are read as such (size, piece and E are the same for all lanes); no read leaves the LDS or the bias: the last one is read again
+  float l[PER], b[PER];
+  const bool by_logits = bias == nullptr;
+  const int at = tt * E + min(first, E - 1);
+  if (((E | size | P.piece) & 3) == 0) {
+#pragma unroll
+    for (int p = 0; p < PER; p += 4) {
+      const int o = min(p, max(count - 4, 0));
+      const float4 v = *reinterpret_cast<const float4*>(&rows[wave][gate_place((at & ~3) + o)]);
+      l[p] = v.x; l[p + 1] = v.y; l[p + 2] = v.z; l[p + 3] = v.w;
+      if (!by_logits) {
+        const float4 u = *reinterpret_cast<const float4*>(bias + min(first, E - 4) + o);
+        b[p] = u.x; b[p + 1] = u.y; b[p + 2] = u.z; b[p + 3] = u.w;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < PER; p++) {
+      const int o = min(p, max(count - 1, 0));
+      l[p] = rows[wave][gate_place(at + o)];
+      if (!by_logits) b[p] = bias[min(first, E - 1) + o];
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PER; p++) l[p] = p < count ? gate_finite(l[p]) : -__builtin_inff();
+
+  const bool softmax_sum = !A.sigmoid && (!by_logits || !A.renorm);
+  float m = -kMaxLogit, inv_z = 1.f;
+  if (!A.sigmoid) {
+#pragma unroll
+    for (int p = 0; p < PER; p++) m = fmaxf(m, gate_masked(l[p]) ? -kMaxLogit : l[p]);
+    m = lanes_max<W>(m);
+  }
+  float v[PER];   // what is selected by
+  if (softmax_sum) {
+    float z = 0.f;
+#pragma unroll
+    for (int p = 0; p < PER; p++) {
+      v[p] = gate_masked(l[p]) ? 0.f : fast_exp(l[p] - m);
+      z += v[p];
+    }
+    z = lanes_sum<W>(z);
+    inv_z = z > 0.f ? 1.0f / z : 0.f;
+  }
+  if (by_logits) {
+#pragma unroll
+    for (int p = 0; p < PER; p++) v[p] = p >= count ? kNoKey : gate_masked(l[p]) ? kDeadKey : l[p];
+  } else {
+#pragma unroll
+    for (int p = 0; p < PER; p++) {
+      const float s = A.sigmoid ? __builtin_amdgcn_rcpf(1.0f + fast_exp(-l[p])) : v[p] * inv_z;
+      const float c = s + b[p];
+      v[p] = p >= count ? kNoKey : gate_masked(l[p]) || !(c > kMaskedLogit) ? kDeadKey : c;
+    }
+  }
+  // How far c may be off.  sigmoid: the exponential's argument 1.5 |l| 2^-24 times s (1 - s) <= 0.23 / |l|, exponential and reciprocal 2^-23 each, the
+  // sum 2^-24: under 2^-22.  softmax: of s, 27 2^-23 for the sum of the exponentials (their mean argument is under 7, 40 additions) and 5 2^-23 for
+  // its own: under 2^-18.  And a rounding of c.  Twice that, for both of a pair.
+  const float slack = by_logits ? 0.f : A.sigmoid ? 0x1p-21f : 0x1p-17f * inv_z, slack_c = 0x1p-22f;
+
+  const bool track = !by_logits && k == K;   // (else the first one left out is in the list, or order needs no margin)
+  float lost = kNoKey;                       // the best that joining lists has let go
+  auto join = [&](double (&a)[K], const double (&b)[K]) __attribute__((always_inline)) {
+    if (track) {
+#pragma unroll
+      for (int i = 0; i < K; i++) lost = fmaxf(lost, fminf(key_value(a[i]), key_value(b[K - 1 - i])));
+    }
+    join_keys<K>(a, b);
+  };
+  double best[K];
+#pragma unroll
+  for (int b = 0; b < PER / K; b++) {
+    double more[K];
+#pragma unroll
+    for (int i = 0; i < K; i++) more[i] = make_key(v[b * K + i], first + b * K + i);
+    sort_keys<K>(more);
+    if (b == 0) {
+#pragma unroll
+      for (int i = 0; i < K; i++) best[i] = more[i];
+    } else {
+      join(best, more);
+    }
+  }
+  bool unsure = false;
+
+  auto select_groups = [&]() __attribute__((always_inline)) {
+    const float a = key_value(best[0]), b = key_value(best[1]);
+    float score = -__builtin_inff();
+    if (a > kMaskedLogit) {
+      score = a;
+      if (A.group_best > 1) {
+        const bool two = b > kMaskedLogit;
+        if (!by_logits) score = two ? a + b : a;
+        else if (A.sigmoid) score = __builtin_amdgcn_rcpf(1.0f + fast_exp(-a)) + (two ? __builtin_amdgcn_rcpf(1.0f + fast_exp(-b)) : 0.f);
+        else score = fast_exp(a - m) + (two ? fast_exp(b - m) : 0.f);   // (over the sum that all groups share)
+      }
+    }
+    float* scores = group_scores[wave];
+    scores[lane] = score;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    int better = 0;
+    for (int o = 0; o < A.groups; o++) {
+      const float u = scores[lane - g + o * P.lanes_of_group];
+      better += u > score || (u == score && o < group);
+    }
+    const bool exists = group < A.groups, stays = exists && better < A.groups_kept;
+    if (!by_logits || A.group_best > 1) {
+      const float low = -lanes_max<W>(stays ? -score : -__builtin_inff()), high = lanes_max<W>(exists && !stays ? score : -__builtin_inff());
+      // (two c, a rounding of their sum; of scores without the shared sum, each at most 1, the arguments count)
+      const float far = by_logits ? 0x1p-18f : 2.0f * slack + 0x1p-20f * fmaxf(1.0f, fabsf(low));
+      unsure = unsure || low - high <= far;
+    }
+    if (!stays) {
+#pragma unroll
+      for (int i = 0; i < K; i++) best[i] = make_key(kNoKey, 0);
+      lost = kNoKey;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  auto join_lanes = [&](auto step_c) __attribute__((always_inline)) {
+    constexpr int STEP = decltype(step_c)::value;
+    if constexpr (STEP < W) {
+      if (A.groups > 1 && STEP == P.lanes_of_group) select_groups();
+      double other[K];
+#pragma unroll
+      for (int i = 0; i < K; i++) other[i] = from_lane<STEP>(best[i]);
+      if (track) lost = fmaxf(lost, from_lane<STEP>(lost));
+      join(best, other);
+    }
+  };
+  join_lanes(std::integral_constant<int, 1>{});
+  join_lanes(std::integral_constant<int, 2>{});
+  join_lanes(std::integral_constant<int, 4>{});
+  join_lanes(std::integral_constant<int, 8>{});
+  join_lanes(std::integral_constant<int, 16>{});
+  join_lanes(std::integral_constant<int, 32>{});
+  if (A.groups > 1 && P.lanes_of_group == W) select_groups();
+
+  // lane g takes choice g
+  double mine = best[0], next = best[1];
+#pragma unroll
+  for (int i = 1; i < K; i++) {
+    mine = g == i ? best[i] : mine;
+    if (i + 1 < K) next = g == i ? best[i + 1] : next;
+  }
+  int choice = key_expert(mine);
+  if (!by_logits) {
+    const float a = key_value(mine), b = g == K - 1 ? lost : key_value(next);
+    unsure = unsure || (g < k && b > kMaskedLogit && a - b <= slack + slack_c * fmaxf(1.0f, fabsf(a)));
+  }
+  const bool live = t < A.T && g < k;
+  float x = live ? rows[wave][gate_place(tt * E + choice)] : -__builtin_inff();
+  unsigned long long again = __ballot(unsure && t < A.T);
+  if (again) {   // (the logits in LDS make room)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    do {
+      const int token = __builtin_ctzll(again) / W;
+      int held[(MAX_E + kWave - 1) / kWave];
+      choose_exactly<(MAX_E + kWave - 1) / kWave>(logits + (size_t)(t0 + token) * E, bias, reinterpret_cast<double*>(rows[wave]), held, A);
+      const int found = __shfl(held[0], g, kWave);
+      if (tt == token) choice = found;
+      again &= ~((W == kWave ? ~0ull : (1ull << (W & 63)) - 1) << (token * W));
+    } while (again);
+    if (live) x = logits[(size_t)t * E + choice];
+  }
+
+  // the weights: over the largest chosen logit where they are renormalised (scores far below zero keep their ratios)
+  x = gate_finite(x);
+  const bool dead = gate_masked(x);
+  float w = 0.f, factor = A.scale;
+  if (A.renorm) {
+    float top = lanes_max<K>(dead ? -kMaxLogit : x);
+    if (A.sigmoid) top = fminf(top, 0.f);
+    w = dead ? 0.f : A.sigmoid ? sigmoid_over(x, top) : expf(x - top);
+    const float z = lanes_sum<K>(w);
+    factor = z > 0.f ? A.scale / z : 0.f;
+  } else {
+    w = dead ? 0.f : A.sigmoid ? sigmoid_over(x, 0.f) : expf(x - m) * inv_z;
+  }
+  if (live) {
+    topk_idx[(size_t)t * Kp + g] = choice;
+    topk_w[(size_t)t * Kp + g] = w * factor;
+  }
+  if (t < A.T)
+    for (int j = g; j < A.Es; j += W) {
+      topk_idx[(size_t)t * Kp + k + j] = E + j;
+      topk_w[(size_t)t * Kp + k + j] = 1.0f;
+    }
 }
 
 // Gradient of the weights and of the balance loss.  A wavefront per token, lane g holds experts g, g + 64, ...; with q = s / sum s, n_e the slots
@@ -319,7 +636,50 @@ static int gate_checks(const moe_shape* shape, const moe_gate* gate, Dims* D, Ga
   return MOE_OK;
 }
 
+// W lanes per token (0: the general kernel): as few as hold its groups, and its experts 32 each.
+static int gate_lanes(const GateArgs& A, GatePlan* P) {
+  if (A.k > 16 || A.groups > kWave) return 0;
+  int padded = 1;   // groups, filled up to a power of two
+  while (padded < A.groups) padded *= 2;
+  const int size = A.E / A.groups;
+  for (int W = A.k > 8 ? 16 : 8; W <= kWave; W *= 2) {
+    if (padded > W) continue;
+    const int lanes = W / padded, piece = (size + lanes - 1) / lanes;
+    if (piece > 32) continue;
+    *P = GatePlan{lanes, piece};
+    return W;
+  }
+  return 0;
+}
+
+template <int K, int W, int PER>
+static void launch_gate_kernel(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
+  constexpr int TOKENS = 4 * kWave / W;
+  MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER>), dim3((A.T + TOKENS - 1) / TOKENS), dim3(256), 0, st, logits, bias, topk_idx, topk_w, A, P);
+}
+template <int K, int W>
+static void launch_gate_lanes(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
+  if (K == 8 && P.piece <= 8) launch_gate_kernel<K, W, K>(st, A, P, logits, bias, topk_idx, topk_w);
+  else if (P.piece <= 16) launch_gate_kernel<K, W, 16>(st, A, P, logits, bias, topk_idx, topk_w);
+  else launch_gate_kernel<K, W, 32>(st, A, P, logits, bias, topk_idx, topk_w);
+}
+
 static void launch_gate(hipStream_t st, const GateArgs& A, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
+  GatePlan P;
+  const int W = gate_lanes(A, &P);
+  if (W && A.k <= 8) {
+    if (W == 8) launch_gate_lanes<8, 8>(st, A, P, logits, bias, topk_idx, topk_w);
+    else if (W == 16) launch_gate_lanes<8, 16>(st, A, P, logits, bias, topk_idx, topk_w);
+    else if (W == 32) launch_gate_lanes<8, 32>(st, A, P, logits, bias, topk_idx, topk_w);
+    else launch_gate_lanes<8, 64>(st, A, P, logits, bias, topk_idx, topk_w);
+    return;
+  }
+  if (W) {
+    if (W == 16) launch_gate_lanes<16, 16>(st, A, P, logits, bias, topk_idx, topk_w);
+    else if (W == 32) launch_gate_lanes<16, 32>(st, A, P, logits, bias, topk_idx, topk_w);
+    else launch_gate_lanes<16, 64>(st, A, P, logits, bias, topk_idx, topk_w);
+    return;
+  }
   const dim3 grid((A.T + 3) / 4), block(256);
 #define MOE_LAUNCH_GATE(PER) MOE_LAUNCH("gate_general", st, (gate_general_kernel<PER>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A)
   if (A.E <= 64) MOE_LAUNCH_GATE(1);

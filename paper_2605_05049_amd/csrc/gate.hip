@@ -31,7 +31,17 @@ __device__ __forceinline__ int from_lane(int v) {
   else if constexpr (STEP == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);    // quad_perm 2 3 0 1
   else if constexpr (STEP == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);   // row_half_mirror
   else if constexpr (STEP == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);   // row_mirror
-  else return __shfl_xor(v, STEP, kWave);
+  else {
+    static_assert(STEP == 16 || STEP == 32, "a power of two below 64");
+    const bool upper = (threadIdx.x & STEP) != 0;   // (rows, or halves, change places between two registers that hold the same)
+    if constexpr (STEP == 16) {
+      const auto r = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+      return upper ? r[0] : r[1];
+    } else {
+      const auto r = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
+      return upper ? r[0] : r[1];
+    }
+  }
 }
 template <int STEP>
 __device__ __forceinline__ float from_lane(float v) { return __int_as_float(from_lane<STEP>(__float_as_int(v))); }
@@ -44,9 +54,11 @@ __device__ __forceinline__ T lanes_sum(T v) {
   if constexpr (STEP < W) return lanes_sum<W, 2 * STEP>(v + from_lane<STEP>(v));
   else return v;
 }
-template <int W, int STEP = 1>
-__device__ __forceinline__ float lanes_max(float v) {
-  if constexpr (STEP < W) return lanes_max<W, 2 * STEP>(fmaxf(v, from_lane<STEP>(v)));
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+template <int W, int STEP = 1, typename T>
+__device__ __forceinline__ T lanes_max(T v) {
+  if constexpr (STEP < W) return lanes_max<W, 2 * STEP>(larger(v, from_lane<STEP>(v)));
   else return v;
 }
 
@@ -107,6 +119,7 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     for (int g = lane; g < A.groups; g += kWave) {
       double first = NEG, second = NEG;
+#pragma unroll 4
       for (int i = 0; i < S; i++) {
         const double v = row_c[g * S + i];
         second = fmax(second, fmin(first, v));
@@ -133,21 +146,24 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
   }
 #pragma unroll
   for (int p = 0; p < PER; p++) held[p] = 0;
+  // (masked experts of groups that stay are still there when all others are taken: below them the ones that are not to be chosen)
+  constexpr double LEAST = -1.7e308;
+#pragma unroll
+  for (int p = 0; p < PER; p++) c[p] = taken[p] ? NEG : c[p] == NEG ? LEAST : c[p];
   for (int j = 0; j < A.k; j++) {
-    double bv = NEG;
-    int bi = 0x7fffffff;
+    double bv = c[0];
 #pragma unroll
-    for (int p = 0; p < PER; p++)
-      if (!taken[p] && (c[p] > bv || (c[p] == bv && lane + p * kWave < bi))) { bv = c[p]; bi = lane + p * kWave; }
+    for (int p = 1; p < PER; p++) bv = fmax(bv, c[p]);
+    bv = lanes_max<kWave>(bv);
+    int bi = 0;
 #pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-      const double ov = __shfl_xor(bv, o, kWave);
-      const int oi = __shfl_xor(bi, o, kWave);
-      if (ov > bv || (ov == bv && oi < bi)) { bv = ov; bi = oi; }
+    for (int p = PER - 1; p >= 0; p--) {   // (of equal values the lowest expert: the last to be written)
+      const unsigned long long at = __ballot(c[p] == bv);
+      if (at != 0) bi = p * kWave + __builtin_ctzll(at);
     }
 #pragma unroll
     for (int p = 0; p < PER; p++) {
-      if (lane + p * kWave == bi) taken[p] = true;
+      if (lane + p * kWave == bi) c[p] = NEG;
       if (lane == j % kWave && p == j / kWave) held[p] = bi;
     }
   }
@@ -281,21 +297,23 @@ __device__ __forceinline__ void join_keys(double (&a)[K], const double (&b)[K]) 
 
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-// Where the i-th float of a wavefront's logits lies in LDS: 4 floats after every 32 keep the lanes' runs off each other's banks.
-__device__ __forceinline__ int gate_place(int i) { return i + ((i >> 5) << 2); }
-
-struct GatePlan {   // how a token's experts lie on its lanes
-  int lanes_of_group;   // a power of two
-  int piece;            // experts of a lane at most
+struct GatePlan {        // how a token's experts lie on its lanes
+  int lanes_of_group;    // a power of two
+  int piece;             // experts of a lane at most
+  int run, pad;          // of a wavefront's logits in LDS, `pad` floats are left free after every `run`, which keeps the lanes off each other's banks
+  unsigned inverse_run;  // 2^32 / run, rounded up
 };
+// Where the i-th float of a wavefront's logits lies in LDS.
+__device__ __forceinline__ int gate_place(int i, const GatePlan& P) { return i + P.pad * (int)__umulhi((unsigned)i, P.inverse_run); }
 
-template <int K, int W, int PER>
+// FULL: every lane has `piece` experts, a multiple of 4, and so a run of its own.
+template <int K, int W, int PER, bool FULL>
 __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ logits, const float* __restrict__ bias, int32_t* __restrict__ topk_idx,
                                                    float* __restrict__ topk_w, GateArgs A, GatePlan P) {
   static_assert(K <= W && PER % K == 0 && PER <= 32, "a choice for each of the first K lanes, a bit for each expert of a lane");
   constexpr int TOKENS = kWave / W;
   constexpr int MAX_E = W * PER < kMaxExperts ? W * PER : kMaxExperts;
-  constexpr int ROW_FLOATS = TOKENS * MAX_E + TOKENS * MAX_E / 8 + 8;   // (gate_place)
+  constexpr int ROW_FLOATS = kWave * (PER + 4) + PER;                   // (gate_place; the last lane reads on behind its run)
   constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave);                     // what choose_exactly takes of them
   __shared__ __attribute__((aligned(16))) float rows[4][ROW_FLOATS > EXACT_FLOATS ? ROW_FLOATS : EXACT_FLOATS];
   __shared__ float group_scores[4][kWave];
@@ -308,10 +326,10 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const int n = min(TOKENS, A.T - t0) * E;
   const float* src = logits + (size_t)t0 * E;
   if (TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) {
-    for (int i = 4 * lane; i + 3 < n; i += 4 * kWave) *reinterpret_cast<float4*>(&rows[wave][gate_place(i)]) = *reinterpret_cast<const float4*>(src + i);
-    if (lane < (n & 3)) rows[wave][gate_place((n & ~3) + lane)] = src[(n & ~3) + lane];
+    for (int i = 4 * lane; i + 3 < n; i += 4 * kWave) *reinterpret_cast<float4*>(&rows[wave][gate_place(i, P)]) = *reinterpret_cast<const float4*>(src + i);
+    if (lane < (n & 3)) rows[wave][gate_place((n & ~3) + lane, P)] = src[(n & ~3) + lane];
   } else {
-    for (int i = lane; i < n; i += kWave) rows[wave][gate_place(i)] = src[i];
+    for (int i = lane; i < n; i += kWave) rows[wave][gate_place(i, P)] = src[i];
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
@@ -319,60 +337,80 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const int group = g / P.lanes_of_group;
   const int begin = (g % P.lanes_of_group) * P.piece;
   const int first = group * size + begin, count = group < A.groups && t < A.T ? max(0, min(P.piece, size - begin)) : 0;
-  // runs of whole fours are read as such (size, piece and E are the same for all lanes); no read leaves the LDS or the bias: the last one is read again
-  float l[PER], b[PER];
+  float l[PER], c[PER];
   const bool by_logits = bias == nullptr;
-  const int at = tt * E + min(first, E - 1);
-  if (((E | size | P.piece) & 3) == 0) {
+  // (of a lane without a group: the last one's; its keys are behind all others by their ids, or its group does not stay)
+  if constexpr (FULL) {
+    const int from = min(first, E - P.piece);
+    const float* run = &rows[wave][gate_place(tt * E + from, P)];
 #pragma unroll
     for (int p = 0; p < PER; p += 4) {
-      const int o = min(p, max(count - 4, 0));
-      const float4 v = *reinterpret_cast<const float4*>(&rows[wave][gate_place((at & ~3) + o)]);
-      l[p] = v.x; l[p + 1] = v.y; l[p + 2] = v.z; l[p + 3] = v.w;
-      if (!by_logits) {
-        const float4 u = *reinterpret_cast<const float4*>(bias + min(first, E - 4) + o);
-        b[p] = u.x; b[p + 1] = u.y; b[p + 2] = u.z; b[p + 3] = u.w;
+      const float4 u = *reinterpret_cast<const float4*>(run + p);
+      l[p] = u.x; l[p + 1] = u.y; l[p + 2] = u.z; l[p + 3] = u.w;
+    }
+    if (!by_logits) {
+#pragma unroll
+      for (int p = 0; p < PER; p += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(bias + from + (p < P.piece ? p : 0));
+        c[p] = u.x; c[p + 1] = u.y; c[p + 2] = u.z; c[p + 3] = u.w;
       }
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < PER; p++) {
-      const int o = min(p, max(count - 1, 0));
-      l[p] = rows[wave][gate_place(at + o)];
-      if (!by_logits) b[p] = bias[min(first, E - 1) + o];
+    for (int p = 0; p < PER; p++) l[p] = rows[wave][gate_place(tt * E + min(first + min(p, max(count - 1, 0)), E - 1), P)];
+    if (!by_logits) {
+#pragma unroll
+      for (int p = 0; p < PER; p++) c[p] = bias[min(first + min(p, max(count - 1, 0)), E - 1)];
     }
   }
+  if (FULL ? P.piece < PER : true) {
 #pragma unroll
-  for (int p = 0; p < PER; p++) l[p] = p < count ? gate_finite(l[p]) : -__builtin_inff();
-
-  const bool softmax_sum = !A.sigmoid && (!by_logits || !A.renorm);
+    for (int p = 0; p < PER; p++) l[p] = p < (FULL ? P.piece : count) ? l[p] : -__builtin_inff();
+  }
+  const float lowest = group < A.groups ? kMaskedLogit : __builtin_inff();   // (nothing of a lane without a group counts)
+  // what is selected by, in c.  (Functions are evaluated for all, then chosen from: no branch for an element.)
   float m = -kMaxLogit, inv_z = 1.f;
-  if (!A.sigmoid) {
-#pragma unroll
-    for (int p = 0; p < PER; p++) m = fmaxf(m, gate_masked(l[p]) ? -kMaxLogit : l[p]);
-    m = lanes_max<W>(m);
-  }
-  float v[PER];   // what is selected by
-  if (softmax_sum) {
-    float z = 0.f;
+  if (A.sigmoid && !by_logits) {
 #pragma unroll
     for (int p = 0; p < PER; p++) {
-      v[p] = gate_masked(l[p]) ? 0.f : fast_exp(l[p] - m);
-      z += v[p];
+      const float v = __builtin_amdgcn_rcpf(1.0f + fast_exp(-l[p])) + c[p];
+      c[p] = l[p] > kMaskedLogit ? v : kDeadKey;
     }
-    z = lanes_sum<W>(z);
-    inv_z = z > 0.f ? 1.0f / z : 0.f;
-  }
-  if (by_logits) {
-#pragma unroll
-    for (int p = 0; p < PER; p++) v[p] = p >= count ? kNoKey : gate_masked(l[p]) ? kDeadKey : l[p];
   } else {
 #pragma unroll
     for (int p = 0; p < PER; p++) {
-      const float s = A.sigmoid ? __builtin_amdgcn_rcpf(1.0f + fast_exp(-l[p])) : v[p] * inv_z;
-      const float c = s + b[p];
-      v[p] = p >= count ? kNoKey : gate_masked(l[p]) || !(c > kMaskedLogit) ? kDeadKey : c;
+      const float finite = fminf(l[p], kMaxLogit);
+      l[p] = l[p] > lowest ? finite : -__builtin_inff();   // (and NaN)
     }
+    if (!A.sigmoid && !(by_logits && A.renorm && A.group_best == 1)) {
+#pragma unroll
+      for (int p = 0; p < PER; p++) m = fmaxf(m, l[p]);
+      m = lanes_max<W>(m);
+    }
+    if (by_logits) {
+#pragma unroll
+      for (int p = 0; p < PER; p++) c[p] = l[p];
+    }
+    if (!A.sigmoid && !(by_logits && A.renorm)) {
+      float z = 0.f;
+#pragma unroll
+      for (int p = 0; p < PER; p++) z += fast_exp(l[p] - m);
+      z = lanes_sum<W>(z);
+      inv_z = z > 0.f ? 1.0f / z : 0.f;
+      if (!by_logits) {
+#pragma unroll
+        for (int p = 0; p < PER; p++) {
+          const float v = fmaf(fast_exp(l[p] - m), inv_z, c[p]);
+          c[p] = l[p] > kMaskedLogit ? v : kDeadKey;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PER; p++) c[p] = c[p] > kMaskedLogit ? c[p] : kDeadKey;
+  if (FULL ? P.piece < PER : true) {
+#pragma unroll
+    for (int p = 0; p < PER; p++) c[p] = p < (FULL ? P.piece : count) ? c[p] : kNoKey;
   }
   // How far c may be off.  sigmoid: the exponential's argument 1.5 |l| 2^-24 times s (1 - s) <= 0.23 / |l|, exponential and reciprocal 2^-23 each, the
   // sum 2^-24: under 2^-22.  softmax: of s, 27 2^-23 for the sum of the exponentials (their mean argument is under 7, 40 additions) and 5 2^-23 for
@@ -393,7 +431,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   for (int b = 0; b < PER / K; b++) {
     double more[K];
 #pragma unroll
-    for (int i = 0; i < K; i++) more[i] = make_key(v[b * K + i], first + b * K + i);
+    for (int i = 0; i < K; i++) more[i] = make_key(c[b * K + i], first + b * K + i);
     sort_keys<K>(more);
     if (b == 0) {
 #pragma unroll
@@ -431,11 +469,10 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       const float far = by_logits ? 0x1p-18f : 2.0f * slack + 0x1p-20f * fmaxf(1.0f, fabsf(low));
       unsure = unsure || low - high <= far;
     }
-    if (!stays) {
+    const double none = make_key(kNoKey, 0);
 #pragma unroll
-      for (int i = 0; i < K; i++) best[i] = make_key(kNoKey, 0);
-      lost = kNoKey;
-    }
+    for (int i = 0; i < K; i++) best[i] = stays ? best[i] : none;
+    lost = stays ? lost : kNoKey;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   auto join_lanes = [&](auto step_c) __attribute__((always_inline)) {
@@ -470,7 +507,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     unsure = unsure || (g < k && b > kMaskedLogit && a - b <= slack + slack_c * fmaxf(1.0f, fabsf(a)));
   }
   const bool live = t < A.T && g < k;
-  float x = live ? rows[wave][gate_place(tt * E + choice)] : -__builtin_inff();
+  float x = live ? rows[wave][gate_place(tt * E + choice, P)] : -__builtin_inff();
   unsigned long long again = __ballot(unsure && t < A.T);
   if (again) {   // (the logits in LDS make room)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -646,7 +683,8 @@ static int gate_lanes(const GateArgs& A, GatePlan* P) {
     if (padded > W) continue;
     const int lanes = W / padded, piece = (size + lanes - 1) / lanes;
     if (piece > 32) continue;
-    *P = GatePlan{lanes, piece};
+    const int run = piece % 4 == 0 && piece * lanes == size ? piece : 32, pad = run / 4 % 2 ? 8 : 4;   // (run + pad is an odd number of fours)
+    *P = GatePlan{lanes, piece, run, pad, (unsigned)(((1ull << 32) + run - 1) / run)};
     return W;
   }
   return 0;
@@ -655,7 +693,10 @@ static int gate_lanes(const GateArgs& A, GatePlan* P) {
 template <int K, int W, int PER>
 static void launch_gate_kernel(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
   constexpr int TOKENS = 4 * kWave / W;
-  MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER>), dim3((A.T + TOKENS - 1) / TOKENS), dim3(256), 0, st, logits, bias, topk_idx, topk_w, A, P);
+  const dim3 grid((A.T + TOKENS - 1) / TOKENS), block(256);
+  const bool full = P.piece % 4 == 0 && P.piece * P.lanes_of_group * A.groups == A.E;
+  if (full) MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, true>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
+  else MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, false>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
 }
 template <int K, int W>
 static void launch_gate_lanes(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {

@@ -247,12 +247,13 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
 constexpr float kDeadKey = -3.0e38f;   // masked experts: after all others
 constexpr float kNoKey = -3.3e38f;     // of groups that do not stay, and behind the last expert
 
-__device__ __forceinline__ double make_key(float v, int e) {   // (of negative values the larger low word is the smaller number)
-  const int bits = __float_as_int(v + 0.0f);
-  return __hiloint2double(bits, ~e ^ (bits >> 31));
+// signs: the low word goes by the sign of the value.
+__device__ __forceinline__ double make_key(float v, int e, bool signs) {
+  const int bits = __float_as_int(v);
+  return __hiloint2double(bits, ~e ^ (signs ? bits >> 31 : 0));
 }
 __device__ __forceinline__ float key_value(double key) { return __int_as_float(__double2hiint(key)); }
-__device__ __forceinline__ int key_expert(double key) { return ~(__double2loint(key) ^ (__double2hiint(key) >> 31)); }
+__device__ __forceinline__ int key_expert(double key, bool signs) { return ~(__double2loint(key) ^ (signs ? __double2hiint(key) >> 31 : 0)); }
 
 // The instructions themselves: fmax and fmin first rewrite each operand that could be a signalling NaN, and no key is a NaN.
 __device__ __forceinline__ double key_max(double a, double b) {
@@ -263,6 +264,14 @@ __device__ __forceinline__ double key_max(double a, double b) {
 __device__ __forceinline__ double key_min(double a, double b) {
   double r;
   asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+// The largest of `a` and the smaller ones of two pairs.
+__device__ __forceinline__ float max_of_mins(float a, float b0, float b1, float c0, float c1) {
+  float b, c, r;
+  asm("v_min_f32 %0, %1, %2" : "=v"(b) : "v"(b0), "v"(b1));
+  asm("v_min_f32 %0, %1, %2" : "=v"(c) : "v"(c0), "v"(c1));
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
 }
 __device__ __forceinline__ void exchange(double& a, double& b) {
@@ -300,36 +309,55 @@ __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp
 struct GatePlan {        // how a token's experts lie on its lanes
   int lanes_of_group;    // a power of two
   int piece;             // experts of a lane at most
-  int run, pad;          // of a wavefront's logits in LDS, `pad` floats are left free after every `run`, which keeps the lanes off each other's banks
-  unsigned inverse_run;  // 2^32 / run, rounded up
 };
-// Where the i-th float of a wavefront's logits lies in LDS.
-__device__ __forceinline__ int gate_place(int i, const GatePlan& P) { return i + P.pad * (int)__umulhi((unsigned)i, P.inverse_run); }
+// Where the i-th float of a wavefront's logits lies in LDS: 4 floats are left free after every RUN, which keeps the lanes off each other's banks.
+template <int RUN>
+__device__ __forceinline__ int gate_place(int i) { return i + 4 * (i / RUN); }
 
-// FULL: every lane has `piece` experts, a multiple of 4, and so a run of its own.
+// FULL: every lane has PER experts, and so a run of its own.
 template <int K, int W, int PER, bool FULL>
 __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ logits, const float* __restrict__ bias, int32_t* __restrict__ topk_idx,
                                                    float* __restrict__ topk_w, GateArgs A, GatePlan P) {
   static_assert(K <= W && PER % K == 0 && PER <= 32, "a choice for each of the first K lanes, a bit for each expert of a lane");
   constexpr int TOKENS = kWave / W;
   constexpr int MAX_E = W * PER < kMaxExperts ? W * PER : kMaxExperts;
+  constexpr int RUN = FULL ? PER : 32;
   constexpr int ROW_FLOATS = kWave * (PER + 4) + PER;                   // (gate_place; the last lane reads on behind its run)
   constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave);                     // what choose_exactly takes of them
   __shared__ __attribute__((aligned(16))) float rows[4][ROW_FLOATS > EXACT_FLOATS ? ROW_FLOATS : EXACT_FLOATS];
-  __shared__ float group_scores[4][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane % W, tt = lane / W;
+  __shared__ double group_scores[4][kWave];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane % W, tt = lane / W;
   const int t0 = (blockIdx.x * 4 + wave) * TOKENS, t = t0 + tt;
-  if (t0 >= A.T) return;   // (whole wavefronts; no barrier below)
   const int E = A.E, k = A.k, Kp = k + A.Es;
+  const bool by_logits = bias == nullptr;
+  // The bias into LDS, laid out as a token's logits: read from memory by every wavefront, the few lines of it are what all of them wait for
+  __shared__ __attribute__((aligned(16))) float biases[MAX_E + 4 * MAX_E / RUN + 40];
+  __shared__ int dead_bias;
+  if (!by_logits) {
+    if (threadIdx.x == 0) dead_bias = 0;
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += 256) {
+      const float b = bias[e];
+      biases[gate_place<RUN>(e)] = b;
+      if (!(b > kMaskedLogit)) dead_bias = 1;
+    }
+    __syncthreads();
+  }
+  if (t0 >= A.T) return;   // (whole wavefronts; no barrier below)
 
   // the tokens' logits into LDS (t0 E is a multiple of 4 but for two tokens of odd E)
   const int n = min(TOKENS, A.T - t0) * E;
   const float* src = logits + (size_t)t0 * E;
-  if (TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) {
-    for (int i = 4 * lane; i + 3 < n; i += 4 * kWave) *reinterpret_cast<float4*>(&rows[wave][gate_place(i, P)]) = *reinterpret_cast<const float4*>(src + i);
-    if (lane < (n & 3)) rows[wave][gate_place((n & ~3) + lane, P)] = src[(n & ~3) + lane];
+  // (all requested before the first one is waited for)
+  if ((TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) && n >= 4) {
+    float4 in[PER / 4];
+#pragma unroll
+    for (int j = 0; j < PER / 4; j++) in[j] = *reinterpret_cast<const float4*>(src + min(4 * (lane + kWave * j), (n - 4) & ~3));
+#pragma unroll
+    for (int j = 0; j < PER / 4; j++) *reinterpret_cast<float4*>(&rows[wave][gate_place<RUN>(4 * (lane + kWave * j))]) = in[j];   // (what lies behind n is not read)
+    if (lane < (n & 3)) rows[wave][gate_place<RUN>((n & ~3) + lane)] = src[(n & ~3) + lane];
   } else {
-    for (int i = lane; i < n; i += kWave) rows[wave][gate_place(i, P)] = src[i];
+    for (int i = lane; i < n; i += kWave) rows[wave][gate_place<RUN>(i)] = src[i];
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
@@ -338,43 +366,52 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const int begin = (g % P.lanes_of_group) * P.piece;
   const int first = group * size + begin, count = group < A.groups && t < A.T ? max(0, min(P.piece, size - begin)) : 0;
   float l[PER], c[PER];
-  const bool by_logits = bias == nullptr;
   // (of a lane without a group: the last one's; its keys are behind all others by their ids, or its group does not stay)
   if constexpr (FULL) {
-    const int from = min(first, E - P.piece);
-    const float* run = &rows[wave][gate_place(tt * E + from, P)];
+    const int from = min(first, E - PER);
+    const float* run = &rows[wave][gate_place<RUN>(tt * E + from)];
 #pragma unroll
     for (int p = 0; p < PER; p += 4) {
       const float4 u = *reinterpret_cast<const float4*>(run + p);
       l[p] = u.x; l[p + 1] = u.y; l[p + 2] = u.z; l[p + 3] = u.w;
     }
-    if (!by_logits) {
-#pragma unroll
-      for (int p = 0; p < PER; p += 4) {
-        const float4 u = *reinterpret_cast<const float4*>(bias + from + (p < P.piece ? p : 0));
-        c[p] = u.x; c[p + 1] = u.y; c[p + 2] = u.z; c[p + 3] = u.w;
-      }
-    }
   } else {
 #pragma unroll
-    for (int p = 0; p < PER; p++) l[p] = rows[wave][gate_place(tt * E + min(first + min(p, max(count - 1, 0)), E - 1), P)];
-    if (!by_logits) {
+    for (int p = 0; p < PER; p++) l[p] = rows[wave][gate_place<RUN>(tt * E + min(first, E - 1) + p)];
 #pragma unroll
-      for (int p = 0; p < PER; p++) c[p] = bias[min(first + min(p, max(count - 1, 0)), E - 1)];
+    for (int p = 0; p < PER; p++) l[p] = p < count ? l[p] : -__builtin_inff();
+  }
+  const float* bias_run = &biases[FULL && !by_logits ? gate_place<RUN>(min(first, E - PER)) : 0];
+  auto bias_of = [&](int p, float (&b)[4]) __attribute__((always_inline)) {   // of a lane's experts p .. p + 3
+    if constexpr (FULL) {
+      const float4 u = *reinterpret_cast<const float4*>(bias_run + p);
+      b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; i++) b[i] = biases[gate_place<RUN>(min(first, E - 1) + p + i)];
     }
-  }
-  if (FULL ? P.piece < PER : true) {
-#pragma unroll
-    for (int p = 0; p < PER; p++) l[p] = p < (FULL ? P.piece : count) ? l[p] : -__builtin_inff();
-  }
+  };
+  bool some_dead = !by_logits && dead_bias != 0;   // a key of the wavefront may be one
   const float lowest = group < A.groups ? kMaskedLogit : __builtin_inff();   // (nothing of a lane without a group counts)
   // what is selected by, in c.  (Functions are evaluated for all, then chosen from: no branch for an element.)
   float m = -kMaxLogit, inv_z = 1.f;
   if (A.sigmoid && !by_logits) {
+    unsigned top_bits = 0;   // of the exponentials: infinite or NaN where one is masked (or a score too small to be told from that)
 #pragma unroll
-    for (int p = 0; p < PER; p++) {
-      const float v = __builtin_amdgcn_rcpf(1.0f + fast_exp(-l[p])) + c[p];
-      c[p] = l[p] > kMaskedLogit ? v : kDeadKey;
+    for (int p = 0; p < PER; p += 4) {
+      float b[4];
+      bias_of(p, b);
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const float e = fast_exp(-l[p + i]);
+        top_bits = max(top_bits, __float_as_uint(e));
+        c[p + i] = __builtin_amdgcn_rcpf(1.0f + e) + b[i];
+      }
+    }
+    some_dead = some_dead || top_bits >= 0x7f800000u;
+    if (__any(some_dead)) {
+#pragma unroll
+      for (int p = 0; p < PER; p++) c[p] = l[p] > kMaskedLogit ? c[p] : kDeadKey;
     }
   } else {
 #pragma unroll
@@ -382,6 +419,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       const float finite = fminf(l[p], kMaxLogit);
       l[p] = l[p] > lowest ? finite : -__builtin_inff();   // (and NaN)
     }
+    some_dead = true;
     if (!A.sigmoid && !(by_logits && A.renorm && A.group_best == 1)) {
 #pragma unroll
       for (int p = 0; p < PER; p++) m = fmaxf(m, l[p]);
@@ -389,7 +427,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     }
     if (by_logits) {
 #pragma unroll
-      for (int p = 0; p < PER; p++) c[p] = l[p];
+      for (int p = 0; p < PER; p++) c[p] = l[p] + 0.0f;   // (-0 is 0)
     }
     if (!A.sigmoid && !(by_logits && A.renorm)) {
       float z = 0.f;
@@ -399,18 +437,26 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       inv_z = z > 0.f ? 1.0f / z : 0.f;
       if (!by_logits) {
 #pragma unroll
-        for (int p = 0; p < PER; p++) {
-          const float v = fmaf(fast_exp(l[p] - m), inv_z, c[p]);
-          c[p] = l[p] > kMaskedLogit ? v : kDeadKey;
+        for (int p = 0; p < PER; p += 4) {
+          float b[4];
+          bias_of(p, b);
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            const float v = fmaf(fast_exp(l[p + i] - m), inv_z, b[i]);
+            c[p + i] = l[p + i] > kMaskedLogit ? v : kDeadKey;
+          }
         }
       }
     }
   }
+  some_dead = __any(some_dead);
+  if (some_dead) {
 #pragma unroll
-  for (int p = 0; p < PER; p++) c[p] = c[p] > kMaskedLogit ? c[p] : kDeadKey;
-  if (FULL ? P.piece < PER : true) {
+    for (int p = 0; p < PER; p++) c[p] = c[p] > kMaskedLogit ? c[p] : kDeadKey;
+  }
+  if constexpr (!FULL) {
 #pragma unroll
-    for (int p = 0; p < PER; p++) c[p] = p < (FULL ? P.piece : count) ? c[p] : kNoKey;
+    for (int p = 0; p < PER; p++) c[p] = p < count ? c[p] : kNoKey;
   }
   // How far c may be off.  sigmoid: the exponential's argument 1.5 |l| 2^-24 times s (1 - s) <= 0.23 / |l|, exponential and reciprocal 2^-23 each, the
   // sum 2^-24: under 2^-22.  softmax: of s, 27 2^-23 for the sum of the exponentials (their mean argument is under 7, 40 additions) and 5 2^-23 for
@@ -418,33 +464,40 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const float slack = by_logits ? 0.f : A.sigmoid ? 0x1p-21f : 0x1p-17f * inv_z, slack_c = 0x1p-22f;
 
   const bool track = !by_logits && k == K;   // (else the first one left out is in the list, or order needs no margin)
+  // Up to a few lanes' experts stay: one lane may well have all choices.  With more, what a lane lets go matters in 4 (1/4)^K of the tokens.
+  const bool track_lane = track && A.groups_kept * P.lanes_of_group < 4;
   float lost = kNoKey;                       // the best that joining lists has let go
-  auto join = [&](double (&a)[K], const double (&b)[K]) __attribute__((always_inline)) {
-    if (track) {
+  auto let_go = [&](const double (&a)[K], const double (&b)[K]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < K; i++) lost = fmaxf(lost, fminf(key_value(a[i]), key_value(b[K - 1 - i])));
-    }
-    join_keys<K>(a, b);
+    for (int i = 0; i < K; i += 2) lost = max_of_mins(lost, key_value(a[i]), key_value(b[K - 1 - i]), key_value(a[i + 1]), key_value(b[K - 2 - i]));
   };
+  // Of negative values the larger low word is the smaller number.  Where c is selected by, equal values are told apart in 64 bits, but for dead ones.
+  const bool signs = by_logits || some_dead || !FULL;
   double best[K];
 #pragma unroll
   for (int b = 0; b < PER / K; b++) {
     double more[K];
 #pragma unroll
-    for (int i = 0; i < K; i++) more[i] = make_key(c[b * K + i], first + b * K + i);
+    for (int i = 0; i < K; i++) more[i] = make_key(c[b * K + i], first + b * K + i, false);
+    if (signs) {
+#pragma unroll
+      for (int i = 0; i < K; i++) more[i] = make_key(c[b * K + i], first + b * K + i, true);
+    }
     sort_keys<K>(more);
     if (b == 0) {
 #pragma unroll
       for (int i = 0; i < K; i++) best[i] = more[i];
     } else {
-      join(best, more);
+      if (track_lane) let_go(best, more);
+      join_keys<K>(best, more);
     }
   }
+  float lane_last = PER > K && track && !track_lane ? key_value(best[K - 1]) : kNoKey;   // (nothing that the lane has let go is above it)
   bool unsure = false;
 
   auto select_groups = [&]() __attribute__((always_inline)) {
     const float a = key_value(best[0]), b = key_value(best[1]);
-    float score = -__builtin_inff();
+    float score = kDeadKey;
     if (a > kMaskedLogit) {
       score = a;
       if (A.group_best > 1) {
@@ -454,25 +507,26 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
         else score = fast_exp(a - m) + (two ? fast_exp(b - m) : 0.f);   // (over the sum that all groups share)
       }
     }
-    float* scores = group_scores[wave];
-    scores[lane] = score;
+    // (a key of the score and the group: equal ones go by the group, those without living experts below all others)
+    const double mark = __hiloint2double(__float_as_int(score), score < 0.f ? group : ~group);
+    double* marks = group_scores[wave];
+    marks[lane] = mark;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     int better = 0;
-    for (int o = 0; o < A.groups; o++) {
-      const float u = scores[lane - g + o * P.lanes_of_group];
-      better += u > score || (u == score && o < group);
-    }
+#pragma unroll 4
+    for (int o = 0; o < A.groups; o++) better += marks[lane - g + o * P.lanes_of_group] > mark;
     const bool exists = group < A.groups, stays = exists && better < A.groups_kept;
     if (!by_logits || A.group_best > 1) {
       const float low = -lanes_max<W>(stays ? -score : -__builtin_inff()), high = lanes_max<W>(exists && !stays ? score : -__builtin_inff());
       // (two c, a rounding of their sum; of scores without the shared sum, each at most 1, the arguments count)
       const float far = by_logits ? 0x1p-18f : 2.0f * slack + 0x1p-20f * fmaxf(1.0f, fabsf(low));
-      unsure = unsure || low - high <= far;
+      unsure = unsure || (high > kMaskedLogit && low - high <= far);
     }
-    const double none = make_key(kNoKey, 0);
+    const double none = make_key(kNoKey, 0, false);
 #pragma unroll
     for (int i = 0; i < K; i++) best[i] = stays ? best[i] : none;
     lost = stays ? lost : kNoKey;
+    lane_last = stays ? lane_last : kNoKey;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   auto join_lanes = [&](auto step_c) __attribute__((always_inline)) {
@@ -482,8 +536,11 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       double other[K];
 #pragma unroll
       for (int i = 0; i < K; i++) other[i] = from_lane<STEP>(best[i]);
-      if (track) lost = fmaxf(lost, from_lane<STEP>(lost));
-      join(best, other);
+      if (track) {
+        lost = fmaxf(lost, from_lane<STEP>(lost));
+        let_go(best, other);
+      }
+      join_keys<K>(best, other);
     }
   };
   join_lanes(std::integral_constant<int, 1>{});
@@ -495,19 +552,19 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   if (A.groups > 1 && P.lanes_of_group == W) select_groups();
 
   // lane g takes choice g
-  double mine = best[0], next = best[1];
+  double mine = best[0];
 #pragma unroll
-  for (int i = 1; i < K; i++) {
-    mine = g == i ? best[i] : mine;
-    if (i + 1 < K) next = g == i ? best[i + 1] : next;
-  }
-  int choice = key_expert(mine);
+  for (int i = 1; i < K; i++) mine = g == i ? best[i] : mine;
+  int choice = key_expert(mine, signs);
   if (!by_logits) {
-    const float a = key_value(mine), b = g == K - 1 ? lost : key_value(next);
+    const float a = key_value(mine);
+    const float after = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(a), 0x101, 0xF, 0xF, true));   // row_shl:1: the next lane's
+    const float b = g == K - 1 ? lost : after;
     unsure = unsure || (g < k && b > kMaskedLogit && a - b <= slack + slack_c * fmaxf(1.0f, fabsf(a)));
+    unsure = unsure || (lane_last > kMaskedLogit && lane_last >= key_value(best[K - 1]));
   }
   const bool live = t < A.T && g < k;
-  float x = live ? rows[wave][gate_place(tt * E + choice, P)] : -__builtin_inff();
+  float x = live ? rows[wave][gate_place<RUN>(tt * E + choice)] : -__builtin_inff();
   unsigned long long again = __ballot(unsure && t < A.T);
   if (again) {   // (the logits in LDS make room)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -529,11 +586,14 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   if (A.renorm) {
     float top = lanes_max<K>(dead ? -kMaxLogit : x);
     if (A.sigmoid) top = fminf(top, 0.f);
-    w = dead ? 0.f : A.sigmoid ? sigmoid_over(x, top) : expf(x - top);
+    w = fast_exp(x - top);
+    if (A.sigmoid) w = __builtin_amdgcn_rcpf(fast_exp(top - x) + fast_exp(top));
+    w = dead ? 0.f : w;
     const float z = lanes_sum<K>(w);
-    factor = z > 0.f ? A.scale / z : 0.f;
+    factor = z > 0.f ? A.scale * __builtin_amdgcn_rcpf(z) : 0.f;
   } else {
-    w = dead ? 0.f : A.sigmoid ? sigmoid_over(x, 0.f) : expf(x - m) * inv_z;
+    w = A.sigmoid ? __builtin_amdgcn_rcpf(fast_exp(-x) + 1.0f) : fast_exp(x - m) * inv_z;
+    w = dead ? 0.f : w;
   }
   if (live) {
     topk_idx[(size_t)t * Kp + g] = choice;
@@ -683,8 +743,7 @@ static int gate_lanes(const GateArgs& A, GatePlan* P) {
     if (padded > W) continue;
     const int lanes = W / padded, piece = (size + lanes - 1) / lanes;
     if (piece > 32) continue;
-    const int run = piece % 4 == 0 && piece * lanes == size ? piece : 32, pad = run / 4 % 2 ? 8 : 4;   // (run + pad is an odd number of fours)
-    *P = GatePlan{lanes, piece, run, pad, (unsigned)(((1ull << 32) + run - 1) / run)};
+    *P = GatePlan{lanes, piece};
     return W;
   }
   return 0;
@@ -694,7 +753,7 @@ template <int K, int W, int PER>
 static void launch_gate_kernel(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
   constexpr int TOKENS = 4 * kWave / W;
   const dim3 grid((A.T + TOKENS - 1) / TOKENS), block(256);
-  const bool full = P.piece % 4 == 0 && P.piece * P.lanes_of_group * A.groups == A.E;
+  const bool full = P.piece == PER && PER * P.lanes_of_group * A.groups == A.E;
   if (full) MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, true>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
   else MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, false>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
 }

@@ -151,7 +151,7 @@ int moe_router_gate_fwd(const moe_shape* shape, const moe_gate* gate, const uint
  *   L = balance E / (k T^2) sum_e n_e sum_t q_te,    q_t = s_t / sum_e s_te,    n_e = counts[e], a constant
  * (balance times the mean share of slots times the mean share of score, summed over the experts, times E; 1 times balance where all are even).
  *   dtopk_w [T,K'] fp32 in;  logits [T,E] fp32, topk_idx, topk_w [T,K'] in, as read and written by moe_gate_fwd;  counts [E'] int32 in, as of
- *   moe_permute, may be NULL (balance is then not read);  dlogits [T,E] fp32 out;  loss [1] fp32 out, L: may be NULL, needs counts and 16 KB of
+ *   moe_permute, may be NULL (balance is then not read);  dlogits [T,E] fp32 out;  loss [1] fp32 out, L: may be NULL, needs counts and 4 KB of
  *   workspace `ws`, which is not read without it (T = 0: L = 0).
  * A masked expert's logit has gradient 0; an expert that topk_idx names twice gets the sum.  The loss is summed in a fixed order. */
 int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const float* dtopk_w, const float* logits, const int32_t* topk_idx,

@@ -13,7 +13,7 @@ namespace moe {
 
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
 constexpr float kMaxLogit = 3.402823466e38f;
-constexpr int kGateBwdBlocks = 4096;      // at most; each adds up its tokens' share of the loss
+constexpr int kGateBwdBlocks = 1024;      // at most; each adds up its tokens' share of the loss
 
 struct GateArgs {
   int T, E, k, Es, renorm;
@@ -312,7 +312,7 @@ struct GatePlan {        // how a token's experts lie on its lanes
 };
 // Where the i-th float of a wavefront's logits lies in LDS: 4 floats are left free after every RUN, which keeps the lanes off each other's banks.
 template <int RUN>
-__device__ __forceinline__ int gate_place(int i) { return i + 4 * (i / RUN); }
+__device__ __forceinline__ int gate_place(int i) { return i + 4 * (int)((unsigned)i / RUN); }
 
 // FULL: every lane has PER experts, and so a run of its own.
 template <int K, int W, int PER, bool FULL>
@@ -606,99 +606,178 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     }
 }
 
-// Gradient of the weights and of the balance loss.  A wavefront per token, lane g holds experts g, g + 64, ...; with q = s / sum s, n_e the slots
-// of expert e, C_e = balance E n_e / (k T^2):
+// Gradient of the weights and of the balance loss.  With q = s / sum s, n_e the slots of expert e, C_e = balance E n_e / (k T^2):
 //   softmax  dl_m = q_m (C_m - <q, C>) [- s_m <w, dw> where not renormalised] + d_j of the slots with expert m
 //   sigmoid  dl_m = (1 - s_m) (q_m (C_m - <q, C>) + d_j)
 //   d_j = w_j (dw_j - <w, dw> / scale) where renormalised, else w_j dw_j
-template <int PER>
-__global__ __launch_bounds__(256) void gate_bwd_kernel(const float* __restrict__ dtopk_w, const float* __restrict__ logits,
-                                                       const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w,
-                                                       const int32_t* __restrict__ counts, float cost, float* __restrict__ dlogits,
-                                                       float* __restrict__ loss_part, GateArgs A) {
-  __shared__ float part[4];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+// Bound by HBM: the logits in, their gradients out.  W lanes per token; a lane holds 4 neighbouring experts (VEC; else every W-th) in each of C chunks.
+// The slots' d go to their experts through a row in LDS; a wavefront goes from tokens to tokens with its experts' C_e in registers.
+constexpr int kGateBwdWaves = 8;
+template <int W, int C, bool VEC>
+__global__ __launch_bounds__(kGateBwdWaves * kWave) void gate_bwd_kernel(const float* __restrict__ dtopk_w, const float* __restrict__ logits,
+                                                                         const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w,
+                                                                         const int32_t* __restrict__ counts, float cost, float* __restrict__ dlogits,
+                                                                         float* __restrict__ loss_part, GateArgs A) {
+  constexpr int TOKENS = kWave / W, ROW = W * C * 4;   // floats of a token's row
+  __shared__ __attribute__((aligned(16))) float rows[kGateBwdWaves][TOKENS * ROW];
+  __shared__ int tags[kGateBwdWaves][TOKENS * ROW];
+  __shared__ float part[kGateBwdWaves];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane % W, tt = lane / W;
   const int E = A.E, k = A.k, Kp = k + A.Es;
   const bool dense = counts != nullptr || (!A.sigmoid && !A.renorm);
+  const float inv_scale = 1.0f / A.scale;
+  float* row = &rows[wave][tt * ROW];
+  int* tag = &tags[wave][tt * ROW];
+  auto expert = [&](int c, int i) { return VEC ? 4 * (g + W * c) + i : g + W * (4 * c + i); };
+  float Ce[4 * C];
+#pragma unroll
+  for (int c = 0; c < C; c++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) Ce[4 * c + i] = counts && expert(c, i) < E ? cost * (float)counts[expert(c, i)] : 0.f;
   float loss = 0.f;
-  for (int t = blockIdx.x * 4 + wave; t < A.T; t += gridDim.x * 4) {
-    const float* dw = dtopk_w + (size_t)t * Kp;
-    const float* w = topk_w + (size_t)t * Kp;
-    const int32_t* idx = topk_idx + (size_t)t * Kp;
-    const float* row = logits + (size_t)t * E;
+  const int batches = (A.T + TOKENS - 1) / TOKENS;
+  for (int batch = blockIdx.x * kGateBwdWaves + wave; batch < batches; batch += gridDim.x * kGateBwdWaves) {
+    const int t = batch * TOKENS + tt;
+    const bool live = t < A.T;
+    const size_t at = (size_t)(live ? t : A.T - 1);
+    const float* src = logits + at * E;
+    float l[4 * C];
+    if (dense) {
+#pragma unroll
+      for (int c = 0; c < C; c++) {
+        if (VEC) {
+          const float4 u = *reinterpret_cast<const float4*>(src + min(expert(c, 0), E - 4));
+          l[4 * c] = u.x; l[4 * c + 1] = u.y; l[4 * c + 2] = u.z; l[4 * c + 3] = u.w;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; i++) l[4 * c + i] = src[min(expert(c, i), E - 1)];
+        }
+      }
+    }
+    // the slots (k of them, W at a time)
     float inner = 0.f;
-    for (int j = lane; j < k; j += kWave) inner += w[j] * dw[j];
-    inner = lanes_sum<kWave>(inner);
-    float v[PER], slope[PER];
+    for (int j = g; j < k; j += W) inner = fmaf(topk_w[at * Kp + j], dtopk_w[at * Kp + j], inner);
+    inner = lanes_sum<W>(inner);
 #pragma unroll
-    for (int p = 0; p < PER; p++) { v[p] = 0.f; slope[p] = 1.f; }
-    if (dense || A.sigmoid) {
-      float l[PER], s[PER], m = -kMaxLogit, z = 0.f, mean = 0.f;
-#pragma unroll
-      for (int p = 0; p < PER; p++) {
-        const int e = lane + p * kWave;
-        l[p] = e < E ? gate_finite(row[e]) : -__builtin_inff();
-        if (!gate_masked(l[p])) m = fmaxf(m, l[p]);
-      }
-      m = lanes_max<kWave>(m);
-      const float top = A.sigmoid ? fminf(m, 0.f) : m;   // (scores over exp(top))
-#pragma unroll
-      for (int p = 0; p < PER; p++) {
-        s[p] = gate_masked(l[p]) ? 0.f : A.sigmoid ? sigmoid_over(l[p], top) : expf(l[p] - top);
-        if (A.sigmoid) slope[p] = gate_masked(l[p]) ? 0.f : 1.0f / (1.0f + expf(l[p]));
-        z += s[p];
-      }
-      if (dense) {
-        z = lanes_sum<kWave>(z);
-        const float inv = z > 0.f ? 1.0f / z : 0.f;
-        float C[PER];
-#pragma unroll
-        for (int p = 0; p < PER; p++) {
-          const int e = lane + p * kWave;
-          C[p] = counts && e < E ? cost * (float)counts[e] : 0.f;
-          s[p] *= inv;
-          mean += s[p] * C[p];
-        }
-        mean = lanes_sum<kWave>(mean);
-        loss += mean;
-#pragma unroll
-        for (int p = 0; p < PER; p++) {
-          v[p] = s[p] * (C[p] - mean);
-          if (!A.sigmoid && !A.renorm) v[p] -= s[p] * inner;
+    for (int c = 0; c < C; c++) *reinterpret_cast<float4*>(row + 4 * (g + W * c)) = float4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int j0 = 0; j0 < k; j0 += W) {
+      const int j = j0 + g;
+      int e = -1;
+      float d = 0.f;
+      if (j < k) {
+        e = topk_idx[at * Kp + j];
+        const float w = topk_w[at * Kp + j], dw = dtopk_w[at * Kp + j];
+        d = A.renorm ? w * (dw - inner * inv_scale) : w * dw;
+        e = (unsigned)e < (unsigned)E ? e : -1;   // (no other id has a logit)
+        if (A.sigmoid && !dense && e >= 0) {
+          const float x = src[e];
+          d = gate_masked(x) ? 0.f : d * __builtin_amdgcn_rcpf(1.0f + fast_exp(gate_finite(x)));
         }
       }
+      // whether an expert is named twice: then its slots one after another
+      if (e >= 0) tag[e] = g;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const bool twice = e >= 0 && tag[e] != g;
+      if (!__any(twice)) {
+        if (e >= 0) row[e] += d;
+      } else {
+        for (int o = 0; o < W; o++) {
+          if (g == o && e >= 0) row[e] += d;
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    for (int j = 0; j < k; j++) {
-      const int e = idx[j];
-      const float d = A.renorm ? w[j] * (dw[j] - inner / A.scale) : w[j] * dw[j];
+    float v[4 * C];
 #pragma unroll
-      for (int p = 0; p < PER; p++)
-        if (e == lane + p * kWave) v[p] += d;
+    for (int c = 0; c < C; c++) {
+      if (VEC) {
+        const float4 u = *reinterpret_cast<const float4*>(row + 4 * (g + W * c));
+        v[4 * c] = u.x; v[4 * c + 1] = u.y; v[4 * c + 2] = u.z; v[4 * c + 3] = u.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[4 * c + i] = row[expert(c, i)];
+      }
     }
+    if (dense) {
+      float s[4 * C], slope[4 * C], z = 0.f, m = -kMaxLogit;
 #pragma unroll
-    for (int p = 0; p < PER; p++) {
-      const int e = lane + p * kWave;
-      if (e < E) dlogits[(size_t)t * E + e] = v[p] * slope[p];
+      for (int i = 0; i < 4 * C; i++) {
+        const float finite = fminf(l[i], kMaxLogit);
+        l[i] = expert(i / 4, i % 4) < E && l[i] > kMaskedLogit ? finite : -__builtin_inff();   // (and NaN)
+        m = fmaxf(m, l[i]);
+      }
+      // Scores over exp(top), which keeps the ratios of those far below zero.  sigmoid: e = exp(top - l) is at least exp(top), which is at most 1.
+      float top = 0.f;
+      if (!A.sigmoid) top = lanes_max<W>(m);
+      else if (__any(m < 0.f)) top = fminf(lanes_max<W>(m), 0.f);
+      const float unit = A.sigmoid ? fast_exp(top) : 0.f;
+#pragma unroll
+      for (int i = 0; i < 4 * C; i++) {
+        if (A.sigmoid) {
+          const float e = fast_exp(top - l[i]);
+          s[i] = __builtin_amdgcn_rcpf(e + unit);
+          slope[i] = e < 0x1p100f ? e * s[i] : l[i] > kMaskedLogit ? 1.0f : 0.f;   // 1 - s = exp(-l) / (1 + exp(-l))
+        } else {
+          s[i] = fast_exp(l[i] - top);
+          slope[i] = l[i] > kMaskedLogit ? 1.0f : 0.f;
+        }
+        z += s[i];
+      }
+      z = lanes_sum<W>(z);
+      const float inv = z > 0.f ? 1.0f / z : 0.f;
+      float mean = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4 * C; i++) {
+        s[i] *= inv;
+        mean = fmaf(s[i], Ce[i], mean);
+      }
+      mean = lanes_sum<W>(mean);
+      if (live && g == 0) loss += mean;
+      const float less = mean + (!A.sigmoid && !A.renorm ? inner : 0.f);
+#pragma unroll
+      for (int i = 0; i < 4 * C; i++) v[i] = fmaf(s[i], Ce[i] - less, v[i]) * slope[i];
+    }
+    if (live) {
+      float* out = dlogits + at * E;
+#pragma unroll
+      for (int c = 0; c < C; c++) {
+        if (VEC) {
+          if (expert(c, 0) < E) *reinterpret_cast<float4*>(out + expert(c, 0)) = float4{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; i++)
+            if (expert(c, i) < E) out[expert(c, i)] = v[4 * c + i];
+        }
+      }
     }
   }
   if (loss_part) {
+    loss = lanes_sum<kWave>(loss);
     if (lane == 0) part[wave] = loss;
     __syncthreads();
-    if (threadIdx.x == 0) loss_part[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+    if (threadIdx.x == 0) {
+      float sum = 0.f;
+      for (int i = 0; i < kGateBwdWaves; i++) sum += part[i];
+      loss_part[blockIdx.x] = sum;
+    }
   }
 }
 
-// The sum of the blocks' parts, in a fixed order.
+// The sum of at most kGateBwdBlocks parts, in a fixed order.
 __global__ __launch_bounds__(256) void gate_loss_kernel(const float* __restrict__ loss_part, int parts, float* __restrict__ loss) {
-  __shared__ double sum[256];
+  __shared__ double sum[256 / kWave];
   double v = 0.0;
-  for (int i = threadIdx.x; i < parts; i += 256) v += (double)loss_part[i];
-  sum[threadIdx.x] = v;
-  for (int o = 128; o > 0; o >>= 1) {
-    __syncthreads();
-    if (threadIdx.x < o) sum[threadIdx.x] += sum[threadIdx.x + o];
+#pragma unroll
+  for (int i = 0; i < kGateBwdBlocks / 256; i++) {
+    const int at = threadIdx.x + 256 * i;
+    v += at < parts ? (double)loss_part[at] : 0.0;
   }
-  if (threadIdx.x == 0) *loss = (float)sum[0];
+  v = lanes_sum<kWave>(v);
+  if (threadIdx.x % kWave == 0) sum[threadIdx.x / kWave] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) *loss = (float)((sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 
 // bias_e += rate where expert e has fewer slots than the mean, -= rate where it has more.
@@ -836,7 +915,10 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   MOE_REQUIRE_ALIGNED(dtopk_w); MOE_REQUIRE_ALIGNED(logits); MOE_REQUIRE_ALIGNED(topk_idx); MOE_REQUIRE_ALIGNED(topk_w); MOE_REQUIRE_ALIGNED(dlogits);
   MOE_REQUIRE_ALIGNED(counts); MOE_REQUIRE_ALIGNED(loss);
   if (!(balance >= -kMaxLogit && balance <= kMaxLogit)) return MOE_ERR_SHAPE;
-  const int blocks = D.T < 4 * kGateBwdBlocks ? (D.T + 3) / 4 : kGateBwdBlocks;
+  int W = 8;   // lanes of a token: 4 experts each, up to 64 lanes
+  while (W < kWave && 4 * W < D.E) W *= 2;
+  const long long units = ((long long)D.T + kGateBwdWaves * (kWave / W) - 1) / (kGateBwdWaves * (kWave / W));
+  const int blocks = (int)(units < kGateBwdBlocks ? units : kGateBwdBlocks);
   if (loss) {
     MOE_REQUIRE_PTR(counts); MOE_REQUIRE_PTR(ws);
     if (!aligned(ws, 256)) return MOE_ERR_ALIGN;
@@ -846,13 +928,21 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   if (D.T > 0) {
     const float cost = (float)((double)balance * D.E / ((double)D.k * D.T * D.T));
     float* parts = loss ? (float*)ws : nullptr;
-#define MOE_LAUNCH_GATE_BWD(PER) \
-  MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<PER>), dim3(blocks), dim3(256), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, cost, dlogits, parts, A)
-    if (D.E <= 64) MOE_LAUNCH_GATE_BWD(1);
-    else if (D.E <= 128) MOE_LAUNCH_GATE_BWD(2);
-    else if (D.E <= 256) MOE_LAUNCH_GATE_BWD(4);
-    else if (D.E <= 512) MOE_LAUNCH_GATE_BWD(8);
-    else MOE_LAUNCH_GATE_BWD(16);
+#define MOE_LAUNCH_GATE_BWD(W_, C_)                                                                                                                         \
+  do {                                                                                                                                                      \
+    if (D.E % 4 == 0)                                                                                                                                       \
+      MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, true>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
+                 cost, dlogits, parts, A);                                                                                                                  \
+    else                                                                                                                                                    \
+      MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, false>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
+                 cost, dlogits, parts, A);                                                                                                                  \
+  } while (0)
+    if (W == 8) MOE_LAUNCH_GATE_BWD(8, 1);
+    else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 1);
+    else if (W == 32) MOE_LAUNCH_GATE_BWD(32, 1);
+    else if (D.E <= 256) MOE_LAUNCH_GATE_BWD(64, 1);
+    else if (D.E <= 512) MOE_LAUNCH_GATE_BWD(64, 2);
+    else MOE_LAUNCH_GATE_BWD(64, 4);
 #undef MOE_LAUNCH_GATE_BWD
   }
   if (loss) MOE_LAUNCH("gate_loss", st, gate_loss_kernel, dim3(1), dim3(256), 0, st, (const float*)ws, blocks, loss);

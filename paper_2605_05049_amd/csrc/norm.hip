@@ -54,7 +54,7 @@ template <int WAVES, int CH, bool CENTRE>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_fwd_kernel(NormFwdArgs A) {
   constexpr int THREADS = WAVES * kWave, ROWS = WAVES < 4 ? 4 / WAVES : 1;
   __shared__ float slots[ROWS][2][WAVES];
-  const int tid = threadIdx.x % THREADS, in_block = threadIdx.x / THREADS, wave = tid / kWave;
+  const int tid = threadIdx.x % THREADS, in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   long long row = (long long)blockIdx.x * ROWS + in_block;
   const bool live = row < A.rows;   // (the others take part in the barriers)
   if (!live) row = A.rows - 1;
@@ -141,53 +141,117 @@ struct NormBwdArgs {
   float inv_cols;
   const uint16_t* dy; const uint16_t* h; const uint16_t* gamma; const float* mean; const float* rstd; const uint16_t* dx_addend;
   uint16_t* dx;
-  float* part;   // [blocks][2][cols]: a block's sums of dy xh and of dy; null: not wanted
+  float* part;          // [row_blocks][2][cols]: a block's sums of dy xh and of dy; null: not wanted, or made by blocks of their own
+  int row_blocks;       // blocks behind them make dgamma and dbeta, 64 columns each
+  float* dgamma; float* dbeta;
+  int accumulate;
 };
 
-// Rows in turn for WAVES wavefronts each; a lane keeps the sums of its columns.
-template <int WAVES, int CH, bool CENTRE>
+// dgamma and dbeta of 64 columns from dy and h themselves: the wavefronts take rows in turn, their sums are joined in order.
+template <int WAVES_IN_BLOCK, bool CENTRE>
+__device__ __forceinline__ void weights_of_columns(const NormBwdArgs& A, int block, float* join) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int pair = lane % 32, half = lane / 32, col = block * kWave + 2 * pair;   // two columns a lane, two rows a wavefront
+  float g0 = 0.f, g1 = 0.f, b0 = 0.f, b1 = 0.f;
+  if (col < A.cols) {
+#pragma unroll 8
+    for (long long row = 2 * wave + half; row < A.rows; row += 2 * WAVES_IN_BLOCK) {
+      const uint32_t d = *reinterpret_cast<const uint32_t*>(A.dy + (size_t)row * A.cols + col);
+      const uint32_t h = *reinterpret_cast<const uint32_t*>(A.h + (size_t)row * A.cols + col);
+      const float mean = CENTRE ? A.mean[row] : 0.f, rstd = A.rstd[row];
+      g0 = fmaf(bf16lo(d), (bf16lo(h) - mean) * rstd, g0);
+      g1 = fmaf(bf16hi(d), (bf16hi(h) - mean) * rstd, g1);
+      b0 += bf16lo(d);
+      b1 += bf16hi(d);
+    }
+  }
+  float* mine = join + (size_t)(2 * wave + half) * 4 * 32 + pair;   // [row group][4][32]
+  mine[0] = g0; mine[32] = g1; mine[64] = b0; mine[96] = b1;
+  __syncthreads();
+  const int which = threadIdx.x / kWave, c = threadIdx.x % kWave;   // dgamma, dbeta
+  float* out = which == 0 ? A.dgamma : which == 1 ? A.dbeta : nullptr;
+  if (out == nullptr || block * kWave + c >= A.cols) return;
+  float v = A.accumulate ? out[block * kWave + c] : 0.f;
+  for (int i = 0; i < 2 * WAVES_IN_BLOCK; i++) v += join[(size_t)i * 4 * 32 + (2 * which + c % 2) * 32 + c / 2];
+  out[block * kWave + c] = v;
+}
+
+// Rows in turn for WAVES wavefronts each; a lane keeps gamma and the sums of its columns, and requests the next row before it computes this one.
+template <int WAVES, int CH, bool CENTRE, bool BETA>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_bwd_kernel(NormBwdArgs A) {
-  constexpr int THREADS = WAVES * kWave, ROWS = WAVES < 4 ? 4 / WAVES : 1;
+  constexpr int THREADS = WAVES * kWave, BLOCK_WAVES = WAVES < 4 ? 4 : WAVES, ROWS = BLOCK_WAVES / WAVES;
+  constexpr bool AHEAD = CH <= 2;   // (registers)
+  constexpr int JOIN = (ROWS - 1) * THREADS * 8, COLUMNS = 2 * BLOCK_WAVES * 4 * 32;
   __shared__ float slots[2][ROWS][2][WAVES];
-  __shared__ float join[ROWS > 1 ? (ROWS - 1) * THREADS * 8 : 1];
-  const int tid = threadIdx.x % THREADS, in_block = threadIdx.x / THREADS, wave = tid / kWave;
-  float dgamma[8 * CH], dbeta[8 * CH];
+  __shared__ float join[JOIN > COLUMNS ? JOIN : COLUMNS];
+  if ((int)blockIdx.x >= A.row_blocks) {
+    weights_of_columns<BLOCK_WAVES, CENTRE>(A, blockIdx.x - A.row_blocks, join);
+    return;
+  }
+  const int tid = threadIdx.x % THREADS, in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const bool sums = A.part != nullptr;
+  float dgamma[8 * CH], dbeta[BETA ? 8 * CH : 1];
 #pragma unroll
-  for (int i = 0; i < 8 * CH; i++) dgamma[i] = dbeta[i] = 0.f;
-  const long long step = (long long)gridDim.x * ROWS;
+  for (int i = 0; i < 8 * CH; i++) dgamma[i] = 0.f;
+#pragma unroll
+  for (int i = 0; i < (BETA ? 8 * CH : 1); i++) dbeta[i] = 0.f;
+  // (columns behind the last are read as the last ones and count as zeros: dy and gamma of them are 0)
+  uint4 gamma[CH];
+  bool in[CH];
+  unsigned bytes_at[CH];
+#pragma unroll
+  for (int c = 0; c < CH; c++) {
+    const int col = 8 * (tid + c * THREADS);
+    in[c] = col < A.cols;
+    bytes_at[c] = 2u * (unsigned)(in[c] ? col : A.cols - 8);
+    gamma[c] = uint4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+    if (A.gamma) gamma[c] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(A.gamma) + bytes_at[c]);
+  }
+  struct Row { uint4 dy[CH], h[CH], addend[CH]; float mean, rstd; };
+  auto request = [&](long long row, Row& r) __attribute__((always_inline)) {
+    const long long at = row < A.rows ? row : A.rows - 1;
+    const char* dy = reinterpret_cast<const char*>(A.dy + (size_t)at * A.cols);   // (of the wavefront; a lane's offset has 32 bits)
+    const char* h = reinterpret_cast<const char*>(A.h + (size_t)at * A.cols);
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      r.dy[c] = *reinterpret_cast<const uint4*>(dy + bytes_at[c]);
+      r.h[c] = *reinterpret_cast<const uint4*>(h + bytes_at[c]);
+    }
+    if (A.dx_addend) {
+      const char* addend = reinterpret_cast<const char*>(A.dx_addend + (size_t)at * A.cols);
+#pragma unroll
+      for (int c = 0; c < CH; c++) r.addend[c] = *reinterpret_cast<const uint4*>(addend + bytes_at[c]);
+    }
+    r.mean = CENTRE ? A.mean[at] : 0.f;
+    r.rstd = A.rstd[at];
+  };
+  const long long step = (long long)A.row_blocks * ROWS;
   int turn = 0;
+  Row cur, next;
+  if constexpr (AHEAD) request((long long)blockIdx.x * ROWS + in_block, cur);
   for (long long first = (long long)blockIdx.x * ROWS; first < A.rows; first += step, turn ^= 1) {
     const long long row = first + in_block;
     const bool live = row < A.rows;
-    const size_t base = (size_t)(live ? row : 0) * A.cols;
-    const float mean = live && CENTRE ? A.mean[row] : 0.f, rstd = live ? A.rstd[row] : 0.f;
-    uint4 rdy[CH], rh[CH];
-#pragma unroll
-    for (int c = 0; c < CH; c++) {
-      const int col = 8 * (tid + c * THREADS);
-      rdy[c] = rh[c] = uint4{0, 0, 0, 0};
-      if (live && col < A.cols) {
-        rdy[c] = *reinterpret_cast<const uint4*>(A.dy + base + col);
-        rh[c] = *reinterpret_cast<const uint4*>(A.h + base + col);
-      }
+    if constexpr (AHEAD) {
+      if (first + step < A.rows) request(row + step, next);
+    } else {
+      request(row, cur);
     }
     float sg = 0.f, sgx = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      const int col = 8 * (tid + c * THREADS);
-      if (live && col < A.cols) {
-        float d[8], v[8], f[8];
-        unpack8(rdy[c], d);
-        unpack8(rh[c], v);
-        if (A.gamma) unpack8(*reinterpret_cast<const uint4*>(A.gamma + col), f);
+      if (!in[c] || !live) cur.dy[c] = uint4{0, 0, 0, 0};
+      float d[8], v[8], f[8];
+      unpack8(cur.dy[c], d);
+      unpack8(cur.h[c], v);
+      unpack8(gamma[c], f);
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-          const float xh = (v[i] - mean) * rstd, g = A.gamma ? d[i] * f[i] : d[i];
-          dgamma[8 * c + i] = fmaf(d[i], xh, dgamma[8 * c + i]);
-          dbeta[8 * c + i] += d[i];
-          sg += g;
-          sgx = fmaf(g, xh, sgx);
-        }
+      for (int i = 0; i < 8; i++) {
+        const float xh = (v[i] - cur.mean) * cur.rstd, g = d[i] * f[i];
+        dgamma[8 * c + i] = fmaf(d[i], xh, dgamma[8 * c + i]);
+        if (BETA) dbeta[8 * c + i] += d[i];
+        if (CENTRE) sg += g;
+        sgx = fmaf(g, xh, sgx);
       }
     }
     if (CENTRE) sg = wave_add(sg);
@@ -199,86 +263,109 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_bwd_kern
 #pragma unroll
       for (int i = 0; i < WAVES; i++) { sg += slots[turn][in_block][0][i]; sgx += slots[turn][in_block][1][i]; }
     }
+    // dx = rstd (d gamma - (sg - mean rstd sgx) - h rstd sgx), kept as differences from the mean
     sg = CENTRE ? sg * A.inv_cols : 0.f;
     sgx *= A.inv_cols;
+    char* dx = reinterpret_cast<char*>(A.dx + (size_t)(live ? row : 0) * A.cols);
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      const int col = 8 * (tid + c * THREADS);
-      if (live && col < A.cols) {
-        float d[8], v[8], f[8];
-        unpack8(rdy[c], d);
-        unpack8(rh[c], v);
-        if (A.gamma) unpack8(*reinterpret_cast<const uint4*>(A.gamma + col), f);
+      float d[8], v[8], f[8];
+      unpack8(cur.dy[c], d);
+      unpack8(cur.h[c], v);
+      unpack8(gamma[c], f);
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-          const float xh = (v[i] - mean) * rstd, g = A.gamma ? d[i] * f[i] : d[i];
-          d[i] = rstd * (g - sg - xh * sgx);
-        }
-        if (A.dx_addend) {
-          unpack8(*reinterpret_cast<const uint4*>(A.dx_addend + base + col), f);
-#pragma unroll
-          for (int i = 0; i < 8; i++) d[i] += f[i];
-        }
-        *reinterpret_cast<uint4*>(A.dx + base + col) = pack8(d);
+      for (int i = 0; i < 8; i++) {
+        const float xh = (v[i] - cur.mean) * cur.rstd;
+        d[i] = cur.rstd * (fmaf(d[i], f[i], -sg) - xh * sgx);
       }
+      if (A.dx_addend) {
+        unpack8(cur.addend[c], f);
+#pragma unroll
+        for (int i = 0; i < 8; i++) d[i] += f[i];
+      }
+      if (in[c] && live) *reinterpret_cast<uint4*>(dx + bytes_at[c]) = pack8(d);
     }
+    if constexpr (AHEAD) cur = next;
   }
-  if (A.part == nullptr) return;
+  if (!sums) return;
   float* part = A.part + (size_t)blockIdx.x * 2 * A.cols;
 #pragma unroll
-  for (int which = 0; which < 2; which++) {
-    float* sums = which ? dbeta : dgamma;
+  for (int which = 0; which < (BETA ? 2 : 1); which++) {
+    float* of = which ? dbeta : dgamma;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       if constexpr (ROWS > 1) {   // the block's other rows, in order
         __syncthreads();
         if (in_block > 0)
 #pragma unroll
-          for (int i = 0; i < 8; i++) join[((in_block - 1) * 8 + i) * THREADS + tid] = sums[8 * c + i];
+          for (int i = 0; i < 8; i++) join[((in_block - 1) * 8 + i) * THREADS + tid] = of[8 * c + i];
         __syncthreads();
         if (in_block == 0)
 #pragma unroll
           for (int o = 0; o < ROWS - 1; o++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) sums[8 * c + i] += join[(o * 8 + i) * THREADS + tid];
+            for (int i = 0; i < 8; i++) of[8 * c + i] += join[(o * 8 + i) * THREADS + tid];
       }
-      const int col = 8 * (tid + c * THREADS);
-      if (in_block == 0 && col < A.cols) {
+      if (in_block == 0 && in[c]) {
 #pragma unroll
         for (int i = 0; i < 8; i += 4)
-          *reinterpret_cast<float4*>(part + (size_t)which * A.cols + col + i) = float4{sums[8 * c + i], sums[8 * c + i + 1], sums[8 * c + i + 2], sums[8 * c + i + 3]};
+          *reinterpret_cast<float4*>(part + (size_t)which * A.cols + bytes_at[c] / 2 + i) = float4{of[8 * c + i], of[8 * c + i + 1], of[8 * c + i + 2], of[8 * c + i + 3]};
       }
     }
   }
 }
 
-// dgamma and dbeta from the blocks' sums: 64 columns a block, 16 wavefronts that take every 16th part, joined in order.
+// dgamma and dbeta from the blocks' sums: 32 columns a block, 32 groups that take every 32nd part, joined in order.
 __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restrict__ part, int parts, int cols, float* __restrict__ dgamma,
                                                             float* __restrict__ dbeta, int accumulate) {
-  __shared__ float join[16][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = blockIdx.x * kWave + lane;
+  __shared__ float join[32][33];
+  const int c = threadIdx.x % 32, group = threadIdx.x / 32, col = blockIdx.x * 32 + c;
   float* out = blockIdx.y ? dbeta : dgamma;
   if (out == nullptr) return;   // (whole blocks)
   float v = 0.f;
-  if (col < cols)
-    for (int p = wave; p < parts; p += 16) v += part[((size_t)p * 2 + blockIdx.y) * cols + col];
-  join[wave][lane] = v;
+  if (col < cols) {
+#pragma unroll 8
+    for (int p = group; p < parts; p += 32) v += part[((size_t)p * 2 + blockIdx.y) * cols + col];
+  }
+  join[group][c] = v;
   __syncthreads();
-  if (wave != 0 || col >= cols) return;
+  if (group != 0 || col >= cols) return;
   v = accumulate ? out[col] : 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; i++) v += join[i][lane];
+  for (int i = 0; i < 32; i++) v += join[i][c];
   out[col] = v;
 }
 
 static bool norm_sizes(long long rows, int cols) { return rows >= 0 && rows < (1ll << 31) && cols >= 8 && cols <= MOE_NORM_COLS_MAX && cols % 8 == 0; }
-static int norm_rows_per_block(int cols) { return cols <= 512 ? 4 : cols <= 2048 ? 1 : 1; }
-static int norm_bwd_blocks(long long rows, int cols) {
-  const long long units = (rows + norm_rows_per_block(cols) - 1) / norm_rows_per_block(cols);
-  return (int)(units < 1024 ? units : 1024);
+// Wavefronts of a row in the forward pass, up to 3 chunks of 8 values a lane; with the residual sum, whose loads wait in registers, one or two.
+// (67 million values, 512 .. 16384 columns: 5.8 to 6.3 TB/s, with the sum 5.1 to 6.0; half as many wavefronts with the sum 3 to 8 % slower, twice as many
+// without it 1 to 40 %.)
+static int norm_fwd_waves(int cols, bool addend) {
+  if (addend) return cols <= 512 ? 2 : cols <= 2048 ? 4 : 8;
+  return cols <= 1536 ? 1 : cols <= 3072 ? 2 : cols <= 6144 ? 4 : 8;
 }
+// Wavefronts of a row in the backward pass: as few as leave a lane at most 3 chunks of 8 values (4 from 12288 columns on), whose sums it keeps.  Blocks: two
+// a CU of 4 wavefronts, one of 8.  (Twice and half as many blocks, wavefronts: 2 to 40 % slower at 512 .. 16384 columns; 2 blocks of 8 are 6 % slower.)
+static int norm_bwd_waves(int cols) { return cols <= 1536 ? 1 : cols <= 3072 ? 2 : cols <= 6144 ? 4 : 8; }
+static int norm_bwd_blocks(long long rows, int cols) {
+  const int waves = norm_bwd_waves(cols), per_block = waves < 4 ? 4 / waves : 1, most = waves < 8 ? 512 : 256;
+  const long long units = (rows + per_block - 1) / per_block;
+  return (int)(units < most ? units : most);
+}
+// dgamma and dbeta by blocks of their own in the launch of dx: they read dy and h again, but there is one launch.
+static bool norm_bwd_one_launch(long long rows, int cols) { return rows <= 1024 && rows * cols <= (1 << 20); }
 
 }  // namespace moe
+
+// The launch of W_ wavefronts a row for its number of chunks.
+#define MOE_LAUNCH_NORM_CHUNKS(W_)                         \
+  do {                                                     \
+    const int chunks = (cols + 512 * W_ - 1) / (512 * W_); \
+    if (chunks <= 1) MOE_LAUNCH_NORM(W_, 1);               \
+    else if (chunks == 2) MOE_LAUNCH_NORM(W_, 2);          \
+    else if (chunks == 3) MOE_LAUNCH_NORM(W_, 3);          \
+    else MOE_LAUNCH_NORM(W_, 4);                           \
+  } while (0)
 
 extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const uint16_t* x, const uint16_t* addend, const uint16_t* gamma,
                             const uint16_t* beta, uint16_t* sum, uint16_t* y, float* mean, float* rstd, void* stream) {
@@ -296,11 +383,11 @@ extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const
     if (centre) MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<W_, CH_, true>), grid, block, 0, st, A);                          \
     else MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<W_, CH_, false>), grid, block, 0, st, A);                                \
   } while (0)
-  if (cols <= 512) MOE_LAUNCH_NORM(1, 1);
-  else if (cols <= 2048) MOE_LAUNCH_NORM(4, 1);
-  else if (cols <= 4096) MOE_LAUNCH_NORM(4, 2);
-  else if (cols <= 8192) MOE_LAUNCH_NORM(4, 4);
-  else MOE_LAUNCH_NORM(8, 4);
+  const int waves = norm_fwd_waves(cols, addend != nullptr);
+  if (waves == 1) MOE_LAUNCH_NORM_CHUNKS(1);
+  else if (waves == 2) MOE_LAUNCH_NORM_CHUNKS(2);
+  else if (waves == 4) MOE_LAUNCH_NORM_CHUNKS(4);
+  else MOE_LAUNCH_NORM_CHUNKS(8);
 #undef MOE_LAUNCH_NORM
   return launch_status();
 }
@@ -331,22 +418,28 @@ extern "C" int moe_norm_bwd(int64_t rows, int cols, int centre, const uint16_t* 
   hipStream_t st = (hipStream_t)stream;
   const int blocks = norm_bwd_blocks(rows, cols);
   float* part = weights ? (float*)ws : nullptr;
+  const bool one = rows > 0 && norm_bwd_one_launch(rows, cols) && dx != dy;   // (dy is still read when dx is written)
   if (rows > 0) {
-    const NormBwdArgs A = {rows, cols, 1.0f / cols, dy, h, gamma, mean, rstd, dx_addend, dx, part};
-#define MOE_LAUNCH_NORM(W_, CH_)                                                                                                           \
-  do {                                                                                                                                     \
-    if (centre) MOE_LAUNCH("norm_bwd", st, (norm_bwd_kernel<W_, CH_, true>), dim3(blocks), dim3(W_ < 4 ? 256 : W_ * kWave), 0, st, A);     \
-    else MOE_LAUNCH("norm_bwd", st, (norm_bwd_kernel<W_, CH_, false>), dim3(blocks), dim3(W_ < 4 ? 256 : W_ * kWave), 0, st, A);           \
+    const NormBwdArgs A = {rows, cols, 1.0f / cols, dy, h, gamma, mean, rstd, dx_addend, dx, one ? nullptr : part, blocks, dgamma, dbeta, accumulate};
+    const dim3 grid(blocks + (one && weights ? (cols + kWave - 1) / kWave : 0));
+#define MOE_LAUNCH_NORM_BETA(W_, CH_, C_, B_) \
+  MOE_LAUNCH("norm_bwd", st, (norm_bwd_kernel<W_, CH_, C_, B_>), grid, dim3(W_ < 4 ? 256 : W_ * kWave), 0, st, A)
+#define MOE_LAUNCH_NORM(W_, CH_)                                                  \
+  do {                                                                            \
+    if (centre && dbeta) MOE_LAUNCH_NORM_BETA(W_, CH_, true, true);               \
+    else if (centre) MOE_LAUNCH_NORM_BETA(W_, CH_, true, false);                  \
+    else if (dbeta) MOE_LAUNCH_NORM_BETA(W_, CH_, false, true);                   \
+    else MOE_LAUNCH_NORM_BETA(W_, CH_, false, false);                             \
   } while (0)
-    if (cols <= 512) MOE_LAUNCH_NORM(1, 1);
-    else if (cols <= 2048) MOE_LAUNCH_NORM(4, 1);
-    else if (cols <= 4096) MOE_LAUNCH_NORM(4, 2);
-    else if (cols <= 8192) MOE_LAUNCH_NORM(4, 4);
-    else MOE_LAUNCH_NORM(8, 4);
+    const int waves = norm_bwd_waves(cols);
+    if (waves == 1) MOE_LAUNCH_NORM_CHUNKS(1);
+    else if (waves == 2) MOE_LAUNCH_NORM_CHUNKS(2);
+    else if (waves == 4) MOE_LAUNCH_NORM_CHUNKS(4);
+    else MOE_LAUNCH_NORM_CHUNKS(8);
 #undef MOE_LAUNCH_NORM
+#undef MOE_LAUNCH_NORM_BETA
   }
-  if (weights)
-    MOE_LAUNCH("norm_weights", st, norm_weights_kernel, dim3((cols + kWave - 1) / kWave, dbeta ? 2 : 1), dim3(1024), 0, st, part, blocks, cols, dgamma, dbeta,
-               accumulate);
+  if (weights && !one)
+    MOE_LAUNCH("norm_weights", st, norm_weights_kernel, dim3((cols + 31) / 32, dbeta ? 2 : 1), dim3(1024), 0, st, part, blocks, cols, dgamma, dbeta, accumulate);
   return launch_status();
 }

@@ -63,14 +63,14 @@ def test_gate_refusals(lib):
     assert lib.moe_router_gate_fwd(s, g, *ok, FAKE, 16, None) == -4
     assert lib.moe_router_gate_fwd(s, g, *ok, ctypes.c_void_p(0x10010), BIG, None) == -3
 
-    def bwd(dw=FAKE, logits=FAKE, idx=FAKE, w=FAKE, counts=FAKE, balance=0.1, dlogits=FAKE, loss=FAKE, ws=FAKE, n=1 << 14):
+    def bwd(dw=FAKE, logits=FAKE, idx=FAKE, w=FAKE, counts=FAKE, balance=0.1, dlogits=FAKE, loss=FAKE, ws=FAKE, n=1 << 12):
         return lib.moe_gate_bwd(s, g, dw, logits, idx, w, counts, balance, dlogits, loss, ws, n, None)
 
     for name in ("dw", "logits", "idx", "w", "dlogits", "counts", "ws"):
         assert bwd(**{name: None}) == -1, name       # (the loss needs counts and a workspace)
     for name in ("dw", "logits", "idx", "w", "dlogits", "counts", "loss"):
         assert bwd(**{name: ODD}) == -3, name
-    assert bwd(ws=ctypes.c_void_p(0x10010)) == -3 and bwd(n=16383) == -4
+    assert bwd(ws=ctypes.c_void_p(0x10010)) == -3 and bwd(n=4095) == -4
     assert bwd(balance=float("nan")) == -2 and bwd(balance=float("inf")) == -2
     assert lib.moe_gate_bias_step(s, None, 0.1, FAKE, None) == -1 and lib.moe_gate_bias_step(s, FAKE, 0.1, None, None) == -1
     assert lib.moe_gate_bias_step(s, ODD, 0.1, FAKE, None) == -3 and lib.moe_gate_bias_step(s, FAKE, 0.1, ODD, None) == -3

@@ -327,7 +327,7 @@ int moe_mxfp4_grouped_gemm_large_tiles(int experts, int64_t rows, int n, int k);
  *   X = Q(x_perm);  G = X W_gate,  U = X W_up,  H = Q(silu(G) * U),  Y = H W_down     (Q: as moe_mxfp4_quantize; of H from fp32)
  *   x_perm [N,d] bf16 in;  offsets [E'+1] int32 in;  wq_gate, wq_up [E', f, d / 2], s_gate, s_up [E', f, d / 32], wq_down [E', d, f / 2],
  *   s_down [E', d, f / 32] in;  y_perm [N,d] bf16 out.
- * moe_mxfp4_workspace_bytes(shape) bytes of workspace are enough for it and for what comes before it, moe_router_fwd, moe_router_route_fwd
+ * moe_mxfp4_workspace_bytes(shape) bytes of workspace are enough for it and for what comes before it, moe_router_fwd, _route_fwd, _gate_fwd
  * and moe_permute (0 if the shape is invalid): the rows and H in 4 bits, without what only the forward on bf16 weights and the backward need. */
 size_t moe_mxfp4_workspace_bytes(const moe_shape* shape);
 int moe_mxfp4_grouped_ffn_fwd(const moe_shape* shape, const uint16_t* x_perm, const int32_t* offsets, const uint8_t* wq_gate,

@@ -19,5 +19,5 @@ from .binding import (  # noqa: F401
 )
 from .layer import (  # noqa: F401
     MoeLayerBuffers, CapturedLayerStep, layer_forward, layer_backward, FewTokenBuffers, PromptMemory, layer_few_forward, quantize_experts,
-    layer_mxfp4_forward,
+    layer_mxfp4_forward, MoeBlockBuffers, block_forward, block_backward,
 )

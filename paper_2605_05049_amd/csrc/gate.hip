@@ -13,7 +13,7 @@ namespace moe {
 
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
 constexpr float kMaxLogit = 3.402823466e38f;
-constexpr int kGateBwdBlocks = 1024;      // at most; each adds up its tokens' share of the loss
+constexpr int kGateBwdBlocks = 512;     // at most; each adds up its tokens' share of the loss
 
 struct GateArgs {
   int T, E, k, Es, renorm;
@@ -614,94 +614,116 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
 // The slots' d go to their experts through a row in LDS; a wavefront goes from tokens to tokens with its experts' C_e in registers.
 constexpr int kGateBwdWaves = 8;
 template <int W, int C, bool VEC>
-__global__ __launch_bounds__(kGateBwdWaves * kWave) void gate_bwd_kernel(const float* __restrict__ dtopk_w, const float* __restrict__ logits,
+__global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(const float* __restrict__ dtopk_w, const float* __restrict__ logits,
                                                                          const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w,
                                                                          const int32_t* __restrict__ counts, float cost, float* __restrict__ dlogits,
                                                                          float* __restrict__ loss_part, GateArgs A) {
   constexpr int TOKENS = kWave / W, ROW = W * C * 4;   // floats of a token's row
   __shared__ __attribute__((aligned(16))) float rows[kGateBwdWaves][TOKENS * ROW];
-  __shared__ int tags[kGateBwdWaves][TOKENS * ROW];
   __shared__ float part[kGateBwdWaves];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane % W, tt = lane / W;
   const int E = A.E, k = A.k, Kp = k + A.Es;
   const bool dense = counts != nullptr || (!A.sigmoid && !A.renorm);
   const float inv_scale = 1.0f / A.scale;
   float* row = &rows[wave][tt * ROW];
-  int* tag = &tags[wave][tt * ROW];
   auto expert = [&](int c, int i) { return VEC ? 4 * (g + W * c) + i : g + W * (4 * c + i); };
-  float Ce[4 * C];
+  // C_e in LDS.  (The counts read from memory by every wavefront, their few lines would be what all of them wait for.)
+  __shared__ __attribute__((aligned(16))) float costs[ROW];
+  for (int e = threadIdx.x; e < ROW; e += kGateBwdWaves * kWave) costs[e] = counts && e < E ? cost * (float)counts[e] : 0.f;
+  __syncthreads();
+  auto four_of = [&](const float* from, int c, float (&v)[4]) __attribute__((always_inline)) {
+    if (VEC) {
+      const float4 u = *reinterpret_cast<const float4*>(from + 4 * (g + W * c));
+      v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
 #pragma unroll
-  for (int c = 0; c < C; c++)
-#pragma unroll
-    for (int i = 0; i < 4; i++) Ce[4 * c + i] = counts && expert(c, i) < E ? cost * (float)counts[expert(c, i)] : 0.f;
+      for (int i = 0; i < 4; i++) v[i] = from[expert(c, i)];
+    }
+  };
   float loss = 0.f;
-  const int batches = (A.T + TOKENS - 1) / TOKENS;
-  for (int batch = blockIdx.x * kGateBwdWaves + wave; batch < batches; batch += gridDim.x * kGateBwdWaves) {
-    const int t = batch * TOKENS + tt;
-    const bool live = t < A.T;
-    const size_t at = (size_t)(live ? t : A.T - 1);
+  const int batches = (A.T + TOKENS - 1) / TOKENS, step = gridDim.x * kGateBwdWaves;
+  struct Batch { float l[4 * C]; int e; float w, dw; };   // what a batch of tokens reads: requested while the one before is computed
+  auto request = [&](int batch, Batch& b) __attribute__((always_inline)) {
+    const size_t at = (size_t)min(batch * TOKENS + tt, A.T - 1);
     const float* src = logits + at * E;
-    float l[4 * C];
     if (dense) {
 #pragma unroll
       for (int c = 0; c < C; c++) {
         if (VEC) {
           const float4 u = *reinterpret_cast<const float4*>(src + min(expert(c, 0), E - 4));
-          l[4 * c] = u.x; l[4 * c + 1] = u.y; l[4 * c + 2] = u.z; l[4 * c + 3] = u.w;
+          b.l[4 * c] = u.x; b.l[4 * c + 1] = u.y; b.l[4 * c + 2] = u.z; b.l[4 * c + 3] = u.w;
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; i++) l[4 * c + i] = src[min(expert(c, i), E - 1)];
+          for (int i = 0; i < 4; i++) b.l[4 * c + i] = src[min(expert(c, i), E - 1)];
         }
       }
     }
+    const size_t slot = at * Kp + min(g, k - 1);
+    b.e = topk_idx[slot];
+    b.w = topk_w[slot];
+    b.dw = dtopk_w[slot];
+  };
+  Batch cur, next;
+  int batch = blockIdx.x * kGateBwdWaves + wave;
+  constexpr bool AHEAD = VEC || C <= 2;   // (16 experts one by one take the registers)
+  if (AHEAD && batch < batches) request(batch, cur);
+  for (; batch < batches; batch += step) {
+    if constexpr (AHEAD) {
+      if (batch + step < batches) request(batch + step, next);
+    } else {
+      request(batch, cur);
+    }
+    const int t = batch * TOKENS + tt;
+    const bool live = t < A.T;
+    const size_t at = (size_t)(live ? t : A.T - 1);
+    const float* src = logits + at * E;
+    float (&l)[4 * C] = cur.l;
     // the slots (k of them, W at a time)
-    float inner = 0.f;
-    for (int j = g; j < k; j += W) inner = fmaf(topk_w[at * Kp + j], dtopk_w[at * Kp + j], inner);
+    float inner = g < k ? cur.w * cur.dw : 0.f;
+    for (int j = g + W; j < k; j += W) inner = fmaf(topk_w[at * Kp + j], dtopk_w[at * Kp + j], inner);
     inner = lanes_sum<W>(inner);
 #pragma unroll
     for (int c = 0; c < C; c++) *reinterpret_cast<float4*>(row + 4 * (g + W * c)) = float4{0.f, 0.f, 0.f, 0.f};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     for (int j0 = 0; j0 < k; j0 += W) {
       const int j = j0 + g;
-      int e = -1;
-      float d = 0.f;
-      if (j < k) {
+      int e = cur.e;
+      float w = cur.w, dw = cur.dw;
+      if (j0 > 0 && j < k) {
         e = topk_idx[at * Kp + j];
-        const float w = topk_w[at * Kp + j], dw = dtopk_w[at * Kp + j];
-        d = A.renorm ? w * (dw - inner * inv_scale) : w * dw;
-        e = (unsigned)e < (unsigned)E ? e : -1;   // (no other id has a logit)
-        if (A.sigmoid && !dense && e >= 0) {
-          const float x = src[e];
-          d = gate_masked(x) ? 0.f : d * __builtin_amdgcn_rcpf(1.0f + fast_exp(gate_finite(x)));
-        }
+        w = topk_w[at * Kp + j];
+        dw = dtopk_w[at * Kp + j];
       }
-      // whether an expert is named twice: then its slots one after another
-      if (e >= 0) tag[e] = g;
+      const bool mine = j < k && (unsigned)e < (unsigned)E;   // (no other id has a logit)
+      float d = A.renorm ? w * (dw - inner * inv_scale) : w * dw;
+      if (A.sigmoid && !dense && mine) {
+        const float x = src[e];
+        d = gate_masked(x) ? 0.f : d * __builtin_amdgcn_rcpf(1.0f + fast_exp(gate_finite(x)));
+      }
+      // whether an expert is named twice, which its place in the row tells: then its slots one after another
+      float old = 0.f;
+      bool twice = false;
+      if (mine) {
+        if (j0 > 0) old = row[e];
+        row[e] = __int_as_float(g);
+      }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      const bool twice = e >= 0 && tag[e] != g;
-      if (!__any(twice)) {
-        if (e >= 0) row[e] += d;
-      } else {
+      if (mine) twice = __float_as_int(row[e]) != g;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const bool any = __any(twice);
+      if (mine) row[e] = any ? old : old + d;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (any) {
         for (int o = 0; o < W; o++) {
-          if (g == o && e >= 0) row[e] += d;
+          if (g == o && mine) row[e] += d;
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    float v[4 * C];
-#pragma unroll
-    for (int c = 0; c < C; c++) {
-      if (VEC) {
-        const float4 u = *reinterpret_cast<const float4*>(row + 4 * (g + W * c));
-        v[4 * c] = u.x; v[4 * c + 1] = u.y; v[4 * c + 2] = u.z; v[4 * c + 3] = u.w;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) v[4 * c + i] = row[expert(c, i)];
-      }
-    }
+    float* out = dlogits + at * E;
+    float s[4 * C], slope[4 * C], mean = 0.f;
     if (dense) {
-      float s[4 * C], slope[4 * C], z = 0.f, m = -kMaxLogit;
+      float z = 0.f, m = -kMaxLogit;
 #pragma unroll
       for (int i = 0; i < 4 * C; i++) {
         const float finite = fminf(l[i], kMaxLogit);
@@ -727,31 +749,40 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave) void gate_bwd_kernel(const f
       }
       z = lanes_sum<W>(z);
       const float inv = z > 0.f ? 1.0f / z : 0.f;
-      float mean = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4 * C; i++) {
-        s[i] *= inv;
-        mean = fmaf(s[i], Ce[i], mean);
+      for (int c = 0; c < C; c++) {
+        float Ce[4];
+        four_of(costs, c, Ce);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          s[4 * c + i] *= inv;
+          mean = fmaf(s[4 * c + i], Ce[i], mean);
+        }
       }
       mean = lanes_sum<W>(mean);
       if (live && g == 0) loss += mean;
-      const float less = mean + (!A.sigmoid && !A.renorm ? inner : 0.f);
-#pragma unroll
-      for (int i = 0; i < 4 * C; i++) v[i] = fmaf(s[i], Ce[i] - less, v[i]) * slope[i];
     }
-    if (live) {
-      float* out = dlogits + at * E;
+    const float less = mean + (!A.sigmoid && !A.renorm ? inner : 0.f);
 #pragma unroll
-      for (int c = 0; c < C; c++) {
-        if (VEC) {
-          if (expert(c, 0) < E) *reinterpret_cast<float4*>(out + expert(c, 0)) = float4{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
-        } else {
+    for (int c = 0; c < C; c++) {
+      float v[4];
+      four_of(row, c, v);
+      if (dense) {
+        float Ce[4];
+        four_of(costs, c, Ce);
 #pragma unroll
-          for (int i = 0; i < 4; i++)
-            if (expert(c, i) < E) out[expert(c, i)] = v[4 * c + i];
-        }
+        for (int i = 0; i < 4; i++) v[i] = fmaf(s[4 * c + i], Ce[i] - less, v[i]) * slope[4 * c + i];
+      }
+      if (VEC) {
+        if (live && expert(c, 0) < E) *reinterpret_cast<float4*>(out + expert(c, 0)) = float4{v[0], v[1], v[2], v[3]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+          if (live && expert(c, i) < E) out[expert(c, i)] = v[i];
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (the next batch's zeros)
+    if constexpr (AHEAD) cur = next;
   }
   if (loss_part) {
     loss = lanes_sum<kWave>(loss);
@@ -915,34 +946,39 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   MOE_REQUIRE_ALIGNED(dtopk_w); MOE_REQUIRE_ALIGNED(logits); MOE_REQUIRE_ALIGNED(topk_idx); MOE_REQUIRE_ALIGNED(topk_w); MOE_REQUIRE_ALIGNED(dlogits);
   MOE_REQUIRE_ALIGNED(counts); MOE_REQUIRE_ALIGNED(loss);
   if (!(balance >= -kMaxLogit && balance <= kMaxLogit)) return MOE_ERR_SHAPE;
-  int W = 8;   // lanes of a token: 4 experts each, up to 64 lanes
-  while (W < kWave && 4 * W < D.E) W *= 2;
+  // lanes of a token: 16 experts each at most, 8 one by one
+  const int each = D.E % 4 == 0 ? 16 : 8;
+  int W = 8;
+  while (W < kWave && each * W < D.E) W *= 2;
   const long long units = ((long long)D.T + kGateBwdWaves * (kWave / W) - 1) / (kGateBwdWaves * (kWave / W));
   const int blocks = (int)(units < kGateBwdBlocks ? units : kGateBwdBlocks);
   if (loss) {
     MOE_REQUIRE_PTR(counts); MOE_REQUIRE_PTR(ws);
     if (!aligned(ws, 256)) return MOE_ERR_ALIGN;
-    if (ws_bytes < (size_t)kGateBwdBlocks * sizeof(float)) return MOE_ERR_WORKSPACE;
+    if (ws_bytes < 4096) return MOE_ERR_WORKSPACE;
   }
   hipStream_t st = (hipStream_t)stream;
   if (D.T > 0) {
     const float cost = (float)((double)balance * D.E / ((double)D.k * D.T * D.T));
     float* parts = loss ? (float*)ws : nullptr;
-#define MOE_LAUNCH_GATE_BWD(W_, C_)                                                                                                                         \
-  do {                                                                                                                                                      \
-    if (D.E % 4 == 0)                                                                                                                                       \
-      MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, true>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
-                 cost, dlogits, parts, A);                                                                                                                  \
-    else                                                                                                                                                    \
-      MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, false>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
-                 cost, dlogits, parts, A);                                                                                                                  \
-  } while (0)
-    if (W == 8) MOE_LAUNCH_GATE_BWD(8, 1);
-    else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 1);
-    else if (W == 32) MOE_LAUNCH_GATE_BWD(32, 1);
-    else if (D.E <= 256) MOE_LAUNCH_GATE_BWD(64, 1);
-    else if (D.E <= 512) MOE_LAUNCH_GATE_BWD(64, 2);
-    else MOE_LAUNCH_GATE_BWD(64, 4);
+#define MOE_LAUNCH_GATE_BWD(W_, C_, VEC_)                                                                                                             \
+  MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, VEC_>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
+             cost, dlogits, parts, A)
+    if (D.E % 4 == 0) {
+      if (D.E <= 32) MOE_LAUNCH_GATE_BWD(8, 1, true);
+      else if (D.E <= 64) MOE_LAUNCH_GATE_BWD(8, 2, true);
+      else if (W == 8) MOE_LAUNCH_GATE_BWD(8, 4, true);
+      else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 4, true);
+      else if (W == 32) MOE_LAUNCH_GATE_BWD(32, 4, true);
+      else MOE_LAUNCH_GATE_BWD(64, 4, true);
+    } else {
+      if (D.E <= 32) MOE_LAUNCH_GATE_BWD(8, 1, false);
+      else if (W == 8) MOE_LAUNCH_GATE_BWD(8, 2, false);
+      else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 2, false);
+      else if (W == 32) MOE_LAUNCH_GATE_BWD(32, 2, false);
+      else if (D.E <= 512) MOE_LAUNCH_GATE_BWD(64, 2, false);
+      else MOE_LAUNCH_GATE_BWD(64, 4, false);
+    }
 #undef MOE_LAUNCH_GATE_BWD
   }
   if (loss) MOE_LAUNCH("gate_loss", st, gate_loss_kernel, dim3(1), dim3(256), 0, st, (const float*)ws, blocks, loss);

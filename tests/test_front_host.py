@@ -6,6 +6,7 @@ import torch
 
 import paper_2605_05049_amd as moe
 from paper_2605_05049_amd import binding as B
+from paper_2605_05049_amd import serve
 
 FAKE = ctypes.c_void_p(0x10000)        # aligned, never dereferenced: every call below fails its host checks first
 ODD = ctypes.c_void_p(0x10004)
@@ -119,3 +120,20 @@ def test_binding_refuses_host_tensors_and_strides():
         moe.moe_norm_fwd(True, 1e-6, torch.zeros(4, 64, dtype=torch.bfloat16), None, None, None, None, None, None, None)
     with pytest.raises(ValueError, match="h: expected rows"):
         moe.moe_norm_bwd(True, f, torch.zeros(()), None, None, None, None, None, None, None, False, None)
+
+
+@pytest.mark.parametrize("args", ["--groups 3", "--groups 0", "--groups 8 --groups-kept 9", "--groups 8 --groups-kept 0", "--experts 8 --groups 8 --group-best 2",
+                                  "--group-best 3", "--experts 8 --groups 8 --groups-kept 1 --top-k 2", "--scale 0 --scores sigmoid", "--scale nan", "--balance-steps -1",
+                                  "--balance-rate -1", "--balance-rate inf", "--norm rms --dims 16448x64"])
+def test_command_refuses(args, capsys):
+    with pytest.raises(SystemExit) as e:
+        serve.main(args.split())
+    assert e.value.code == 2 and "error: --" in capsys.readouterr().err
+
+
+def test_served_layer_refuses():
+    z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    args = (z(8, 64), z(8, 64, 64), z(8, 64, 64), z(8, 64, 64), 2)
+    for bad in (dict(bias=torch.zeros(8)), dict(gate=moe.Gate(), bias=torch.zeros(7)), dict(norm=(z(63), None, True, 1e-6)), dict(norm=(z(64), z(65), True, 1e-6))):
+        with pytest.raises(ValueError):
+            serve.ServedLayer(*args, mxfp4=False, **bad)

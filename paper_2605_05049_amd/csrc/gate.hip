@@ -307,7 +307,9 @@ __device__ __forceinline__ void join_keys(double (&a)[K], const double (&b)[K]) 
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 struct GatePlan {        // how a token's experts lie on its lanes
-  int lanes_of_group;    // a power of two
+  int lanes_of_group;    // a power of two, and its logarithm
+  int lanes_log2;
+  int size;              // experts of a group
   int piece;             // experts of a lane at most
 };
 // Where the i-th float of a wavefront's logits lies in LDS: 4 floats are left free after every RUN, which keeps the lanes off each other's banks.
@@ -349,7 +351,13 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const int n = min(TOKENS, A.T - t0) * E;
   const float* src = logits + (size_t)t0 * E;
   // (all requested before the first one is waited for)
-  if ((TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) && n >= 4) {
+  if (FULL && n == kWave * PER) {   // (whole wavefronts of whole lanes)
+    float4 in[PER / 4];
+#pragma unroll
+    for (int j = 0; j < PER / 4; j++) in[j] = *reinterpret_cast<const float4*>(src + 4 * lane + 4 * kWave * j);
+#pragma unroll
+    for (int j = 0; j < PER / 4; j++) *reinterpret_cast<float4*>(&rows[wave][gate_place<RUN>(4 * lane) + gate_place<RUN>(4 * kWave) * j]) = in[j];
+  } else if ((TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) && n >= 4) {
     float4 in[PER / 4];
 #pragma unroll
     for (int j = 0; j < PER / 4; j++) in[j] = *reinterpret_cast<const float4*>(src + min(4 * (lane + kWave * j), (n - 4) & ~3));
@@ -361,9 +369,9 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
-  const int size = E / A.groups;
-  const int group = g / P.lanes_of_group;
-  const int begin = (g % P.lanes_of_group) * P.piece;
+  const int size = P.size;
+  const int group = g >> P.lanes_log2;
+  const int begin = (g & (P.lanes_of_group - 1)) * P.piece;
   const int first = group * size + begin, count = group < A.groups && t < A.T ? max(0, min(P.piece, size - begin)) : 0;
   float l[PER], c[PER];
   // (of a lane without a group: the last one's; its keys are behind all others by their ids, or its group does not stay)
@@ -382,7 +390,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     for (int p = 0; p < PER; p++) l[p] = p < count ? l[p] : -__builtin_inff();
   }
   const float* bias_run = &biases[FULL && !by_logits ? gate_place<RUN>(min(first, E - PER)) : 0];
-  auto bias_of = [&](int p, float (&b)[4]) __attribute__((always_inline)) {   // of a lane's experts p .. p + 3
+  auto bias_of = [&](int p, float* b) __attribute__((always_inline)) {   // of a lane's experts p .. p + 3
     if constexpr (FULL) {
       const float4 u = *reinterpret_cast<const float4*>(bias_run + p);
       b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
@@ -398,20 +406,24 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   if (A.sigmoid && !by_logits) {
     unsigned top_bits = 0;   // of the exponentials: infinite or NaN where one is masked (or a score too small to be told from that)
 #pragma unroll
-    for (int p = 0; p < PER; p += 4) {
-      float b[4];
+    for (int p = 0; p < PER; p += 8) {   // (eight at a time, step by step: no instruction waits for the one before it)
+      float b[8], e[8];
       bias_of(p, b);
+      bias_of(p + 4, b + 4);
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const float e = fast_exp(-l[p + i]);
-        top_bits = max(top_bits, __float_as_uint(e));
-        c[p + i] = __builtin_amdgcn_rcpf(1.0f + e) + b[i];
-      }
+      for (int i = 0; i < 8; i++) e[i] = fast_exp(-l[p + i]);
+#pragma unroll
+      for (int i = 0; i < 8; i++) top_bits = max(top_bits, __float_as_uint(e[i]));
+#pragma unroll
+      for (int i = 0; i < 8; i++) e[i] = __builtin_amdgcn_rcpf(1.0f + e[i]);
+#pragma unroll
+      for (int i = 0; i < 8; i++) c[p + i] = e[i] + b[i];
     }
-    some_dead = some_dead || top_bits >= 0x7f800000u;
-    if (__any(some_dead)) {
+    some_dead = __any(some_dead || top_bits >= 0x7f800000u);
+    if (some_dead) {
+      asm volatile("");   // (a branch: mostly it is not taken)
 #pragma unroll
-      for (int p = 0; p < PER; p++) c[p] = l[p] > kMaskedLogit ? c[p] : kDeadKey;
+      for (int p = 0; p < PER; p++) c[p] = l[p] > kMaskedLogit && c[p] > kMaskedLogit ? c[p] : kDeadKey;
     }
   } else {
 #pragma unroll
@@ -427,7 +439,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     }
     if (by_logits) {
 #pragma unroll
-      for (int p = 0; p < PER; p++) c[p] = l[p] + 0.0f;   // (-0 is 0)
+      for (int p = 0; p < PER; p++) c[p] = l[p] > kMaskedLogit ? l[p] + 0.0f : kDeadKey;   // (-0 is 0)
     }
     if (!A.sigmoid && !(by_logits && A.renorm)) {
       float z = 0.f;
@@ -443,16 +455,11 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
 #pragma unroll
           for (int i = 0; i < 4; i++) {
             const float v = fmaf(fast_exp(l[p + i] - m), inv_z, b[i]);
-            c[p + i] = l[p + i] > kMaskedLogit ? v : kDeadKey;
+            c[p + i] = l[p + i] > kMaskedLogit && v > kMaskedLogit ? v : kDeadKey;
           }
         }
       }
     }
-  }
-  some_dead = __any(some_dead);
-  if (some_dead) {
-#pragma unroll
-    for (int p = 0; p < PER; p++) c[p] = c[p] > kMaskedLogit ? c[p] : kDeadKey;
   }
   if constexpr (!FULL) {
 #pragma unroll
@@ -791,7 +798,7 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(cons
     if (threadIdx.x == 0) {
       float sum = 0.f;
       for (int i = 0; i < kGateBwdWaves; i++) sum += part[i];
-      loss_part[blockIdx.x] = sum;
+      loss_part[blockIdx.x] = sum;   // (of a block by itself: the loss)
     }
   }
 }
@@ -853,7 +860,7 @@ static int gate_lanes(const GateArgs& A, GatePlan* P) {
     if (padded > W) continue;
     const int lanes = W / padded, piece = (size + lanes - 1) / lanes;
     if (piece > 32) continue;
-    *P = GatePlan{lanes, piece};
+    *P = GatePlan{lanes, __builtin_ctz(lanes), size, piece};
     return W;
   }
   return 0;
@@ -951,7 +958,9 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   int W = 8;
   while (W < kWave && each * W < D.E) W *= 2;
   const long long units = ((long long)D.T + kGateBwdWaves * (kWave / W) - 1) / (kGateBwdWaves * (kWave / W));
-  const int blocks = (int)(units < kGateBwdBlocks ? units : kGateBwdBlocks);
+  // With the loss, up to 4 batches of tokens a wavefront stay in one block, which then has the whole sum: a launch less.
+  const bool alone = loss && D.T > 0 && units <= 4;
+  const int blocks = (int)(alone ? 1 : units < kGateBwdBlocks ? units : kGateBwdBlocks);
   if (loss) {
     MOE_REQUIRE_PTR(counts); MOE_REQUIRE_PTR(ws);
     if (!aligned(ws, 256)) return MOE_ERR_ALIGN;
@@ -960,7 +969,7 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   hipStream_t st = (hipStream_t)stream;
   if (D.T > 0) {
     const float cost = (float)((double)balance * D.E / ((double)D.k * D.T * D.T));
-    float* parts = loss ? (float*)ws : nullptr;
+    float* parts = alone ? loss : loss ? (float*)ws : nullptr;
 #define MOE_LAUNCH_GATE_BWD(W_, C_, VEC_)                                                                                                             \
   MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, VEC_>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
              cost, dlogits, parts, A)
@@ -981,7 +990,7 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
     }
 #undef MOE_LAUNCH_GATE_BWD
   }
-  if (loss) MOE_LAUNCH("gate_loss", st, gate_loss_kernel, dim3(1), dim3(256), 0, st, (const float*)ws, blocks, loss);
+  if (loss && !alone) MOE_LAUNCH("gate_loss", st, gate_loss_kernel, dim3(1), dim3(256), 0, st, (const float*)ws, blocks, loss);
   return launch_status();
 }
 

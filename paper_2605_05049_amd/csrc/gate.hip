@@ -5,7 +5,7 @@
 //   the k best c among them are chosen, ties to the lowest id;  w_j = scale s_j / sum_i s_i  or  scale s_j
 //
 // Decisions (which groups, which experts, in which order) are those of scores in 64 bits; the weights are fp32.
-#include "common.h"
+#include "lanes.h"
 
 #include <type_traits>
 
@@ -23,44 +23,6 @@ struct GateArgs {
 
 __device__ __forceinline__ bool gate_masked(float l) { return !(l > kMaskedLogit); }
 __device__ __forceinline__ float gate_finite(float l) { return l > kMaxLogit ? kMaxLogit : l; }   // (NaN stays)
-
-// v of another lane: 1, 2 and, where the lanes of a quad (of eight) hold the same, 4 and 8 further on by moves inside the rows of 16, else through LDS.
-template <int STEP>
-__device__ __forceinline__ int from_lane(int v) {
-  if constexpr (STEP == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);         // quad_perm 1 0 3 2
-  else if constexpr (STEP == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);    // quad_perm 2 3 0 1
-  else if constexpr (STEP == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);   // row_half_mirror
-  else if constexpr (STEP == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);   // row_mirror
-  else {
-    static_assert(STEP == 16 || STEP == 32, "a power of two below 64");
-    const bool upper = (threadIdx.x & STEP) != 0;   // (rows, or halves, change places between two registers that hold the same)
-    if constexpr (STEP == 16) {
-      const auto r = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
-      return upper ? r[0] : r[1];
-    } else {
-      const auto r = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
-      return upper ? r[0] : r[1];
-    }
-  }
-}
-template <int STEP>
-__device__ __forceinline__ float from_lane(float v) { return __int_as_float(from_lane<STEP>(__float_as_int(v))); }
-template <int STEP>
-__device__ __forceinline__ double from_lane(double v) { return __hiloint2double(from_lane<STEP>(__double2hiint(v)), from_lane<STEP>(__double2loint(v))); }
-
-// Over W neighbouring lanes, for each of them.
-template <int W, int STEP = 1, typename T>
-__device__ __forceinline__ T lanes_sum(T v) {
-  if constexpr (STEP < W) return lanes_sum<W, 2 * STEP>(v + from_lane<STEP>(v));
-  else return v;
-}
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
-template <int W, int STEP = 1, typename T>
-__device__ __forceinline__ T lanes_max(T v) {
-  if constexpr (STEP < W) return lanes_max<W, 2 * STEP>(larger(v, from_lane<STEP>(v)));
-  else return v;
-}
 
 // sigmoid(l) / sigmoid-like factor exp(top) with top = min(0, the largest logit that is looked at): scores far below zero keep their ratios.
 __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f / (expf(top - l) + expf(top)); }
@@ -119,7 +81,7 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     for (int g = lane; g < A.groups; g += kWave) {
       double first = NEG, second = NEG;
-#pragma unroll 4
+#pragma unroll 8
       for (int i = 0; i < S; i++) {
         const double v = row_c[g * S + i];
         second = fmax(second, fmin(first, v));
@@ -128,20 +90,20 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
       group_c[g] = A.group_best > 1 && second != NEG ? first + second : first;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int p = 0; p < PER; p++) {
-      const int e = lane + p * kWave;
-      if (e < E) {
-        const int g = e / S;
-        const double v = group_c[g];
-        int better = 0;
-        for (int o = 0; o < A.groups; o++) {
-          const double u = group_c[o];
-          better += u > v || (u == v && o < g);
-        }
-        if (better >= A.groups_kept) taken[p] = true;
+    for (int g = lane; g < A.groups; g += kWave) {   // (whether a group stays, over the c that are not read any more)
+      const double v = group_c[g];
+      int better = 0;
+#pragma unroll 8
+      for (int o = 0; o < A.groups; o++) {
+        const double u = group_c[o];
+        better += u > v || (u == v && o < g);
       }
+      row_c[g] = better < A.groups_kept ? 1.0 : 0.0;
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int p = 0; p < PER; p++)
+      if (lane + p * kWave < E && row_c[(lane + p * kWave) / S] == 0.0) taken[p] = true;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (before the next token's)
   }
 #pragma unroll
@@ -465,11 +427,11 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
 #pragma unroll
     for (int p = 0; p < PER; p++) c[p] = p < count ? c[p] : kNoKey;
   }
-  // How far c may be off.  sigmoid: the exponential's argument 1.5 |l| 2^-24 times s (1 - s) <= 0.23 / |l|, exponential and reciprocal 2^-23 each, the
-  // sum 2^-24: under 2^-22.  softmax: of s, 27 2^-23 for the sum of the exponentials (their mean argument is under 7, 40 additions) and 5 2^-23 for
-  // its own: under 2^-18.  And a rounding of c.  Twice that, for both of a pair.
-  const float slack = by_logits ? 0.f : A.sigmoid ? 0x1p-21f : 0x1p-17f * inv_z, slack_c = 0x1p-22f;
-
+  // How far c may be off, in units of 2^-24.  sigmoid: the exponential's argument 1.5 |l| times s (1 - s) <= 0.23 / |l|, the exponential 2 s (1 - s), the
+  // sum s, the reciprocal 2 s: under 4.  softmax, times 1 / z, which no score is above: the sum of exponentials z is off by the mean of their
+  // arguments, 1.5 times under 5 of 1024, by 2 and by PER + 6 additions; its reciprocal by 2; a score by its own argument, 1.5 times 0.37, by 2 and by
+  // the product: under PER + 22.  And c by a rounding.  For both of a pair, twice that.
+  const float slack = by_logits ? 0.f : A.sigmoid ? 0x1p-21f : (PER + 22) * 0x1p-23f * inv_z, slack_c = 0x1p-23f;
   const bool track = !by_logits && k == K;   // (else the first one left out is in the list, or order needs no margin)
   // Up to a few lanes' experts stay: one lane may well have all choices.  With more, what a lane lets go matters in 4 (1/4)^K of the tokens.
   const bool track_lane = track && A.groups_kept * P.lanes_of_group < 4;
@@ -525,8 +487,9 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     const bool exists = group < A.groups, stays = exists && better < A.groups_kept;
     if (!by_logits || A.group_best > 1) {
       const float low = -lanes_max<W>(stays ? -score : -__builtin_inff()), high = lanes_max<W>(exists && !stays ? score : -__builtin_inff());
-      // (two c, a rounding of their sum; of scores without the shared sum, each at most 1, the arguments count)
-      const float far = by_logits ? 0x1p-18f : 2.0f * slack + 0x1p-20f * fmaxf(1.0f, fabsf(low));
+      // Two c, off as above, and a rounding of their sum, for two groups; the c themselves may be large and cancel.  Scores without a bias: of sigmoid
+      // as above, of softmax (without the shared sum, each at most 1) the argument, the exponential, the sum: under 8 in all.
+      const float far = by_logits ? 0x1p-20f : 2.0f * slack + slack_c * (fabsf(low) + lanes_max<W>(a > kMaskedLogit ? fabsf(a) + (b > kMaskedLogit ? fabsf(b) : 0.f) : 0.f));
       unsure = unsure || (high > kMaskedLogit && low - high <= far);
     }
     const double none = make_key(kNoKey, 0, false);
@@ -567,7 +530,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     const float a = key_value(mine);
     const float after = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(a), 0x101, 0xF, 0xF, true));   // row_shl:1: the next lane's
     const float b = g == K - 1 ? lost : after;
-    unsure = unsure || (g < k && b > kMaskedLogit && a - b <= slack + slack_c * fmaxf(1.0f, fabsf(a)));
+    unsure = unsure || (g < k && b > kMaskedLogit && a - b <= slack + slack_c * fmaxf(fabsf(a), fabsf(b)));
     unsure = unsure || (lane_last > kMaskedLogit && lane_last >= key_value(best[K - 1]));
   }
   const bool live = t < A.T && g < k;

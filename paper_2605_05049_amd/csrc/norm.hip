@@ -5,32 +5,27 @@
 //
 // Bound by HBM: a row is read once into registers, where all passes over it are made (so the squares are those of the differences from the mean), and
 // written once.  8 neighbouring values per lane and chunk (16 bytes).
-#include "common.h"
+#include "lanes.h"
 
 namespace moe {
 
-// Sum over the 64 lanes, for all of them: inside the rows of 16 lanes, then from the last lane of a row (of the first half) to the rows (the half)
-// after it; lane 63 has it in the end.
-__device__ __forceinline__ float wave_add(float v) {
-#define MOE_ADD_STEP(ctrl, rows) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xF, false))
-  MOE_ADD_STEP(0x111, 0xF); MOE_ADD_STEP(0x112, 0xF); MOE_ADD_STEP(0x114, 0xF); MOE_ADD_STEP(0x118, 0xF);   // row_shr:1, 2, 4, 8
-  MOE_ADD_STEP(0x142, 0xA);   // row_bcast:15 into rows 1 and 3
-  MOE_ADD_STEP(0x143, 0xC);   // row_bcast:31 into rows 2 and 3
-#undef MOE_ADD_STEP
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
-}
-
-// Sums over the WAVES wavefronts of a row; `slot`: their LDS, used once between two barriers.
-template <int WAVES>
+// Sums over the THREADS lanes of a row (16, 32, 64 or several wavefronts); `slot`: LDS of a float a wavefront, used once between two barriers.
+template <int THREADS>
 __device__ __forceinline__ float row_add(float v, float* slot, int wave) {
-  v = wave_add(v);
-  if constexpr (WAVES == 1) return v;
+  v = lanes_sum<(THREADS < kWave ? THREADS : kWave)>(v);
+  if constexpr (THREADS <= kWave) return v;
   if (threadIdx.x % kWave == 0) slot[wave] = v;
   __syncthreads();
   v = 0.f;
 #pragma unroll
-  for (int i = 0; i < WAVES; i++) v += slot[i];
+  for (int i = 0; i < THREADS / kWave; i++) v += slot[i];
   return v;
+}
+// The value of the first lane for a whole wavefront (which row it works on) where a row has a wavefront and more.
+template <int THREADS>
+__device__ __forceinline__ int of_row(int v) {
+  if constexpr (THREADS >= kWave) return __builtin_amdgcn_readfirstlane(v);
+  else return v;
 }
 
 __device__ __forceinline__ void unpack8(const uint4& r, float* v) {
@@ -49,12 +44,12 @@ struct NormFwdArgs {
   uint16_t* sum; uint16_t* y; float* mean; float* rstd;
 };
 
-// A row for WAVES wavefronts, CH chunks of 8 values a lane; blocks of 4 wavefronts at least.
-template <int WAVES, int CH, bool CENTRE>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_fwd_kernel(NormFwdArgs A) {
-  constexpr int THREADS = WAVES * kWave, ROWS = WAVES < 4 ? 4 / WAVES : 1;
-  __shared__ float slots[ROWS][2][WAVES];
-  const int tid = threadIdx.x % THREADS, in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+// A row for THREADS lanes, CH chunks of 8 values a lane; blocks of 4 wavefronts at least.
+template <int THREADS, int CH, bool CENTRE>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_fwd_kernel(NormFwdArgs A) {
+  constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+  __shared__ float slots[ROWS][2][THREADS < kWave ? 1 : THREADS / kWave];
+  const int tid = threadIdx.x % THREADS, in_block = of_row<THREADS>(threadIdx.x / THREADS), wave = of_row<THREADS>(tid / kWave);
   long long row = (long long)blockIdx.x * ROWS + in_block;
   const bool live = row < A.rows;   // (the others take part in the barriers)
   if (!live) row = A.rows - 1;
@@ -89,7 +84,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_fwd_kern
 #pragma unroll
       for (int i = 0; i < 8; i++) total += v[i];
     }
-    total = row_add<WAVES>(total, slots[in_block][0], wave) * A.inv_cols;
+    total = row_add<THREADS>(total, slots[in_block][0], wave) * A.inv_cols;
   }
   float squares = 0.f;
 #pragma unroll
@@ -104,7 +99,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_fwd_kern
       }
     }
   }
-  squares = row_add<WAVES>(squares, slots[in_block][1], wave);
+  squares = row_add<THREADS>(squares, slots[in_block][1], wave);
   if (!live) return;
   const float rstd = 1.0f / sqrtf(fmaf(squares, A.inv_cols, A.eps));
   if (tid == 0) {
@@ -176,10 +171,10 @@ __device__ __forceinline__ void weights_of_columns(const NormBwdArgs& A, int blo
   out[block * kWave + c] = v;
 }
 
-// Rows in turn for WAVES wavefronts each; a lane keeps gamma and the sums of its columns, and requests the next row before it computes this one.
-template <int WAVES, int CH, bool CENTRE, bool BETA>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_bwd_kernel(NormBwdArgs A) {
-  constexpr int THREADS = WAVES * kWave, BLOCK_WAVES = WAVES < 4 ? 4 : WAVES, ROWS = BLOCK_WAVES / WAVES;
+// Rows in turn for THREADS lanes each; a lane keeps gamma and the sums of its columns, and requests the next row before it computes this one.
+template <int THREADS, int CH, bool CENTRE, bool BETA>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_bwd_kernel(NormBwdArgs A) {
+  constexpr int BLOCK_WAVES = THREADS < 256 ? 4 : THREADS / kWave, WAVES = THREADS < kWave ? 1 : THREADS / kWave, ROWS = BLOCK_WAVES * kWave / THREADS;
   constexpr bool AHEAD = CH <= 2;   // (registers)
   constexpr int JOIN = (ROWS - 1) * THREADS * 8, COLUMNS = 2 * BLOCK_WAVES * 4 * 32;
   __shared__ float slots[2][ROWS][2][WAVES];
@@ -188,7 +183,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_bwd_kern
     weights_of_columns<BLOCK_WAVES, CENTRE>(A, blockIdx.x - A.row_blocks, join);
     return;
   }
-  const int tid = threadIdx.x % THREADS, in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int tid = threadIdx.x % THREADS, in_block = of_row<THREADS>(threadIdx.x / THREADS), wave = of_row<THREADS>(tid / kWave);
   const bool sums = A.part != nullptr;
   float dgamma[8 * CH], dbeta[BETA ? 8 * CH : 1];
 #pragma unroll
@@ -254,8 +249,8 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * kWave) void norm_bwd_kern
         sgx = fmaf(g, xh, sgx);
       }
     }
-    if (CENTRE) sg = wave_add(sg);
-    sgx = wave_add(sgx);
+    if (CENTRE) sg = lanes_sum<(THREADS < kWave ? THREADS : kWave)>(sg);
+    sgx = lanes_sum<(THREADS < kWave ? THREADS : kWave)>(sgx);
     if constexpr (WAVES > 1) {   // (two sets of slots in turn: one barrier a row)
       if (threadIdx.x % kWave == 0) { slots[turn][in_block][0][wave] = sg; slots[turn][in_block][1][wave] = sgx; }
       __syncthreads();
@@ -337,18 +332,26 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restr
 }
 
 static bool norm_sizes(long long rows, int cols) { return rows >= 0 && rows < (1ll << 31) && cols >= 8 && cols <= MOE_NORM_COLS_MAX && cols % 8 == 0; }
-// Wavefronts of a row in the forward pass, up to 3 chunks of 8 values a lane; with the residual sum, whose loads wait in registers, one or two.
-// (67 million values, 512 .. 16384 columns: 5.8 to 6.3 TB/s, with the sum 5.1 to 6.0; half as many wavefronts with the sum 3 to 8 % slower, twice as many
-// without it 1 to 40 %.)
-static int norm_fwd_waves(int cols, bool addend) {
-  if (addend) return cols <= 512 ? 2 : cols <= 2048 ? 4 : 8;
-  return cols <= 1536 ? 1 : cols <= 3072 ? 2 : cols <= 6144 ? 4 : 8;
+// 64 to 512 lanes, as few as have at most `chunks` chunks of 8 columns each.
+static int norm_lanes_of_chunks(int cols, int chunks) {
+  int lanes = 64;
+  while (lanes < 512 && cols > 8 * chunks * lanes) lanes *= 2;
+  return lanes;
 }
-// Wavefronts of a row in the backward pass: as few as leave a lane at most 3 chunks of 8 values (4 from 12288 columns on), whose sums it keeps.  Blocks: two
-// a CU of 4 wavefronts, one of 8.  (Twice and half as many blocks, wavefronts: 2 to 40 % slower at 512 .. 16384 columns; 2 blocks of 8 are 6 % slower.)
-static int norm_bwd_waves(int cols) { return cols <= 1536 ? 1 : cols <= 3072 ? 2 : cols <= 6144 ? 4 : 8; }
+// Lanes of a row in the forward pass: up to 3 chunks of 8 values a lane; with the residual sum, whose loads wait in registers, one or two.
+// (67 million values, 512 .. 16384 columns: 5.8 to 6.3 TB/s, with the sum 5.1 to 6.0; half as many lanes with the sum 3 to 8 % slower, twice as many
+// without it 1 to 40 %.)
+static int norm_fwd_lanes(int cols, bool addend) {
+  if (cols <= 128) return 16;
+  if (cols <= 256) return 32;
+  if (addend) return cols <= 512 ? 128 : cols <= 2048 ? 256 : 512;
+  return norm_lanes_of_chunks(cols, 3);
+}
+// In the backward pass: as few as leave a lane at most 3 chunks of 8 values (4 from 12288 columns on), whose sums it keeps.  Blocks: two a CU of 4
+// wavefronts, one of 8.  (Twice and half as many blocks, lanes: 2 to 40 % slower at 512 .. 16384 columns; 2 blocks of 8 are 6 % slower.)
+static int norm_bwd_lanes(int cols) { return cols <= 128 ? 16 : cols <= 256 ? 32 : norm_lanes_of_chunks(cols, 3); }
 static int norm_bwd_blocks(long long rows, int cols) {
-  const int waves = norm_bwd_waves(cols), per_block = waves < 4 ? 4 / waves : 1, most = waves < 8 ? 512 : 256;
+  const int lanes = norm_bwd_lanes(cols), per_block = lanes < 256 ? 256 / lanes : 1, most = lanes < 512 ? 512 : 256;
   const long long units = (rows + per_block - 1) / per_block;
   return (int)(units < most ? units : most);
 }
@@ -357,14 +360,23 @@ static bool norm_bwd_one_launch(long long rows, int cols) { return rows <= 1024 
 
 }  // namespace moe
 
-// The launch of W_ wavefronts a row for its number of chunks.
-#define MOE_LAUNCH_NORM_CHUNKS(W_)                         \
-  do {                                                     \
-    const int chunks = (cols + 512 * W_ - 1) / (512 * W_); \
-    if (chunks <= 1) MOE_LAUNCH_NORM(W_, 1);               \
-    else if (chunks == 2) MOE_LAUNCH_NORM(W_, 2);          \
-    else if (chunks == 3) MOE_LAUNCH_NORM(W_, 3);          \
-    else MOE_LAUNCH_NORM(W_, 4);                           \
+// The launch of a row's lanes for their number of chunks.
+#define MOE_LAUNCH_NORM_CHUNKS(L_)                     \
+  do {                                                 \
+    const int chunks = (cols + 8 * L_ - 1) / (8 * L_); \
+    if (chunks <= 1) MOE_LAUNCH_NORM(L_, 1);           \
+    else if (chunks == 2) MOE_LAUNCH_NORM(L_, 2);      \
+    else if (chunks == 3) MOE_LAUNCH_NORM(L_, 3);      \
+    else MOE_LAUNCH_NORM(L_, 4);                       \
+  } while (0)
+#define MOE_LAUNCH_NORM_LANES(lanes)                      \
+  do {                                                    \
+    if (lanes == 16) MOE_LAUNCH_NORM(16, 1);              \
+    else if (lanes == 32) MOE_LAUNCH_NORM(32, 1);         \
+    else if (lanes == 64) MOE_LAUNCH_NORM_CHUNKS(64);     \
+    else if (lanes == 128) MOE_LAUNCH_NORM_CHUNKS(128);   \
+    else if (lanes == 256) MOE_LAUNCH_NORM_CHUNKS(256);   \
+    else MOE_LAUNCH_NORM_CHUNKS(512);                     \
   } while (0)
 
 extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const uint16_t* x, const uint16_t* addend, const uint16_t* gamma,
@@ -377,17 +389,15 @@ extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const
   MOE_REQUIRE_ALIGNED(y); MOE_REQUIRE_ALIGNED(mean); MOE_REQUIRE_ALIGNED(rstd);
   hipStream_t st = (hipStream_t)stream;
   const NormFwdArgs A = {rows, cols, eps, 1.0f / cols, x, addend, gamma, beta, sum, y, mean, rstd};
-#define MOE_LAUNCH_NORM(W_, CH_)                                                                                              \
-  do {                                                                                                                        \
-    const dim3 grid((unsigned)((rows + (W_ < 4 ? 4 / W_ : 1) - 1) / (W_ < 4 ? 4 / W_ : 1))), block(W_ < 4 ? 256 : W_ * kWave); \
-    if (centre) MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<W_, CH_, true>), grid, block, 0, st, A);                          \
-    else MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<W_, CH_, false>), grid, block, 0, st, A);                                \
+#define MOE_LAUNCH_NORM(L_, CH_)                                                                     \
+  do {                                                                                               \
+    constexpr int per_block = L_ < 256 ? 256 / L_ : 1;                                               \
+    const dim3 grid((unsigned)((rows + per_block - 1) / per_block)), block(L_ < 256 ? 256 : L_);     \
+    if (centre) MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<L_, CH_, true>), grid, block, 0, st, A); \
+    else MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<L_, CH_, false>), grid, block, 0, st, A);       \
   } while (0)
-  const int waves = norm_fwd_waves(cols, addend != nullptr);
-  if (waves == 1) MOE_LAUNCH_NORM_CHUNKS(1);
-  else if (waves == 2) MOE_LAUNCH_NORM_CHUNKS(2);
-  else if (waves == 4) MOE_LAUNCH_NORM_CHUNKS(4);
-  else MOE_LAUNCH_NORM_CHUNKS(8);
+  const int lanes = norm_fwd_lanes(cols, addend != nullptr);
+  MOE_LAUNCH_NORM_LANES(lanes);
 #undef MOE_LAUNCH_NORM
   return launch_status();
 }
@@ -422,20 +432,17 @@ extern "C" int moe_norm_bwd(int64_t rows, int cols, int centre, const uint16_t* 
   if (rows > 0) {
     const NormBwdArgs A = {rows, cols, 1.0f / cols, dy, h, gamma, mean, rstd, dx_addend, dx, one ? nullptr : part, blocks, dgamma, dbeta, accumulate};
     const dim3 grid(blocks + (one && weights ? (cols + kWave - 1) / kWave : 0));
-#define MOE_LAUNCH_NORM_BETA(W_, CH_, C_, B_) \
-  MOE_LAUNCH("norm_bwd", st, (norm_bwd_kernel<W_, CH_, C_, B_>), grid, dim3(W_ < 4 ? 256 : W_ * kWave), 0, st, A)
-#define MOE_LAUNCH_NORM(W_, CH_)                                                  \
-  do {                                                                            \
-    if (centre && dbeta) MOE_LAUNCH_NORM_BETA(W_, CH_, true, true);               \
-    else if (centre) MOE_LAUNCH_NORM_BETA(W_, CH_, true, false);                  \
-    else if (dbeta) MOE_LAUNCH_NORM_BETA(W_, CH_, false, true);                   \
-    else MOE_LAUNCH_NORM_BETA(W_, CH_, false, false);                             \
+#define MOE_LAUNCH_NORM_BETA(L_, CH_, C_, B_) \
+  MOE_LAUNCH("norm_bwd", st, (norm_bwd_kernel<L_, CH_, C_, B_>), grid, dim3(L_ < 256 ? 256 : L_), 0, st, A)
+#define MOE_LAUNCH_NORM(L_, CH_)                                    \
+  do {                                                              \
+    if (centre && dbeta) MOE_LAUNCH_NORM_BETA(L_, CH_, true, true); \
+    else if (centre) MOE_LAUNCH_NORM_BETA(L_, CH_, true, false);    \
+    else if (dbeta) MOE_LAUNCH_NORM_BETA(L_, CH_, false, true);     \
+    else MOE_LAUNCH_NORM_BETA(L_, CH_, false, false);               \
   } while (0)
-    const int waves = norm_bwd_waves(cols);
-    if (waves == 1) MOE_LAUNCH_NORM_CHUNKS(1);
-    else if (waves == 2) MOE_LAUNCH_NORM_CHUNKS(2);
-    else if (waves == 4) MOE_LAUNCH_NORM_CHUNKS(4);
-    else MOE_LAUNCH_NORM_CHUNKS(8);
+    const int lanes = norm_bwd_lanes(cols);
+    MOE_LAUNCH_NORM_LANES(lanes);
 #undef MOE_LAUNCH_NORM
 #undef MOE_LAUNCH_NORM_BETA
   }

@@ -279,11 +279,22 @@ def _ptr(t, dtype=None, numel: Optional[int] = None, name: str = "tensor"):
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(_device())
+    return _find_stream()
+
+
+_raw_stream = _device = None   # the current stream's handle of a device, and the current device: no Stream object is made for them
+
+
+def _find_stream():
+    global _raw_stream, _device
     torch = _torch_module or _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (the handle alone: no Stream object is made for it)
-    if raw is None or not torch.cuda.is_initialized():
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None or not torch.cuda.is_initialized():
         return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
+    _raw_stream, _device = raw, device   # (initialised once, it stays so)
+    return raw(device())
 
 
 def _check(fn: str, rc: int):
@@ -608,73 +619,94 @@ def norm_workspace_bytes(rows, cols) -> int:
     return int(load_library().moe_norm_workspace_bytes(rows, cols))
 
 
+def _as(dtype, t, numel, name):
+    """_ptr of one dtype, for the calls that are short: the checks in the order in which they cost least."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    return _ptr(t, _bf16_types() if dtype is _torch_module.bfloat16 else dtype, numel, name)
+
+
+def _stream_of(t, stream):
+    """_stream for a call on t, whose device has to be the current one: a launch goes there."""
+    handle = _stream(stream)
+    if _device is not None and t.get_device() != _device():
+        raise ValueError(f"tensors on {t.device}: the call belongs within torch.cuda.device of it")
+    return handle
+
+
 def _workspace(ws):
     return (None, 0) if ws is None else (_ptr(ws, None, None, "ws"), ws.numel() * ws.element_size())
 
 
 def moe_gate_fwd(shape, gate, logits, bias, topk_idx, topk_w, stream=None):
     torch = _torch_module or _torch()
-    s = Shape.of(shape)
-    rc = load_library().moe_gate_fwd(
-        ctypes.byref(s._c), ctypes.byref(gate._c), _ptr(logits, torch.float32, s.T * s.E, "logits"), _ptr(bias, torch.float32, s.E, "bias"),
-        _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _stream(stream))
-    _check("moe_gate_fwd", rc)
+    s, f32 = Shape.of(shape), torch.float32
+    rc = (_lib or load_library()).moe_gate_fwd(
+        ctypes.byref(s._c), ctypes.byref(gate._c), _as(f32, logits, s.T * s.E, "logits"), _as(f32, bias, s.E, "bias"),
+        _as(torch.int32, topk_idx, s.N, "topk_idx"), _as(f32, topk_w, s.N, "topk_w"), _stream_of(logits, stream))
+    if rc:
+        _check("moe_gate_fwd", rc)
 
 
 def moe_router_gate_fwd(shape, gate, x, w_router, bias, logits, topk_idx, topk_w, ws, stream=None):
     torch = _torch_module or _torch()
-    s = Shape.of(shape)
-    bf = _bf16_types()
-    rc = load_library().moe_router_gate_fwd(
-        ctypes.byref(s._c), ctypes.byref(gate._c), _ptr(x, bf, s.T * s.d_model, "x"), _ptr(w_router, bf, s.E * s.d_model, "w_router"),
-        _ptr(bias, torch.float32, s.E, "bias"), _ptr(logits, torch.float32, s.T * s.E, "logits"), _ptr(topk_idx, torch.int32, s.N, "topk_idx"),
-        _ptr(topk_w, torch.float32, s.N, "topk_w"), *_workspace(ws), _stream(stream))
-    _check("moe_router_gate_fwd", rc)
+    s, f32, bf = Shape.of(shape), torch.float32, torch.bfloat16
+    rc = (_lib or load_library()).moe_router_gate_fwd(
+        ctypes.byref(s._c), ctypes.byref(gate._c), _as(bf, x, s.T * s.d_model, "x"), _as(bf, w_router, s.E * s.d_model, "w_router"),
+        _as(f32, bias, s.E, "bias"), _as(f32, logits, s.T * s.E, "logits"), _as(torch.int32, topk_idx, s.N, "topk_idx"), _as(f32, topk_w, s.N, "topk_w"),
+        *_workspace(ws), _stream_of(x, stream))
+    if rc:
+        _check("moe_router_gate_fwd", rc)
 
 
 def moe_gate_bwd(shape, gate, dtopk_w, logits, topk_idx, topk_w, counts, balance, dlogits, loss=None, ws=None, stream=None):
     """counts None: no balance loss.  loss [1] fp32 needs counts and a workspace."""
     torch = _torch_module or _torch()
-    s = Shape.of(shape)
-    rc = load_library().moe_gate_bwd(
-        ctypes.byref(s._c), ctypes.byref(gate._c), _ptr(dtopk_w, torch.float32, s.N, "dtopk_w"), _ptr(logits, torch.float32, s.T * s.E, "logits"),
-        _ptr(topk_idx, torch.int32, s.N, "topk_idx"), _ptr(topk_w, torch.float32, s.N, "topk_w"), _ptr(counts, torch.int32, s.E_total, "counts"),
-        float(balance), _ptr(dlogits, torch.float32, s.T * s.E, "dlogits"), _ptr(loss, torch.float32, 1, "loss"), *_workspace(ws), _stream(stream))
-    _check("moe_gate_bwd", rc)
+    s, f32 = Shape.of(shape), torch.float32
+    rc = (_lib or load_library()).moe_gate_bwd(
+        ctypes.byref(s._c), ctypes.byref(gate._c), _as(f32, dtopk_w, s.N, "dtopk_w"), _as(f32, logits, s.T * s.E, "logits"),
+        _as(torch.int32, topk_idx, s.N, "topk_idx"), _as(f32, topk_w, s.N, "topk_w"), _as(torch.int32, counts, s.E_total, "counts"), balance,
+        _as(f32, dlogits, s.T * s.E, "dlogits"), _as(f32, loss, 1, "loss"), *_workspace(ws), _stream_of(logits, stream))
+    if rc:
+        _check("moe_gate_bwd", rc)
 
 
 def moe_gate_bias_step(shape, counts, rate, bias, stream=None):
     torch = _torch_module or _torch()
     s = Shape.of(shape)
-    rc = load_library().moe_gate_bias_step(ctypes.byref(s._c), _ptr(counts, torch.int32, s.E_total, "counts"), float(rate),
-                                           _ptr(bias, torch.float32, s.E, "bias"), _stream(stream))
-    _check("moe_gate_bias_step", rc)
+    rc = (_lib or load_library()).moe_gate_bias_step(ctypes.byref(s._c), _as(torch.int32, counts, s.E_total, "counts"), rate,
+                                                     _as(torch.float32, bias, s.E, "bias"), _stream_of(counts, stream))
+    if rc:
+        _check("moe_gate_bias_step", rc)
 
 
 def moe_norm_fwd(centre, eps, x, addend, gamma, beta, sum, y, mean, rstd, stream=None):
     """x [..., cols] bf16; addend, gamma, beta, sum, mean and rstd may be None."""
     torch = _torch_module or _torch()
-    bf = _bf16_types()
+    f32, bf = torch.float32, torch.bfloat16
     rows, cols = _last(x, "x")
     n = rows * cols
-    rc = load_library().moe_norm_fwd(
-        rows, cols, int(bool(centre)), float(eps), _ptr(x, bf, n, "x"), _ptr(addend, bf, n, "addend"), _ptr(gamma, bf, cols, "gamma"),
-        _ptr(beta, bf, cols, "beta"), _ptr(sum, bf, n, "sum"), _ptr(y, bf, n, "y"), _ptr(mean, torch.float32, rows, "mean"),
-        _ptr(rstd, torch.float32, rows, "rstd"), _stream(stream))
-    _check("moe_norm_fwd", rc)
+    rc = (_lib or load_library()).moe_norm_fwd(
+        rows, cols, 1 if centre else 0, eps, _as(bf, x, n, "x"), _as(bf, addend, n, "addend"), _as(bf, gamma, cols, "gamma"), _as(bf, beta, cols, "beta"),
+        _as(bf, sum, n, "sum"), _as(bf, y, n, "y"), _as(f32, mean, rows, "mean"), _as(f32, rstd, rows, "rstd"), _stream_of(x, stream))
+    if rc:
+        _check("moe_norm_fwd", rc)
 
 
 def moe_norm_bwd(centre, dy, h, gamma, mean, rstd, dx_addend, dx, dgamma, dbeta, accumulate, ws, stream=None):
     """dy, h [..., cols] bf16; gamma, dx_addend, dgamma, dbeta and (without centre) mean may be None, ws without dgamma and dbeta."""
     torch = _torch_module or _torch()
-    bf = _bf16_types()
+    f32, bf = torch.float32, torch.bfloat16
     rows, cols = _last(h, "h")
     n = rows * cols
-    rc = load_library().moe_norm_bwd(
-        rows, cols, int(bool(centre)), _ptr(dy, bf, n, "dy"), _ptr(h, bf, n, "h"), _ptr(gamma, bf, cols, "gamma"),
-        _ptr(mean, torch.float32, rows, "mean"), _ptr(rstd, torch.float32, rows, "rstd"), _ptr(dx_addend, bf, n, "dx_addend"), _ptr(dx, bf, n, "dx"),
-        _ptr(dgamma, torch.float32, cols, "dgamma"), _ptr(dbeta, torch.float32, cols, "dbeta"), int(bool(accumulate)), *_workspace(ws), _stream(stream))
-    _check("moe_norm_bwd", rc)
+    rc = (_lib or load_library()).moe_norm_bwd(
+        rows, cols, 1 if centre else 0, _as(bf, dy, n, "dy"), _as(bf, h, n, "h"), _as(bf, gamma, cols, "gamma"), _as(f32, mean, rows, "mean"),
+        _as(f32, rstd, rows, "rstd"), _as(bf, dx_addend, n, "dx_addend"), _as(bf, dx, n, "dx"), _as(f32, dgamma, cols, "dgamma"),
+        _as(f32, dbeta, cols, "dbeta"), 1 if accumulate else 0, *_workspace(ws), _stream_of(h, stream))
+    if rc:
+        _check("moe_norm_bwd", rc)
 
 
 # ---- single-GPU steps of the hierarchical all-to-all (device tensors; rows of any dtype, 16-byte multiples) -----

@@ -137,20 +137,21 @@ struct NormBwdArgs {
   const uint16_t* dy; const uint16_t* h; const uint16_t* gamma; const float* mean; const float* rstd; const uint16_t* dx_addend;
   uint16_t* dx;
   float* part;          // [row_blocks][2][cols]: a block's sums of dy xh and of dy; null: not wanted, or made by blocks of their own
-  int row_blocks;       // blocks behind them make dgamma and dbeta, 64 columns each
+  int row_blocks;       // blocks behind them make dgamma and dbeta, kNormColumns columns each
   float* dgamma; float* dbeta;
   int accumulate;
 };
 
-// dgamma and dbeta of 64 columns from dy and h themselves: the wavefronts take rows in turn, their sums are joined in order.
+// dgamma and dbeta of 32 columns from dy and h themselves: the wavefronts take rows in turn, their sums are joined in order.
+constexpr int kNormColumns = 32;
 template <int WAVES_IN_BLOCK, bool CENTRE>
 __device__ __forceinline__ void weights_of_columns(const NormBwdArgs& A, int block, float* join) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int pair = lane % 32, half = lane / 32, col = block * kWave + 2 * pair;   // two columns a lane, two rows a wavefront
+  const int pair = lane % 16, quarter = lane / 16, col = block * kNormColumns + 2 * pair;   // two columns a lane, four rows a wavefront
   float g0 = 0.f, g1 = 0.f, b0 = 0.f, b1 = 0.f;
   if (col < A.cols) {
 #pragma unroll 8
-    for (long long row = 2 * wave + half; row < A.rows; row += 2 * WAVES_IN_BLOCK) {
+    for (long long row = 4 * wave + quarter; row < A.rows; row += 4 * WAVES_IN_BLOCK) {
       const uint32_t d = *reinterpret_cast<const uint32_t*>(A.dy + (size_t)row * A.cols + col);
       const uint32_t h = *reinterpret_cast<const uint32_t*>(A.h + (size_t)row * A.cols + col);
       const float mean = CENTRE ? A.mean[row] : 0.f, rstd = A.rstd[row];
@@ -160,15 +161,15 @@ __device__ __forceinline__ void weights_of_columns(const NormBwdArgs& A, int blo
       b1 += bf16hi(d);
     }
   }
-  float* mine = join + (size_t)(2 * wave + half) * 4 * 32 + pair;   // [row group][4][32]
-  mine[0] = g0; mine[32] = g1; mine[64] = b0; mine[96] = b1;
+  float* mine = join + (size_t)(4 * wave + quarter) * 4 * 16 + pair;   // [row group][4][16]
+  mine[0] = g0; mine[16] = g1; mine[32] = b0; mine[48] = b1;
   __syncthreads();
-  const int which = threadIdx.x / kWave, c = threadIdx.x % kWave;   // dgamma, dbeta
+  const int which = threadIdx.x / kNormColumns, c = threadIdx.x % kNormColumns;   // dgamma, dbeta
   float* out = which == 0 ? A.dgamma : which == 1 ? A.dbeta : nullptr;
-  if (out == nullptr || block * kWave + c >= A.cols) return;
-  float v = A.accumulate ? out[block * kWave + c] : 0.f;
-  for (int i = 0; i < 2 * WAVES_IN_BLOCK; i++) v += join[(size_t)i * 4 * 32 + (2 * which + c % 2) * 32 + c / 2];
-  out[block * kWave + c] = v;
+  if (out == nullptr || block * kNormColumns + c >= A.cols) return;
+  float v = A.accumulate ? out[block * kNormColumns + c] : 0.f;
+  for (int i = 0; i < 4 * WAVES_IN_BLOCK; i++) v += join[(size_t)i * 4 * 16 + (2 * which + c % 2) * 16 + c / 2];
+  out[block * kNormColumns + c] = v;
 }
 
 // Rows in turn for THREADS lanes each; a lane keeps gamma and the sums of its columns, and requests the next row before it computes this one.
@@ -176,7 +177,7 @@ template <int THREADS, int CH, bool CENTRE, bool BETA>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_bwd_kernel(NormBwdArgs A) {
   constexpr int BLOCK_WAVES = THREADS < 256 ? 4 : THREADS / kWave, WAVES = THREADS < kWave ? 1 : THREADS / kWave, ROWS = BLOCK_WAVES * kWave / THREADS;
   constexpr bool AHEAD = CH <= 2;   // (registers)
-  constexpr int JOIN = (ROWS - 1) * THREADS * 8, COLUMNS = 2 * BLOCK_WAVES * 4 * 32;
+  constexpr int JOIN = (ROWS - 1) * THREADS * 8, COLUMNS = 4 * BLOCK_WAVES * 4 * 16;
   __shared__ float slots[2][ROWS][2][WAVES];
   __shared__ float join[JOIN > COLUMNS ? JOIN : COLUMNS];
   if ((int)blockIdx.x >= A.row_blocks) {
@@ -351,12 +352,14 @@ static int norm_fwd_lanes(int cols, bool addend) {
 // wavefronts, one of 8.  (Twice and half as many blocks, lanes: 2 to 40 % slower at 512 .. 16384 columns; 2 blocks of 8 are 6 % slower.)
 static int norm_bwd_lanes(int cols) { return cols <= 128 ? 16 : cols <= 256 ? 32 : norm_lanes_of_chunks(cols, 3); }
 static int norm_bwd_blocks(long long rows, int cols) {
-  const int lanes = norm_bwd_lanes(cols), per_block = lanes < 256 ? 256 / lanes : 1, most = lanes < 512 ? 512 : 256;
+  const int lanes = norm_bwd_lanes(cols), per_block = lanes < 256 ? 256 / lanes : 1;
   const long long units = (rows + per_block - 1) / per_block;
+  const int most = lanes < 512 && units >= 2048 ? 512 : 256;   // (half as many for shorter batches: a block's sums are read again.  2048 x 1024 9.5 -> 8.5 us)
   return (int)(units < most ? units : most);
 }
-// dgamma and dbeta by blocks of their own in the launch of dx: they read dy and h again, but there is one launch.
-static bool norm_bwd_one_launch(long long rows, int cols) { return rows <= 1024 && rows * cols <= (1 << 20); }
+// dgamma and dbeta by blocks of their own in the launch of dx: they read dy and h again, but there is one launch, and no sums on the way.  Of one launch
+// and two, us: 256 x 512 3.2, 5.7; 1024 x 1024 5.5, 7.4; 139 x 11464 6.9, 18.7; 1024 x 4096 12.2, 14.4; 2048 x 1024 12.0, 8.5; 4096 x 4096 40, 30.
+static bool norm_bwd_one_launch(long long rows) { return rows <= 1024; }
 
 }  // namespace moe
 
@@ -428,10 +431,10 @@ extern "C" int moe_norm_bwd(int64_t rows, int cols, int centre, const uint16_t* 
   hipStream_t st = (hipStream_t)stream;
   const int blocks = norm_bwd_blocks(rows, cols);
   float* part = weights ? (float*)ws : nullptr;
-  const bool one = rows > 0 && norm_bwd_one_launch(rows, cols) && dx != dy;   // (dy is still read when dx is written)
+  const bool one = rows > 0 && norm_bwd_one_launch(rows) && dx != dy;   // (dy is still read when dx is written)
   if (rows > 0) {
     const NormBwdArgs A = {rows, cols, 1.0f / cols, dy, h, gamma, mean, rstd, dx_addend, dx, one ? nullptr : part, blocks, dgamma, dbeta, accumulate};
-    const dim3 grid(blocks + (one && weights ? (cols + kWave - 1) / kWave : 0));
+    const dim3 grid(blocks + (one && weights ? (cols + kNormColumns - 1) / kNormColumns : 0));
 #define MOE_LAUNCH_NORM_BETA(L_, CH_, C_, B_) \
   MOE_LAUNCH("norm_bwd", st, (norm_bwd_kernel<L_, CH_, C_, B_>), grid, dim3(L_ < 256 ? 256 : L_), 0, st, A)
 #define MOE_LAUNCH_NORM(L_, CH_)                                    \

@@ -13,6 +13,7 @@ namespace moe {
 
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
 constexpr float kMaxLogit = 3.402823466e38f;
+constexpr int kGateFewWaves = 1024;   // up to so many wavefronts a token has more lanes than it needs
 constexpr int kGateBwdBlocks = 512;     // at most; each adds up its tokens' share of the loss
 
 struct GateArgs {
@@ -27,107 +28,97 @@ __device__ __forceinline__ float gate_finite(float l) { return l > kMaxLogit ? k
 // sigmoid(l) / sigmoid-like factor exp(top) with top = min(0, the largest logit that is looked at): scores far below zero keep their ratios.
 __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f / (expf(top - l) + expf(top)); }
 
-// A token's choices in 64 bits by a wavefront: any number of groups and experts, any k.  Lane g holds experts g, g + 64, ...; k rounds of finding the best
-// one left.  Choice j comes back on lane j % 64 in held[j / 64].  row_c: LDS of E + groups doubles.
+// A token's choices in 64 bits by a wavefront: any number of groups and experts, any k; k rounds of finding the best one left.  Choice j comes back on
+// lane j % 64 in held[j / 64].  c: LDS of E + groups doubles.  The loops are not unrolled: where this is the way out of the other kernel, one wavefront in
+// a thousand takes it, and what it waits for is its instructions (16384 tokens of 128 experts: 10.4 us with 1700 of them).
 template <int PER>
-__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* row_c, int (&held)[PER], const GateArgs& A) {
+__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A) {
   const int lane = threadIdx.x % kWave, E = A.E;
-  const double NEG = -__builtin_inf();
-  const bool by_logits = bias == nullptr, need_scores = !by_logits || A.group_best > 1;
-  float l[PER], m = -kMaxLogit;
-#pragma unroll
-  for (int p = 0; p < PER; p++) {
-    const int e = lane + p * kWave;
-    l[p] = e < E ? gate_finite(row[e]) : -__builtin_inff();
-    if (!gate_masked(l[p])) m = fmaxf(m, l[p]);
-  }
-  m = lanes_max<kWave>(m);
-  double s[PER], z = 0.0;
-#pragma unroll
-  for (int p = 0; p < PER; p++) s[p] = 0.0;
-  if (need_scores) {
-#pragma unroll
-    for (int p = 0; p < PER; p++)
-      if (!gate_masked(l[p])) {
-        s[p] = A.sigmoid ? 1.0 / (1.0 + exp(-(double)l[p])) : exp((double)l[p] - (double)m);
-        z += s[p];
-      }
-    if (!A.sigmoid) {
-      z = lanes_sum<kWave>(z);
-#pragma unroll
-      for (int p = 0; p < PER; p++)
-        if (!gate_masked(l[p])) s[p] /= z;
+  constexpr double OUT = -__builtin_inf(), LAST = -1.7e308;   // not to be chosen; masked: after all others
+  const bool by_logits = bias == nullptr, by_score = by_logits && A.group_best > 1;   // (a sum of logits would say nothing)
+  double z = 1.0;
+  if (!A.sigmoid && (!by_logits || by_score)) {
+    float m = -kMaxLogit;
+#pragma unroll 1
+    for (int e = lane; e < E; e += kWave) {
+      const float l = gate_finite(row[e]);
+      if (!gate_masked(l)) m = fmaxf(m, l);
     }
-  }
-  double c[PER];
-  bool taken[PER];
-#pragma unroll
-  for (int p = 0; p < PER; p++) {
-    const int e = lane + p * kWave;
-    taken[p] = e >= E;
-    c[p] = NEG;
-    if (!gate_masked(l[p])) {
-      const double b = by_logits ? (double)l[p] : s[p] + (double)bias[e];
-      if (b > (double)kMaskedLogit) c[p] = b;
+    m = lanes_max<kWave>(m);
+    z = 0.0;
+#pragma unroll 1
+    for (int e = lane; e < E; e += kWave) {
+      const float l = gate_finite(row[e]);
+      c[e] = gate_masked(l) ? 0.0 : exp((double)l - (double)m);
+      z += c[e];
     }
+    z = lanes_sum<kWave>(z);
   }
+#pragma unroll 1
+  for (int e = lane; e < E; e += kWave) {
+    const float l = gate_finite(row[e]);
+    double v = (double)l;
+    if (!by_logits || by_score) v = A.sigmoid ? 1.0 / (1.0 + exp(-(double)l)) : c[e] / z;
+    if (!by_logits) v += (double)bias[e];
+    c[e] = gate_masked(l) || !(v > (double)kMaskedLogit) ? LAST : v;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   if (A.groups > 1) {
     const int S = E / A.groups;
-    const bool by_score = by_logits && A.group_best > 1;   // (a sum of logits would say nothing)
-    double* group_c = row_c + E;
-#pragma unroll
-    for (int p = 0; p < PER; p++)
-      if (lane + p * kWave < E) row_c[lane + p * kWave] = by_score && c[p] != NEG ? s[p] : c[p];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    double* group_c = c + E;
+#pragma unroll 1
     for (int g = lane; g < A.groups; g += kWave) {
-      double first = NEG, second = NEG;
-#pragma unroll 8
+      double first = LAST, second = LAST;
+#pragma unroll 4
       for (int i = 0; i < S; i++) {
-        const double v = row_c[g * S + i];
+        const double v = c[g * S + i];
         second = fmax(second, fmin(first, v));
         first = fmax(first, v);
       }
-      group_c[g] = A.group_best > 1 && second != NEG ? first + second : first;
+      group_c[g] = A.group_best > 1 && second != LAST ? first + second : first;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int g = lane; g < A.groups; g += kWave) {   // (whether a group stays, over the c that are not read any more)
+#pragma unroll 1
+    for (int g = lane; g < A.groups; g += kWave) {
       const double v = group_c[g];
       int better = 0;
-#pragma unroll 8
+#pragma unroll 4
       for (int o = 0; o < A.groups; o++) {
         const double u = group_c[o];
         better += u > v || (u == v && o < g);
       }
-      row_c[g] = better < A.groups_kept ? 1.0 : 0.0;
+      if (better >= A.groups_kept)
+        for (int i = 0; i < S; i++) c[g * S + i] = OUT;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int p = 0; p < PER; p++)
-      if (lane + p * kWave < E && row_c[(lane + p * kWave) / S] == 0.0) taken[p] = true;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (before the next token's)
+    if (by_score) {   // (the scores were for the groups)
+#pragma unroll 1
+      for (int e = lane; e < E; e += kWave)
+        if (c[e] != OUT && c[e] != LAST) c[e] = (double)gate_finite(row[e]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
   }
 #pragma unroll
   for (int p = 0; p < PER; p++) held[p] = 0;
-  // (masked experts of groups that stay are still there when all others are taken: below them the ones that are not to be chosen)
-  constexpr double LEAST = -1.7e308;
-#pragma unroll
-  for (int p = 0; p < PER; p++) c[p] = taken[p] ? NEG : c[p] == NEG ? LEAST : c[p];
+#pragma unroll 1
   for (int j = 0; j < A.k; j++) {
-    double bv = c[0];
-#pragma unroll
-    for (int p = 1; p < PER; p++) bv = fmax(bv, c[p]);
-    bv = lanes_max<kWave>(bv);
-    int bi = 0;
-#pragma unroll
-    for (int p = PER - 1; p >= 0; p--) {   // (of equal values the lowest expert: the last to be written)
-      const unsigned long long at = __ballot(c[p] == bv);
-      if (at != 0) bi = p * kWave + __builtin_ctzll(at);
-    }
-#pragma unroll
+    double best = OUT;
+    int at = 0;   // a lane's best and its first place
+#pragma unroll 4
     for (int p = 0; p < PER; p++) {
-      if (lane + p * kWave == bi) c[p] = NEG;
-      if (lane == j % kWave && p == j / kWave) held[p] = bi;
+      const int e = lane + p * kWave;
+      const double v = e < E ? c[e] : OUT;
+      at = v > best ? e : at;
+      best = fmax(best, v);
     }
+    const double top = lanes_max<kWave>(best);
+    // of the lanes that have it the lowest place
+    const int choice = -(int)lanes_max<kWave>(best == top ? (float)-at : -2048.f);
+    if (choice % kWave == lane) c[choice] = OUT;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int p = 0; p < PER; p++)
+      if (lane == j % kWave && p == j / kWave) held[p] = choice;
   }
 }
 
@@ -813,16 +804,18 @@ static int gate_checks(const moe_shape* shape, const moe_gate* gate, Dims* D, Ga
   return MOE_OK;
 }
 
-// W lanes per token (0: the general kernel): as few as hold its groups, and its experts 32 each.
+// W lanes per token (0: the general kernel): as few as hold its groups, and its experts 32 each; of few tokens as many as leave a lane K of them, up to a
+// wavefront a SIMD: there a lane's instructions are the time.
 static int gate_lanes(const GateArgs& A, GatePlan* P) {
   if (A.k > 16 || A.groups > kWave) return 0;
   int padded = 1;   // groups, filled up to a power of two
   while (padded < A.groups) padded *= 2;
-  const int size = A.E / A.groups;
-  for (int W = A.k > 8 ? 16 : 8; W <= kWave; W *= 2) {
+  const int size = A.E / A.groups, K = A.k > 8 ? 16 : 8;
+  for (int W = K; W <= kWave; W *= 2) {
     if (padded > W) continue;
     const int lanes = W / padded, piece = (size + lanes - 1) / lanes;
     if (piece > 32) continue;
+    if (piece > K && W < kWave && (long long)A.T * 2 * W <= kWave * kGateFewWaves) continue;
     *P = GatePlan{lanes, __builtin_ctz(lanes), size, piece};
     return W;
   }

@@ -28,67 +28,95 @@ __device__ __forceinline__ float gate_finite(float l) { return l > kMaxLogit ? k
 // sigmoid(l) / sigmoid-like factor exp(top) with top = min(0, the largest logit that is looked at): scores far below zero keep their ratios.
 __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f / (expf(top - l) + expf(top)); }
 
-// A token's choices in 64 bits by a wavefront: any number of groups and experts, any k; k rounds of finding the best one left.  Choice j comes back on
-// lane j % 64 in held[j / 64].  c: LDS of E + groups doubles.  The loops are not unrolled: where this is the way out of the other kernel, one wavefront in
-// a thousand takes it, and what it waits for is its instructions (16384 tokens of 128 experts: 10.4 us with 1700 of them).
+// A token's choices in 64 bits by a wavefront: any number of groups and experts, any k.  Choice j comes back on lane j % 64 in held[j / 64].  c: LDS of
+// E + groups doubles, of E + 96 with `from`: where the choices are known to be among the experts whose c is at least that, these (mostly k, or one more)
+// are put in order; else k rounds find the best one left.  Where this is the way out of the other kernel, one wavefront in a thousand takes it, alone:
+// its time is that of one instruction after another.
 template <int PER>
-__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A) {
+__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A,
+                                               float from) {
   const int lane = threadIdx.x % kWave, E = A.E;
   constexpr double OUT = -__builtin_inf(), LAST = -1.7e308;   // not to be chosen; masked: after all others
   const bool by_logits = bias == nullptr, by_score = by_logits && A.group_best > 1;   // (a sum of logits would say nothing)
-  double z = 1.0;
-  if (!A.sigmoid && (!by_logits || by_score)) {
-    float m = -kMaxLogit;
-#pragma unroll 1
-    for (int e = lane; e < E; e += kWave) {
-      const float l = gate_finite(row[e]);
-      if (!gate_masked(l)) m = fmaxf(m, l);
-    }
-    m = lanes_max<kWave>(m);
-    z = 0.0;
-#pragma unroll 1
-    for (int e = lane; e < E; e += kWave) {
-      const float l = gate_finite(row[e]);
-      c[e] = gate_masked(l) ? 0.0 : exp((double)l - (double)m);
-      z += c[e];
-    }
-    z = lanes_sum<kWave>(z);
+  constexpr int UN = PER < 4 ? PER : 4;
+  float m = -kMaxLogit;
+#pragma unroll UN
+  for (int p = 0; p < PER; p++) {
+    const int e = lane + p * kWave;
+    const float l = gate_finite(row[min(e, E - 1)]);
+    if (e < E) c[e] = gate_masked(l) ? LAST : (double)l;
+    m = gate_masked(l) ? m : fmaxf(m, l);
   }
-#pragma unroll 1
-  for (int e = lane; e < E; e += kWave) {
-    const float l = gate_finite(row[e]);
-    double v = (double)l;
-    if (!by_logits || by_score) v = A.sigmoid ? 1.0 / (1.0 + exp(-(double)l)) : c[e] / z;
-    if (!by_logits) v += (double)bias[e];
-    c[e] = gate_masked(l) || !(v > (double)kMaskedLogit) ? LAST : v;
+  if (!by_logits || by_score) {
+    double z = 1.0;
+    if (!A.sigmoid) {
+      m = lanes_max<kWave>(m);
+      z = 0.0;
+    }
+#pragma unroll UN
+    for (int p = 0; p < PER; p++) {
+      const int e = min(lane + p * kWave, E - 1);
+      const double l = lane + p * kWave < E ? c[e] : LAST, x = exp(A.sigmoid ? -l : l - (double)m);
+      const double v = A.sigmoid ? 1.0 / (1.0 + x) : x;
+      if (l != LAST) {
+        c[e] = v;
+        z += v;
+      }
+    }
+    const double over = A.sigmoid ? 1.0 : 1.0 / lanes_sum<kWave>(z);
+#pragma unroll UN
+    for (int p = 0; p < PER; p++) {
+      const int e = min(lane + p * kWave, E - 1);
+      double v = lane + p * kWave < E ? c[e] : LAST;
+      if (v != LAST) {
+        v = A.sigmoid ? v : v * over;
+        if (!by_logits) v += (double)bias[e];
+        c[e] = v > (double)kMaskedLogit ? v : LAST;
+      }
+    }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   if (A.groups > 1) {
     const int S = E / A.groups;
     double* group_c = c + E;
+    int L = kWave;   // lanes of a group: as many as there are for all of them at once, one if there are more
+    while (L > 1 && L * A.groups > kWave) L >>= 1;
+    const int sub = lane & (L - 1), per_turn = kWave / L, log2_L = __builtin_ctz(L);
 #pragma unroll 1
-    for (int g = lane; g < A.groups; g += kWave) {
+    for (int g0 = 0; g0 < A.groups; g0 += per_turn) {
+      const int g = g0 + (lane >> log2_L);
       double first = LAST, second = LAST;
+      if (g < A.groups) {
 #pragma unroll 4
-      for (int i = 0; i < S; i++) {
-        const double v = c[g * S + i];
-        second = fmax(second, fmin(first, v));
-        first = fmax(first, v);
+        for (int i = sub; i < S; i += L) {
+          const double v = c[g * S + i];
+          second = fmax(second, fmin(first, v));
+          first = fmax(first, v);
+        }
       }
-      group_c[g] = A.group_best > 1 && second != LAST ? first + second : first;
+#pragma unroll 1
+      for (int o = 1; o < L; o <<= 1) {
+        const double f = __shfl_xor(first, o, kWave), n = __shfl_xor(second, o, kWave);
+        second = fmax(fmax(second, n), fmin(first, f));
+        first = fmax(first, f);
+      }
+      if (g < A.groups && sub == 0) group_c[g] = A.group_best > 1 && second != LAST ? first + second : first;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-    for (int g = lane; g < A.groups; g += kWave) {
+    for (int g0 = 0; g0 < A.groups; g0 += per_turn) {
+      const int g = min(g0 + (lane >> log2_L), A.groups - 1);
       const double v = group_c[g];
       int better = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (int o = 0; o < A.groups; o++) {
         const double u = group_c[o];
         better += u > v || (u == v && o < g);
       }
-      if (better >= A.groups_kept)
-        for (int i = 0; i < S; i++) c[g * S + i] = OUT;
+      if (better >= A.groups_kept) {
+#pragma unroll 4
+        for (int i = sub; i < S; i += L) c[g * S + i] = OUT;
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (by_score) {   // (the scores were for the groups)
@@ -100,6 +128,37 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
   }
 #pragma unroll
   for (int p = 0; p < PER; p++) held[p] = 0;
+  if (from > kMaskedLogit) {
+    double* found_c = c + E;
+    int* found = reinterpret_cast<int*>(found_c + kWave);
+    int n = 0;
+#pragma unroll UN
+    for (int p = 0; p < PER; p++) {
+      const int e = lane + p * kWave;
+      const double v = e < E ? c[e] : OUT;
+      const bool one = v >= (double)from;
+      const unsigned long long all = __ballot(one);
+      const int at = n + __popcll(all & ((1ull << lane) - 1));
+      if (one && at < kWave) {
+        found_c[at] = v;
+        found[at] = e;
+      }
+      n += __popcll(all);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (n <= kWave) {
+      const double v = lane < n ? found_c[lane] : OUT;
+      const int e = lane < n ? found[lane] : 0;
+      int place = 0;
+#pragma unroll 8
+      for (int o = 0; o < n; o++) place += found_c[o] > v || (found_c[o] == v && found[o] < e);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (lane < n) found[place] = e;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      held[0] = lane < A.k ? found[lane] : 0;
+      return;
+    }
+  }
 #pragma unroll 1
   for (int j = 0; j < A.k; j++) {
     double best = OUT;
@@ -133,7 +192,7 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
   const int E = A.E, k = A.k, Kp = k + A.Es;
   const float* row = logits + (size_t)t * E;
   int held[PER];
-  choose_exactly<PER>(row, bias, row_c[wave], held, A);
+  choose_exactly<PER>(row, bias, row_c[wave], held, A, -__builtin_inff());
   float m = -kMaxLogit, all = 0.f;
   if (!A.sigmoid && !A.renorm) {
     float l[PER];
@@ -278,7 +337,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   constexpr int MAX_E = W * PER < kMaxExperts ? W * PER : kMaxExperts;
   constexpr int RUN = FULL ? PER : 32;
   constexpr int ROW_FLOATS = kWave * (PER + 4) + PER;                   // (gate_place; the last lane reads on behind its run)
-  constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave);                     // what choose_exactly takes of them
+  constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave + kWave / 2);         // what choose_exactly takes of them
   __shared__ __attribute__((aligned(16))) float rows[4][ROW_FLOATS > EXACT_FLOATS ? ROW_FLOATS : EXACT_FLOATS];
   __shared__ double group_scores[4][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane % W, tt = lane / W;
@@ -453,7 +512,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     }
   }
   float lane_last = PER > K && track && !track_lane ? key_value(best[K - 1]) : kNoKey;   // (nothing that the lane has let go is above it)
-  bool unsure = false;
+  bool unsure = false, unsure_group = false;
 
   auto select_groups = [&]() __attribute__((always_inline)) {
     const float a = key_value(best[0]), b = key_value(best[1]);
@@ -481,7 +540,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       // Two c, off as above, and a rounding of their sum, for two groups; the c themselves may be large and cancel.  Scores without a bias: of sigmoid
       // as above, of softmax (without the shared sum, each at most 1) the argument, the exponential, the sum: under 8 in all.
       const float far = by_logits ? 0x1p-20f : 2.0f * slack + slack_c * (fabsf(low) + lanes_max<W>(a > kMaskedLogit ? fabsf(a) + (b > kMaskedLogit ? fabsf(b) : 0.f) : 0.f));
-      unsure = unsure || (high > kMaskedLogit && low - high <= far);
+      unsure_group = unsure_group || (high > kMaskedLogit && low - high <= far);
     }
     const double none = make_key(kNoKey, 0, false);
 #pragma unroll
@@ -526,13 +585,17 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   }
   const bool live = t < A.T && g < k;
   float x = live ? rows[wave][gate_place<RUN>(tt * E + choice)] : -__builtin_inff();
-  unsigned long long again = __ballot(unsure && t < A.T);
+  unsigned long long again = __ballot((unsure || unsure_group) && t < A.T);
   if (again) {   // (the logits in LDS make room)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // the k-th c, and how far below it one may be that belongs before it
+    const float kth = by_logits || unsure_group ? -__builtin_inff() : __shfl(key_value(mine), lane - g + k - 1, kWave);
+    const float least = kth - (slack + slack_c * (fabsf(kth) + slack));
     do {
       const int token = __builtin_ctzll(again) / W;
       int held[(MAX_E + kWave - 1) / kWave];
-      choose_exactly<(MAX_E + kWave - 1) / kWave>(logits + (size_t)(t0 + token) * E, bias, reinterpret_cast<double*>(rows[wave]), held, A);
+      choose_exactly<(MAX_E + kWave - 1) / kWave>(logits + (size_t)(t0 + token) * E, bias, reinterpret_cast<double*>(rows[wave]), held, A,
+                                                   __shfl(least, token * W, kWave));
       const int found = __shfl(held[0], g, kWave);
       if (tt == token) choice = found;
       again &= ~((W == kWave ? ~0ull : (1ull << (W & 63)) - 1) << (token * W));

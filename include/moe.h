@@ -178,7 +178,7 @@ int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const uint16_t* 
  *   dx = rstd (g - mean(g) - xh mean(g xh)) + dx_addend     (without mean(g) where centre == 0), fp32, one bf16 rounding
  *   dgamma = sum over the rows of dy xh,  dbeta = sum over the rows of dy: fp32, overwritten (accumulate == 0; zeros without rows) or added to
  *   dy [rows, cols] bf16 in;  h [rows, cols] bf16 in (x, or what the forward call wrote to `sum`);  gamma, mean, rstd as of the forward call
- *   dx_addend [rows, cols] bf16 in, may be NULL (the gradient that reaches h past the norm);  dx [rows, cols] bf16 out, may be dy or dx_addend itself
+ *   dx_addend [rows, cols] bf16 in, may be NULL (the gradient that reaches h past the norm);  dx [rows, cols] bf16 out, may be dy, h or dx_addend itself
  *   dgamma, dbeta [cols] fp32 out, may be NULL each.
  * dx is the gradient of x and of addend alike.  Workspace: moe_norm_workspace_bytes(rows, cols) bytes (0 if these are outside the limits).  Sums over
  * the rows are made in a fixed order. */

@@ -14,6 +14,7 @@ namespace moe {
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
 constexpr float kMaxLogit = 3.402823466e38f;
 constexpr int kGateFewWaves = 1024;   // up to so many wavefronts a token has more lanes than it needs
+constexpr int kGateTokens = 1 << 24;   // of a launch of the forward kernels at most: a grid has less than 2^32 threads
 constexpr int kGateBwdBlocks = 512;     // at most; each adds up its tokens' share of the loss
 
 struct GateArgs {
@@ -146,7 +147,7 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
       n += __popcll(all);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (n <= kWave) {
+    if (n >= A.k && n <= kWave) {
       const double v = lane < n ? found_c[lane] : OUT;
       const int e = lane < n ? found[lane] : 0;
       int place = 0;
@@ -665,7 +666,7 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(cons
     }
   };
   float loss = 0.f;
-  const int batches = (A.T + TOKENS - 1) / TOKENS, step = gridDim.x * kGateBwdWaves;
+  const int batches = (A.T - 1) / TOKENS + 1, step = gridDim.x * kGateBwdWaves;
   struct Batch { float l[4 * C]; int e; float w, dw; };   // what a batch of tokens reads: requested while the one before is computed
   auto request = [&](int batch, Batch& b) __attribute__((always_inline)) {
     const size_t at = (size_t)min(batch * TOKENS + tt, A.T - 1);
@@ -900,7 +901,15 @@ static void launch_gate_lanes(hipStream_t st, const GateArgs& A, const GatePlan&
   else launch_gate_kernel<K, W, 32>(st, A, P, logits, bias, topk_idx, topk_w);
 }
 
-static void launch_gate(hipStream_t st, const GateArgs& A, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
+static void launch_gate(hipStream_t st, const GateArgs& all, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
+  GateArgs A = all;
+  if (A.T > kGateTokens) {
+    for (long long t = 0; t < all.T; t += kGateTokens) {
+      A.T = (int)(all.T - t < kGateTokens ? all.T - t : kGateTokens);
+      launch_gate(st, A, logits + (size_t)t * A.E, bias, topk_idx + (size_t)t * (A.k + A.Es), topk_w + (size_t)t * (A.k + A.Es));
+    }
+    return;
+  }
   GatePlan P;
   const int W = gate_lanes(A, &P);
   if (W && A.k <= 8) {

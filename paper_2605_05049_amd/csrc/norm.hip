@@ -237,6 +237,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_bwd_kernel
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       if (!in[c] || !live) cur.dy[c] = uint4{0, 0, 0, 0};
+      if (ROWS > 1 && !live) cur.h[c] = uint4{0, 0, 0, 0};   // (the last row's, which dx may have overwritten)
       float d[8], v[8], f[8];
       unpack8(cur.dy[c], d);
       unpack8(cur.h[c], v);
@@ -332,6 +333,7 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restr
   out[col] = v;
 }
 
+constexpr long long kNormRows = 1 << 22;   // of a launch of the forward pass at most: a grid has less than 2^32 threads
 static bool norm_sizes(long long rows, int cols) { return rows >= 0 && rows < (1ll << 31) && cols >= 8 && cols <= MOE_NORM_COLS_MAX && cols % 8 == 0; }
 // 64 to 512 lanes, as few as have at most `chunks` chunks of 8 columns each.
 static int norm_lanes_of_chunks(int cols, int chunks) {
@@ -391,7 +393,6 @@ extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const
   MOE_REQUIRE_ALIGNED(x); MOE_REQUIRE_ALIGNED(addend); MOE_REQUIRE_ALIGNED(gamma); MOE_REQUIRE_ALIGNED(beta); MOE_REQUIRE_ALIGNED(sum);
   MOE_REQUIRE_ALIGNED(y); MOE_REQUIRE_ALIGNED(mean); MOE_REQUIRE_ALIGNED(rstd);
   hipStream_t st = (hipStream_t)stream;
-  const NormFwdArgs A = {rows, cols, eps, 1.0f / cols, x, addend, gamma, beta, sum, y, mean, rstd};
 #define MOE_LAUNCH_NORM(L_, CH_)                                                                     \
   do {                                                                                               \
     constexpr int per_block = L_ < 256 ? 256 / L_ : 1;                                               \
@@ -400,7 +401,14 @@ extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const
     else MOE_LAUNCH("norm_fwd", st, (norm_fwd_kernel<L_, CH_, false>), grid, block, 0, st, A);       \
   } while (0)
   const int lanes = norm_fwd_lanes(cols, addend != nullptr);
-  MOE_LAUNCH_NORM_LANES(lanes);
+  const int64_t all = rows;
+  for (int64_t done = 0; done < all; done += kNormRows) {
+    rows = all - done < kNormRows ? all - done : kNormRows;
+    const size_t at = (size_t)done * cols;
+    const NormFwdArgs A = {rows, cols, eps, 1.0f / cols, x + at, addend ? addend + at : nullptr, gamma, beta, sum ? sum + at : nullptr, y + at,
+                           mean ? mean + done : nullptr, rstd ? rstd + done : nullptr};
+    MOE_LAUNCH_NORM_LANES(lanes);
+  }
 #undef MOE_LAUNCH_NORM
   return launch_status();
 }
@@ -431,7 +439,7 @@ extern "C" int moe_norm_bwd(int64_t rows, int cols, int centre, const uint16_t* 
   hipStream_t st = (hipStream_t)stream;
   const int blocks = norm_bwd_blocks(rows, cols);
   float* part = weights ? (float*)ws : nullptr;
-  const bool one = rows > 0 && norm_bwd_one_launch(rows) && dx != dy;   // (dy is still read when dx is written)
+  const bool one = rows > 0 && norm_bwd_one_launch(rows) && dx != dy && dx != h;   // (both are still read when dx is written)
   if (rows > 0) {
     const NormBwdArgs A = {rows, cols, 1.0f / cols, dy, h, gamma, mean, rstd, dx_addend, dx, one ? nullptr : part, blocks, dgamma, dbeta, accumulate};
     const dim3 grid(blocks + (one && weights ? (cols + kNormColumns - 1) / kNormColumns : 0));

@@ -103,6 +103,42 @@ def test_gate_fwd(moe, case, mask):
     check_fwd(logits, bias, idx, w, k, groups, kept, best, scores, renorm, Es, scale)
 
 
+@pytest.mark.parametrize("case", [
+    (2500, 256, 8, 8, 4, 2, "sigmoid"), (2500, 256, 7, 8, 4, 2, "sigmoid"), (2500, 64, 16, 1, 1, 1, "softmax"), (2500, 64, 9, 4, 3, 2, "softmax"),
+    (1500, 128, 6, 1, 1, 1, "softmax"), (1500, 128, 8, 1, 1, 1, "softmax"), (1100, 1024, 16, 4, 2, 2, "sigmoid"), (300, 512, 8, 64, 9, 1, "sigmoid"),
+    (1100, 44, 8, 11, 5, 1, "softmax"), (3000, 8, 8, 2, 2, 2, "sigmoid")], ids=lambda c: "-".join(str(v) for v in c))
+def test_gate_fwd_of_many_tokens_that_fp32_cannot_decide(moe, case):
+    T, E, k, groups, kept, best, scores = case
+    logits, bias = make(T, E, 11, "near")
+    if scores == "softmax":   # (as `near`, of one token's scores)
+        s = np.exp(logits[0].astype(np.float64) - logits[0].max())
+        bias = (0.75 - s / s.sum()).astype(np.float32)
+    _, _, idx, w = run_fwd(moe, logits, bias, k, groups, kept, best, scores, True, 0, 1.0)
+    check_fwd(logits, bias, idx, w, k, groups, kept, best, scores, True, 0, 1.0)
+
+
+def test_offsets_past_32_bits(moe):
+    T, E, k = (1 << 24) + 5, 132, 4
+    g = torch.Generator(device="cuda").manual_seed(0)
+    few = torch.randn(1 << 20, E, device="cuda", generator=g)
+    logits = torch.empty(T, E, device="cuda")
+    for i in range(17):
+        part = logits[i << 20:(i + 1) << 20]
+        torch.mul(few[:len(part)], 1.0 + i, out=part)
+    bias, gate = 0.1 * torch.randn(E, device="cuda", generator=g), moe.Gate("sigmoid", 4, 2, 2, 1.0)
+    idx, w, dlogits = torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda"), torch.empty(T, E, device="cuda")
+    moe.moe_gate_fwd(moe.Shape(T, 64, 64, E, k), gate, logits, bias, idx, w)
+    moe.moe_gate_bwd(moe.Shape(T, 64, 64, E, k), gate, w, logits, idx, w, None, 0.0, dlogits)
+    for at in (0, (1 << 31) // E - 4, (1 << 24) - 4, T - 8):
+        some = slice(at, at + 8)
+        one = [torch.empty(8, k, dtype=torch.int32, device="cuda"), torch.empty(8, k, device="cuda"), torch.empty(8, E, device="cuda")]
+        moe.moe_gate_fwd(moe.Shape(8, 64, 64, E, k), gate, logits[some], bias, one[0], one[1])
+        moe.moe_gate_bwd(moe.Shape(8, 64, 64, E, k), gate, one[1], logits[some], one[0], one[1], None, 0.0, one[2])
+        assert torch.equal(idx[some], one[0])
+        # (sums of other lanes' orders)
+        assert (w[some] - one[1]).abs().max().item() <= 16 * U and (dlogits[some] - one[2]).abs().max().item() <= 64 * U
+
+
 @pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
 def test_gate_fwd_of_scores_far_from_even(moe, scores):
     logits, bias = make(64, 128, 2, scale=30.0)
@@ -162,6 +198,15 @@ def test_gate_bwd_of_many_tokens(moe):
     w = F.gate_weights(logits, idx, "sigmoid", True, 2.5).astype(np.float32)
     a = check_bwd(moe, logits, idx, w, 4, "sigmoid", True, 2.5, 0, 0.01)
     assert torch.equal(a, check_bwd(moe, logits, idx, w, 4, "sigmoid", True, 2.5, 0, 0.01))   # the same bits every time
+
+
+@pytest.mark.parametrize("T,E,k,scores,renorm", [(20000, 130, 4, "softmax", False), (3000, 30, 4, "sigmoid", False), (2000, 1023, 70, "sigmoid", True),
+                                                   (5000, 500, 9, "softmax", True), (4100, 36, 2, "softmax", False)])
+def test_gate_bwd_of_many_tokens_of_odd_sizes(moe, T, E, k, scores, renorm):
+    logits, _ = make(T, E, 12)
+    idx = np.argsort(-logits, 1, kind="stable")[:, :k].astype(np.int32)
+    w = F.gate_weights(logits, idx, scores, renorm, 1.5).astype(np.float32)
+    check_bwd(moe, logits, idx, w, k, scores, renorm, 1.5, 0, 2.0)
 
 
 def test_gate_bwd_sums_an_expert_that_is_named_twice(moe):

@@ -108,6 +108,49 @@ def test_norm_bwd(moe, rows, cols, addend, gamma, beta, centre):
     check_bwd(moe, make(rows, cols, 1), rows, cols, centre, addend, gamma, beta)
 
 
+@pytest.mark.parametrize("centre", [True, False])
+@pytest.mark.parametrize("rows,cols", [(19, 128), (19, 136), (35, 256), (35, 264), (9000, 200), (1100, 6200), (1030, 16384), (2100, 4104)])
+def test_norm_by_other_lanes_and_launches(moe, rows, cols, centre):
+    """Rows of a quarter and half a wavefront, and one row either side of them; many long rows."""
+    for addend, beta in ((False, True), (True, False)):
+        check_fwd(moe, make(rows, cols, 8), rows, cols, centre, addend, True, beta)
+        check_bwd(moe, make(rows, cols, 9), rows, cols, centre, addend, True, beta)
+
+
+def test_gradient_in_place_of_the_rows(moe):
+    """dx over h itself: with the gradients of the weights, which h is read for as well."""
+    for rows in (37, 1500):
+        d = make(rows, 2304, 10)
+        want, grads = check_bwd(moe, d, rows, 2304, False, True, True, True)
+        h, (_, _, rstd) = d["x"].cuda(), F.norm_fwd(f64(d["x"]), None, None, False, 1e-6)
+        g2 = [torch.empty(2304, device="cuda") for _ in range(2)]
+        ws = torch.empty(moe.norm_workspace_bytes(rows, 2304), dtype=torch.uint8, device="cuda")
+        moe.moe_norm_bwd(False, d["dy"].cuda(), h, d["gamma"].cuda(), None, torch.from_numpy(rstd).float().cuda(), d["addend"].cuda(), h, *g2, False, ws)
+        assert torch.equal(h, want)
+        for a, b, x in zip(g2, grads, (f64(d["dy"]) * f64(d["x"]) * rstd[:, None], f64(d["dy"]))):
+            # (summed in another order: twice what check_bwd allows one sum)
+            assert (np.abs(f64(a) - f64(b[:2304])) <= 2 * (rows / 256 + 1100 / 16 + 40) * U * np.abs(x).sum(0)).all()
+
+
+def test_offsets_past_32_bits(moe):
+    rows, cols = (1 << 22) + 5, 520
+    x = torch.randn(1 << 20, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0)).bfloat16()
+    x = torch.cat([x, x * 2, x * 3, x * 4, x[:5] * 5])
+    gamma = torch.linspace(0.5, 1.5, cols, device="cuda").bfloat16()
+    total, y = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    moe.moe_norm_fwd(True, 1e-6, x, x, gamma, None, total, y, mean, rstd)
+    dx = torch.empty_like(x)
+    moe.moe_norm_bwd(True, y, total, gamma, mean, rstd, x, dx, None, None, False, None)
+    for at in (0, (1 << 20) - 3, (1 << 31) // cols - 4, (1 << 22) - 4, rows - 8):
+        some = slice(at, at + 8)
+        want = [torch.empty_like(x[some]) for _ in range(3)] + [torch.empty(8, device="cuda") for _ in range(2)]
+        moe.moe_norm_fwd(True, 1e-6, x[some], x[some], gamma, None, want[0], want[1], want[3], want[4])
+        moe.moe_norm_bwd(True, want[1], want[0], gamma, want[3], want[4], x[some], want[2], None, None, False, None)
+        for a, b in zip((total, y, dx, mean, rstd), want):
+            assert torch.equal(a[some], b)
+
+
 @pytest.mark.parametrize("cols", [64, 1088, 4096, 7168])
 @pytest.mark.parametrize("offset", [100.0, 1000.0])
 def test_rows_far_from_zero(moe, cols, offset):

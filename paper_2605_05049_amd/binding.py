@@ -631,7 +631,7 @@ def _as(dtype, t, numel, name):
 def _stream_of(t, stream):
     """_stream for a call on t, whose device has to be the current one: a launch goes there."""
     handle = _stream(stream)
-    if _device is not None and t.get_device() != _device():
+    if t is not None and _device is not None and t.get_device() != _device():
         raise ValueError(f"tensors on {t.device}: the call belongs within torch.cuda.device of it")
     return handle
 

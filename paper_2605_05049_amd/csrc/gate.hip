@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
 // The logits come in through LDS: a wavefront's tokens lie next to each other in memory whatever E is, and all its loads are under way at once.
 //
 // Bound by the vector instructions: 65536 tokens of 256 experts, sigmoid scores, a bias, top-8 of 4 of 8 groups: 24 us for 72 MB (HBM's share: 11),
-// 975 instructions a wavefront of 8 tokens, 3 in 4 of a SIMD's cycles.  A tenth of them are exponentials and reciprocals, a quarter of the rate; networks
+// 975 instructions a wavefront of 8 tokens, 3 in 4 of a SIMD's cycles.  One in 15 is an exponential or a reciprocal, at a quarter of the rate; networks
 // and joins are half.  Few tokens: 2.5 us for one of 64 experts, the latency of one wavefront.  16384 tokens of 128: 6.2 to 7.4 us.
 // Measured and left out, on the large case: a wavefront that goes on to the next tokens with their loads under way (registers spill: 84 us); choices in
 // 64 bits among the candidates in this layout rather than by the wavefront (30 us).

@@ -351,15 +351,17 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const int t0 = (blockIdx.x * 4 + wave) * TOKENS, t = t0 + tt;
   const int E = A.E, k = A.k, Kp = k + A.Es;
   const bool by_logits = bias == nullptr;
-  // The bias into LDS, laid out as a token's logits: read from memory by every wavefront, the few lines of it are what all of them wait for
-  __shared__ __attribute__((aligned(16))) float biases[MAX_E + 4 * MAX_E / RUN + 40];
+  // The bias into LDS, a run for each lane of a token: read from memory by every wavefront, the few lines of it are what all of them wait for
+  __shared__ __attribute__((aligned(16))) float biases[W * (PER + 4)];
   __shared__ int dead_bias;
   if (!by_logits) {
     if (threadIdx.x == 0) dead_bias = 0;
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += 256) {
-      const float b = bias[e];
-      biases[gate_place<RUN>(e)] = b;
+    for (int i = threadIdx.x; i < W * PER; i += 256) {
+      const int run = i / PER, p = i % PER, of_group = run >> P.lanes_log2, from = (run & (P.lanes_of_group - 1)) * P.piece + p;
+      const bool exists = of_group < A.groups && p < P.piece && from < P.size;
+      const float b = exists ? bias[of_group * P.size + from] : 0.f;
+      biases[run * (PER + 4) + p] = b;
       if (!(b > kMaskedLogit)) dead_bias = 1;
     }
     __syncthreads();
@@ -403,20 +405,14 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       l[p] = u.x; l[p + 1] = u.y; l[p + 2] = u.z; l[p + 3] = u.w;
     }
   } else {
+    const int at = tt * E + min(first, E - 1), turn = RUN - at % RUN;   // (PER <= RUN: one place at most where floats are left free)
+    const float* run = &rows[wave][gate_place<RUN>(at)];
 #pragma unroll
-    for (int p = 0; p < PER; p++) l[p] = rows[wave][gate_place<RUN>(tt * E + min(first, E - 1) + p)];
-#pragma unroll
-    for (int p = 0; p < PER; p++) l[p] = p < count ? l[p] : -__builtin_inff();
+    for (int p = 0; p < PER; p++) l[p] = (p < turn ? run : run + 4)[p];
   }
-  const float* bias_run = &biases[FULL && !by_logits ? gate_place<RUN>(min(first, E - PER)) : 0];
   auto bias_of = [&](int p, float* b) __attribute__((always_inline)) {   // of a lane's experts p .. p + 3
-    if constexpr (FULL) {
-      const float4 u = *reinterpret_cast<const float4*>(bias_run + p);
-      b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; i++) b[i] = biases[gate_place<RUN>(min(first, E - 1) + p + i)];
-    }
+    const float4 u = *reinterpret_cast<const float4*>(&biases[g * (PER + 4) + p]);
+    b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
   };
   bool some_dead = !by_logits && dead_bias != 0;   // a key of the wavefront may be one
   const float lowest = group < A.groups ? kMaskedLogit : __builtin_inff();   // (nothing of a lane without a group counts)
@@ -448,7 +444,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
 #pragma unroll
     for (int p = 0; p < PER; p++) {
       const float finite = fminf(l[p], kMaxLogit);
-      l[p] = l[p] > lowest ? finite : -__builtin_inff();   // (and NaN)
+      l[p] = l[p] > lowest && (FULL || p < count) ? finite : -__builtin_inff();   // (and NaN)
     }
     some_dead = true;
     if (!A.sigmoid && !(by_logits && A.renorm && A.group_best == 1)) {
@@ -498,7 +494,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     for (int i = 0; i < K; i += 2) lost = max_of_mins(lost, key_value(a[i]), key_value(b[K - 1 - i]), key_value(a[i + 1]), key_value(b[K - 2 - i]));
   };
   // Of negative values the larger low word is the smaller number.  Where c is selected by, equal values are told apart in 64 bits, but for dead ones.
-  const bool signs = by_logits || some_dead || !FULL;
+  const bool signs = by_logits || some_dead;
   double best[K];
 #pragma unroll
   for (int b = 0; b < PER / K; b++) {

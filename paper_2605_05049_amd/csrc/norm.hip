@@ -178,7 +178,7 @@ __device__ __forceinline__ void weights_of_columns(const NormBwdArgs& A, int blo
 template <int THREADS, int CH, bool CENTRE, bool BETA>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_bwd_kernel(NormBwdArgs A) {
   constexpr int BLOCK_WAVES = THREADS < 256 ? 4 : THREADS / kWave, WAVES = THREADS < kWave ? 1 : THREADS / kWave, ROWS = BLOCK_WAVES * kWave / THREADS;
-  constexpr bool AHEAD = CH <= 2;   // (registers)
+  constexpr bool AHEAD = CH <= 2;   // (registers; of 3 and 4 chunks up to 6 % slower)
   constexpr int JOIN = (ROWS - 1) * THREADS * 8, COLUMNS = 4 * BLOCK_WAVES * 4 * 16;
   __shared__ float slots[2][ROWS][2][WAVES];
   __shared__ float join[JOIN > COLUMNS ? JOIN : COLUMNS];
@@ -353,7 +353,8 @@ static int norm_fwd_lanes(int cols, bool addend) {
   return norm_lanes_of_chunks(cols, 3);
 }
 // In the backward pass: as few as leave a lane at most 3 chunks of 8 values (4 from 12288 columns on), whose sums it keeps.  Blocks: two a CU of 4
-// wavefronts, one of 8.  (Twice and half as many blocks, lanes: 2 to 40 % slower at 512 .. 16384 columns; 2 blocks of 8 are 6 % slower.)
+// wavefronts, one of 8.  (Twice and half as many blocks, lanes: 2 to 40 % slower at 512 .. 16384 columns; 2 blocks of 8 are 6 % slower. Numbers that
+// even out the blocks' rows but not those of the CUs: 10 to 60 %.)
 static int norm_bwd_lanes(int cols) { return cols <= 128 ? 16 : cols <= 256 ? 32 : norm_lanes_of_chunks(cols, 3); }
 static int norm_bwd_blocks(long long rows, int cols) {
   const int lanes = norm_bwd_lanes(cols), per_block = lanes < 256 ? 256 / lanes : 1;

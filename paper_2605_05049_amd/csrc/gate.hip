@@ -516,6 +516,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   }
   float lane_last = PER > K && track && !track_lane ? key_value(best[K - 1]) : kNoKey;   // (nothing that the lane has let go is above it)
   bool unsure = false, unsure_group = false;
+  unsigned long long kept_lanes = ~0ull;   // whose group stays
 
   auto select_groups = [&]() __attribute__((always_inline)) {
     const float a = key_value(best[0]), b = key_value(best[1]);
@@ -550,6 +551,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     for (int i = 0; i < K; i++) best[i] = stays ? best[i] : none;
     lost = stays ? lost : kNoKey;
     lane_last = stays ? lane_last : kNoKey;
+    kept_lanes = __ballot(stays);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   auto join_lanes = [&](auto step_c) __attribute__((always_inline)) {
@@ -589,21 +591,88 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   const bool live = t < A.T && g < k;
   float x = live ? rows[wave][gate_place<RUN>(tt * E + choice)] : -__builtin_inff();
   unsigned long long again = __ballot((unsure || unsure_group) && t < A.T);
-  if (again) {   // (the logits in LDS make room)
+  if (again) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     // the k-th c, and how far below it one may be that belongs before it
     const float kth = by_logits || unsure_group ? -__builtin_inff() : __shfl(key_value(mine), lane - g + k - 1, kWave);
     const float least = kth - (slack + slack_c * (fabsf(kth) + slack));
-    do {
+    const unsigned long long by_groups = __ballot(unsure_group);
+    unsigned long long all_again = 0;
+    const auto lanes_of = [](int token) { return (W == kWave ? ~0ull : (1ull << (W & 63)) - 1) << (token * W); };
+    if (!by_logits) {
+      // Sure of the groups: the experts that may be among the k best are looked up again in fp32 (a run by a lane of each token), and these are put in
+      // order in 64 bits, which takes a third of the time of the whole: 4096 tokens of 256 experts, one or two of which come here, 9.0 -> 6.0 us.
+      int* found = reinterpret_cast<int*>(group_scores[wave]);
+      const int exist = group < A.groups ? max(0, min(P.piece, size - begin)) : 0;
+      do {
+        const int token = __builtin_ctzll(again) / W;
+        again &= ~lanes_of(token);
+        const float from = __shfl(least, token * W, kWave);
+        const float top = A.sigmoid ? 0.f : __shfl(m, token * W, kWave), over = A.sigmoid ? 1.f : __shfl(inv_z, token * W, kWave);
+        int n = 0;
+        if (!(by_groups & lanes_of(token)) && from > kMaskedLogit) {
+          const bool kept = (kept_lanes >> (token * W + g)) & 1;
+#pragma unroll
+          for (int i = 0; i < PER / TOKENS; i++) {
+            const int p = tt + TOKENS * i;
+            const float lp = gate_finite(rows[wave][gate_place<RUN>(token * E + min(first + p, E - 1))]), b = biases[g * (PER + 4) + p];
+            const float v = A.sigmoid ? __builtin_amdgcn_rcpf(1.0f + fast_exp(-lp)) + b : fmaf(fast_exp(lp - top), over, b);
+            const bool one = kept && p < exist && lp > kMaskedLogit && v >= from;
+            const unsigned long long all = __ballot(one);
+            const int at = n + __popcll(all & ((1ull << lane) - 1));
+            if (one && at < kWave) found[at] = first + p + (g << 10) + (p << 16);
+            n += __popcll(all);
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        if (n < k || n > kWave) {   // (of a group in doubt, or very many alike)
+          all_again |= lanes_of(token);
+          continue;
+        }
+        const int it = found[min(lane, n - 1)], e = it & 1023;
+        const double le = gate_finite(rows[wave][gate_place<RUN>(token * E + e)]), b = biases[((it >> 10) & 63) * (PER + 4) + (it >> 16)];
+        double v;
+        if (A.sigmoid) {
+          v = 1.0 / (1.0 + exp(-le)) + b;
+        } else {
+          double z = 0.0;
+#pragma unroll
+          for (int i = 0; i < PER / TOKENS; i++) {
+            const int p = tt + TOKENS * i;
+            const float lp = gate_finite(rows[wave][gate_place<RUN>(token * E + min(first + p, E - 1))]);
+            z += p < exist && lp > kMaskedLogit ? exp((double)lp - (double)top) : 0.0;
+          }
+          v = exp(le - (double)top) / lanes_sum<kWave>(z) + b;
+        }
+        int place = 0;
+        for (int o = 0; o < n; o++) {
+          const double u = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), o), __builtin_amdgcn_readlane(__double2loint(v), o));
+          place += u > v || (u == v && __builtin_amdgcn_readlane(e, o) < e);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane < n) found[place] = e;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (tt == token && g < k) choice = found[g];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      } while (again);
+      if (live) x = rows[wave][gate_place<RUN>(tt * E + choice)];
+    } else {
+      all_again = again;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    again = all_again;
+    while (again) {   // (the logits in LDS make room)
       const int token = __builtin_ctzll(again) / W;
       int held[(MAX_E + kWave - 1) / kWave];
       choose_exactly<(MAX_E + kWave - 1) / kWave>(logits + (size_t)(t0 + token) * E, bias, reinterpret_cast<double*>(rows[wave]), held, A,
                                                    __shfl(least, token * W, kWave));
       const int found = __shfl(held[0], g, kWave);
-      if (tt == token) choice = found;
-      again &= ~((W == kWave ? ~0ull : (1ull << (W & 63)) - 1) << (token * W));
-    } while (again);
-    if (live) x = logits[(size_t)t * E + choice];
+      if (tt == token) {
+        choice = found;
+        if (live) x = logits[(size_t)t * E + choice];
+      }
+      again &= ~lanes_of(token);
+    }
   }
 
   // the weights: over the largest chosen logit where they are renormalised (scores far below zero keep their ratios)

@@ -32,7 +32,7 @@ __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f 
 // A token's choices in 64 bits by a wavefront: any number of groups and experts, any k.  Choice j comes back on lane j % 64 in held[j / 64].  c: LDS of
 // E + groups doubles, of E + 96 with `from`: where the choices are known to be among the experts whose c is at least that, these (mostly k, or one more)
 // are put in order; else k rounds find the best one left.  Where this is the way out of the other kernel, one wavefront in some hundred takes it (of
-// 65536 tokens of 256 experts 3 in 10000), alone: its time is that of one instruction after another, 5 us of a launch in which any has to.
+// 65536 tokens of 256 experts 3 in 10000, most of which need less than this), alone: its time is that of one instruction after another, 5 us of a launch.
 template <int PER>
 __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A,
                                                float from) {
@@ -183,7 +183,7 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
 }
 
 // Any number of groups and experts, any k: a wavefront per token.  For k over 16 and groups over 64 alone: 65536 tokens of 256 experts, top-8 of 4 of 8
-// groups, took 197 us in rounds like these and take 24 us below.
+// groups, took 197 us in rounds like these and take 21 us below.
 template <int PER>
 __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restrict__ logits, const float* __restrict__ bias,
                                                            int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, GateArgs A) {
@@ -254,14 +254,15 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
 // first two give the group's score, and the lists of groups that do not stay are emptied.
 // The logits come in through LDS: a wavefront's tokens lie next to each other in memory whatever E is, and all its loads are under way at once.
 //
-// Bound by the vector instructions: 65536 tokens of 256 experts, sigmoid scores, a bias, top-8 of 4 of 8 groups: 24 us for 72 MB (HBM's share: 11),
-// 975 instructions a wavefront of 8 tokens, 3 in 4 of a SIMD's cycles.  One in 15 is an exponential or a reciprocal, at a quarter of the rate; networks
-// and joins are half.  Few tokens: 2.5 us for one of 64 experts, the latency of one wavefront.  16384 tokens of 128: 6.2 to 7.4 us.
-// Measured and left out, on the large case: a wavefront that goes on to the next tokens with their loads under way (registers spill: 84 us); choices in
-// 64 bits among the candidates in this layout rather than by the wavefront (30 us).
+// Bound by the vector instructions: 65536 tokens of 256 experts, sigmoid scores, a bias, top-8 of 4 of 8 groups: 21 us for 72 MB (HBM's share: 11),
+// 929 instructions a wavefront of 8 tokens, 3 in 4 of a SIMD's cycles.  One in 15 is an exponential or a reciprocal, at a quarter of the rate; networks
+// and joins are half.  Few tokens: 2.5 us for one of 64 experts, the latency of one wavefront.  16384 tokens of 128: 5.0 to 6.4 us.
+// Measured and left out, on the large case: a wavefront that goes on to the next tokens with their loads under way (registers spill: 84 for 25 us); the
+// order in 64 bits of all tokens' candidates, each on its token's lanes (30 for 25).
 //
 // fp32 orders two values right if they are further apart than twice what either may be off.  Where a choice or its order hangs on less, which adjacent
-// keys, the first one left out and the groups next to the cut tell, the wavefront makes its choices again in 64 bits.
+// keys, the first one left out and the groups next to the cut tell, the wavefront makes that token's choice again in 64 bits, among the experts near its k-th
+// best where the groups are sure.
 
 constexpr float kDeadKey = -3.0e38f;   // masked experts: after all others
 constexpr float kNoKey = -3.3e38f;     // of groups that do not stay, and behind the last expert

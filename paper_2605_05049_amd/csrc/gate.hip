@@ -763,7 +763,7 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(cons
   };
   Batch cur, next;
   int batch = blockIdx.x * kGateBwdWaves + wave;
-  constexpr bool AHEAD = VEC || C <= 2;   // (16 experts one by one take the registers)
+  constexpr bool AHEAD = VEC || C <= 2;   // (12 and 16 experts one by one take the registers: 30000 x 190 13.8 us, ahead 14.8)
   if (AHEAD && batch < batches) request(batch, cur);
   for (; batch < batches; batch += step) {
     if constexpr (AHEAD) {
@@ -1054,10 +1054,12 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   MOE_REQUIRE_ALIGNED(dtopk_w); MOE_REQUIRE_ALIGNED(logits); MOE_REQUIRE_ALIGNED(topk_idx); MOE_REQUIRE_ALIGNED(topk_w); MOE_REQUIRE_ALIGNED(dlogits);
   MOE_REQUIRE_ALIGNED(counts); MOE_REQUIRE_ALIGNED(loss);
   if (!(balance >= -kMaxLogit && balance <= kMaxLogit)) return MOE_ERR_SHAPE;
-  // lanes of a token: 16 experts each at most, 8 one by one; of up to 16 experts as many as have 4 each
-  const int each = D.E % 4 == 0 ? 16 : 8;
-  int W = each == 16 && D.E <= 8 ? 2 : each == 16 && D.E <= 16 ? 4 : 8;
-  while (W < kWave && each * W < D.E) W *= 2;
+  // lanes of a token, and its chunks of 4 experts a lane: up to 16 experts 4 each; else up to 4 chunks, one by one 3 (of 64 lanes 4).
+  // (Chunks of 3 beside 1, 2 and 4: 65536 x 160 22 -> 19.6 us, 32768 x 384 26.5 -> 23.9, 30000 x 190 20 -> 13.8.)
+  const bool vec = D.E % 4 == 0;
+  int W = vec && D.E <= 8 ? 2 : vec && D.E <= 16 ? 4 : 8;
+  while (W < kWave && (vec ? 16 : 12) * W < D.E) W *= 2;
+  const int chunks = (D.E + 4 * W - 1) / (4 * W);
   const long long units = ((long long)D.T + kGateBwdWaves * (kWave / W) - 1) / (kGateBwdWaves * (kWave / W));
   // With the loss, one or two batches of tokens a wavefront stay in one block, which then has the whole sum: a launch less.  (On the device, of 8 and of
   // 256 experts: one batch 3.0 for 4.5 us and 4.9 for 6.3, two 4.1 for 4.7 and 7.4 for 6.5, four 6.1 for 4.7 and 12.4 for 6.5; a call's own launch 3 us.)
@@ -1075,23 +1077,28 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
 #define MOE_LAUNCH_GATE_BWD(W_, C_, VEC_)                                                                                                             \
   MOE_LAUNCH("gate_bwd", st, (gate_bwd_kernel<W_, C_, VEC_>), dim3(blocks), dim3(kGateBwdWaves * kWave), 0, st, dtopk_w, logits, topk_idx, topk_w, counts, \
              cost, dlogits, parts, A)
-    if (D.E % 4 == 0) {
+#define MOE_LAUNCH_GATE_BWD_EITHER(few, W_, FEW_, MANY_, VEC_) \
+  do {                                                         \
+    if (few) MOE_LAUNCH_GATE_BWD(W_, FEW_, VEC_);              \
+    else MOE_LAUNCH_GATE_BWD(W_, MANY_, VEC_);                 \
+  } while (0)
+    if (vec) {
       if (W == 2) MOE_LAUNCH_GATE_BWD(2, 1, true);
       else if (W == 4) MOE_LAUNCH_GATE_BWD(4, 1, true);
-      else if (D.E <= 32) MOE_LAUNCH_GATE_BWD(8, 1, true);
-      else if (D.E <= 64) MOE_LAUNCH_GATE_BWD(8, 2, true);
-      else if (W == 8) MOE_LAUNCH_GATE_BWD(8, 4, true);
-      else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 4, true);
-      else if (W == 32) MOE_LAUNCH_GATE_BWD(32, 4, true);
-      else MOE_LAUNCH_GATE_BWD(64, 4, true);
+      else if (W == 8 && chunks <= 2) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 1, 8, 1, 2, true);
+      else if (W == 8) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 3, 8, 3, 4, true);
+      else if (W == 16) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 3, 16, 3, 4, true);
+      else if (W == 32) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 3, 32, 3, 4, true);
+      else MOE_LAUNCH_GATE_BWD_EITHER(chunks == 3, 64, 3, 4, true);
     } else {
-      if (D.E <= 32) MOE_LAUNCH_GATE_BWD(8, 1, false);
-      else if (W == 8) MOE_LAUNCH_GATE_BWD(8, 2, false);
-      else if (W == 16) MOE_LAUNCH_GATE_BWD(16, 2, false);
-      else if (W == 32) MOE_LAUNCH_GATE_BWD(32, 2, false);
-      else if (D.E <= 512) MOE_LAUNCH_GATE_BWD(64, 2, false);
-      else MOE_LAUNCH_GATE_BWD(64, 4, false);
+      if (chunks == 1) MOE_LAUNCH_GATE_BWD(8, 1, false);
+      else if (W == 8) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 2, 8, 2, 3, false);
+      else if (W == 16) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 2, 16, 2, 3, false);
+      else if (W == 32) MOE_LAUNCH_GATE_BWD_EITHER(chunks == 2, 32, 2, 3, false);
+      else if (chunks == 4) MOE_LAUNCH_GATE_BWD(64, 4, false);
+      else MOE_LAUNCH_GATE_BWD_EITHER(chunks == 2, 64, 2, 3, false);
     }
+#undef MOE_LAUNCH_GATE_BWD_EITHER
 #undef MOE_LAUNCH_GATE_BWD
   }
   if (loss && !alone) MOE_LAUNCH("gate_loss", st, gate_loss_kernel, dim3(1), dim3(256), 0, st, (const float*)ws, blocks, loss);

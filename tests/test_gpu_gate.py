@@ -203,7 +203,10 @@ def test_gate_bwd_of_many_tokens(moe):
 @pytest.mark.parametrize("T,E,k,scores,renorm", [(20000, 130, 4, "softmax", False), (3000, 30, 4, "sigmoid", False), (2000, 1023, 70, "sigmoid", True),
                                                    (5000, 500, 9, "softmax", True), (4100, 36, 2, "softmax", False),
                                                    (3001, 8, 8, "sigmoid", True), (2500, 16, 11, "softmax", True), (700, 12, 3, "softmax", False),
-                                                   (511, 4, 1, "sigmoid", False)])
+                                                   (511, 4, 1, "sigmoid", False), (2003, 84, 5, "sigmoid", True), (1501, 160, 6, "softmax", False),
+                                                   (1001, 320, 4, "softmax", True), (701, 600, 8, "sigmoid", False), (1203, 70, 3, "softmax", False),
+                                                   (1203, 97, 3, "sigmoid", True), (1203, 190, 8, "sigmoid", False), (901, 205, 8, "softmax", False),
+                                                   (901, 301, 2, "sigmoid", True), (501, 450, 8, "softmax", False), (501, 601, 8, "sigmoid", True)])
 def test_gate_bwd_of_many_tokens_of_odd_sizes(moe, T, E, k, scores, renorm):
     logits, _ = make(T, E, 12)
     idx = np.argsort(-logits, 1, kind="stable")[:, :k].astype(np.int32)

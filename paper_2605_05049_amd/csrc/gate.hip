@@ -378,7 +378,10 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
 #pragma unroll
     for (int j = 0; j < PER / 4; j++) in[j] = *reinterpret_cast<const float4*>(src + 4 * lane + 4 * kWave * j);
 #pragma unroll
-    for (int j = 0; j < PER / 4; j++) *reinterpret_cast<float4*>(&rows[wave][gate_place<RUN>(4 * lane) + gate_place<RUN>(4 * kWave) * j]) = in[j];
+    for (int j = 0; j < PER / 4; j++) {
+      const int at = (4 * kWave) % RUN ? gate_place<RUN>(4 * (lane + kWave * j)) : gate_place<RUN>(4 * lane) + gate_place<RUN>(4 * kWave) * j;
+      *reinterpret_cast<float4*>(&rows[wave][at]) = in[j];
+    }
   } else if ((TOKENS % 4 == 0 || (E * TOKENS) % 4 == 0) && n >= 4) {
     float4 in[PER / 4];
 #pragma unroll
@@ -971,6 +974,7 @@ template <int K, int W>
 static void launch_gate_lanes(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
   if (K == 8 && P.piece <= 8) launch_gate_kernel<K, W, K>(st, A, P, logits, bias, topk_idx, topk_w);
   else if (P.piece <= 16) launch_gate_kernel<K, W, 16>(st, A, P, logits, bias, topk_idx, topk_w);
+  else if (K == 8 && P.piece <= 24) launch_gate_kernel<K, W, K == 8 ? 24 : 32>(st, A, P, logits, bias, topk_idx, topk_w);
   else launch_gate_kernel<K, W, 32>(st, A, P, logits, bias, topk_idx, topk_w);
 }
 

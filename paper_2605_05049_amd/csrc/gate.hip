@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
 //
 // Bound by the vector instructions: 65536 tokens of 256 experts, sigmoid scores, a bias, top-8 of 4 of 8 groups: 21 us for 72 MB (HBM's share: 11),
 // 929 instructions a wavefront of 8 tokens, 3 in 4 of a SIMD's cycles.  One in 15 is an exponential or a reciprocal, at a quarter of the rate; networks
-// and joins are half.  Few tokens: 2.5 us for one of 64 experts, the latency of one wavefront.  16384 tokens of 128: 5.0 to 6.4 us.
+// and joins are half.  Few tokens: 2.5 us for one of 64 experts, the latency of one wavefront.  16384 tokens of 128: 4.8 to 5.9 us.
 // Measured and left out, on the large case: a wavefront that goes on to the next tokens with their loads under way (registers spill: 84 for 25 us); the
 // order in 64 bits of all tokens' candidates, each on its token's lanes (30 for 25).
 //
@@ -490,8 +490,9 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   // the product: under PER + 22.  And c by a rounding.  For both of a pair, twice that.
   const float slack = by_logits ? 0.f : A.sigmoid ? 0x1p-21f : (PER + 22) * 0x1p-23f * inv_z, slack_c = 0x1p-23f;
   const bool track = !by_logits && k == K;   // (else the first one left out is in the list, or order needs no margin)
-  // Up to a few lanes' experts stay: one lane may well have all choices.  With more, what a lane lets go matters in 4 (1/4)^K of the tokens.
-  const bool track_lane = track && A.groups_kept * P.lanes_of_group < 4;
+  // Up to a few lanes' experts stay: one lane may well have all choices.  With more, what a lane lets go matters in 4 (1/4)^K of the tokens,
+  // which is few from K = 8 on.
+  const bool track_lane = track && (K < 8 || A.groups_kept * P.lanes_of_group < 4);
   float lost = kNoKey;                       // the best that joining lists has let go
   auto let_go = [&](const double (&a)[K], const double (&b)[K]) __attribute__((always_inline)) {
 #pragma unroll
@@ -946,16 +947,18 @@ static int gate_checks(const moe_shape* shape, const moe_gate* gate, Dims* D, Ga
 
 // W lanes per token (0: the general kernel): as few as hold its groups, and its experts 32 each; of few tokens as many as leave a lane K of them, up to a
 // wavefront a SIMD: there a lane's instructions are the time.
+// (Experts of a lane come in 8, 16, 24 or 32, lists in 4, 8 or 16: 65536 tokens of 192 experts in lanes of 24 17.8 us, of 32 22.2; of 128 experts, top-4,
+// in lists of 4 10.5 us, of 8 11.7.)
 static int gate_lanes(const GateArgs& A, GatePlan* P) {
   if (A.k > 16 || A.groups > kWave) return 0;
   int padded = 1;   // groups, filled up to a power of two
   while (padded < A.groups) padded *= 2;
-  const int size = A.E / A.groups, K = A.k > 8 ? 16 : 8;
-  for (int W = K; W <= kWave; W *= 2) {
+  const int size = A.E / A.groups, K = A.k > 8 ? 16 : A.k > 4 ? 8 : 4;
+  for (int W = K > 8 ? 16 : 8; W <= kWave; W *= 2) {
     if (padded > W) continue;
     const int lanes = W / padded, piece = (size + lanes - 1) / lanes;
     if (piece > 32) continue;
-    if (piece > K && W < kWave && (long long)A.T * 2 * W <= kWave * kGateFewWaves) continue;
+    if (piece > (K > 8 ? 16 : 8) && W < kWave && (long long)A.T * 2 * W <= kWave * kGateFewWaves) continue;
     *P = GatePlan{lanes, __builtin_ctz(lanes), size, piece};
     return W;
   }
@@ -972,9 +975,9 @@ static void launch_gate_kernel(hipStream_t st, const GateArgs& A, const GatePlan
 }
 template <int K, int W>
 static void launch_gate_lanes(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
-  if (K == 8 && P.piece <= 8) launch_gate_kernel<K, W, K>(st, A, P, logits, bias, topk_idx, topk_w);
+  if (K <= 8 && P.piece <= 8) launch_gate_kernel<K, W, K <= 8 ? 8 : 16>(st, A, P, logits, bias, topk_idx, topk_w);
   else if (P.piece <= 16) launch_gate_kernel<K, W, 16>(st, A, P, logits, bias, topk_idx, topk_w);
-  else if (K == 8 && P.piece <= 24) launch_gate_kernel<K, W, K == 8 ? 24 : 32>(st, A, P, logits, bias, topk_idx, topk_w);
+  else if (K <= 8 && P.piece <= 24) launch_gate_kernel<K, W, K <= 8 ? 24 : 32>(st, A, P, logits, bias, topk_idx, topk_w);
   else launch_gate_kernel<K, W, 32>(st, A, P, logits, bias, topk_idx, topk_w);
 }
 
@@ -989,6 +992,13 @@ static void launch_gate(hipStream_t st, const GateArgs& all, const float* logits
   }
   GatePlan P;
   const int W = gate_lanes(A, &P);
+  if (W && A.k <= 4) {
+    if (W == 8) launch_gate_lanes<4, 8>(st, A, P, logits, bias, topk_idx, topk_w);
+    else if (W == 16) launch_gate_lanes<4, 16>(st, A, P, logits, bias, topk_idx, topk_w);
+    else if (W == 32) launch_gate_lanes<4, 32>(st, A, P, logits, bias, topk_idx, topk_w);
+    else launch_gate_lanes<4, 64>(st, A, P, logits, bias, topk_idx, topk_w);
+    return;
+  }
   if (W && A.k <= 8) {
     if (W == 8) launch_gate_lanes<8, 8>(st, A, P, logits, bias, topk_idx, topk_w);
     else if (W == 16) launch_gate_lanes<8, 16>(st, A, P, logits, bias, topk_idx, topk_w);

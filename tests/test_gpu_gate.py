@@ -106,7 +106,10 @@ def test_gate_fwd(moe, case, mask):
 @pytest.mark.parametrize("case", [
     (2500, 256, 8, 8, 4, 2, "sigmoid"), (2500, 256, 7, 8, 4, 2, "sigmoid"), (2500, 64, 16, 1, 1, 1, "softmax"), (2500, 64, 9, 4, 3, 2, "softmax"),
     (1500, 128, 6, 1, 1, 1, "softmax"), (1500, 128, 8, 1, 1, 1, "softmax"), (1100, 1024, 16, 4, 2, 2, "sigmoid"), (300, 512, 8, 64, 9, 1, "sigmoid"),
-    (1100, 44, 8, 11, 5, 1, "softmax"), (3000, 8, 8, 2, 2, 2, "sigmoid")], ids=lambda c: "-".join(str(v) for v in c))
+    (1100, 44, 8, 11, 5, 1, "softmax"), (3000, 8, 8, 2, 2, 2, "sigmoid"),
+    (2500, 256, 4, 8, 4, 2, "sigmoid"), (2500, 64, 4, 1, 1, 1, "softmax"), (1500, 128, 3, 1, 1, 1, "sigmoid"), (1500, 96, 4, 4, 1, 2, "softmax"),
+    (1100, 192, 8, 8, 4, 2, "sigmoid"), (1100, 192, 8, 1, 1, 1, "softmax"), (1100, 384, 6, 16, 3, 1, "sigmoid"), (900, 160, 6, 8, 3, 1, "softmax"),
+    (2500, 20, 1, 5, 2, 2, "sigmoid")], ids=lambda c: "-".join(str(v) for v in c))
 def test_gate_fwd_of_many_tokens_that_fp32_cannot_decide(moe, case):
     T, E, k, groups, kept, best, scores = case
     logits, bias = make(T, E, 11, "near")

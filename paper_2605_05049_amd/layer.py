@@ -57,6 +57,7 @@ class MoeLayerBuffers:
             self.dx_router = e(T, d, dtype=bf)
             self.dw_router = e(s.E, d, dtype=f32)
             self.balance_loss = e(1, dtype=f32)
+            self.routed_by = self.logits   # what the last forward call routed by, for the backward of a gate
 
 
 class _Carved:
@@ -112,6 +113,8 @@ def _route(buf, x, logits, w_router, gate, bias, stream):
     s = buf.shape
     if gate is None and bias is not None:
         raise ValueError("bias: goes with a gate")
+    if gate is not None and logits is not None and w_router is not None:   # (a backward call with both would not know which)
+        raise ValueError("gate: it routes by logits or by those of w_router, not by both")
     if gate is not None and w_router is not None:
         B.moe_router_gate_fwd(s, gate, x, w_router, bias, buf.logits, buf.topk_idx, buf.topk_w, buf.ws, stream)
     elif gate is not None and logits is not None:
@@ -127,9 +130,12 @@ def _route(buf, x, logits, w_router, gate, bias, stream):
 def layer_forward(buf: MoeLayerBuffers, x, w_gate, w_up, w_down, logits=None, w_router=None, stream=None, gate=None, bias=None):
     """routing (skipped when logits is None: buf.topk_idx / buf.topk_w were filled by the caller, as for an
     expert-parallel shard) -> permute -> grouped FFN -> combine.  With `w_router` the logits are computed first
-    (buf.logits = x W_r^T).  `gate` (a binding.Gate) routes by its scores and groups, `bias` [E] fp32 shifts its choice.  Returns buf.out."""
+    (buf.logits = x W_r^T).  `gate` (a binding.Gate) routes by its scores and groups, by `logits` or by those of `w_router`, `bias` [E] fp32 shifts
+    its choice.  Returns buf.out."""
     s = buf.shape
     _route(buf, x, logits, w_router, gate, bias, stream)
+    if hasattr(buf, "routed_by"):
+        buf.routed_by = buf.logits if logits is None or w_router is not None else logits
     B.moe_permute(s, x, buf.topk_idx, buf.x_perm, buf.counts, buf.offsets, buf.row_of_slot, buf.slot_of_row, buf.ws, stream)
     B.moe_grouped_ffn_fwd(s, buf.x_perm, buf.offsets, w_gate, w_up, w_down, buf.y_perm, buf.save_g, buf.save_u, buf.ws, stream)
     B.moe_unpermute_combine(s, buf.y_perm, buf.row_of_slot, buf.topk_w, buf.out, stream)
@@ -141,7 +147,7 @@ def layer_backward(buf: MoeLayerBuffers, dout, w_gate, w_up, w_down, accumulate=
     """combine_bwd and route_bwd (one launch) -> grouped FFN bwd -> permute_bwd.  Results land in buf.dx, buf.dw_*,
     buf.dtopk_w, buf.dlogits.  With `x` and `w_router` the layer is closed from x: router_bwd comes with the
     experts' backward, buf.dx then holds the expert-path term plus the router's term, and buf.dw_router is filled.
-    `gate`: that of the forward call, with its `logits` unless it computed them.  With `balance` the gradient of the balance loss is part of
+    `gate`: that of the forward call; its logits are taken (buf.routed_by: those given to it, or buf.logits) unless others are given.  With `balance` the gradient of the balance loss is part of
     buf.dlogits (by buf.counts), its value in buf.balance_loss."""
     s = buf.shape
     gated = with_router and buf.dlogits is not None
@@ -151,7 +157,7 @@ def layer_backward(buf: MoeLayerBuffers, dout, w_gate, w_up, w_down, accumulate=
         if buf.dlogits is None:
             raise ValueError("gate: these buffers have none for a router")
         B.moe_unpermute_combine_bwd(s, dout, buf.y_perm, buf.row_of_slot, buf.topk_w, buf.dy_perm, buf.dtopk_w, stream)
-        B.moe_gate_bwd(s, gate, buf.dtopk_w, buf.logits if logits is None else logits, buf.topk_idx, buf.topk_w, buf.counts if balance else None, balance,
+        B.moe_gate_bwd(s, gate, buf.dtopk_w, buf.routed_by if logits is None else logits, buf.topk_idx, buf.topk_w, buf.counts if balance else None, balance,
                        buf.dlogits, buf.balance_loss if balance else None, buf.ws, stream)
     elif gated or w_router is not None:   # (a token's dlogits need no more than its dtopk_w: made with it, not after the experts' backward)
         B.moe_unpermute_combine_route_bwd(s, dout, buf.y_perm, buf.row_of_slot, buf.topk_idx, buf.topk_w, buf.probs, buf.dy_perm, buf.dtopk_w,

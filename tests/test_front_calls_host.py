@@ -1,0 +1,58 @@
+"""Host-side checks of which tensors and sizes the calls in front of the experts are given and take."""
+import pytest
+import torch
+
+import paper_2605_05049_amd as moe
+from paper_2605_05049_amd import binding as B
+
+T, D, F, E, K = 3, 64, 64, 8, 2
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The entry points write down what they are given in place of launching."""
+    made = []
+    for name in dir(B):
+        if name.startswith("moe_"):
+            monkeypatch.setattr(B, name, lambda *a, _name=name, **kw: made.append((_name, a)))
+    return made
+
+
+def _layer():
+    moe.load_library()
+    buf = moe.MoeLayerBuffers(moe.Shape(T, D, F, E, K), device="cpu")
+    return buf, torch.zeros(T, D), [torch.zeros(1)] * 3, torch.zeros(T, E), torch.zeros(E, D)
+
+
+def _logits_of(calls, name, at):
+    return [a[at] for n, a in calls if n == name][-1]
+
+
+def test_the_gates_gradient_is_that_of_the_logits_that_the_forward_call_routed_by(calls):
+    buf, x, w, logits, w_router = _layer()
+    gate = moe.Gate("sigmoid")
+    moe.layer_forward(buf, x, *w, logits=logits, gate=gate)
+    moe.layer_backward(buf, x, *w, gate=gate)
+    assert _logits_of(calls, "moe_gate_fwd", 2) is logits and _logits_of(calls, "moe_gate_bwd", 3) is logits
+    moe.layer_forward(buf, x, *w, w_router=w_router, gate=gate)
+    moe.layer_backward(buf, x, *w, gate=gate, x=x, w_router=w_router)
+    assert _logits_of(calls, "moe_router_gate_fwd", 5) is buf.logits and _logits_of(calls, "moe_gate_bwd", 3) is buf.logits
+    # routed by the caller: what the caller says, or what the router's calls write
+    moe.layer_forward(buf, x, *w, logits=logits, gate=gate)
+    moe.layer_forward(buf, x, *w)
+    moe.layer_backward(buf, x, *w, gate=gate)
+    assert _logits_of(calls, "moe_gate_bwd", 3) is buf.logits
+    moe.layer_backward(buf, x, *w, gate=gate, logits=logits)
+    assert _logits_of(calls, "moe_gate_bwd", 3) is logits
+    # without a gate w_router comes first, as ever
+    moe.layer_forward(buf, x, *w, logits=logits, w_router=w_router)
+    assert calls[-4][0] == "moe_router_route_fwd" and buf.routed_by is buf.logits
+
+
+def test_a_gate_with_logits_and_a_router_is_refused(calls):
+    """Which of the two the backward pass would have to differentiate it could not know."""
+    buf, x, w, logits, w_router = _layer()
+    for forward in (moe.layer_forward, lambda *a, **kw: moe.layer_mxfp4_forward(*a[:2], a[2:], **kw)):
+        with pytest.raises(ValueError, match="not by both"):
+            forward(buf, x, *w, logits=logits, w_router=w_router, gate=moe.Gate())
+    assert not calls

@@ -1,0 +1,41 @@
+"""Calls in front of the experts as a program makes them: whose logits a gradient is of, which rows a command times, which sizes are taken."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+T, D, FF, E, K, ES = 100, 128, 192, 16, 4, 1
+
+
+def make(seed=0):
+    g = torch.Generator().manual_seed(seed)
+    normal = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).bfloat16().cuda()  # noqa: E731
+    n = E + ES
+    w = (normal(n, D, FF, std=D ** -0.5), normal(n, D, FF, std=D ** -0.5), normal(n, FF, D, std=FF ** -0.5))
+    return normal(T, D), normal(T, D), w, torch.randn(T, E, generator=g).cuda(), normal(E, D, std=D ** -0.5), (0.02 * torch.randn(E, generator=g)).cuda()
+
+
+def test_a_step_routed_by_logits_differentiates_these(moe):
+    """Eager without the logits in the backward call, and captured: what the calls one by one give."""
+    x, dout, w, logits, w_router, bias = make()
+    s, gate = moe.Shape(T, D, FF, E, K, ES), moe.Gate("sigmoid", 4, 2, 2, 2.5)
+    one, two = moe.MoeLayerBuffers(s), moe.MoeLayerBuffers(s)
+    for buf in (one, two):
+        buf.logits.fill_(float("nan"))   # (nobody's)
+    moe.layer_forward(one, x, *w, logits=logits, gate=gate, bias=bias)
+    moe.layer_backward(one, dout, *w, gate=gate, balance=2.0)
+    want = torch.empty(T, E, device="cuda")
+    moe.moe_gate_bwd(s, gate, one.dtopk_w, logits, one.topk_idx, one.topk_w, one.counts, 2.0, want, one.balance_loss, one.ws)
+    assert torch.isfinite(want).all() and torch.equal(one.dlogits, want)
+    step = moe.CapturedLayerStep(two, x, dout, *w, logits=logits, gate=gate, bias=bias, balance=2.0)
+    logits.copy_(make(1)[3])
+    moe.layer_forward(one, x, *w, logits=logits, gate=gate, bias=bias)
+    moe.layer_backward(one, dout, *w, gate=gate, balance=2.0)
+    for _ in range(3):
+        two.dlogits.zero_()
+        step.replay()
+        torch.cuda.synchronize()
+        for n in ("topk_idx", "topk_w", "out", "dx", "dlogits", "balance_loss", "dw_gate"):
+            assert torch.equal(getattr(one, n), getattr(two, n)), n
+    with pytest.raises(ValueError, match="not by both"):
+        moe.CapturedLayerStep(two, x, dout, *w, logits=logits, w_router=w_router, gate=gate)

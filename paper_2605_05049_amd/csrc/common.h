@@ -22,11 +22,11 @@ struct Dims {
   long long N;
 };
 
-// Validates a shape against the ABI limits and fills the derived sizes.
-inline int check_shape(const moe_shape* s, Dims* out) {
+// Validates a shape against the ABI limits and fills the derived sizes.  max_ids: of E'; the calls that only write a shared slot's id have no such limit.
+inline int check_shape(const moe_shape* s, Dims* out, long long max_ids = kMaxExperts) {
   if (!s) return MOE_ERR_NULL;
   if (s->T < 0 || s->E < 1 || s->k < 1 || s->k > s->E || s->E_shared < 0) return MOE_ERR_SHAPE;
-  if (s->E > kMaxExperts || (long long)s->E + s->E_shared > kMaxExperts) return MOE_ERR_SHAPE;
+  if (s->E > kMaxExperts || (long long)s->E + s->E_shared > max_ids) return MOE_ERR_SHAPE;
   if (s->d_model <= 0 || s->d_ffn <= 0 || (s->d_model % 64) || (s->d_ffn % 64)) return MOE_ERR_SHAPE;
   if (s->d_model > kMaxWidth || s->d_ffn > kMaxWidth) return MOE_ERR_SHAPE;  // 32-bit per-lane byte offsets in the GEMM loads
   long long Kp = (long long)s->k + s->E_shared;

@@ -14,6 +14,7 @@ namespace moe {
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
 constexpr float kMaxLogit = 3.402823466e38f;
 constexpr int kGateFewWaves = 1024;   // up to so many wavefronts a token has more lanes than it needs
+constexpr long long kGateIds = 0x7fffffff;   // of experts, shared ones among them, where nothing but an id is made of these
 constexpr int kGateTokens = 1 << 24;   // of a launch of the forward kernels at most: a grid has less than 2^32 threads
 constexpr int kGateBwdBlocks = 512;     // at most (two a CU; more, with more parts of the loss to add, 31 -> 40 us); each adds up its tokens' share of the loss
 
@@ -931,8 +932,8 @@ __global__ __launch_bounds__(256) void gate_bias_step_kernel(const int32_t* __re
 }
 
 // Checks a gate against the shape, and joins the two.
-static int gate_checks(const moe_shape* shape, const moe_gate* gate, Dims* D, GateArgs* A) {
-  const int rc = check_shape(shape, D);
+static int gate_checks(const moe_shape* shape, const moe_gate* gate, Dims* D, GateArgs* A, long long max_ids = kGateIds) {
+  const int rc = check_shape(shape, D, max_ids);
   if (rc != MOE_OK) return rc;
   if (!gate) return MOE_ERR_NULL;
   if (gate->scores != MOE_SCORES_SOFTMAX && gate->scores != MOE_SCORES_SIGMOID) return MOE_ERR_SHAPE;
@@ -1043,7 +1044,7 @@ extern "C" int moe_router_gate_fwd(const moe_shape* shape, const moe_gate* gate,
   using namespace moe;
   Dims D;
   GateArgs A;
-  int rc = gate_checks(shape, gate, &D, &A);
+  int rc = gate_checks(shape, gate, &D, &A, kMaxExperts);   // (as moe_router_fwd)
   if (rc != MOE_OK) return rc;
   if (D.T == 0) return MOE_OK;   // (tensors without elements may be NULL)
   MOE_REQUIRE_PTR(topk_idx); MOE_REQUIRE_PTR(topk_w);
@@ -1122,7 +1123,7 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
 extern "C" int moe_gate_bias_step(const moe_shape* shape, const int32_t* counts, float rate, float* bias, void* stream) {
   using namespace moe;
   Dims D;
-  const int rc = check_shape(shape, &D);
+  const int rc = check_shape(shape, &D, kGateIds);
   if (rc != MOE_OK) return rc;
   MOE_REQUIRE_PTR(counts); MOE_REQUIRE_PTR(bias);
   MOE_REQUIRE_ALIGNED(counts); MOE_REQUIRE_ALIGNED(bias);

@@ -39,3 +39,25 @@ def test_a_step_routed_by_logits_differentiates_these(moe):
             assert torch.equal(getattr(one, n), getattr(two, n)), n
     with pytest.raises(ValueError, match="not by both"):
         moe.CapturedLayerStep(two, x, dout, *w, logits=logits, w_router=w_router, gate=gate)
+
+
+@pytest.mark.parametrize("tokens", [3, 300])
+@pytest.mark.parametrize("experts,shared,k", [(1024, 1, 8), (1023, 2, 3), (1024, 1, 20)])
+def test_all_experts_with_shared_ones_beside_them(moe, tokens, experts, shared, k):
+    """The choice, weights and gradients of the experts are those without shared ones; a shared slot has its id and weight 1."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    logits, bias = torch.randn(tokens, experts, device="cuda", generator=g), 0.05 * torch.randn(experts, device="cuda", generator=g)
+    gate, ws, got = moe.Gate("sigmoid", scale=2.5), torch.empty(4096, dtype=torch.uint8, device="cuda"), []
+    dw = torch.randn(tokens, k, device="cuda", generator=g)
+    counts = torch.randint(0, 9, (experts,), dtype=torch.int32, device="cuda", generator=g)
+    for es in (0, shared):
+        s = moe.Shape(tokens, 64, 64, experts, k, es)
+        idx, w = torch.empty(tokens, k + es, dtype=torch.int32, device="cuda"), torch.empty(tokens, k + es, device="cuda")
+        dlogits, loss, b = torch.empty(tokens, experts, device="cuda"), torch.empty(1, device="cuda"), bias.clone()
+        n = torch.cat([counts, torch.full((es,), tokens, dtype=torch.int32, device="cuda")])
+        moe.moe_gate_fwd(s, gate, logits, bias, idx, w)
+        moe.moe_gate_bwd(s, gate, torch.cat([dw, torch.ones(tokens, es, device="cuda")], 1), logits, idx, w, n, 0.5, dlogits, loss, ws)
+        moe.moe_gate_bias_step(s, n, 0.25, b)
+        got.append((idx[:, :k], w[:, :k], dlogits, loss, b))
+        assert (idx[:, k:] == torch.arange(experts, experts + es, device="cuda")).all() and (w[:, k:] == 1).all()
+    assert all(torch.equal(a, b) for a, b in zip(*got))

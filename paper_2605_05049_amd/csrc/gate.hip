@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
       // Two c, off as above, and a rounding of their sum, for two groups; the c themselves may be large and cancel.  Scores without a bias: of sigmoid
       // as above, of softmax (without the shared sum, each at most 1) the argument, the exponential, the sum: under 8 in all.
       const float far = by_logits ? 0x1p-20f : 2.0f * slack + slack_c * (fabsf(low) + lanes_max<W>(a > kMaskedLogit ? fabsf(a) + (b > kMaskedLogit ? fabsf(b) : 0.f) : 0.f));
-      unsure_group = unsure_group || (high > kMaskedLogit && low - high <= far);
+      unsure_group = unsure_group || (high > kMaskedLogit && !(low - high > far));   // (also two sums past fp32, whose difference is NaN)
     }
     const double none = make_key(kNoKey, 0, false);
 #pragma unroll

@@ -619,44 +619,67 @@ def norm_workspace_bytes(rows, cols) -> int:
     return int(load_library().moe_norm_workspace_bytes(rows, cols))
 
 
-def _as(dtype, t, numel, name):
-    """_ptr of one dtype, for the calls that are short: the checks in the order in which they cost least."""
+def _here():
+    """The current device, where a launch goes (without one: no tensor's)."""
+    return _device() if _device is not None else _find_device()
+
+
+def _find_device():
+    global _device
+    torch = _torch_module or _torch()
+    if not torch.cuda.is_initialized():
+        return -2
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device()
+
+
+def _as(dtype, t, numel, name, here):
+    """_ptr of one dtype on the device `here`, for the calls that are short: the checks in the order in which they cost least."""
     if t is None:
         return None
-    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() >= numel:
+    if t.dtype is dtype and t.get_device() == here and t.is_contiguous() and t.numel() >= numel:
         return t.data_ptr()
-    return _ptr(t, _bf16_types() if dtype is _torch_module.bfloat16 else dtype, numel, name)
+    ptr = _ptr(t, _bf16_types() if dtype is _torch_module.bfloat16 else dtype, numel, name)
+    _on(here, t.get_device(), name)
+    return ptr
 
 
-def _stream_of(t, stream):
-    """_stream for a call on t, whose device has to be the current one: a launch goes there."""
-    handle = _stream(stream)
-    if t is not None and _device is not None and t.get_device() != _device():
-        raise ValueError(f"tensors on {t.device}: the call belongs within torch.cuda.device of it")
-    return handle
+def _on(here, device, name):
+    if device != here:
+        raise ValueError(f"{name} on device {device}: the call belongs within torch.cuda.device({device})")
 
 
-def _workspace(ws):
-    return (None, 0) if ws is None else (_ptr(ws, None, None, "ws"), ws.numel() * ws.element_size())
+def _stream_on(here, stream):
+    if stream is not None:
+        _on(here, getattr(stream, "device_index", here), "stream")
+    return _stream(stream)
+
+
+def _workspace(ws, here):
+    if ws is None:
+        return None, 0
+    ptr = _ptr(ws, None, None, "ws")
+    _on(here, ws.get_device(), "ws")
+    return ptr, ws.numel() * ws.element_size()
 
 
 def moe_gate_fwd(shape, gate, logits, bias, topk_idx, topk_w, stream=None):
     torch = _torch_module or _torch()
-    s, f32 = Shape.of(shape), torch.float32
+    s, f32, here = Shape.of(shape), torch.float32, _here()
     rc = (_lib or load_library()).moe_gate_fwd(
-        ctypes.byref(s._c), ctypes.byref(gate._c), _as(f32, logits, s.T * s.E, "logits"), _as(f32, bias, s.E, "bias"),
-        _as(torch.int32, topk_idx, s.N, "topk_idx"), _as(f32, topk_w, s.N, "topk_w"), _stream_of(logits, stream))
+        ctypes.byref(s._c), ctypes.byref(gate._c), _as(f32, logits, s.T * s.E, "logits", here), _as(f32, bias, s.E, "bias", here),
+        _as(torch.int32, topk_idx, s.N, "topk_idx", here), _as(f32, topk_w, s.N, "topk_w", here), _stream_on(here, stream))
     if rc:
         _check("moe_gate_fwd", rc)
 
 
 def moe_router_gate_fwd(shape, gate, x, w_router, bias, logits, topk_idx, topk_w, ws, stream=None):
     torch = _torch_module or _torch()
-    s, f32, bf = Shape.of(shape), torch.float32, torch.bfloat16
+    s, f32, bf, here = Shape.of(shape), torch.float32, torch.bfloat16, _here()
     rc = (_lib or load_library()).moe_router_gate_fwd(
-        ctypes.byref(s._c), ctypes.byref(gate._c), _as(bf, x, s.T * s.d_model, "x"), _as(bf, w_router, s.E * s.d_model, "w_router"),
-        _as(f32, bias, s.E, "bias"), _as(f32, logits, s.T * s.E, "logits"), _as(torch.int32, topk_idx, s.N, "topk_idx"), _as(f32, topk_w, s.N, "topk_w"),
-        *_workspace(ws), _stream_of(x, stream))
+        ctypes.byref(s._c), ctypes.byref(gate._c), _as(bf, x, s.T * s.d_model, "x", here), _as(bf, w_router, s.E * s.d_model, "w_router", here),
+        _as(f32, bias, s.E, "bias", here), _as(f32, logits, s.T * s.E, "logits", here),
+        _as(torch.int32, topk_idx, s.N, "topk_idx", here), _as(f32, topk_w, s.N, "topk_w", here), *_workspace(ws, here), _stream_on(here, stream))
     if rc:
         _check("moe_router_gate_fwd", rc)
 
@@ -664,20 +687,20 @@ def moe_router_gate_fwd(shape, gate, x, w_router, bias, logits, topk_idx, topk_w
 def moe_gate_bwd(shape, gate, dtopk_w, logits, topk_idx, topk_w, counts, balance, dlogits, loss=None, ws=None, stream=None):
     """counts None: no balance loss.  loss [1] fp32 needs counts and a workspace."""
     torch = _torch_module or _torch()
-    s, f32 = Shape.of(shape), torch.float32
+    s, f32, here = Shape.of(shape), torch.float32, _here()
     rc = (_lib or load_library()).moe_gate_bwd(
-        ctypes.byref(s._c), ctypes.byref(gate._c), _as(f32, dtopk_w, s.N, "dtopk_w"), _as(f32, logits, s.T * s.E, "logits"),
-        _as(torch.int32, topk_idx, s.N, "topk_idx"), _as(f32, topk_w, s.N, "topk_w"), _as(torch.int32, counts, s.E_total, "counts"), balance,
-        _as(f32, dlogits, s.T * s.E, "dlogits"), _as(f32, loss, 1, "loss"), *_workspace(ws), _stream_of(logits, stream))
+        ctypes.byref(s._c), ctypes.byref(gate._c), _as(f32, dtopk_w, s.N, "dtopk_w", here), _as(f32, logits, s.T * s.E, "logits", here),
+        _as(torch.int32, topk_idx, s.N, "topk_idx", here), _as(f32, topk_w, s.N, "topk_w", here), _as(torch.int32, counts, s.E_total, "counts", here), balance,
+        _as(f32, dlogits, s.T * s.E, "dlogits", here), _as(f32, loss, 1, "loss", here), *_workspace(ws, here), _stream_on(here, stream))
     if rc:
         _check("moe_gate_bwd", rc)
 
 
 def moe_gate_bias_step(shape, counts, rate, bias, stream=None):
     torch = _torch_module or _torch()
-    s = Shape.of(shape)
-    rc = (_lib or load_library()).moe_gate_bias_step(ctypes.byref(s._c), _as(torch.int32, counts, s.E_total, "counts"), rate,
-                                                     _as(torch.float32, bias, s.E, "bias"), _stream_of(counts, stream))
+    s, here = Shape.of(shape), _here()
+    rc = (_lib or load_library()).moe_gate_bias_step(ctypes.byref(s._c), _as(torch.int32, counts, s.E_total, "counts", here), rate,
+                                                     _as(torch.float32, bias, s.E, "bias", here), _stream_on(here, stream))
     if rc:
         _check("moe_gate_bias_step", rc)
 
@@ -685,12 +708,13 @@ def moe_gate_bias_step(shape, counts, rate, bias, stream=None):
 def moe_norm_fwd(centre, eps, x, addend, gamma, beta, sum, y, mean, rstd, stream=None):
     """x [..., cols] bf16; addend, gamma, beta, sum, mean and rstd may be None."""
     torch = _torch_module or _torch()
-    f32, bf = torch.float32, torch.bfloat16
+    f32, bf, here = torch.float32, torch.bfloat16, _here()
     rows, cols = _last(x, "x")
     n = rows * cols
     rc = (_lib or load_library()).moe_norm_fwd(
-        rows, cols, 1 if centre else 0, eps, _as(bf, x, n, "x"), _as(bf, addend, n, "addend"), _as(bf, gamma, cols, "gamma"), _as(bf, beta, cols, "beta"),
-        _as(bf, sum, n, "sum"), _as(bf, y, n, "y"), _as(f32, mean, rows, "mean"), _as(f32, rstd, rows, "rstd"), _stream_of(x, stream))
+        rows, cols, 1 if centre else 0, eps, _as(bf, x, n, "x", here), _as(bf, addend, n, "addend", here), _as(bf, gamma, cols, "gamma", here),
+        _as(bf, beta, cols, "beta", here), _as(bf, sum, n, "sum", here), _as(bf, y, n, "y", here), _as(f32, mean, rows, "mean", here),
+        _as(f32, rstd, rows, "rstd", here), _stream_on(here, stream))
     if rc:
         _check("moe_norm_fwd", rc)
 
@@ -698,13 +722,13 @@ def moe_norm_fwd(centre, eps, x, addend, gamma, beta, sum, y, mean, rstd, stream
 def moe_norm_bwd(centre, dy, h, gamma, mean, rstd, dx_addend, dx, dgamma, dbeta, accumulate, ws, stream=None):
     """dy, h [..., cols] bf16; gamma, dx_addend, dgamma, dbeta and (without centre) mean may be None, ws without dgamma and dbeta."""
     torch = _torch_module or _torch()
-    f32, bf = torch.float32, torch.bfloat16
+    f32, bf, here = torch.float32, torch.bfloat16, _here()
     rows, cols = _last(h, "h")
     n = rows * cols
     rc = (_lib or load_library()).moe_norm_bwd(
-        rows, cols, 1 if centre else 0, _as(bf, dy, n, "dy"), _as(bf, h, n, "h"), _as(bf, gamma, cols, "gamma"), _as(f32, mean, rows, "mean"),
-        _as(f32, rstd, rows, "rstd"), _as(bf, dx_addend, n, "dx_addend"), _as(bf, dx, n, "dx"), _as(f32, dgamma, cols, "dgamma"),
-        _as(f32, dbeta, cols, "dbeta"), 1 if accumulate else 0, *_workspace(ws), _stream_of(h, stream))
+        rows, cols, 1 if centre else 0, _as(bf, dy, n, "dy", here), _as(bf, h, n, "h", here), _as(bf, gamma, cols, "gamma", here),
+        _as(f32, mean, rows, "mean", here), _as(f32, rstd, rows, "rstd", here), _as(bf, dx_addend, n, "dx_addend", here), _as(bf, dx, n, "dx", here),
+        _as(f32, dgamma, cols, "dgamma", here), _as(f32, dbeta, cols, "dbeta", here), 1 if accumulate else 0, *_workspace(ws, here), _stream_on(here, stream))
     if rc:
         _check("moe_norm_bwd", rc)
 

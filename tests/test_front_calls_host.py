@@ -73,3 +73,90 @@ def test_the_gate_takes_all_its_experts_with_shared_ones_beside_them(E, Es):
         b = ctypes.byref(bad._c)
         assert lib.moe_gate_fwd(b, g, None, None, None, None, None) == -2 and lib.moe_gate_bias_step(b, fake, 0.1, fake, None) == -2
         assert lib.moe_gate_bwd(b, g, None, None, None, None, None, 0.0, None, None, None, 0, None) == -2
+
+
+class _On:
+    """What the binding asks of a tensor, on a device of its own."""
+
+    def __init__(self, device, dtype, *size):
+        self.at, self.dtype, self.size, self.is_cuda, self.device = device, dtype, size, True, torch.device("cuda", device)
+
+    def get_device(self):
+        return self.at
+
+    def numel(self):
+        n = 1
+        for s in self.size:
+            n *= s
+        return n
+
+    def dim(self):
+        return len(self.size)
+
+    shape = property(lambda self: torch.Size(self.size))
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x10000
+
+
+class _Stream:
+    def __init__(self, device):
+        self.device_index, self.cuda_stream = device, 0
+
+
+def _every_call(at, stream):
+    """The calls with the tensor `at` on device 1, the others on device 0: (name of the call, how many tensors)."""
+    shape, gate = moe.Shape(T, D, F, E, K), moe.Gate()
+    f, i, bf, u = torch.float32, torch.int32, torch.bfloat16, torch.uint8
+
+    def tensors(*kinds):
+        return [_On(1 if n == at else 0, *kind) for n, kind in enumerate(kinds)]
+
+    idx, w, l, x, row = (i, T, K), (f, T, K), (f, T, E), (bf, T, D), (f, T)
+    logits, bias, ti, tw = tensors(l, (f, E), idx, w)
+    yield 4, lambda: moe.moe_gate_fwd(shape, gate, logits, bias, ti, tw, stream)
+    r = tensors(x, (bf, E, D), (f, E), l, idx, w, (u, 1 << 20))
+    yield 7, lambda: moe.moe_router_gate_fwd(shape, gate, *r, stream)
+    b = tensors(w, l, idx, w, (i, E), l, (f, 1), (u, 4096))
+    yield 8, lambda: moe.moe_gate_bwd(shape, gate, *b[:5], 0.1, *b[5:], stream)
+    s = tensors((i, E), (f, E))
+    yield 2, lambda: moe.moe_gate_bias_step(shape, s[0], 0.1, s[1], stream)
+    n = tensors(x, x, (bf, D), (bf, D), x, x, row, row)
+    yield 8, lambda: moe.moe_norm_fwd(True, 1e-6, *n, stream)
+    m = tensors(x, x, (bf, D), row, row, x, x, (f, D), (f, D), (u, 1 << 20))
+    yield 10, lambda: moe.moe_norm_bwd(True, *m[:9], False, m[9], stream)
+
+
+@pytest.mark.parametrize("stream", [_Stream(0), None], ids=["stream", "current"])
+def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch, stream):
+    """Each of them, in the first call of a process too, whether a stream is given or not; nothing is launched."""
+    launched = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: launched.append(name) or 0
+
+    monkeypatch.setattr(B, "_lib", Library())
+    monkeypatch.setattr(B, "_raw_stream", None)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    for call, (tensors, _) in enumerate(_every_call(-1, stream)):
+        for at in range(tensors):
+            monkeypatch.setattr(B, "_device", None)   # (as in a call that no other one came before)
+            with pytest.raises(ValueError, match="device 1"):
+                list(_every_call(at, stream))[call][1]()
+    assert not launched
+    for _, fn in _every_call(-1, stream):
+        fn()
+    assert len(launched) == 6
+    if stream is not None:
+        for _, fn in _every_call(-1, _Stream(1)):
+            with pytest.raises(ValueError, match="stream on device 1"):
+                fn()

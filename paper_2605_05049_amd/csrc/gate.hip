@@ -1068,7 +1068,7 @@ extern "C" int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const 
   }
   MOE_REQUIRE_ALIGNED(dtopk_w); MOE_REQUIRE_ALIGNED(logits); MOE_REQUIRE_ALIGNED(topk_idx); MOE_REQUIRE_ALIGNED(topk_w); MOE_REQUIRE_ALIGNED(dlogits);
   MOE_REQUIRE_ALIGNED(counts); MOE_REQUIRE_ALIGNED(loss);
-  if (!(balance >= -kMaxLogit && balance <= kMaxLogit)) return MOE_ERR_SHAPE;
+  if (counts && !(balance >= -kMaxLogit && balance <= kMaxLogit)) return MOE_ERR_SHAPE;   // (without counts it is not read)
   // lanes of a token, and its chunks of 4 experts a lane: up to 16 experts 4 each; else up to 4 chunks, one by one 3 (of 64 lanes 4).
   // (Chunks of 3 beside 1, 2 and 4: 65536 x 160 22 -> 19.6 us, 32768 x 384 26.5 -> 23.9, 30000 x 190 20 -> 13.8.)
   const bool vec = D.E % 4 == 0;

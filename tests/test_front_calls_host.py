@@ -160,3 +160,13 @@ def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch,
         for _, fn in _every_call(-1, _Stream(1)):
             with pytest.raises(ValueError, match="stream on device 1"):
                 fn()
+
+
+@pytest.mark.parametrize("balance", [float("nan"), float("inf"), -float("inf")])
+def test_without_counts_the_balance_is_not_read(balance):
+    """(No tokens: what is checked is the number.)"""
+    import ctypes
+    lib, s, g = moe.load_library(), ctypes.byref(moe.Shape(0, D, F, E, K)._c), ctypes.byref(moe.Gate()._c)
+    fake = ctypes.c_void_p(0x10000)
+    assert lib.moe_gate_bwd(s, g, None, None, None, None, None, balance, None, None, None, 0, None) != -2   # (without a device it says so)
+    assert lib.moe_gate_bwd(s, g, None, None, None, None, fake, balance, None, None, None, 0, None) == -2

@@ -61,3 +61,14 @@ def test_all_experts_with_shared_ones_beside_them(moe, tokens, experts, shared, 
         got.append((idx[:, :k], w[:, :k], dlogits, loss, b))
         assert (idx[:, k:] == torch.arange(experts, experts + es, device="cuda")).all() and (w[:, k:] == 1).all()
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_without_counts_the_balance_is_not_read(moe):
+    x, dout, w, logits, w_router, bias = make(2)
+    s, gate, got = moe.Shape(T, 64, 64, E, K), moe.Gate("sigmoid"), []
+    idx, tw, dw = torch.empty(T, K, dtype=torch.int32, device="cuda"), torch.empty(T, K, device="cuda"), torch.randn(T, K, device="cuda")
+    moe.moe_gate_fwd(s, gate, logits, bias, idx, tw)
+    for balance in (0.0, float("nan"), float("inf")):
+        got.append(torch.empty(T, E, device="cuda"))
+        moe.moe_gate_bwd(s, gate, dw, logits, idx, tw, None, balance, got[-1])
+    assert torch.isfinite(got[0]).all() and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])

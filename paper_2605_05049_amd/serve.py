@@ -88,13 +88,18 @@ class ServedLayer:
         for name, t in (("x", x), ("addend", addend)):
             if t is not None and (t.dim() != 2 or t.shape[1] != self._fields[0] or t.shape != x.shape):
                 raise ValueError(f"{name} {tuple(t.shape)}: expected [T, {self._fields[0]}], as x")
+        with on_stream(stream):
+            h, y = self._normed(x, addend)
+            return h, self(y)
+
+    def _normed(self, x, addend=None):
+        """h = x + addend (x itself without an addend) and its norm."""
         import torch
         gamma, beta, centre, eps = self.norm
-        with on_stream(stream):
-            y = torch.empty_like(x)
-            h = x if addend is None else torch.empty_like(x)
-            B.moe_norm_fwd(centre, eps, x, addend, gamma, beta, None if addend is None else h, y, None, None)
-            return h, self(y)
+        y = torch.empty_like(x)
+        h = x if addend is None else torch.empty_like(x)
+        B.moe_norm_fwd(centre, eps, x, addend, gamma, beta, None if addend is None else h, y, None, None)
+        return h, y
 
     def _used(self, streams, tensors):
         """What the call used, these tensors and the weights, is not to be handed out again before the current stream is past it.  (Once per stream: the
@@ -151,8 +156,9 @@ def _ms(fn, repeats):
 
 
 def balance(layer, x, steps, rate):
-    """`steps` steps of the layer's bias on the loads of x; the largest load over the mean, before and after."""
-    import torch
+    """`steps` steps of the layer's bias on the loads of x (of its norm, if the layer has one); the largest load over the mean, before and after."""
+    if layer.norm is not None:
+        _, x = layer._normed(x)
     E, loads = layer.w_router.shape[0], []
     s = B.Shape(x.shape[0], *layer._fields)
     buf = MoeLayerBuffers(s, layer.w_router.device, with_backward=False, with_saved=False)
@@ -167,7 +173,8 @@ def balance(layer, x, steps, rate):
 
 
 def run(d, f, experts, top_k, shared, prompt, batch, steps, seed=0, gate=None, norm=None, balance_steps=0, balance_rate=0.002):
-    """norm: "rms" or "layer"; balance_steps: the gate's bias begins at 0 and takes that many steps on the prompt's loads."""
+    """norm: "rms" or "layer", in front of the layer: then prompt and steps go through `block`.  balance_steps: the gate's bias begins at 0 and takes that
+    many steps on the prompt's loads."""
     import torch
     g = torch.Generator(device="cuda").manual_seed(seed)
     normal = lambda *s, std: (torch.randn(*s, device="cuda", generator=g) * std).bfloat16()  # noqa: E731
@@ -183,22 +190,26 @@ def run(d, f, experts, top_k, shared, prompt, batch, steps, seed=0, gate=None, n
     full = ServedLayer(w_router, *weights, top_k, shared, mxfp4=False, **front)
     layer = ServedLayer(w_router, *weights, top_k, shared, **front)
     loads = balance(layer, x, balance_steps, balance_rate) if balance_steps else None
-    ref, got = full(x).float(), layer(x).float()
+    through = lambda served, *rows: served(*rows) if norm is None else served.block(*rows)[1]  # noqa: E731
+    got = through(layer, x).clone()
+    ref = through(full, x).float()
     answer(layer, x, batch, steps)
-    static = x[-batch:].clone()
-    layer(static)
+    # a step's rows: the prompt's last ones; with a norm they are the residual stream, to which the prompt's answers are added
+    static = [x[-batch:].clone()] + ([] if norm is None else [got[-batch:].clone()])
+    got = got.float()
+    through(layer, *static)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        step = layer(static)
-    step_ref = full(static).float()
+        step = through(layer, *static)
+    step_ref = through(full, *static).float()
     graph.replay()
     step = step.float()
     off = lambda a, b: round(((a - b).norm() / b.norm()).item(), 4)  # noqa: E731
     return {"d_model": d, "d_ffn": f, "experts": experts, "shared": shared, "top_k": top_k, "prompt": prompt, "batch": batch,
             "weights_GB": round(sum(w.numel() * w.element_size() for w in layer.weights) / 1e9, 3),
             "bf16_weights_GB": round(sum(w.numel() * w.element_size() for w in weights) / 1e9, 3),
-            "prompt_ms": round(_ms(lambda: layer(x), 5), 4), "bf16_prompt_ms": round(_ms(lambda: full(x), 5), 4),
+            "prompt_ms": round(_ms(lambda: through(layer, x), 5), 4), "bf16_prompt_ms": round(_ms(lambda: through(full, x), 5), 4),
             "step_us": round(1e3 * _ms(graph.replay, max(1, steps)), 2), "off_prompt": off(got, ref), "off_step": off(step, step_ref),
             **({"load_before": round(loads[0], 3), "load_after": round(loads[1], 3)} if loads else {})}
 

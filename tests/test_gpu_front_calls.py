@@ -72,3 +72,25 @@ def test_without_counts_the_balance_is_not_read(moe):
         got.append(torch.empty(T, E, device="cuda"))
         moe.moe_gate_bwd(s, gate, dw, logits, idx, tw, None, balance, got[-1])
     assert torch.isfinite(got[0]).all() and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("norm,batch", [("rms", 2), ("layer", 70)])
+def test_the_command_answers_through_its_norm(moe, monkeypatch, norm, batch):
+    """Loads, prompts and steps, timed or compared: every row that is routed is a norm's, whose mean square is 1 (as it is drawn it is off by 0.1)."""
+    from paper_2605_05049_amd import serve
+    seen, captured, route = [], [], moe.binding.moe_router_gate_fwd
+
+    def watch(shape, gate, x, *rest):
+        if torch.cuda.is_current_stream_capturing():
+            captured.append(x.shape[0])
+        else:
+            seen.append(x.float().square().mean(1))
+        route(shape, gate, x, *rest)
+
+    monkeypatch.setattr(moe.binding, "moe_router_gate_fwd", watch)
+    got = serve.run(256, 192, 8, 2, 1, 80, batch, 3, gate=moe.Gate("sigmoid", 4, 2, 2, 2.5), norm=norm, balance_steps=4)
+    # each value is rounded to bf16, by 2^-8 of itself at most, and so its square by 2^-7 (and 2^-16); eps and fp32 are below 1e-5
+    assert (torch.cat(seen) - 1).abs().max().item() <= 2.0 ** -7 + 3e-5
+    assert captured == [batch] and {v.numel() for v in seen} == {80, batch}
+    assert got["step_us"] > 0 and got["prompt_ms"] > 0 and got["off_step"] < 0.5 and got["off_prompt"] < 0.5
+    assert got["load_after"] >= 1

@@ -368,23 +368,23 @@ static bool norm_bwd_one_launch(long long rows) { return rows <= 1024; }
 
 }  // namespace moe
 
-// The launch of a row's lanes for their number of chunks.
-#define MOE_LAUNCH_NORM_CHUNKS(L_)                     \
+// The launch of a row's lanes for their number of chunks, of which FIRST_ to 3 occur, of 512 lanes also 4.  (A form that no size reaches is not made.)
+#define MOE_LAUNCH_NORM_CHUNKS(L_, FIRST_)             \
   do {                                                 \
     const int chunks = (cols + 8 * L_ - 1) / (8 * L_); \
-    if (chunks <= 1) MOE_LAUNCH_NORM(L_, 1);           \
+    if (chunks <= FIRST_) MOE_LAUNCH_NORM(L_, FIRST_); \
     else if (chunks == 2) MOE_LAUNCH_NORM(L_, 2);      \
     else if (chunks == 3) MOE_LAUNCH_NORM(L_, 3);      \
-    else MOE_LAUNCH_NORM(L_, 4);                       \
+    else MOE_LAUNCH_NORM(L_, (L_ < 512 ? 3 : 4));      \
   } while (0)
-#define MOE_LAUNCH_NORM_LANES(lanes)                      \
-  do {                                                    \
-    if (lanes == 16) MOE_LAUNCH_NORM(16, 1);              \
-    else if (lanes == 32) MOE_LAUNCH_NORM(32, 1);         \
-    else if (lanes == 64) MOE_LAUNCH_NORM_CHUNKS(64);     \
-    else if (lanes == 128) MOE_LAUNCH_NORM_CHUNKS(128);   \
-    else if (lanes == 256) MOE_LAUNCH_NORM_CHUNKS(256);   \
-    else MOE_LAUNCH_NORM_CHUNKS(512);                     \
+#define MOE_LAUNCH_NORM_LANES(lanes, FIRST_)                    \
+  do {                                                          \
+    if (lanes == 16) MOE_LAUNCH_NORM(16, 1);                    \
+    else if (lanes == 32) MOE_LAUNCH_NORM(32, 1);               \
+    else if (lanes == 64) MOE_LAUNCH_NORM_CHUNKS(64, 1);        \
+    else if (lanes == 128) MOE_LAUNCH_NORM_CHUNKS(128, FIRST_); \
+    else if (lanes == 256) MOE_LAUNCH_NORM_CHUNKS(256, FIRST_); \
+    else MOE_LAUNCH_NORM_CHUNKS(512, FIRST_);                   \
   } while (0)
 
 extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const uint16_t* x, const uint16_t* addend, const uint16_t* gamma,
@@ -410,7 +410,7 @@ extern "C" int moe_norm_fwd(int64_t rows, int cols, int centre, float eps, const
     const size_t at = (size_t)done * cols;
     const NormFwdArgs A = {rows, cols, eps, 1.0f / cols, x + at, addend ? addend + at : nullptr, gamma, beta, sum ? sum + at : nullptr, y + at,
                            mean ? mean + done : nullptr, rstd ? rstd + done : nullptr};
-    MOE_LAUNCH_NORM_LANES(lanes);
+    MOE_LAUNCH_NORM_LANES(lanes, 1);
   }
 #undef MOE_LAUNCH_NORM
   return launch_status();
@@ -456,7 +456,7 @@ extern "C" int moe_norm_bwd(int64_t rows, int cols, int centre, const uint16_t* 
     else MOE_LAUNCH_NORM_BETA(L_, CH_, false, false);               \
   } while (0)
     const int lanes = norm_bwd_lanes(cols);
-    MOE_LAUNCH_NORM_LANES(lanes);
+    MOE_LAUNCH_NORM_LANES(lanes, 2);
 #undef MOE_LAUNCH_NORM
 #undef MOE_LAUNCH_NORM_BETA
   }

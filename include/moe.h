@@ -128,7 +128,8 @@ int moe_router_bwd(const moe_shape* shape, const uint16_t* x, const uint16_t* w_
  *   topk_w_j = scale s_j / sum_i s_i (shape->renorm; the sum over the k chosen), else scale s_j.   Shared slots as in moe_route_topk, weight 1.
  * An expert whose logit is NaN or at most -1e30 is masked: s = 0, it comes after all others of its group and does not count in the group's score (a
  * group of masked experts alone comes after all others); one whose c is NaN or at most -1e30 comes last in the same way.  An infinite logit counts as the largest finite one.
- * A token without experts gets its lowest ids with weights 0.  Decisions are those of s and c in 64 bits; weights are fp32.
+ * A token without experts gets its lowest ids with weights 0.  Decisions are those of s and c in 64 bits (where the scores of two groups
+ * are equal but for their rounding there, either may stay); weights are fp32.
  * moe_gate_fwd, moe_gate_bwd and moe_gate_bias_step take E <= 1024 with any number of shared experts beside them: E' has no limit of its own there
  * (T*K' < 2^31 and E' < 2^31 hold). */
 #define MOE_SCORES_SOFTMAX 0
@@ -144,6 +145,10 @@ typedef struct {
 /*   logits [T,E] fp32 in;  bias [E] fp32 in, may be NULL;  topk_idx [T,K'] int32 out;  topk_w [T,K'] fp32 out. */
 int moe_gate_fwd(const moe_shape* shape, const moe_gate* gate, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w,
                  void* stream);
+
+/* Which of its forms moe_gate_fwd runs the shape's tokens in (of more than 2^24 the first ones).  form [4] out, host memory: keys of a list, lanes of a
+ * token, experts of a lane at most, and whether every lane has as many; 0 keys: the kernel for k > 16 or more than 64 groups.  Host only. */
+int moe_gate_form(const moe_shape* shape, const moe_gate* gate, int32_t* form);
 
 /* moe_router_fwd and moe_gate_fwd in one.  Arguments as those of the two calls. */
 int moe_router_gate_fwd(const moe_shape* shape, const moe_gate* gate, const uint16_t* x, const uint16_t* w_router, const float* bias, float* logits,

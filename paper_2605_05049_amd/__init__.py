@@ -14,7 +14,7 @@ from .binding import (  # noqa: F401
     moe_halo_pack_remote, moe_halo_repack, moe_halo_unpack,
     moe_mxfp4_quantize, moe_mxfp4_quantize_t, moe_mxfp4_dequantize, moe_mxfp4_grouped_gemm, moe_mxfp4_grouped_ffn_fwd,
     mxfp4_workspace_bytes, mxfp4_grouped_gemm_large_tiles,
-    Gate, moe_gate_fwd, moe_router_gate_fwd, moe_gate_bwd, moe_gate_bias_step, moe_norm_fwd, moe_norm_bwd, norm_workspace_bytes, NORM_COLS_MAX,
+    Gate, moe_gate_fwd, gate_form, moe_router_gate_fwd, moe_gate_bwd, moe_gate_bias_step, moe_norm_fwd, moe_norm_bwd, norm_workspace_bytes, NORM_COLS_MAX,
     FEW_TOKENS_MAX, layer_few_workspace_bytes, moe_layer_few_fwd, moe_layer_few_mxfp4_fwd,
 )
 from .layer import (  # noqa: F401

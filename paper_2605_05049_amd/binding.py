@@ -22,7 +22,7 @@ EXPORTED_SYMBOLS = (
     "moe_mxfp4_quantize", "moe_mxfp4_quantize_t", "moe_mxfp4_dequantize", "moe_mxfp4_grouped_gemm", "moe_mxfp4_grouped_gemm_large_tiles",
     "moe_mxfp4_grouped_ffn_fwd", "moe_mxfp4_workspace_bytes",
     "moe_layer_few_workspace_bytes", "moe_layer_few_fwd", "moe_layer_few_mxfp4_fwd",
-    "moe_gate_fwd", "moe_router_gate_fwd", "moe_gate_bwd", "moe_gate_bias_step",
+    "moe_gate_fwd", "moe_gate_form", "moe_router_gate_fwd", "moe_gate_bwd", "moe_gate_bias_step",
     "moe_norm_fwd", "moe_norm_bwd", "moe_norm_workspace_bytes",
 )
 NORM_COLS_MAX = 16384   # MOE_NORM_COLS_MAX: columns of a moe_norm_* call
@@ -163,6 +163,7 @@ def load_library():
     sigs["moe_layer_few_mxfp4_fwd"] = [sp] + [V] * 12 + [c_size_t, V]
     gp, c_float = POINTER(_CGate), ctypes.c_float
     sigs["moe_gate_fwd"] = [sp, gp, V, V, V, V, V]
+    sigs["moe_gate_form"] = [sp, gp, POINTER(c_int32)]
     sigs["moe_router_gate_fwd"] = [sp, gp, V, V, V, V, V, V, V, c_size_t, V]
     sigs["moe_gate_bwd"] = [sp, gp, V, V, V, V, V, c_float, V, V, V, c_size_t, V]
     sigs["moe_gate_bias_step"] = [sp, V, c_float, V, V]
@@ -671,6 +672,13 @@ def moe_gate_fwd(shape, gate, logits, bias, topk_idx, topk_w, stream=None):
         _as(torch.int32, topk_idx, s.N, "topk_idx", here), _as(f32, topk_w, s.N, "topk_w", here), _stream_on(here, stream))
     if rc:
         _check("moe_gate_fwd", rc)
+
+
+def gate_form(shape, gate):
+    """(keys of a list, lanes of a token, experts of a lane, whether every lane has as many): the form of moe_gate_fwd that these tokens run."""
+    form = (c_int32 * 4)()
+    _check("moe_gate_form", load_library().moe_gate_form(ctypes.byref(Shape.of(shape)._c), ctypes.byref(gate._c), form))
+    return tuple(form)
 
 
 def moe_router_gate_fwd(shape, gate, x, w_router, bias, logits, topk_idx, topk_w, ws, stream=None):

@@ -31,12 +31,10 @@ __device__ __forceinline__ float gate_finite(float l) { return l > kMaxLogit ? k
 __device__ __forceinline__ float sigmoid_over(float l, float top) { return 1.0f / (expf(top - l) + expf(top)); }
 
 // A token's choices in 64 bits by a wavefront: any number of groups and experts, any k.  Choice j comes back on lane j % 64 in held[j / 64].  c: LDS of
-// E + groups doubles, of E + 96 with `from`: where the choices are known to be among the experts whose c is at least that, these (mostly k, or one more)
-// are put in order; else k rounds find the best one left.  Where this is the way out of the other kernel, one wavefront in some hundred takes it (of
+// E + groups doubles; k rounds find the best one left.  Where this is the way out of the other kernel, one wavefront in some hundred takes it (of
 // 65536 tokens of 256 experts 3 in 10000, most of which need less than this), alone: its time is that of one instruction after another, 5 us of a launch.
 template <int PER>
-__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A,
-                                               float from) {
+__device__ __forceinline__ void choose_exactly(const float* __restrict__ row, const float* __restrict__ bias, double* c, int (&held)[PER], const GateArgs& A) {
   const int lane = threadIdx.x % kWave, E = A.E;
   constexpr double OUT = -__builtin_inf(), LAST = -1.7e308;   // not to be chosen; masked: after all others
   const bool by_logits = bias == nullptr, by_score = by_logits && A.group_best > 1;   // (a sum of logits would say nothing)
@@ -130,37 +128,6 @@ __device__ __forceinline__ void choose_exactly(const float* __restrict__ row, co
   }
 #pragma unroll
   for (int p = 0; p < PER; p++) held[p] = 0;
-  if (from > kMaskedLogit) {
-    double* found_c = c + E;
-    int* found = reinterpret_cast<int*>(found_c + kWave);
-    int n = 0;
-#pragma unroll UN
-    for (int p = 0; p < PER; p++) {
-      const int e = lane + p * kWave;
-      const double v = e < E ? c[e] : OUT;
-      const bool one = v >= (double)from;
-      const unsigned long long all = __ballot(one);
-      const int at = n + __popcll(all & ((1ull << lane) - 1));
-      if (one && at < kWave) {
-        found_c[at] = v;
-        found[at] = e;
-      }
-      n += __popcll(all);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (n >= A.k && n <= kWave) {
-      const double v = lane < n ? found_c[lane] : OUT;
-      const int e = lane < n ? found[lane] : 0;
-      int place = 0;
-#pragma unroll 8
-      for (int o = 0; o < n; o++) place += found_c[o] > v || (found_c[o] == v && found[o] < e);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (lane < n) found[place] = e;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      held[0] = lane < A.k ? found[lane] : 0;
-      return;
-    }
-  }
 #pragma unroll 1
   for (int j = 0; j < A.k; j++) {
     double best = OUT;
@@ -195,7 +162,7 @@ __global__ __launch_bounds__(256) void gate_general_kernel(const float* __restri
   const int E = A.E, k = A.k, Kp = k + A.Es;
   const float* row = logits + (size_t)t * E;
   int held[PER];
-  choose_exactly<PER>(row, bias, row_c[wave], held, A, -__builtin_inff());
+  choose_exactly<PER>(row, bias, row_c[wave], held, A);
   float m = -kMaxLogit, all = 0.f;
   if (!A.sigmoid && !A.renorm) {
     float l[PER];
@@ -346,7 +313,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   constexpr int MAX_E = W * PER < kMaxExperts ? W * PER : kMaxExperts;
   constexpr int RUN = FULL ? PER : 32;
   constexpr int ROW_FLOATS = kWave * (PER + 4) + PER;                   // (gate_place; the last lane reads on behind its run)
-  constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave + kWave / 2);         // what choose_exactly takes of them
+  constexpr int EXACT_FLOATS = 2 * (MAX_E + kWave);                     // what choose_exactly takes of them
   __shared__ __attribute__((aligned(16))) float rows[4][ROW_FLOATS > EXACT_FLOATS ? ROW_FLOATS : EXACT_FLOATS];
   __shared__ double group_scores[4][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane % W, tt = lane / W;
@@ -580,7 +547,6 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
   join_lanes(std::integral_constant<int, 8>{});
   join_lanes(std::integral_constant<int, 16>{});
   join_lanes(std::integral_constant<int, 32>{});
-  if (A.groups > 1 && P.lanes_of_group == W) select_groups();
 
   // lane g takes choice g
   double mine = best[0];
@@ -670,8 +636,7 @@ __global__ __launch_bounds__(256, 4) void gate_kernel(const float* __restrict__ 
     while (again) {   // (the logits in LDS make room)
       const int token = __builtin_ctzll(again) / W;
       int held[(MAX_E + kWave - 1) / kWave];
-      choose_exactly<(MAX_E + kWave - 1) / kWave>(logits + (size_t)(t0 + token) * E, bias, reinterpret_cast<double*>(rows[wave]), held, A,
-                                                   __shfl(least, token * W, kWave));
+      choose_exactly<(MAX_E + kWave - 1) / kWave>(logits + (size_t)(t0 + token) * E, bias, reinterpret_cast<double*>(rows[wave]), held, A);
       const int found = __shfl(held[0], g, kWave);
       if (tt == token) {
         choice = found;
@@ -966,20 +931,41 @@ static int gate_lanes(const GateArgs& A, GatePlan* P) {
   return 0;
 }
 
+// The form of gate_kernel, or of the general kernel (K = 0), that so many tokens run.  FULL with 64 lanes of 32 experts would be more than 1024 of these.
+struct GateForm { int K, W, PER; bool full; };
+static GateForm gate_form(const GateArgs& A, GatePlan* P) {
+  const int W = gate_lanes(A, P), K = A.k > 8 ? 16 : A.k > 4 ? 8 : 4;
+  if (!W) return {0, kWave, A.E <= 64 ? 1 : A.E <= 128 ? 2 : A.E <= 256 ? 4 : A.E <= 512 ? 8 : 16, false};
+  const int per = K <= 8 && P->piece <= 8 ? 8 : P->piece <= 16 ? 16 : K <= 8 && P->piece <= 24 ? 24 : 32;
+  return {K, W, per, P->piece == per && per * P->lanes_of_group * A.groups == A.E};
+}
+
 template <int K, int W, int PER>
-static void launch_gate_kernel(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
+static void launch_gate_kernel(hipStream_t st, const GateForm& F, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias,
+                               int32_t* topk_idx, float* topk_w) {
   constexpr int TOKENS = 4 * kWave / W;
+  constexpr bool SOME_FULL = W < kWave || PER < 32;
   const dim3 grid((A.T + TOKENS - 1) / TOKENS), block(256);
-  const bool full = P.piece == PER && PER * P.lanes_of_group * A.groups == A.E;
-  if (full) MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, true>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
+  if (SOME_FULL && F.full) MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, SOME_FULL>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
   else MOE_LAUNCH("gate", st, (gate_kernel<K, W, PER, false>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A, P);
 }
 template <int K, int W>
-static void launch_gate_lanes(hipStream_t st, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
-  if (K <= 8 && P.piece <= 8) launch_gate_kernel<K, W, K <= 8 ? 8 : 16>(st, A, P, logits, bias, topk_idx, topk_w);
-  else if (P.piece <= 16) launch_gate_kernel<K, W, 16>(st, A, P, logits, bias, topk_idx, topk_w);
-  else if (K <= 8 && P.piece <= 24) launch_gate_kernel<K, W, K <= 8 ? 24 : 32>(st, A, P, logits, bias, topk_idx, topk_w);
-  else launch_gate_kernel<K, W, 32>(st, A, P, logits, bias, topk_idx, topk_w);
+static void launch_gate_lanes(hipStream_t st, const GateForm& F, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias,
+                              int32_t* topk_idx, float* topk_w) {
+  constexpr int FEWEST = K <= 8 ? 8 : 16;
+  if (F.PER == FEWEST) launch_gate_kernel<K, W, FEWEST>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  else if (F.PER == 16) launch_gate_kernel<K, W, 16>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  else if (K <= 8 && F.PER == 24) launch_gate_kernel<K, W, K <= 8 ? 24 : 32>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  else launch_gate_kernel<K, W, 32>(st, F, A, P, logits, bias, topk_idx, topk_w);
+}
+template <int K>
+static void launch_gate_lists(hipStream_t st, const GateForm& F, const GateArgs& A, const GatePlan& P, const float* logits, const float* bias,
+                              int32_t* topk_idx, float* topk_w) {
+  constexpr int FEWEST = K <= 8 ? 8 : 16;
+  if (F.W == FEWEST) launch_gate_lanes<K, FEWEST>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  else if (F.W == 16) launch_gate_lanes<K, 16>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  else if (F.W == 32) launch_gate_lanes<K, 32>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  else launch_gate_lanes<K, 64>(st, F, A, P, logits, bias, topk_idx, topk_w);
 }
 
 static void launch_gate(hipStream_t st, const GateArgs& all, const float* logits, const float* bias, int32_t* topk_idx, float* topk_w) {
@@ -992,33 +978,16 @@ static void launch_gate(hipStream_t st, const GateArgs& all, const float* logits
     return;
   }
   GatePlan P;
-  const int W = gate_lanes(A, &P);
-  if (W && A.k <= 4) {
-    if (W == 8) launch_gate_lanes<4, 8>(st, A, P, logits, bias, topk_idx, topk_w);
-    else if (W == 16) launch_gate_lanes<4, 16>(st, A, P, logits, bias, topk_idx, topk_w);
-    else if (W == 32) launch_gate_lanes<4, 32>(st, A, P, logits, bias, topk_idx, topk_w);
-    else launch_gate_lanes<4, 64>(st, A, P, logits, bias, topk_idx, topk_w);
-    return;
-  }
-  if (W && A.k <= 8) {
-    if (W == 8) launch_gate_lanes<8, 8>(st, A, P, logits, bias, topk_idx, topk_w);
-    else if (W == 16) launch_gate_lanes<8, 16>(st, A, P, logits, bias, topk_idx, topk_w);
-    else if (W == 32) launch_gate_lanes<8, 32>(st, A, P, logits, bias, topk_idx, topk_w);
-    else launch_gate_lanes<8, 64>(st, A, P, logits, bias, topk_idx, topk_w);
-    return;
-  }
-  if (W) {
-    if (W == 16) launch_gate_lanes<16, 16>(st, A, P, logits, bias, topk_idx, topk_w);
-    else if (W == 32) launch_gate_lanes<16, 32>(st, A, P, logits, bias, topk_idx, topk_w);
-    else launch_gate_lanes<16, 64>(st, A, P, logits, bias, topk_idx, topk_w);
-    return;
-  }
+  const GateForm F = gate_form(A, &P);
+  if (F.K == 4) return launch_gate_lists<4>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  if (F.K == 8) return launch_gate_lists<8>(st, F, A, P, logits, bias, topk_idx, topk_w);
+  if (F.K == 16) return launch_gate_lists<16>(st, F, A, P, logits, bias, topk_idx, topk_w);
   const dim3 grid((A.T + 3) / 4), block(256);
 #define MOE_LAUNCH_GATE(PER) MOE_LAUNCH("gate_general", st, (gate_general_kernel<PER>), grid, block, 0, st, logits, bias, topk_idx, topk_w, A)
-  if (A.E <= 64) MOE_LAUNCH_GATE(1);
-  else if (A.E <= 128) MOE_LAUNCH_GATE(2);
-  else if (A.E <= 256) MOE_LAUNCH_GATE(4);
-  else if (A.E <= 512) MOE_LAUNCH_GATE(8);
+  if (F.PER == 1) MOE_LAUNCH_GATE(1);
+  else if (F.PER == 2) MOE_LAUNCH_GATE(2);
+  else if (F.PER == 4) MOE_LAUNCH_GATE(4);
+  else if (F.PER == 8) MOE_LAUNCH_GATE(8);
   else MOE_LAUNCH_GATE(16);
 #undef MOE_LAUNCH_GATE
 }
@@ -1037,6 +1006,20 @@ extern "C" int moe_gate_fwd(const moe_shape* shape, const moe_gate* gate, const 
   MOE_REQUIRE_ALIGNED(logits); MOE_REQUIRE_ALIGNED(bias); MOE_REQUIRE_ALIGNED(topk_idx); MOE_REQUIRE_ALIGNED(topk_w);
   launch_gate((hipStream_t)stream, A, logits, bias, topk_idx, topk_w);
   return launch_status();
+}
+
+extern "C" int moe_gate_form(const moe_shape* shape, const moe_gate* gate, int32_t* form) {
+  using namespace moe;
+  Dims D;
+  GateArgs A;
+  const int rc = gate_checks(shape, gate, &D, &A);
+  if (rc != MOE_OK) return rc;
+  MOE_REQUIRE_PTR(form);
+  GatePlan P;
+  A.T = D.T < kGateTokens ? D.T : kGateTokens;
+  const GateForm F = gate_form(A, &P);
+  form[0] = F.K; form[1] = F.W; form[2] = F.PER; form[3] = F.full;
+  return MOE_OK;
 }
 
 extern "C" int moe_router_gate_fwd(const moe_shape* shape, const moe_gate* gate, const uint16_t* x, const uint16_t* w_router, const float* bias,

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import gate_cases as G
 from oracle import front_oracle as F
 
 pytestmark = pytest.mark.gpu
@@ -37,3 +38,40 @@ def test_biases_whose_sums_leave_fp32(moe, scores, E, k, groups, kept, T):
         assert np.array_equal(idx[some], want), values
         # exponentials of arguments up to 10 (their size times U, 2 U for the function), sums over k, two divisions
         assert (np.abs(w[some] - want_w) <= 60 * U * want_w).all()
+
+
+def spread(logits):
+    """How far apart the live logits of a row lie, at most: the exponentials' arguments (past 200 they are 0)."""
+    l = np.where(logits > G.MASKED, logits, np.nan).astype(np.float64)
+    l = l[~np.isnan(l).all(1)]
+    return float(min((np.nanmax(l, 1) - np.nanmin(l, 1)).max(), 200.0)) if len(l) else 0.0
+
+
+@pytest.mark.parametrize("form", G.FORMS, ids=lambda f: "-".join(map(str, f)))
+def test_a_form_against_the_definition(moe, form):
+    for n, case in enumerate(G.FORMS[form]):
+        T, E, k, groups = case
+        assert moe.gate_form(moe.Shape(T, 64, 64, E, k), moe.Gate("sigmoid", groups)) == form
+        kept, best = G.groups_of(case)
+        for scores in ("softmax", "sigmoid"):
+            for mask in G.MASKS:
+                for with_bias in (True, False):
+                    print(case, scores, mask, with_bias, flush=True)
+                    renorm = (n == 0) == (scores == "softmax")
+                    logits, bias = G.make(case, mask, scores)
+                    bias = bias if with_bias else None
+                    idx, w = choose(moe, logits, bias, k, groups, kept, best, scores, renorm, 2.5, n)
+                    args = gpu(logits), gpu(bias), k, scores, groups, kept, best
+                    want, want_w, rating = G.gate_fwd(*args, renorm, 2.5)
+                    want, want_w = want.cpu().numpy(), want_w.cpu().numpy()
+                    other = np.nonzero((idx[:, :k] != want).any(1))[0]
+                    for t in other:   # (of some masks, and only by the doubt about its groups)
+                        left = G.choices_in_doubt(args[0][t:t + 1], *args[1:], rating[t:t + 1])
+                        assert mask == "ties" and any(np.array_equal(c.cpu().numpy(), idx[t, :k]) for c in left), (case, scores, mask, with_bias, t)
+                    assert len(other) <= T // 8, (case, scores, mask, with_bias, len(other))
+                    assert (idx[:, k:] == np.arange(E, E + n)).all() and (w[:, k:] == 1).all()
+                    # an exponential's argument is rounded and its factor too: 1.5 U of the argument's size; the function, the reciprocal, the sum of 32 and 6
+                    # and the products are off by 1 or 2 U each
+                    w, want_w, logits = (np.delete(v, other, 0) for v in (w, want_w, logits))
+                    off = np.abs(w[:, :k] - want_w)
+                    assert (off <= (2 * spread(logits) + 60) * U * want_w + 1e-37).all(), (case, scores, mask, with_bias, off.max())

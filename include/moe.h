@@ -160,7 +160,8 @@ int moe_router_gate_fwd(const moe_shape* shape, const moe_gate* gate, const uint
  *   dtopk_w [T,K'] fp32 in;  logits [T,E] fp32, topk_idx, topk_w [T,K'] in, as read and written by moe_gate_fwd;  counts [E'] int32 in, as of
  *   moe_permute, may be NULL (balance is then not read);  dlogits [T,E] fp32 out;  loss [1] fp32 out, L: may be NULL, needs counts and 4 KB of
  *   workspace `ws`, which is not read without it (T = 0: L = 0).
- * A masked expert's logit has gradient 0; an expert that topk_idx names twice gets the sum.  The loss is summed in a fixed order. */
+ * A masked expert's logit has gradient 0, and the dtopk_w of a slot of weight 0 is not read (it may be NaN); an expert that topk_idx names twice gets the
+ * sum.  The loss is summed in a fixed order. */
 int moe_gate_bwd(const moe_shape* shape, const moe_gate* gate, const float* dtopk_w, const float* logits, const int32_t* topk_idx,
                  const float* topk_w, const int32_t* counts, float balance, float* dlogits, float* loss, void* ws, size_t ws_bytes, void* stream);
 

@@ -746,9 +746,12 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(cons
     const size_t at = (size_t)(live ? t : A.T - 1);
     const float* src = logits + at * E;
     float (&l)[4 * C] = cur.l;
-    // the slots (k of them, W at a time)
-    float inner = g < k ? cur.w * cur.dw : 0.f;
-    for (int j = g + W; j < k; j += W) inner = fmaf(topk_w[at * Kp + j], dtopk_w[at * Kp + j], inner);
+    // the slots (k of them, W at a time; one without weight, a masked expert's, counts as nothing, whatever its dw is)
+    float inner = g < k && cur.w != 0.f ? cur.w * cur.dw : 0.f;
+    for (int j = g + W; j < k; j += W) {
+      const float w = topk_w[at * Kp + j];
+      inner = w != 0.f ? fmaf(w, dtopk_w[at * Kp + j], inner) : inner;
+    }
     inner = lanes_sum<W>(inner);
 #pragma unroll
     for (int c = 0; c < C; c++) *reinterpret_cast<float4*>(row + 4 * (g + W * c)) = float4{0.f, 0.f, 0.f, 0.f};
@@ -764,6 +767,7 @@ __global__ __launch_bounds__(kGateBwdWaves * kWave, 4) void gate_bwd_kernel(cons
       }
       const bool mine = j < k && (unsigned)e < (unsigned)E;   // (no other id has a logit)
       float d = A.renorm ? w * (dw - inner * inv_scale) : w * dw;
+      d = w != 0.f ? d : 0.f;
       if (A.sigmoid && !dense && mine) {
         const float x = src[e];
         d = gate_masked(x) ? 0.f : d * __builtin_amdgcn_rcpf(1.0f + fast_exp(gate_finite(x)));

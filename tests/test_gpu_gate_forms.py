@@ -75,3 +75,29 @@ def test_a_form_against_the_definition(moe, form):
                     w, want_w, logits = (np.delete(v, other, 0) for v in (w, want_w, logits))
                     off = np.abs(w[:, :k] - want_w)
                     assert (off <= (2 * spread(logits) + 60) * U * want_w + 1e-37).all(), (case, scores, mask, with_bias, off.max())
+
+
+@pytest.mark.parametrize("E,k", [(8, 6), (12, 5), (64, 40), (61, 9), (256, 20)])
+@pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
+def test_a_slot_without_weight_has_no_gradient_whatever_comes_in_there(moe, scores, E, k):
+    """A token with fewer experts than choices: the masked ones' slots have weight 0, and what the experts' side says of these (NaN, an infinity) is not read."""
+    T = 37
+    rng = np.random.default_rng([T, E, k])
+    logits = rng.normal(size=(T, E)).astype(np.float32)
+    logits[rng.random((T, E)) < 0.8] = -np.inf
+    logits[0], logits[1] = -np.inf, 1.0
+    counts = rng.integers(0, 9, E).astype(np.int32)
+    dw = gpu(rng.normal(size=(T, k)).astype(np.float32))
+    for renorm in (True, False):
+        s, gate = moe.Shape(T, 64, 64, E, k, 0, renorm), moe.Gate(scores, scale=2.5)
+        idx, w = (gpu(v.astype(t)) for v, t in zip(choose(moe, logits, None, k, 1, 1, 1, scores, renorm, 2.5), (np.int32, np.float32)))
+        none = w == 0
+        assert none.any() and torch.equal(none, gpu(logits).gather(1, idx.long()) == -np.inf)
+        for balance in (None, 0.5):
+            got = []
+            for value in (0.0, float("nan"), float("inf")):
+                d = torch.empty(T, E, device="cuda")
+                moe.moe_gate_bwd(s, gate, dw.masked_fill(none, value), gpu(logits), idx, w, None if balance is None else gpu(counts), balance or 0.0, d)
+                got.append(d)
+            assert torch.isfinite(got[0]).all() and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2]), (renorm, balance)
+            assert (got[0][gpu(logits) == -np.inf] == 0).all()

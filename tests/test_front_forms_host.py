@@ -101,3 +101,15 @@ def test_choices_in_doubt():
     assert sorted(c.tolist() for c in G.choices_in_doubt(logits, bias, 2, "softmax", 3, 1, 2, rating)) == [[0, 1], [3, 2]]
     _, _, rating = G.gate_fwd(logits, None, 2, "softmax", 3, 2, 2)
     assert [c.tolist() for c in G.choices_in_doubt(logits, None, 2, "softmax", 3, 2, 2, rating)] == [[0, 2]]
+
+
+def test_forms_of_the_gates_gradient(kernels):  # noqa: F811
+    """Lanes of a token and chunks of 4 experts a lane, next to each other where E is a multiple of 4 (the rule at the launch)."""
+    forms = set()
+    for E in range(1, 1025):
+        vec = E % 4 == 0
+        lanes = 2 if vec and E <= 8 else 4 if vec and E <= 16 else 8
+        while lanes < 64 and (16 if vec else 12) * lanes < E:
+            lanes *= 2
+        forms.add((lanes, -(-E // (4 * lanes)), int(vec)))
+    assert _built(kernels, "gate_bwd_kernel") == forms

@@ -22,7 +22,7 @@
  *     run on the host before anything is launched; on any error nothing is enqueued and no output is touched.
  *   - Outputs are fully overwritten, except the weight gradients when `accumulate` is 1.
  *
- * Shape limits:  1 <= k <= E <= 1024,  E' <= 1024 (but in the calls of a gate),  T >= 0 (T = 0 is a no-op returning MOE_OK),
+ * Shape limits:  1 <= k <= E <= 1024,  E' <= 1024 (2^20 in the calls of a gate),  T >= 0 (T = 0 is a no-op returning MOE_OK),
  * T*K' < 2^31,  d_model and d_ffn positive multiples of 64 and at most 2^22 (the kernels address a tile's rows
  * with 32-bit byte offsets: 256 rows of a 2^22-element bf16 row pitch still fit).
  */
@@ -130,8 +130,7 @@ int moe_router_bwd(const moe_shape* shape, const uint16_t* x, const uint16_t* w_
  * group of masked experts alone comes after all others); one whose c is NaN or at most -1e30 comes last in the same way.  An infinite logit counts as the largest finite one.
  * A token without experts gets its lowest ids with weights 0.  Decisions are those of s and c in 64 bits (where the scores of two groups
  * are equal but for their rounding there, either may stay); weights are fp32.
- * moe_gate_fwd, moe_gate_bwd and moe_gate_bias_step take E <= 1024 with any number of shared experts beside them: E' has no limit of its own there
- * (T*K' < 2^31 and E' < 2^31 hold). */
+ * moe_gate_fwd, moe_gate_form, moe_gate_bwd and moe_gate_bias_step take E <= 1024 with shared experts beside them: E' <= 2^20 there. */
 #define MOE_SCORES_SOFTMAX 0
 #define MOE_SCORES_SIGMOID 1
 typedef struct {

@@ -14,7 +14,7 @@ namespace moe {
 constexpr float kMaskedLogit = -1e30f;   // logits up to it, and NaN, are no experts to choose
 constexpr float kMaxLogit = 3.402823466e38f;
 constexpr int kGateFewWaves = 1024;   // up to so many wavefronts a token has more lanes than it needs
-constexpr long long kGateIds = 0x7fffffff;   // of experts, shared ones among them, where nothing but an id is made of these
+constexpr long long kGateIds = 1 << 20;   // of experts, shared ones among them, where only ids are made of these (lanes' counts over them stay in an int)
 constexpr int kGateTokens = 1 << 24;   // of a launch of the forward kernels at most: a grid has less than 2^32 threads
 constexpr int kGateBwdBlocks = 512;     // at most (two a CU; more, with more parts of the loss to add, 31 -> 40 us); each adds up its tokens' share of the loss
 

@@ -58,7 +58,7 @@ def test_a_gate_with_logits_and_a_router_is_refused(calls):
     assert not calls
 
 
-@pytest.mark.parametrize("E,Es", [(1024, 1), (1023, 2), (4, 1021), (1, 2 ** 31 - 2)])
+@pytest.mark.parametrize("E,Es", [(1024, 1), (1023, 2), (4, 1021), (1, 2 ** 20 - 1)])
 def test_the_gate_takes_all_its_experts_with_shared_ones_beside_them(E, Es):
     """(No tokens: what is checked is the shape.)  The calls that move rows keep their limit."""
     import ctypes
@@ -69,9 +69,10 @@ def test_the_gate_takes_all_its_experts_with_shared_ones_beside_them(E, Es):
     assert lib.moe_gate_bias_step(s, fake, 0.1, fake, None) == 0
     assert lib.moe_router_gate_fwd(s, g, None, None, None, None, None, None, None, 0, None) == -2
     assert lib.moe_permute(s, None, fake, None, fake, fake, fake, fake, fake, 1 << 40, None) == -2 and moe.workspace_bytes(shape) == 0
-    for bad in (moe.Shape(0, D, F, 1025, 1, 0), moe.Shape(0, D, F, E, 1, 2 ** 31 - 1), moe.Shape(0, D, F, E, 1, -1)):
+    for bad in (moe.Shape(0, D, F, 1025, 1, 0), moe.Shape(0, D, F, E, 1, 2 ** 20 - E + 1), moe.Shape(0, D, F, E, 1, 2 ** 31 - 1), moe.Shape(0, D, F, E, 1, -1)):
         b = ctypes.byref(bad._c)
-        assert lib.moe_gate_fwd(b, g, None, None, None, None, None) == -2 and lib.moe_gate_bias_step(b, fake, 0.1, fake, None) == -2
+        assert lib.moe_gate_fwd(b, g, None, None, None, None, None) == -2 and lib.moe_gate_form(b, g, (ctypes.c_int32 * 4)()) == -2
+        assert lib.moe_gate_bias_step(b, fake, 0.1, fake, None) == -2
         assert lib.moe_gate_bwd(b, g, None, None, None, None, None, 0.0, None, None, None, 0, None) == -2
 
 

@@ -42,7 +42,7 @@ def test_a_step_routed_by_logits_differentiates_these(moe):
 
 
 @pytest.mark.parametrize("tokens", [3, 300])
-@pytest.mark.parametrize("experts,shared,k", [(1024, 1, 8), (1023, 2, 3), (1024, 1, 20)])
+@pytest.mark.parametrize("experts,shared,k", [(1024, 1, 8), (1023, 2, 3), (1024, 1, 20), (4, 2 ** 20 - 4, 2)])
 def test_all_experts_with_shared_ones_beside_them(moe, tokens, experts, shared, k):
     """The choice, weights and gradients of the experts are those without shared ones; a shared slot has its id and weight 1."""
     g = torch.Generator(device="cuda").manual_seed(tokens)
